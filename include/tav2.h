@@ -328,6 +328,162 @@ tav2_status tav2_select_encode_eq2(const tav2_seq* seq, const tav2_eq2* eq2,
                                    void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Windowed attention of packed sequences: every token of a request's sequence (here
+ * oldest first: position 0 is the first token) attends causally to the sequence, within
+ * the last `window` positions (itself among them; 0: no window) and to the first `sinks`
+ * tokens, which stay visible.  It encodes a whole history, where the encoders above take the
+ * rows that a search selected.
+ *   head h of position p:  s_j = scale <q_p,h , k_j,g>,  g = h / (heads / kv_heads), over
+ *     the positions j <= p with window == 0, p - j < window or j < sinks;
+ *   out = sum_j softmax(s)_j v_j,g ;  lse = log sum_j exp(s_j)  (natural logarithm).
+ * The softmax's statistics and every sum are fp32; bf16: its weights are rounded to bf16 as
+ * operands of the matrix product (at most 2^-9 of a weight).
+ * q, k and v are rows of heads: token i's head h starts at q + i * q_ld + h * head_dim
+ * (elements), so that all three can be slices of one projection's output.  Sequence r owns rows
+ * [offset[r], offset[r] + len[r]); rows of no sequence are neither read nor written.
+ */
+typedef struct tav2_window {
+  const void*    q;            /* device, rows of [heads, head_dim], dtype; values finite */
+  const void*    k;            /* device, rows of [kv_heads, head_dim], dtype; values finite */
+  const void*    v;            /* device, rows of [kv_heads, head_dim], dtype; values finite */
+  int64_t q_ld, k_ld, v_ld;    /* elements from a row to the next: at least a row, multiples of
+                                  8 (bf16) or 4 (fp32) */
+  void*          out;          /* device [rows, heads, head_dim], dtype: token i's row i */
+  float*         lse;          /* device [rows, heads], or NULL */
+  const int64_t* offset;       /* device [R]: first row of each sequence */
+  const int32_t* len;          /* device [R]: rows of each sequence, 0 <= len[r] <= max_len */
+  int32_t num_requests;        /* R >= 0 */
+  int32_t max_len;             /* host-side bound: tokens past it are not computed */
+  int32_t heads, kv_heads;     /* kv_heads divides heads */
+  int32_t head_dim;            /* 32, 64 or 128 */
+  int32_t dtype;               /* TAV2_F32 or TAV2_BF16 */
+  int32_t window, sinks;       /* >= 0 */
+  float   scale;               /* > 0, or 0 for 1 / sqrt(head_dim) */
+  int32_t reserved;            /* set to 0 */
+} tav2_window;
+/* q, k, v, out 16-byte aligned.  Errors: TAV2_ERR_NULL, TAV2_ERR_SHAPE, TAV2_ERR_DTYPE,
+ * TAV2_ERR_UNSUPPORTED (another head_dim; over 2^31 - 1 workgroups), TAV2_ERR_HIP. */
+tav2_status tav2_attend_window(const tav2_window* a, void* stream);
+
+/*
+ * A paged cache of keys and values in 8 bits, for histories that stay resident between
+ * requests (one copy for all of a request's candidates, as Sec. 3.4.2's de-duplication
+ * keeps the rows).  A sequence's tokens are held oldest first in blocks of TAV2_KV_PAGE tokens.
+ * A full block lies in one page of the pool, the same page in every layer and head: int8 codes
+ * with one scale for each block, head and side (keys, values),
+ *   scale = max|x| / 127 ,  code = 127 x / max|x| rounded half to even ,  value = code * scale
+ * (a block whose values are all below 2^-100 is stored as zeros with scale 1).  The tokens after
+ * the last full block, fewer than TAV2_KV_PAGE, stay in bf16 in the sequence's tail until they fill
+ * a block, so a value is rounded once, and a page never changes once written: sequences share
+ * pages (tav2_kv_fork), counted in refs.
+ * The caller owns every buffer.  A new cache has len 0 for every sequence, refs 0 for every
+ * page and table -1; the other buffers need no initial value.  All state is on the device, so every call
+ * can be captured into a graph; calls on one cache must be ordered (one stream, or events).
+ */
+#define TAV2_KV_PAGE 64
+#define TAV2_KV_SEQS_MAX 32768
+typedef struct tav2_kv {
+  int8_t*   k;         /* device [layers, pages, kv_heads, 64, head_dim]: codes by token */
+  int8_t*   v;         /* device [layers, pages, kv_heads, head_dim, 64]: codes by feature */
+  float*    k_scale;   /* device [layers, pages, kv_heads] */
+  float*    v_scale;   /* device [layers, pages, kv_heads] */
+  uint16_t* k_tail;    /* device [layers, num_seqs, kv_heads, 64, head_dim] bf16 */
+  uint16_t* v_tail;    /* device [layers, num_seqs, kv_heads, head_dim, 64] bf16 */
+  int32_t*  table;     /* device [num_seqs, max_blocks]: page of each full block, -1: none */
+  int32_t*  len;       /* device [num_seqs]: tokens, 0 .. 64 max_blocks + 63 */
+  int32_t*  fresh;     /* device [num_seqs]: tokens that the last tav2_kv_extend granted */
+  int32_t*  refs;      /* device [pages]: sequences that hold the page (0: free) */
+  int32_t num_seqs;    /* 1 .. TAV2_KV_SEQS_MAX */
+  int32_t layers;      /* >= 1 */
+  int32_t pages;       /* >= 1 */
+  int32_t max_blocks;  /* 1 .. 2^20 */
+  int32_t kv_heads;    /* >= 1 */
+  int32_t head_dim;    /* 32, 64 or 128 */
+  int32_t max_len;     /* host-side estimate of the longest sequence: tav2_kv_attend divides
+                          its work by it (results do not depend on it) */
+  int32_t reserved;    /* set to 0 */
+} tav2_kv;
+
+/*
+ * Room for new tokens: sequence s grows by count[s] tokens (device int32 [num_seqs]; 0 or less: not),
+ * taking the lowest free pages for the blocks that these fill, sequences in order.  A sequence
+ * that would pass max_blocks is not extended; from the first one that the free pages do not
+ * suffice for on, none is.  fresh[s] says what was granted (count[s] or 0).  The tokens' keys and values
+ * are written afterwards, layer by layer, by tav2_kv_append; until then the sequence is not to be
+ * forked, trimmed or attended to in the layers that lack them.
+ * Errors (of all tav2_kv_ calls): TAV2_ERR_NULL, TAV2_ERR_SHAPE, TAV2_ERR_UNSUPPORTED, TAV2_ERR_HIP.
+ */
+tav2_status tav2_kv_extend(const tav2_kv* c, const int32_t* count, void* stream);
+
+/*
+ * The keys and values of the tokens that the last tav2_kv_extend granted, for one layer
+ * (once per layer and extension): sequence s's fresh[s] tokens are rows offset[s].. of k and v
+ * (bf16 rows of [kv_heads, head_dim], row strides k_ld and v_ld elements, multiples of 8; 16-byte
+ * aligned; values finite).  Blocks that are full now go to their pages, the rest to the tail.
+ *   offset    device int64 [num_seqs]
+ *   max_count host-side bound of fresh[s]; tokens of a sequence past it are not written
+ */
+tav2_status tav2_kv_append(const tav2_kv* c, int32_t layer, const void* k, int64_t k_ld,
+                           const void* v, int64_t v_ld, const int64_t* offset, int32_t max_count,
+                           void* stream);
+
+/*
+ * Attention of new queries over one layer of the cache: single new tokens, chunks of them, or the
+ * candidates of a request.  Sequence s has the queries [offset[s], offset[s+1]) , n_s of them.
+ *   TAV2_MASK_CAUSAL: they are the sequence's last n_s tokens (appended before): query i is at
+ *     position len[s] - n_s + i and sees the positions up to its own (none where that is negative);
+ *   TAV2_MASK_NONE: each is a candidate to follow the sequence, at position len[s]: it sees
+ *     every cached token.
+ * window and sinks as for tav2_attend_window, counted from the query's position; blocks that were
+ * released (tav2_kv_trim) are not seen.  out and lse as there; a query that sees nothing gets
+ * zeros and -inf.  Queries and outputs are bf16; products take the codes exactly, the scales in fp32.
+ *   ws  device workspace of tav2_kv_attend_workspace() bytes, 256-byte aligned.
+ * Errors: those above, TAV2_ERR_WORKSPACE.
+ */
+typedef struct tav2_kv_queries {
+  const void*    q;            /* device bf16: query i's head h at q + i * ld + h * head_dim */
+  const int64_t* offset;       /* device [num_seqs + 1]; offset[0] = 0, offset[num_seqs] = total */
+  int64_t total;               /* host: number of queries (>= 0) */
+  int64_t ld;                  /* elements between queries: a multiple of 8 */
+  int32_t max_count;           /* host-side bound of a sequence's queries */
+  int32_t heads;               /* a multiple of kv_heads */
+  int32_t window, sinks;       /* >= 0 */
+  float   scale;               /* > 0, or 0 for 1 / sqrt(head_dim) */
+  int32_t reserved;            /* set to 0 */
+} tav2_kv_queries;
+size_t tav2_kv_attend_workspace(const tav2_kv* c, const tav2_kv_queries* q);
+tav2_status tav2_kv_attend(const tav2_kv* c, int32_t layer, const tav2_kv_queries* q,
+                           uint32_t flags, void* out, float* lse, void* ws, size_t ws_bytes,
+                           void* stream);
+
+/*
+ * Copies of sequences: for every s with parent[s] >= 0 (device int32 [num_seqs]), empty sequence s
+ * becomes a continuation of sequence parent[s]: it shares that one's pages and gets a copy of
+ * its tail, in every layer.  Left as it is where s is not empty, or parent[s] is no sequence or is
+ * itself given a parent in this call.
+ */
+tav2_status tav2_kv_fork(const tav2_kv* c, const int32_t* parent, void* stream);
+
+/* Sequences s with drop[s] != 0 (device uint8 [num_seqs]) give up their pages and are empty. */
+tav2_status tav2_kv_free(const tav2_kv* c, const uint8_t* drop, void* stream);
+
+/*
+ * Every sequence gives up the pages that no later query with this window and these sinks sees: the
+ * blocks wholly past the first `sinks` tokens and before the last window - 1.  window >= 1.
+ */
+tav2_status tav2_kv_trim(const tav2_kv* c, int32_t window, int32_t sinks, void* stream);
+
+/*
+ * Moves the used pages to the front of the pool: with U pages in use, those at U and behind go to
+ * the free ones below, both in ascending order; tables and refs follow.  *used (device int32)
+ * = U; the pool's pages from U on are free then.
+ *   ws  device workspace of tav2_kv_compact_workspace() bytes, 256-byte aligned.
+ */
+size_t tav2_kv_compact_workspace(const tav2_kv* c);
+tav2_status tav2_kv_compact(const tav2_kv* c, int32_t* used, void* ws, size_t ws_bytes,
+                            void* stream);
+
+/*
  * Measurement hook for benchmarks and profilers (not needed for serving).
  * tav2_profile_enable(1, site) makes every later kernel launch of the library
  * whose site name equals `site` (NULL: every site) record a HIP event before
@@ -341,7 +497,9 @@ tav2_status tav2_select_encode_eq2(const tav2_seq* seq, const tav2_eq2* eq2,
  * more than 4096 rows), nn_resident (the search in one launch: rows of at most 64 bytes
  * with d 32 or 64, few candidates), score_bf16, score_i8, score_f32, topk (the NN search over
  * materialised score rows), gather, pack_weights, cand_proj, encoder_fused (the
- * bf16 encoder of d_model 256), encoder_small (d_model 64), encode_f32.
+ * bf16 encoder of d_model 256), encoder_small (d_model 64), encode_f32, attend_window,
+ * kv_extend, kv_append, kv_attend, kv_merge (kv_attend's second launch), kv_fork, kv_free,
+ * kv_trim, kv_plan and kv_compact (the two of tav2_kv_compact).
  */
 int32_t tav2_profile_enable(int32_t on, const char* only_site);
 int64_t tav2_profile_report(char* buf, size_t buf_bytes);

@@ -19,7 +19,8 @@ LIB = os.path.join(PKG, "libtav2.so")
 SOURCES = ["api.cpp", "batcher.cpp", "profile.cpp", "select.hip", "select_fused.hip",
            "select_resident.hip", "gather.hip",
            "encoder_fused.hip", "encoder_fused_unmasked.hip", "encoder_fused_short.hip",
-           "encoder_small.hip", "encoder_f32.hip"]
+           "encoder_small.hip", "encoder_f32.hip", "attend_window.hip", "kv_attend.hip",
+           "kv_append.hip", "kv_pages.hip", "kv_api.cpp"]
 ARCH = "gfx950"
 
 
@@ -44,13 +45,17 @@ def compile_flags():
 # d_model-64 encoder is made of short dependent steps: the max-ILP scheduler orders
 # them 1 - 4 % better than the default one (192 positions and fewer; the other
 # sources gain nothing from it).  The int8 score kernels' division and square root
-# must round correctly (the compiler's default for HIP, stated explicitly).
+# and the cache's scales must round correctly (the compiler's default for HIP, stated
+# explicitly).
 EXTRA_FLAGS = {"encoder_fused.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "encoder_fused_unmasked.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "encoder_fused_short.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "encoder_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "encoder_small.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-mllvm",
                                      "-amdgpu-sched-strategy=max-ilp"],
+               "attend_window.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "kv_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "kv_append.hip": ["-fhip-fp32-correctly-rounded-divide-sqrt"],
                "select.hip": ["-fhip-fp32-correctly-rounded-divide-sqrt"],
                "select_resident.hip": ["-fhip-fp32-correctly-rounded-divide-sqrt", "-mllvm",
                                        "-amdgpu-mfma-vgpr-form"],

@@ -1,0 +1,128 @@
+// The step that the attention kernels share: 32 keys against 32 QT queries of one wave, products on the
+// 32x32x16 bf16 matrix instructions, everything between them in registers.
+//
+// Scores are taken transposed, S^T = K Q^T: a lane then holds one query (column l % 32) and, where the
+// tile's rows are keys in the order pi(8j + 4h + i) = 16h + 4j + i, the 16 consecutive keys
+// 16h .. 16h + 15 of it (h = l / 32), register r being key 16h + r.  Those registers, rounded to
+// bf16, are the operand of O^T = V^T P^T as they stand, against 16 consecutive keys of a feature: one
+// or two 16-byte loads where V lies by feature.  No lane exchanges but the joining of the two
+// halves' maxima.
+//
+// The softmax's reference m is raised only where a score passes it by more than 2^8
+// (RAISE): the weights stay below 2^8 and the sums are fp32, so any reference within that
+// gives the same quotient, and raising it is rare after a query's first keys.
+#pragma once
+
+#include <float.h>
+
+#include "common.h"
+
+namespace tav2 {
+
+constexpr float RAISE = 8.f;       // in powers of two
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+
+// Row of a 32-key tile that lane l % 32 = m loads, so that register r is key 16h + r.
+__device__ __forceinline__ int key_row(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
+
+// What a wave keeps of 32 QT queries: O^T unnormalised (D / 32 tiles of 32 features), the
+// reference m (powers of two; -FLT_MAX: no key yet, finite so that no difference is a NaN) and the
+// sum l of this lane half's weights.
+template <int D, int QT>
+struct AttState {
+  f32x16 o[D / 32][QT];
+  float m[QT], l[QT];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+      m[q] = -FLT_MAX;
+      l[q] = 0.f;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][q][r] = 0.f;
+    }
+  }
+};
+
+// Which keys a lane's queries see: positions below hi that are at least lo or below sinks.
+template <int QT>
+struct AttSeen {
+  int hi[QT], lo[QT];
+  int sinks;
+};
+
+// s: this lane's 16 scores of query tile q before scaling (c > 0 turns them into powers of two);
+// key0: position of its first key.  Returns the weights, times 2^lv, in s; inv = 2^-lv.
+template <int D, int QT>
+__device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16& s, float c, float lv,
+                                            float inv, bool masked, const AttSeen<QT>& seen, int key0) {
+  if (masked) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = key0 + r;
+      const bool see = key < seen.hi[q] && (key >= seen.lo[q] || key < seen.sinks);
+      s[r] = see ? s[r] : -INFINITY;
+    }
+  }
+  float top = s[0];
+#pragma unroll
+  for (int r = 1; r < 16; ++r) top = vmax(top, s[r]);
+  top = xmax32(top) * c;
+  if (__any(top > st.m[q] + RAISE)) {
+    const float m = top > st.m[q] ? top : st.m[q];
+    const float f = __builtin_amdgcn_exp2f(st.m[q] - m);
+    st.m[q] = m;
+    st.l[q] *= f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st.o[d][q][r] *= f;
+  }
+  const float b = lv - st.m[q];
+  float sum = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, b));
+    sum += s[r];
+  }
+  st.l[q] = __builtin_fmaf(sum, inv, st.l[q]);
+}
+
+// 16 weights as the operands of two products.
+__device__ __forceinline__ void att_operands(const f32x16& p, bf16x8 (&f)[2]) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    f[t] = as_bf16x8(make_uint4(pack2(p[8 * t], p[8 * t + 1]), pack2(p[8 * t + 2], p[8 * t + 3]),
+                                pack2(p[8 * t + 4], p[8 * t + 5]), pack2(p[8 * t + 6], p[8 * t + 7])));
+}
+
+// kf[t]: the key row's features h D / 2 + 8t ..; qf the queries' likewise; vf[d][t]: feature
+// 32 d + l % 32, keys 16h + 8t ...
+template <int D, int QT>
+__device__ __forceinline__ void att_step(AttState<D, QT>& st, const bf16x8 (&kf)[D / 16],
+                                         const bf16x8 (&vf)[D / 32][2],
+                                         const bf16x8 (&qf)[QT][D / 16], float c, float lv,
+                                         float inv, bool masked, const AttSeen<QT>& seen, int key0) {
+  f32x16 s[QT];
+#pragma unroll
+  for (int q = 0; q < QT; ++q) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[q][r] = 0.f;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) s[q] = mfma32(kf[t], qf[q][t], s[q]);
+  }
+#pragma unroll
+  for (int q = 0; q < QT; ++q) {
+    att_softmax<D, QT>(st, q, s[q], c, lv, inv, masked, seen, key0);
+    bf16x8 pf[2];
+    att_operands(s[q], pf);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) st.o[d][q] = mfma32(vf[d][t], pf[t], st.o[d][q]);
+  }
+}
+
+}  // namespace tav2

@@ -1,0 +1,343 @@
+// Causal attention of packed sequences with a window and sink tokens.
+//
+// A workgroup takes 4 x 32 QT consecutive (position, head) rows of one kv head of a sequence; its
+// four waves share each 64-key tile through LDS: keys as rows, values by feature (two keys a 32-bit
+// word, turned while they are written), both in 16-byte pieces whose places are permuted so that
+// neither the writes nor the operand reads meet in a bank.  The next tile's loads are in flight while
+// the present one is multiplied, one barrier a tile.  Tiles that no row of the workgroup sees are not
+// visited, and a wave skips those that none of its own sees, so the work is that of the window.
+// Bound by the vector units: an exponential, a scaling, a maximum, a sum and a rounding for each
+// score, beside 4 D matrix operations.
+#include <algorithm>
+
+#include "attend_core.h"
+#include "internal.h"
+
+namespace tav2 {
+
+namespace {
+
+constexpr int TK = 64;   // keys of a tile (bf16)
+
+struct WindowArgs {
+  tav2_window a;
+  float scale;
+  int tiles;   // row tiles per (sequence, kv head)
+};
+
+// Rows of this workgroup: positions lo .. hi of a sequence of len tokens.
+struct Rows {
+  int64_t off;
+  int len, rows, row0, h, G;
+};
+
+__device__ __forceinline__ bool rows_of(const WindowArgs& w, int per, Rows& r) {
+  const tav2_window& a = w.a;
+  int64_t u = blockIdx.x;
+  const int units = a.num_requests * a.kv_heads;
+  const int unit = int(u % units);
+  const int tile = w.tiles - 1 - int(u / units);   // the longest rows first
+  const int s = unit / a.kv_heads;
+  r.h = unit % a.kv_heads;
+  r.G = a.heads / a.kv_heads;
+  r.off = a.offset[s];
+  r.len = a.len[s] < a.max_len ? a.len[s] : a.max_len;
+  r.rows = r.len * r.G;
+  r.row0 = tile * per;
+  return r.row0 < r.rows;
+}
+
+// The tiles that positions lo .. hi see: [0, sink) and [first, last).
+struct Tiles {
+  int sink, first, last;
+  __device__ __forceinline__ int count() const { return sink + last - first; }
+  __device__ __forceinline__ int at(int i) const { return i < sink ? i : first + i - sink; }
+};
+__device__ __forceinline__ Tiles tiles_seen(int lo, int hi, int window, int sinks, int tk) {
+  Tiles t;
+  t.last = hi / tk + 1;
+  t.first = window > 0 && lo >= window ? (lo - window + 1) / tk : 0;
+  t.sink = window > 0 ? min(int((int64_t(sinks) + tk - 1) / tk), t.first) : 0;
+  return t;
+}
+
+// What a wave's rows see of the tile at k0: 0 nothing, 1 some, 2 all of it.
+__device__ __forceinline__ int tile_seen(int k0, int tk, int lo, int hi, int window, int sinks) {
+  if (k0 > hi) return 0;
+  if (window > 0 && int64_t(k0) + tk + window <= int64_t(lo) + 1 && k0 >= sinks) return 0;
+  const bool low = window == 0 || int64_t(k0) + window > hi || int64_t(k0) + tk <= sinks;
+  return low && k0 + tk - 1 <= lo ? 2 : 1;
+}
+
+__device__ __forceinline__ int swz_v(int d) { return (d & 7) ^ ((d >> 3) & 7); }
+template <int D>
+__device__ __forceinline__ int swz_k(int row) {
+  return D == 32 ? ((row >> 1) & 1) | ((row >> 4) & 1) << 1 : (row & 3) | ((row >> 4) & 1) << 2;
+}
+
+template <int D, int QT>
+__global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_bf16(WindowArgs w) {
+  constexpr int CH = D / 8;                       // 16-byte pieces of a row
+  constexpr int NK = (TK * CH + 255) / 256;       // pieces of K per thread
+  constexpr int NV = (TK / 2 * CH + 255) / 256;   // pairs of pieces of V per thread
+  __shared__ __align__(16) uint8_t lk[2][TK * D * 2], lv[2][D * TK * 2];
+  Rows r;
+  if (!rows_of(w, 128 * QT, r)) return;
+  const tav2_window& a = w.a;
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE, m = lane % 32, half = lane / 32;
+  const int wrow0 = r.row0 + wave * 32 * QT;
+  const bf16_t* kb = static_cast<const bf16_t*>(a.k) + r.off * a.k_ld + r.h * D;
+  const bf16_t* vb = static_cast<const bf16_t*>(a.v) + r.off * a.v_ld + r.h * D;
+
+  bf16x8 qf[QT][D / 16];
+  AttSeen<QT> seen;
+  seen.sinks = a.sinks;
+#pragma unroll
+  for (int q = 0; q < QT; ++q) {
+    const int row = min(wrow0 + 32 * q + m, r.rows - 1);
+    const int pos = row / r.G;
+    const bf16_t* p = static_cast<const bf16_t*>(a.q) + (r.off + pos) * a.q_ld +
+                      (r.h * r.G + row % r.G) * D + half * (D / 2);
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) qf[q][t] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 8 * t));
+    seen.hi[q] = pos + 1;
+    seen.lo[q] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+  }
+  const int last_row = min(r.row0 + 128 * QT, r.rows) - 1;
+  const Tiles tiles = tiles_seen(r.row0 / r.G, last_row / r.G, a.window, a.sinks, TK);
+  const bool idle = wrow0 >= r.rows;
+  const int wlo = wrow0 / r.G, whi = min(wrow0 + 32 * QT - 1, r.rows - 1) / r.G;
+
+  uint4 gk[NK], gv[NV][2];
+  auto load = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int e = tid + 256 * i;
+      if (TK * CH % 256 && e >= TK * CH) continue;
+      const int row = min(k0 + e / CH, r.len - 1);
+      gk[i] = *reinterpret_cast<const uint4*>(kb + int64_t(row) * a.k_ld + e % CH * 8);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int e = tid + 256 * i;
+      if (TK / 2 * CH % 256 && e >= TK / 2 * CH) continue;
+      const int row = k0 + e / CH * 2;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        gv[i][j] = *reinterpret_cast<const uint4*>(vb + int64_t(min(row + j, r.len - 1)) * a.v_ld +
+                                                   e % CH * 8);
+    }
+  };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int e = tid + 256 * i;
+      if (TK * CH % 256 && e >= TK * CH) continue;
+      const int row = e / CH, ch = e % CH;
+      *reinterpret_cast<uint4*>(lk[buf] + row * D * 2 + (ch ^ swz_k<D>(row)) * 16) = gk[i];
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int e = tid + 256 * i;
+      if (TK / 2 * CH % 256 && e >= TK / 2 * CH) continue;
+      const int kp = e / CH, d0 = e % CH * 8;
+      const uint32_t x[4] = {gv[i][0].x, gv[i][0].y, gv[i][0].z, gv[i][0].w};
+      const uint32_t y[4] = {gv[i][1].x, gv[i][1].y, gv[i][1].z, gv[i][1].w};
+#pragma unroll
+      for (int f = 0; f < 8; ++f) {
+        const uint32_t word = __builtin_amdgcn_perm(y[f / 2], x[f / 2], f % 2 ? 0x07060302u : 0x05040100u);
+        const int d = d0 + f;
+        *reinterpret_cast<uint32_t*>(lv[buf] + d * TK * 2 + ((kp / 4) ^ swz_v(d)) * 16 + kp % 4 * 4) = word;
+      }
+    }
+  };
+
+  AttState<D, QT> st;
+  st.clear();
+  const float c = w.scale * LOG2E;
+  const int n = tiles.count();
+  load(tiles.at(0) * TK);
+  store(0);
+  __syncthreads();
+  for (int i = 0; i < n; ++i) {
+    const int k0 = tiles.at(i) * TK, buf = i & 1;
+    if (i + 1 < n) load(tiles.at(i + 1) * TK);
+    const int see = idle ? 0 : tile_seen(k0, TK, wlo, whi, a.window, a.sinks);
+    if (see) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        bf16x8 kf[D / 16], vf[D / 32][2];
+        const int row = 32 * u + key_row(m);
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t)
+          kf[t] = as_bf16x8(*reinterpret_cast<const uint4*>(
+              lk[buf] + row * D * 2 + ((half * (D / 16) + t) ^ swz_k<D>(row)) * 16));
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int f = 32 * d + m;
+            vf[d][t] = as_bf16x8(*reinterpret_cast<const uint4*>(
+                lv[buf] + f * TK * 2 + ((4 * u + 2 * half + t) ^ swz_v(f)) * 16));
+          }
+        att_step<D, QT>(st, kf, vf, qf, c, 0.f, 1.f, see == 1, seen, k0 + 32 * u + 16 * half);
+      }
+    }
+    if (i + 1 < n) store(buf ^ 1);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int q = 0; q < QT; ++q) {
+    const int row = wrow0 + 32 * q + m;
+    const float l = xsum32(st.l[q]);
+    if (row >= r.rows) continue;
+    const int64_t at = (r.off + row / r.G) * a.heads + r.h * r.G + row % r.G;
+    const float inv = 1.f / l;   // a row sees itself: l > 0
+    bf16_t* out = static_cast<bf16_t*>(a.out) + at * D + 4 * half;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<uint2*>(out + 32 * d + 8 * j) =
+            make_uint2(pack2(st.o[d][q][4 * j] * inv, st.o[d][q][4 * j + 1] * inv),
+                       pack2(st.o[d][q][4 * j + 2] * inv, st.o[d][q][4 * j + 3] * inv));
+    if (a.lse && half == 0) a.lse[at] = (st.m[q] + __builtin_amdgcn_logf(l)) * LN2;
+  }
+}
+
+// fp32: the same on 32x32x2 fp32 products, 32 keys a tile; the weights are operands as they
+// are.
+constexpr int TF = 32;
+
+template <int D>
+__global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
+  constexpr int KS = D + 4, VS = TF + 4;   // LDS rows (floats)
+  constexpr int CH = D / 4, NC = TF * CH / 256;
+  __shared__ __align__(16) float lk[TF * KS], lv[D * VS];
+  Rows r;
+  if (!rows_of(w, 128, r)) return;
+  const tav2_window& a = w.a;
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE, m = lane % 32, half = lane / 32;
+  const int wrow0 = r.row0 + wave * 32;
+  const float* kb = static_cast<const float*>(a.k) + r.off * a.k_ld + r.h * D;
+  const float* vb = static_cast<const float*>(a.v) + r.off * a.v_ld + r.h * D;
+  float4 qf[D / 8];
+  AttSeen<1> seen;
+  seen.sinks = a.sinks;
+  {
+    const int row = min(wrow0 + m, r.rows - 1), pos = row / r.G;
+    const float* p = static_cast<const float*>(a.q) + (r.off + pos) * a.q_ld +
+                     (r.h * r.G + row % r.G) * D + half * (D / 2);
+#pragma unroll
+    for (int t = 0; t < D / 8; ++t) qf[t] = *reinterpret_cast<const float4*>(p + 4 * t);
+    seen.hi[0] = pos + 1;
+    seen.lo[0] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+  }
+  const int last_row = min(r.row0 + 128, r.rows) - 1;
+  const Tiles tiles = tiles_seen(r.row0 / r.G, last_row / r.G, a.window, a.sinks, TF);
+  const bool idle = wrow0 >= r.rows;
+  const int wlo = wrow0 / r.G, whi = min(wrow0 + 31, r.rows - 1) / r.G;
+  float4 gk[NC], gv[NC];
+  auto load = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int e = tid + 256 * i, row = min(k0 + e / CH, r.len - 1), ch = e % CH * 4;
+      gk[i] = *reinterpret_cast<const float4*>(kb + int64_t(row) * a.k_ld + ch);
+      gv[i] = *reinterpret_cast<const float4*>(vb + int64_t(row) * a.v_ld + ch);
+    }
+  };
+  AttState<D, 1> st;
+  st.clear();
+  const float c = w.scale * LOG2E;
+  const int n = tiles.count();
+  load(tiles.at(0) * TF);
+  for (int i = 0; i < n; ++i) {
+    const int k0 = tiles.at(i) * TF;
+    if (i) __syncthreads();   // the last tile has been read
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int e = tid + 256 * j, row = e / CH, ch = e % CH * 4;
+      *reinterpret_cast<float4*>(lk + row * KS + ch) = gk[j];
+      lv[(ch + 0) * VS + row] = gv[j].x;
+      lv[(ch + 1) * VS + row] = gv[j].y;
+      lv[(ch + 2) * VS + row] = gv[j].z;
+      lv[(ch + 3) * VS + row] = gv[j].w;
+    }
+    __syncthreads();
+    if (i + 1 < n) load(tiles.at(i + 1) * TF);
+    const int see = idle ? 0 : tile_seen(k0, TF, wlo, whi, a.window, a.sinks);
+    if (!see) continue;
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+    const float* kr = lk + key_row(m) * KS + half * (D / 2);
+#pragma unroll
+    for (int t = 0; t < D / 8; ++t) {
+      const float4 k4 = *reinterpret_cast<const float4*>(kr + 4 * t);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.x, qf[t].x, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.y, qf[t].y, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.z, qf[t].z, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.w, qf[t].w, s, 0, 0, 0);
+    }
+    att_softmax<D, 1>(st, 0, s, c, 0.f, 1.f, see == 1, seen, k0 + 16 * half);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+      const float* vr = lv + (32 * d + m) * VS + 16 * half;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float4 v4 = *reinterpret_cast<const float4*>(vr + 4 * t);
+        st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v4.x, s[4 * t], st.o[d][0], 0, 0, 0);
+        st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v4.y, s[4 * t + 1], st.o[d][0], 0, 0, 0);
+        st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v4.z, s[4 * t + 2], st.o[d][0], 0, 0, 0);
+        st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v4.w, s[4 * t + 3], st.o[d][0], 0, 0, 0);
+      }
+    }
+  }
+  const int row = wrow0 + m;
+  const float l = xsum32(st.l[0]);
+  if (row >= r.rows) return;
+  const int64_t at = (r.off + row / r.G) * a.heads + r.h * r.G + row % r.G;
+  const float inv = 1.f / l;
+  float* out = static_cast<float*>(a.out) + at * D + 4 * half;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<float4*>(out + 32 * d + 8 * j) =
+          make_float4(st.o[d][0][4 * j] * inv, st.o[d][0][4 * j + 1] * inv,
+                      st.o[d][0][4 * j + 2] * inv, st.o[d][0][4 * j + 3] * inv);
+  if (a.lse && half == 0) a.lse[at] = (st.m[0] + __builtin_amdgcn_logf(l)) * LN2;
+}
+
+int rows_per_group(const tav2_window& a) {
+  if (a.dtype == TAV2_F32 || a.head_dim == 128) return 128;
+  return 256;
+}
+
+}  // namespace
+
+int64_t attend_window_groups(const tav2_window& a) {
+  return int64_t(a.num_requests) * a.kv_heads *
+         cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), rows_per_group(a));
+}
+
+hipError_t launch_attend_window(const tav2_window& a, hipStream_t st) {
+  WindowArgs w;
+  w.a = a;
+  w.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf(float(a.head_dim));
+  w.tiles = int(cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), rows_per_group(a)));
+  const unsigned grid = unsigned(attend_window_groups(a));
+  ProfScope prof("attend_window", st);
+  if (a.dtype == TAV2_F32) {
+    if (a.head_dim == 32) attend_window_f32<32><<<grid, 256, 0, st>>>(w);
+    else if (a.head_dim == 64) attend_window_f32<64><<<grid, 256, 0, st>>>(w);
+    else attend_window_f32<128><<<grid, 256, 0, st>>>(w);
+  } else {
+    if (a.head_dim == 32) attend_window_bf16<32, 2><<<grid, 256, 0, st>>>(w);
+    else if (a.head_dim == 64) attend_window_bf16<64, 2><<<grid, 256, 0, st>>>(w);
+    else attend_window_bf16<128, 1><<<grid, 256, 0, st>>>(w);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace tav2

@@ -135,4 +135,23 @@ bool encode_f32_fits(int T, const tav2_weights& w);
 hipError_t launch_encode_f32(const TokenSource& src, const void* cand_emb, int64_t total,
                              const tav2_weights& w, float* out, bool unmasked, hipStream_t st);
 
+// ---- attend_window.hip: causal attention of packed sequences, window and sinks
+int64_t attend_window_groups(const tav2_window& a);   // workgroups of the launch
+hipError_t launch_attend_window(const tav2_window& a, hipStream_t st);
+
+// ---- kv_pages.hip, kv_append.hip, kv_attend.hip: the paged 8-bit cache
+hipError_t launch_kv_extend(const tav2_kv& c, const int32_t* count, hipStream_t st);
+hipError_t launch_kv_fork(const tav2_kv& c, const int32_t* parent, hipStream_t st);
+hipError_t launch_kv_free(const tav2_kv& c, const uint8_t* drop, hipStream_t st);
+hipError_t launch_kv_trim(const tav2_kv& c, int window, int sinks, hipStream_t st);
+size_t kv_plan_bytes(const tav2_kv& c);
+hipError_t launch_kv_compact(const tav2_kv& c, int32_t* used, void* ws, hipStream_t st);
+int64_t kv_append_groups(const tav2_kv& c, int max_count);
+hipError_t launch_kv_append(const tav2_kv& c, int layer, const void* k, int64_t k_ld, const void* v,
+                            int64_t v_ld, const int64_t* offset, int max_count, hipStream_t st);
+int64_t kv_attend_groups(const tav2_kv& c, const tav2_kv_queries& q);
+size_t kv_attend_bytes(const tav2_kv& c, const tav2_kv_queries& q);
+hipError_t launch_kv_attend(const tav2_kv& c, int layer, const tav2_kv_queries& q, bool causal,
+                            void* out, float* lse, void* ws, hipStream_t st);
+
 }  // namespace tav2

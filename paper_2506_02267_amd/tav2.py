@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, c_float, c_int32, c_int64, c_size_t, c_void_p
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtav2.so"
 F32, BF16, I8 = 0, 1, 2
 MASK_CAUSAL, MASK_NONE = 0, 1
 K_MAX, T_MAX = 1024, 2048
+KV_PAGE, KV_SEQS_MAX = 64, 32768
 STATUS = {0: "ok", -1: "null", -2: "shape", -3: "dtype", -4: "unsupported", -5: "workspace",
           -6: "hip", -7: "too_large"}
 
@@ -73,6 +74,28 @@ class Request(ctypes.Structure):
                 ("cand_emb", c_void_p), ("n_cands", c_int32), ("reserved", c_int32)]
 
 
+class Window(ctypes.Structure):
+    _fields_ = [("q", c_void_p), ("k", c_void_p), ("v", c_void_p), ("q_ld", c_int64),
+                ("k_ld", c_int64), ("v_ld", c_int64), ("out", c_void_p), ("lse", c_void_p),
+                ("offset", c_void_p), ("len", c_void_p), ("num_requests", c_int32),
+                ("max_len", c_int32), ("heads", c_int32), ("kv_heads", c_int32),
+                ("head_dim", c_int32), ("dtype", c_int32), ("window", c_int32), ("sinks", c_int32),
+                ("scale", c_float), ("reserved", c_int32)]
+
+
+class Kv(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("k", "v", "k_scale", "v_scale", "k_tail", "v_tail", "table",
+                                        "len", "fresh", "refs")] + [
+        (n, c_int32) for n in ("num_seqs", "layers", "pages", "max_blocks", "kv_heads", "head_dim",
+                               "max_len", "reserved")]
+
+
+class KvQueries(ctypes.Structure):
+    _fields_ = [("q", c_void_p), ("offset", c_void_p), ("total", c_int64), ("ld", c_int64),
+                ("max_count", c_int32), ("heads", c_int32), ("window", c_int32),
+                ("sinks", c_int32), ("scale", c_float), ("reserved", c_int32)]
+
+
 FUNCTIONS = {
     "tav2_status_string": (ctypes.c_char_p, [c_int32]),
     "tav2_abi_version": (c_int32, []),
@@ -106,6 +129,18 @@ FUNCTIONS = {
     "tav2_batcher_add": (c_int32, [c_void_p, POINTER(Request)]),
     "tav2_batcher_upload": (c_int32, [c_void_p, c_void_p]),
     "tav2_batcher_views": (c_int32, [c_void_p, POINTER(Seq), POINTER(Seq), POINTER(Cands)]),
+    "tav2_attend_window": (c_int32, [POINTER(Window), c_void_p]),
+    "tav2_kv_extend": (c_int32, [POINTER(Kv), c_void_p, c_void_p]),
+    "tav2_kv_append": (c_int32, [POINTER(Kv), c_int32, c_void_p, c_int64, c_void_p, c_int64,
+                                 c_void_p, c_int32, c_void_p]),
+    "tav2_kv_attend_workspace": (c_size_t, [POINTER(Kv), POINTER(KvQueries)]),
+    "tav2_kv_attend": (c_int32, [POINTER(Kv), c_int32, POINTER(KvQueries), ctypes.c_uint32,
+                                 c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "tav2_kv_fork": (c_int32, [POINTER(Kv), c_void_p, c_void_p]),
+    "tav2_kv_free": (c_int32, [POINTER(Kv), c_void_p, c_void_p]),
+    "tav2_kv_trim": (c_int32, [POINTER(Kv), c_int32, c_int32, c_void_p]),
+    "tav2_kv_compact_workspace": (c_size_t, [POINTER(Kv)]),
+    "tav2_kv_compact": (c_int32, [POINTER(Kv), c_void_p, c_void_p, c_size_t, c_void_p]),
     "tav2_profile_enable": (c_int32, [c_int32, ctypes.c_char_p]),
     "tav2_profile_report": (ctypes.c_int64, [ctypes.c_char_p, c_size_t]),
 }
@@ -490,6 +525,224 @@ def profile_report() -> dict:
 
 def select_encode(seq, rt, cands, k, w, stream=None, flags: int = MASK_CAUSAL):
     return SelectEncode(seq, rt, cands, k, w, flags)(stream)
+
+
+# ------------------------------------------------------- attention over whole histories
+def _heads(name: str, x: torch.Tensor, dtype) -> int:
+    """Elements from a row of x [rows, heads, head_dim] to the next (heads packed in a row)."""
+    if x.dim() != 3 or x.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype} [rows, heads, head_dim]")
+    if x.shape[0] > 0 and (x.stride(2) != 1 or x.stride(1) != x.shape[2]):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    width = x.shape[1] * x.shape[2]
+    return x.stride(0) if x.shape[0] > 1 else width
+
+
+def _dense(name: str, x: Optional[torch.Tensor], shape, dtype):
+    if x is not None and (tuple(x.shape) != tuple(shape) or x.dtype != dtype
+                          or not x.is_contiguous()):
+        raise ValueError(f"{name}: expected contiguous {dtype} {list(shape)}")
+
+
+def _run(fn: str, dev: torch.device, stream, args, *used):
+    """Call entry point `fn` with `args` and the stream, on the device that holds the tensors
+    (`used`: all of them), whichever device is current."""
+    if dev.type != "cuda":
+        raise ValueError(f"{fn}: expected tensors on a GPU")
+    for t in used:
+        if t is not None and t.device != dev:
+            raise ValueError(f"{fn}: tensors on {t.device} and {dev}")
+    call = getattr(load_library(), fn)
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            _check(fn, call(*args, _stream_handle(stream)))
+            _used_on(stream, *used)
+    else:
+        _check(fn, call(*args, _stream_handle(stream)))
+        _used_on(stream, *used)
+
+
+def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offset: torch.Tensor,
+                  length: torch.Tensor, max_len: int, window: int = 0, sinks: int = 0,
+                  scale: float = 0.0, out: Optional[torch.Tensor] = None,
+                  lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """tav2_attend_window: causal attention of packed sequences (oldest token first).
+
+    q [rows, heads, head_dim], k and v [rows, kv_heads, head_dim], bf16 or fp32, may be slices of
+    one projection; offset int64 [R], length int32 [R].  window 0: none; the first `sinks` tokens
+    stay visible.  lse (optional, fp32 [rows, heads]) receives the log of the sums."""
+    dt = torch.float32 if q.dtype == torch.float32 else torch.bfloat16
+    lds = [_heads(n, x, dt) for n, x in (("q", q), ("k", k), ("v", v))]
+    rows, heads, D = q.shape
+    if k.shape != v.shape or k.shape[0] != rows or k.shape[2] != D:
+        raise ValueError("k, v: expected [rows, kv_heads, head_dim] of q's rows and head_dim")
+    R = offset.shape[0]
+    _dense("offset", offset, (R,), torch.int64)
+    _dense("length", length, (R,), torch.int32)
+    if out is None:
+        out = torch.empty((rows, heads, D), dtype=dt, device=q.device)
+    _dense("out", out, (rows, heads, D), dt)
+    _dense("lse", lse, (rows, heads), torch.float32)
+    a = Window(q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), q_ld=lds[0], k_ld=lds[1],
+               v_ld=lds[2], out=out.data_ptr(), lse=None if lse is None else lse.data_ptr(),
+               offset=offset.data_ptr(), len=length.data_ptr(), num_requests=R, max_len=max_len,
+               heads=heads, kv_heads=k.shape[1], head_dim=D,
+               dtype=F32 if dt == torch.float32 else BF16, window=window, sinks=sinks,
+               scale=scale, reserved=0)
+    _run("tav2_attend_window", q.device, stream, (ctypes.byref(a),), q, k, v, offset, length, out,
+         lse)
+    return out
+
+
+class KvCache:
+    """A tav2_kv: a paged cache of keys and values in 8 bits on the GPU (buffers as the header
+    lays them out).  `max_len` is the host's estimate of the longest sequence, by which kv_attend
+    divides its work; it may be set anew as sequences grow."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor,
+                 v_scale: torch.Tensor, k_tail: torch.Tensor, v_tail: torch.Tensor,
+                 table: torch.Tensor, length: torch.Tensor, fresh: torch.Tensor,
+                 refs: torch.Tensor, max_len: int):
+        layers, pages, heads, P, D = k.shape
+        seqs, blocks = table.shape
+        i8, f32, bf, i32 = torch.int8, torch.float32, torch.bfloat16, torch.int32
+        if P != KV_PAGE:
+            raise ValueError(f"k: expected [layers, pages, kv_heads, {KV_PAGE}, head_dim]")
+        for name, x, shape, dt in (
+                ("k", k, (layers, pages, heads, KV_PAGE, D), i8),
+                ("v", v, (layers, pages, heads, D, KV_PAGE), i8),
+                ("k_scale", k_scale, (layers, pages, heads), f32),
+                ("v_scale", v_scale, (layers, pages, heads), f32),
+                ("k_tail", k_tail, (layers, seqs, heads, KV_PAGE, D), bf),
+                ("v_tail", v_tail, (layers, seqs, heads, D, KV_PAGE), bf),
+                ("table", table, (seqs, blocks), i32), ("length", length, (seqs,), i32),
+                ("fresh", fresh, (seqs,), i32), ("refs", refs, (pages,), i32)):
+            _dense(name, x, shape, dt)
+            if x.device != k.device:
+                raise ValueError(f"{name}: on {x.device}, k on {k.device}")
+        self.device = k.device
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.k_tail, self.v_tail, self.table = k_tail, v_tail, table
+        self.length, self.fresh, self.refs = length, fresh, refs
+        self.s = Kv(k=k.data_ptr(), v=v.data_ptr(), k_scale=k_scale.data_ptr(),
+                    v_scale=v_scale.data_ptr(), k_tail=k_tail.data_ptr(), v_tail=v_tail.data_ptr(),
+                    table=table.data_ptr(), len=length.data_ptr(), fresh=fresh.data_ptr(),
+                    refs=refs.data_ptr(), num_seqs=seqs, layers=layers, pages=pages,
+                    max_blocks=blocks, kv_heads=heads, head_dim=D, max_len=max_len, reserved=0)
+
+    @classmethod
+    def create(cls, layers: int, pages: int, seqs: int, max_blocks: int, kv_heads: int,
+               head_dim: int, max_len: Optional[int] = None, device="cuda"):
+        """An empty cache (pages and tails uninitialised)."""
+        e = lambda dt, *shape: torch.empty(shape, dtype=dt, device=device)
+        i32 = dict(dtype=torch.int32, device=device)
+        P, H, D = KV_PAGE, kv_heads, head_dim
+        return cls(k=e(torch.int8, layers, pages, H, P, D), v=e(torch.int8, layers, pages, H, D, P),
+                   k_scale=e(torch.float32, layers, pages, H),
+                   v_scale=e(torch.float32, layers, pages, H),
+                   k_tail=e(torch.bfloat16, layers, seqs, H, P, D),
+                   v_tail=e(torch.bfloat16, layers, seqs, H, D, P),
+                   table=torch.full((seqs, max_blocks), -1, **i32),
+                   length=torch.zeros(seqs, **i32), fresh=torch.zeros(seqs, **i32),
+                   refs=torch.zeros(pages, **i32),
+                   max_len=max_blocks * P + P - 1 if max_len is None else max_len)
+
+    @property
+    def max_len(self) -> int:
+        return self.s.max_len
+
+    @max_len.setter
+    def max_len(self, n: int):
+        self.s.max_len = n
+
+    @property
+    def seqs(self) -> int:
+        return self.s.num_seqs
+
+
+def kv_extend(cache: KvCache, count: torch.Tensor, stream=None):
+    """tav2_kv_extend: room for count[s] (int32 [seqs]) new tokens of every sequence;
+    cache.fresh says what was granted."""
+    _dense("count", count, (cache.seqs,), torch.int32)
+    _run("tav2_kv_extend", cache.device, stream, (ctypes.byref(cache.s), count.data_ptr()), count)
+
+
+def kv_append(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, offset: torch.Tensor,
+              max_count: int, stream=None):
+    """tav2_kv_append: one layer's keys and values (bf16 [rows, kv_heads, head_dim], possibly slices
+    of one projection) of the tokens that the last kv_extend granted; sequence s's begin at row
+    offset[s] (int64 [seqs] or longer)."""
+    ld = [_heads(n, x, torch.bfloat16) for n, x in (("k", k), ("v", v))]
+    for n, x in (("k", k), ("v", v)):
+        if x.shape[1] != cache.s.kv_heads or x.shape[2] != cache.s.head_dim:
+            raise ValueError(f"{n}: expected [rows, kv_heads, head_dim] of the cache's sizes")
+    if offset.dtype != torch.int64 or offset.dim() != 1 or offset.shape[0] < cache.seqs \
+            or not offset.is_contiguous():
+        raise ValueError("offset: expected contiguous int64 [seqs] or longer")
+    _run("tav2_kv_append", cache.device, stream,
+         (ctypes.byref(cache.s), layer, k.data_ptr(), ld[0], v.data_ptr(), ld[1],
+          offset.data_ptr(), max_count), k, v, offset)
+
+
+def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, offset: torch.Tensor, max_count: int,
+              out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+              flags: int = MASK_CAUSAL, window: int = 0, sinks: int = 0, scale: float = 0.0,
+              ws: Optional[Workspace] = None, stream=None) -> torch.Tensor:
+    """tav2_kv_attend: queries q (bf16 [total, heads, head_dim]) over one layer of the cache; sequence
+    s has the queries offset[s] .. offset[s+1] (int64 [seqs + 1]), at most max_count.
+    MASK_CAUSAL: its last tokens; MASK_NONE: candidates to follow it."""
+    ld = _heads("q", q, torch.bfloat16)
+    total, heads, D = q.shape
+    if D != cache.s.head_dim:
+        raise ValueError("q: expected the cache's head_dim")
+    _dense("offset", offset, (cache.seqs + 1,), torch.int64)
+    if out is None:
+        out = torch.empty((total, heads, D), dtype=torch.bfloat16, device=q.device)
+    _dense("out", out, (total, heads, D), torch.bfloat16)
+    _dense("lse", lse, (total, heads), torch.float32)
+    a = KvQueries(q=q.data_ptr(), offset=offset.data_ptr(), total=total, ld=ld,
+                  max_count=max_count, heads=heads, window=window, sinks=sinks, scale=scale,
+                  reserved=0)
+    ws = ws or Workspace(q.device)
+    need = load_library().tav2_kv_attend_workspace(ctypes.byref(cache.s), ctypes.byref(a))
+    wp, wb = ws.get(need)
+    _run("tav2_kv_attend", cache.device, stream,
+         (ctypes.byref(cache.s), layer, ctypes.byref(a), flags, out.data_ptr(),
+          None if lse is None else lse.data_ptr(), wp, wb), q, offset, out, lse, ws.buf)
+    return out
+
+
+def kv_fork(cache: KvCache, parent: torch.Tensor, stream=None):
+    """tav2_kv_fork: empty sequences s become continuations of sequence parent[s] (int32 [seqs],
+    -1: not)."""
+    _dense("parent", parent, (cache.seqs,), torch.int32)
+    _run("tav2_kv_fork", cache.device, stream, (ctypes.byref(cache.s), parent.data_ptr()), parent)
+
+
+def kv_free(cache: KvCache, drop: torch.Tensor, stream=None):
+    """tav2_kv_free: sequences with drop[s] != 0 (uint8 [seqs]) give up their pages."""
+    _dense("drop", drop, (cache.seqs,), torch.uint8)
+    _run("tav2_kv_free", cache.device, stream, (ctypes.byref(cache.s), drop.data_ptr()), drop)
+
+
+def kv_trim(cache: KvCache, window: int, sinks: int = 0, stream=None):
+    """tav2_kv_trim: every sequence gives up the pages that this window and these sinks no longer
+    see."""
+    _run("tav2_kv_trim", cache.device, stream, (ctypes.byref(cache.s), window, sinks))
+
+
+def kv_compact(cache: KvCache, used: Optional[torch.Tensor] = None,
+               ws: Optional[Workspace] = None, stream=None) -> torch.Tensor:
+    """tav2_kv_compact: the used pages move to the front of the pool; returns their number
+    (device int32 [1])."""
+    if used is None:
+        used = torch.empty(1, dtype=torch.int32, device=cache.device)
+    _dense("used", used, (1,), torch.int32)
+    ws = ws or Workspace(cache.device)
+    wp, wb = ws.get(load_library().tav2_kv_compact_workspace(ctypes.byref(cache.s)))
+    _run("tav2_kv_compact", cache.device, stream,
+         (ctypes.byref(cache.s), used.data_ptr(), wp, wb), used, ws.buf)
+    return used
 
 
 class Batcher:

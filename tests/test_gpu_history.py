@@ -1,0 +1,571 @@
+"""Attention over whole histories on the GPU against the 64-bit oracle (oracle/history.py): the
+windowed attention of packed sequences, and the paged 8-bit cache, whose tables, counts and codes are
+compared exactly.
+
+Bounds.  A rounding to bf16 is off by at most B = 2^-8 of the value.  An output is a sum of weights
+times values, rounded once; its weights are rounded to bf16 once (bf16 path), so with
+size = sum of weights times |v|:  |error| <= B |o| + B size + what fp32 adds.  A score's fp32 dot
+product of D terms is off by at most d = (D + 4) 2^-24 reach (reach: scale * sum |q k|), and its
+exponent's argument by 2^-23 of its magnitude, which reach bounds too; both move a weight by that
+relative amount, and the normalising sum again: 2 (d + 2 reach 2^-23) size.  Sums of n weights in
+fp32 add at most n 2^-24, exponentials and reciprocals a few 2^-23."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import history
+from paper_2506_02267_amd import tav2 as T
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+P = T.KV_PAGE
+
+
+def bound(out, size, reach, n, D, dtype):
+    """(bound of the outputs' error, of lse's)."""
+    d = (D + 4) * 2.0 ** -24 * reach + 2 * 2.0 ** -23 * reach
+    fp = 2 * d + (n + 40) * 2.0 ** -23
+    half = 2.0 ** -8 if dtype == BF else 2.0 ** -24
+    weights = 2.0 ** -8 if dtype == BF else 0.0
+    tol = half * np.abs(out) + (weights + fp[..., None]) * size * (1 + 2.0 ** -7) + 1e-38
+    return tol, d + (n + 40) * 2.0 ** -23 + 2.0 ** -22 * reach
+
+
+def check(got, lse, want, D, dtype, n):
+    out, ref_lse, size, reach = want
+    g = got.double().cpu().numpy()
+    assert np.isfinite(g).all()
+    tol, ltol = bound(out, size, reach, n, D, dtype)
+    bad = np.argwhere(np.abs(g - out) > tol)
+    assert bad.size == 0, (f"{len(bad)} of {g.size} values off, worst "
+                           f"{np.max(np.abs(g - out) / tol):.2f} of its bound, first {bad[:4].tolist()}")
+    z = lse.double().cpu().numpy()
+    some = ~np.isinf(ref_lse)
+    assert (z[~some] == -np.inf).all()
+    z, ref_lse = z[some], ref_lse[some]
+    assert (np.abs(z - ref_lse) <= ltol[some] + 2.0 ** -23 * np.abs(ref_lse)).all()
+
+
+def rows(g, n, H, D, dtype=BF, scale=1.0):
+    return (torch.randn(n, H, D, generator=g) * scale).to(dtype).cuda()
+
+
+# ------------------------------------------------------------------------- attend_window
+WINDOW_CASES = [
+    # lens, heads, kv_heads, D, dtype, window, sinks
+    ([1], 1, 1, 64, BF, 0, 0),
+    ([0, 1, 2, 0], 2, 2, 32, BF, 1, 0),
+    ([63, 64, 65], 4, 4, 64, BF, 0, 0),
+    ([127, 129, 255, 257, 31], 4, 2, 64, BF, 0, 0),
+    ([300, 7, 411], 8, 2, 32, BF, 65, 3),
+    ([511, 130], 2, 1, 128, BF, 100, 1),
+    ([200, 90], 6, 2, 128, BF, 0, 0),
+    ([700], 4, 4, 64, BF, 64, 64),
+    ([700], 4, 4, 64, BF, 1, 1),
+    ([650, 20], 4, 1, 64, BF, 130, 200),
+    ([900], 3, 3, 64, BF, 899, 5),
+    ([900], 3, 3, 64, BF, 900, 5),
+    ([1200], 16, 1, 64, BF, 333, 70),
+    ([1], 1, 1, 32, F32, 0, 0),
+    ([31, 32, 33, 0, 100], 4, 4, 32, F32, 0, 0),
+    ([129, 257], 4, 2, 64, F32, 0, 0),
+    ([300, 150], 2, 1, 128, F32, 50, 2),
+    ([500], 8, 2, 64, F32, 128, 33),
+    ([400], 3, 3, 32, F32, 1, 40),
+]
+
+
+@pytest.mark.parametrize("lens,H,Hkv,D,dtype,window,sinks", WINDOW_CASES)
+def test_attend_window(lens, H, Hkv, D, dtype, window, sinks):
+    print(f"attend_window {lens} heads {H}/{Hkv} D {D} {dtype} window {window} sinks {sinks}",
+          flush=True)
+    g = torch.Generator().manual_seed(sum(lens) * 7 + H + D + window)
+    total = sum(lens)
+    q, k, v = (rows(g, total, h, D, dtype) for h in (H, Hkv, Hkv))
+    off = torch.tensor(np.concatenate([[0], np.cumsum(lens)])[:-1].astype(np.int64)).cuda()
+    length = torch.tensor(lens, dtype=torch.int32).cuda()
+    lse = torch.full((total, H), 7.0, device="cuda")
+    out = T.attend_window(q, k, v, off, length, max(lens), window=window, sinks=sinks, lse=lse)
+    torch.cuda.synchronize()
+    at = 0
+    for L in lens:
+        sl = slice(at, at + L)
+        want = history.window_attention(*(x[sl].double().cpu().numpy() for x in (q, k, v)), window, sinks)
+        check(out[sl], lse[sl], want, D, dtype, L)
+        at += L
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attend_window_slices_of_one_projection_and_rows_of_nobody(dtype):
+    """q, k and v as slices of one buffer; sequences out of order with gaps between and behind, whose
+    rows hold NaN and stay as they were; tokens past max_len are not computed."""
+    H, Hkv, D = 4, 2, 64
+    g = torch.Generator().manual_seed(3)
+    rows_total = 700
+    buf = torch.full((rows_total, H + 2 * Hkv + 1, D), float("nan"), dtype=dtype, device="cuda")
+    spans = [(400, 131), (5, 200), (230, 64), (690, 0)]
+    for a, n in spans:
+        buf[a:a + n] = rows(g, n, H + 2 * Hkv + 1, D, dtype)
+    q, k, v = buf[:, :H], buf[:, H:H + Hkv], buf[:, H + Hkv:H + 2 * Hkv]
+    out = torch.full((rows_total, H, D), 5.0, dtype=dtype, device="cuda")
+    lse = torch.full((rows_total, H), 5.0, device="cuda")
+    off = torch.tensor([a for a, _ in spans]).cuda()
+    length = torch.tensor([n for _, n in spans], dtype=torch.int32).cuda()
+    T.attend_window(q, k, v, off, length, 150, window=70, sinks=2, scale=0.2, out=out, lse=lse)
+    torch.cuda.synchronize()
+    mine = torch.zeros(rows_total, dtype=torch.bool, device="cuda")
+    for a, n in spans:
+        n = min(n, 150)
+        sl = slice(a, a + n)
+        want = history.window_attention(*(x[sl].double().cpu().numpy() for x in (q, k, v)), 70, 2, 0.2)
+        check(out[sl], lse[sl], want, D, dtype, max(n, 1))
+        mine[sl] = True
+    assert (out[~mine] == 5.0).all() and (lse[~mine] == 5.0).all()
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (BF, 128), (F32, 64)])
+def test_attend_window_extreme_scores(dtype, D):
+    """Scores of thousands, growing and falling along the sequence, as one-hot softmaxes are."""
+    L, H = 300, 2
+    g = torch.Generator().manual_seed(11)
+    q, k, v = (rows(g, L, H, D, dtype) for _ in range(3))
+    ramp = torch.linspace(-1, 1, L).view(L, 1, 1).cuda()
+    for kk in (k * 50 * (1 + ramp), k * 50 * (1 - ramp), k * 1e-30, k * 0):
+        kk = kk.to(dtype)
+        lse = torch.empty(L, H, device="cuda")
+        out = T.attend_window(q, kk, v, torch.zeros(1, dtype=torch.int64).cuda(),
+                              torch.tensor([L], dtype=torch.int32).cuda(), L, lse=lse)
+        want = history.window_attention(*(x.double().cpu().numpy() for x in (q, kk, v)))
+        check(out, lse, want, D, dtype, L)
+
+
+def test_attend_window_does_not_see_the_future():
+    """NaN and infinities in later tokens' tiles do not reach the rows of earlier tiles."""
+    L, H, D = 600, 2, 64
+    g = torch.Generator().manual_seed(12)
+    q, k, v = (rows(g, L, H, D) for _ in range(3))
+    off, length = torch.zeros(1, dtype=torch.int64).cuda(), torch.tensor([L], dtype=torch.int32).cuda()
+    want = T.attend_window(q, k, v, off, length, L)
+    k2, v2 = k.clone(), v.clone()
+    k2[576:], v2[576:] = float("nan"), float("inf")
+    got = T.attend_window(q, k2, v2, off, length, L)
+    assert torch.equal(want[:512], got[:512])
+
+
+# ------------------------------------------------------------------------- the cache's state
+def new_cache(seqs, pages, blocks, H, D, layers=1, dirty=True):
+    c = T.KvCache.create(layers, pages, seqs, blocks, H, D)
+    if dirty:   # what the buffers held before does not matter
+        for x in (c.k, c.v):
+            x.fill_(113)
+        for x in (c.k_scale, c.v_scale, c.k_tail, c.v_tail):
+            x.fill_(float("nan"))
+    return c
+
+
+class Pair:
+    """A cache on the GPU and the oracle's, driven alike."""
+
+    def __init__(self, seqs, pages, blocks, H, D, layers=1, seed=0):
+        self.gpu = new_cache(seqs, pages, blocks, H, D, layers)
+        self.ref = history.Cache(seqs, pages, blocks, layers)
+        self.g = torch.Generator().manual_seed(seed)
+        self.seqs, self.layers, self.H, self.D = seqs, layers, H, D
+
+    def grow(self, count, spread=1.0):
+        """extend + append of random tokens."""
+        off = np.concatenate([[0], np.cumsum(np.maximum(count, 0))])
+        total = int(off[-1])
+        kv = rows(self.g, max(total, 1) * self.layers, 2 * self.H, self.D, scale=spread)
+        kv = kv.view(self.layers, max(total, 1), 2 * self.H, self.D)
+        d_off = torch.from_numpy(off).cuda()
+        T.kv_extend(self.gpu, torch.tensor(count, dtype=torch.int32).cuda())
+        for layer in range(self.layers):
+            T.kv_append(self.gpu, layer, kv[layer, :, :self.H], kv[layer, :, self.H:], d_off,
+                        max(max(count), 0))
+        self.ref.extend(list(count))
+        host = kv.double().cpu().numpy()
+        self.ref.append(host[:, :, :self.H], host[:, :, self.H:], off)
+
+    def fork(self, parent):
+        T.kv_fork(self.gpu, torch.tensor(parent, dtype=torch.int32).cuda())
+        self.ref.fork(parent)
+
+    def free(self, drop):
+        T.kv_free(self.gpu, torch.tensor(drop, dtype=torch.uint8).cuda())
+        self.ref.free(drop)
+
+    def trim(self, window, sinks):
+        T.kv_trim(self.gpu, window, sinks)
+        self.ref.trim(window, sinks)
+
+    def compact(self):
+        used = T.kv_compact(self.gpu)
+        assert int(used) == self.ref.compact()
+
+    def same(self, content=True):
+        """The whole state: tables, lengths, counts, and what pages and tails hold, exactly."""
+        c, r = self.gpu, self.ref
+        torch.cuda.synchronize()
+        assert c.length.tolist() == r.len
+        assert c.fresh.tolist() == r.fresh
+        assert c.refs.tolist() == r.refs
+        table = c.table.cpu().numpy()
+        for s in range(self.seqs):
+            want = [-1 if p is None else p for p in r.table[s]]
+            assert table[s].tolist() == want + [-1] * (table.shape[1] - len(want)), s
+        if not content:
+            return
+        for s in range(self.seqs):
+            for layer in range(self.layers):
+                for b, page in enumerate(r.table[s]):
+                    if page is None:
+                        continue
+                    for rows_, codes, scale, turn in ((r.k[s], c.k, c.k_scale, False),
+                                                      (r.v[s], c.v, c.v_scale, True)):
+                        x = np.stack([t[layer] for t in rows_[b * P:(b + 1) * P]])   # [64, H, D]
+                        got = codes[layer, page].cpu().numpy()
+                        sc = scale[layer, page].cpu().numpy()
+                        for h in range(self.H):
+                            q, unit = history.quantise(x[:, h])
+                            assert np.array_equal(got[h].T if turn else got[h], q), (s, b, h, turn)
+                            assert sc[h] == np.float32(unit)
+                n = r.len[s] % P
+                if n:
+                    kt = c.k_tail[layer, s, :, :n].double().cpu().numpy()
+                    vt = c.v_tail[layer, s, :, :, :n].double().cpu().numpy()
+                    for h in range(self.H):
+                        assert np.array_equal(kt[h], [t[layer][h] for t in r.k[s][-n:]]), (s, h)
+                        assert np.array_equal(vt[h].T, [t[layer][h] for t in r.v[s][-n:]]), (s, h)
+
+
+@pytest.mark.parametrize("D,H", [(32, 3), (64, 2), (128, 1)])
+def test_append_in_steps(D, H):
+    """Tokens one by one, in chunks that end inside, at and past a block's end, and many blocks at
+    once; nothing for some sequences."""
+    p = Pair(seqs=5, pages=40, blocks=8, H=H, D=D, layers=2, seed=D)
+    for count in ([1, 63, 64, 65, 0], [1, 1, 0, 62, 200], [62, 64, 128, 1, 1], [0, 0, 0, 0, 0],
+                  [0, 0, 3, 0, 55], [1, 127, 61, 129, 0]):
+        p.grow(count)
+        p.same()
+
+
+def test_append_values_of_every_size():
+    """Blocks that are zero, tiny, huge, and full of exact halves."""
+    p = Pair(seqs=1, pages=8, blocks=8, H=1, D=64, seed=1)
+    for spread in (0.0, 2.0 ** -104, 2.0 ** -99, 1e-20, 3.0, 1e30, 2.0 ** 120):
+        p.grow([64], spread)
+    p.same()
+    q = Pair(seqs=1, pages=2, blocks=2, H=1, D=32, seed=2)
+    T.kv_extend(q.gpu, torch.tensor([128], dtype=torch.int32).cuda())
+    g = np.random.default_rng(3)
+    x = torch.from_numpy(g.integers(-254, 255, size=(128, 2, 32))).to(BF)
+    x[0], x[70] = 254, -254
+    x[64:] *= 2.0 ** -60
+    x = x.cuda()
+    T.kv_append(q.gpu, 0, x[:, :1], x[:, 1:], torch.zeros(1, dtype=torch.int64).cuda(), 128)
+    q.ref.extend([128])
+    h = x.double().cpu().numpy()[None]
+    q.ref.append(h[:, :, :1], h[:, :, 1:], [0])
+    q.same()
+
+
+def test_extend_refusals():
+    """A sequence past its table is not extended; where the pool runs dry, none from there on is,
+    and no page is lost."""
+    p = Pair(seqs=6, pages=5, blocks=3, H=1, D=32, seed=4)
+    p.grow([70, 256, 10, 64, 0, -5])       # the second would need 4 blocks
+    p.same()
+    p.grow([60, 64, 70, 130, 1, 0])        # 2 + 1 of 5 pages left for 1 + 1 + ...: the fourth is dry
+    p.same()
+    p.free([1, 0, 0, 0, 0, 0])
+    p.grow([0, 0, 0, 64, 64, 255])
+    p.same()
+    T.kv_extend(p.gpu, torch.tensor([2 ** 31 - 1] * 6, dtype=torch.int32).cuda())
+    p.ref.extend([2 ** 31 - 1] * 6)
+    p.same(content=False)
+
+
+def test_extend_many_sequences_and_pages():
+    """More sequences than threads, more pages than one step of the scan, holes everywhere."""
+    n, pages = 2500, 9000
+    c = new_cache(n, pages, 8, 1, 32, dirty=False)
+    ref = history.Cache(n, pages, 8)
+    g = np.random.default_rng(6)
+    held = g.random(pages) < 0.4
+    c.refs.copy_(torch.from_numpy(held.astype(np.int32)))
+    ref.refs = [int(x) for x in held]
+    for step in range(4):
+        count = g.integers(-20, 200, size=n) * (g.random(n) < 0.7)
+        T.kv_extend(c, torch.from_numpy(count.astype(np.int32)).cuda())
+        ref.extend([int(x) for x in count])
+        assert c.fresh.tolist() == ref.fresh, step
+        assert c.refs.tolist() == ref.refs and c.length.tolist() == ref.len
+    table = c.table.cpu().numpy()
+    for s in range(n):
+        assert table[s, :len(ref.table[s])].tolist() == ref.table[s]
+
+
+def test_fork_shares_pages_and_copies_tails():
+    p = Pair(seqs=8, pages=30, blocks=6, H=2, D=64, layers=2, seed=7)
+    p.grow([130, 64, 5, 0, 0, 0, 0, 0])
+    #          itself a child; not empty; no such sequence; an empty parent
+    p.fork([-1, -1, 0, 0, 0, 3, 99, 7])
+    p.same()
+    p.fork([-1, -1, -1, -1, -1, 2, 1, -1])
+    p.same()
+    p.grow([1, 1, 60, 62, 0, 59, 130, 64])     # the copies go their own ways
+    p.same()
+    p.free([1, 0, 0, 0, 0, 1, 0, 0])
+    p.same()
+    p.free([0, 1, 1, 1, 1, 0, 1, 1])
+    p.same()
+    assert int(p.gpu.refs.abs().sum()) == 0 and int((p.gpu.table != -1).sum()) == 0
+
+
+def test_trim_and_compact():
+    p = Pair(seqs=4, pages=64, blocks=16, H=1, D=32, layers=3, seed=8)
+    p.grow([1000, 64, 63, 640])
+    p.fork([-1, -1, -1, -1])
+    p.trim(2000, 0)
+    p.same()
+    p.trim(300, 65)
+    p.same()
+    p.trim(300, 65)       # again: nothing more
+    p.same()
+    p.compact()
+    p.same()
+    p.compact()           # again: nothing moves
+    p.same()
+    p.grow([64, 64, 64, 64])
+    p.free([0, 1, 0, 0])
+    p.compact()
+    p.same()
+    p.trim(1, 0)
+    p.same()
+    p.free([1, 1, 1, 1])
+    p.compact()
+    p.same()
+
+
+def test_random_walk():
+    """Any order of calls leaves the oracle's state."""
+    g = np.random.default_rng(9)
+    p = Pair(seqs=7, pages=60, blocks=9, H=1, D=32, layers=1, seed=10)
+    for step in range(40):
+        what = g.choice(["grow", "grow", "grow", "fork", "free", "trim", "compact"])
+        if what == "grow":
+            p.grow([int(x) for x in g.integers(0, 150, size=7) * (g.random(7) < 0.6)])
+        elif what == "fork":
+            p.fork([int(x) for x in np.where(g.random(7) < 0.4, g.integers(0, 7, size=7), -1)])
+        elif what == "free":
+            p.free([int(x) for x in g.random(7) < 0.25])
+        elif what == "trim":
+            p.trim(int(g.integers(1, 300)), int(g.integers(0, 100)))
+        else:
+            p.compact()
+        p.same(content=step % 8 == 7)
+    p.same()
+
+
+# ------------------------------------------------------------------------- kv_attend
+def attend_pair(p, n, heads, causal, window=0, sinks=0, layer=0, scale=0.0, max_len=None, seed=0):
+    """kv_attend of n[s] queries for every sequence against the oracle."""
+    g = torch.Generator().manual_seed(seed + 77)
+    off = np.concatenate([[0], np.cumsum(n)])
+    total = int(off[-1])
+    q = rows(g, total, heads + 1, p.D, scale=1.5)[:, 1:]      # a slice: rows lie further apart
+    out = torch.full((total, heads, p.D), 9.0, dtype=BF, device="cuda")
+    lse = torch.full((total, heads), 9.0, device="cuda")
+    if max_len is not None:
+        p.gpu.max_len = max_len
+    T.kv_attend(p.gpu, layer, q, torch.from_numpy(off).cuda(), max(n), out=out, lse=lse,
+                flags=T.MASK_CAUSAL if causal else T.MASK_NONE, window=window, sinks=sinks, scale=scale)
+    torch.cuda.synchronize()
+    for s in range(p.seqs):
+        sl = slice(int(off[s]), int(off[s + 1]))
+        if n[s] == 0:
+            continue
+        want = p.ref.attend(s, layer, q[sl].double().cpu().numpy(), causal, window, sinks,
+                            scale if scale else None)
+        check(out[sl], lse[sl], want, p.D, BF, p.ref.len[s])
+    return q, out, lse
+
+
+ATTEND_CASES = [
+    # lens, queries, kv_heads, heads, D, causal, window, sinks
+    ([1], [1], 1, 1, 64, True, 0, 0),
+    ([0], [3], 1, 2, 32, False, 0, 0),
+    ([5, 0, 64], [1, 1, 1], 2, 2, 64, True, 0, 0),
+    ([63, 64, 65, 128, 200], [1, 2, 3, 0, 4], 2, 4, 64, False, 0, 0),
+    ([63, 64, 65, 128, 200], [1, 64, 3, 70, 4], 2, 4, 64, True, 0, 0),
+    ([10, 300], [20, 5], 1, 1, 64, True, 0, 0),           # more queries than tokens
+    ([700, 130], [40, 7], 2, 8, 32, False, 100, 3),
+    ([700, 130], [40, 7], 2, 8, 32, True, 100, 70),
+    ([640, 641], [100, 33], 1, 4, 128, True, 129, 0),
+    ([500, 90, 64], [65, 3, 2], 2, 2, 128, False, 0, 0),
+    ([511], [300], 1, 1, 64, True, 1, 0),
+    ([1000], [3], 1, 16, 64, False, 1, 1),
+    ([2000, 3], [1, 1], 4, 4, 64, False, 0, 0),           # split over workgroups
+    ([2500, 900], [2, 1], 1, 2, 32, True, 1500, 5),
+    ([3000], [5], 1, 1, 128, False, 0, 0),
+]
+
+
+@pytest.mark.parametrize("lens,n,Hkv,H,D,causal,window,sinks", ATTEND_CASES)
+def test_kv_attend(lens, n, Hkv, H, D, causal, window, sinks):
+    print(f"kv_attend {lens} queries {n} heads {H}/{Hkv} D {D} causal {causal} window {window} "
+          f"sinks {sinks}", flush=True)
+    blocks = max(lens) // P + 1
+    p = Pair(seqs=len(lens), pages=sum(x // P for x in lens) + 2, blocks=blocks, H=Hkv, D=D, layers=2,
+             seed=sum(lens))
+    p.grow(lens)
+    attend_pair(p, n, H, causal, window, sinks, layer=1)
+
+
+def test_kv_attend_does_not_depend_on_the_estimate():
+    """max_len divides the work; far too small or large ones give the same attention."""
+    p = Pair(seqs=2, pages=40, blocks=32, H=2, D=64, seed=21)
+    p.grow([1500, 333])
+    for max_len in (0, 1, 300, 1500, 10 ** 6, 2 ** 31 - 1):
+        attend_pair(p, [2, 3], 4, False, max_len=max_len)
+
+
+def test_kv_attend_trimmed_pages_are_not_seen():
+    p = Pair(seqs=3, pages=60, blocks=20, H=1, D=64, seed=22)
+    p.grow([1000, 300, 64])
+    p.trim(200, 10)
+    attend_pair(p, [4, 4, 4], 2, False, 200, 10)      # the trimmed window: all of it is there
+    attend_pair(p, [4, 4, 4], 2, False, 0, 0)         # the whole: what is gone is not seen
+    p.trim(1, 0)
+    attend_pair(p, [2, 70, 3], 2, False, 0, 0)        # a sequence with nothing left sees nothing
+
+
+def test_kv_attend_extreme_scales():
+    """Blocks whose scales differ by many powers of two, and zero blocks."""
+    p = Pair(seqs=1, pages=10, blocks=10, H=1, D=64, seed=23)
+    for spread in (1.0, 0.0, 2.0 ** -60, 30.0, 1e-3, 2.0 ** -99, 0.5):
+        p.grow([64], spread)
+    p.grow([9])
+    attend_pair(p, [3], 1, False)
+    attend_pair(p, [3], 1, False, scale=2.0)
+    attend_pair(p, [70], 1, True, scale=1e-3)
+
+
+def test_steps_of_a_serving_loop():
+    """Histories enter, candidates are scored, new actions arrive one at a time, slates fork and
+    continue, the window moves on, pages are handed back: every attention against the oracle."""
+    p = Pair(seqs=6, pages=80, blocks=20, H=2, D=64, layers=2, seed=24)
+    p.grow([500, 70, 900, 0, 0, 0])
+    attend_pair(p, [20, 3, 1, 0, 0, 0], 4, False, seed=1)
+    for step in range(4):
+        p.grow([1, 1, 1, 0, 0, 0])
+        attend_pair(p, [1, 1, 1, 0, 0, 0], 4, True, 256, 4, layer=step % 2, seed=step)
+    p.fork([-1, -1, -1, 0, 0, 2])
+    p.grow([0, 0, 0, 5, 70, 64])
+    attend_pair(p, [0, 0, 0, 5, 70, 64], 4, True, seed=9)
+    p.trim(256, 4)
+    p.compact()
+    attend_pair(p, [7, 7, 7, 7, 7, 7], 4, False, 256, 4, layer=1, seed=10)
+    p.free([1, 0, 0, 1, 0, 0])
+    p.compact()
+    attend_pair(p, [1, 1, 1, 1, 1, 1], 2, False, 256, 4, seed=11)
+    p.same()
+
+
+def test_offsets_past_32_bits():
+    """A pool of more than 2^31 codes a side: pages at its end."""
+    pages, H, D = 135000, 4, 64
+    c = T.KvCache.create(1, pages, 2, 10, H, D)
+    assert c.k.numel() > 2 ** 31
+    c.refs.fill_(1)
+    c.refs[-6:] = 0
+    off = torch.tensor([0, 200, 400]).cuda()
+    g = torch.Generator().manual_seed(31)
+    kv = rows(g, 400, 2 * H, D)
+    T.kv_extend(c, torch.tensor([200, 200], dtype=torch.int32).cuda())
+    T.kv_append(c, 0, kv[:, :H], kv[:, H:], off, 200)
+    assert c.table[:, :3].flatten().tolist() == list(range(pages - 6, pages))
+    q = rows(g, 4, H, D)
+    lse = torch.empty(4, H, device="cuda")
+    qoff = torch.tensor([0, 2, 4]).cuda()
+    out = T.kv_attend(c, 0, q, qoff, 2, lse=lse, flags=T.MASK_NONE)
+    ref = history.Cache(2, 6, 10)
+    ref.extend([200, 200])
+    h = kv.double().cpu().numpy()[None]
+    ref.append(h[:, :, :H], h[:, :, H:], [0, 200])
+    for s in range(2):
+        want = ref.attend(s, 0, q[2 * s:2 * s + 2].double().cpu().numpy(), False)
+        check(out[2 * s:2 * s + 2], lse[2 * s:2 * s + 2], want, D, BF, 200)
+    c.refs.zero_()
+    c.refs[c.table[c.table >= 0].long()] = 1
+    assert int(T.kv_compact(c)) == 6      # from the end to the front
+    assert c.table[:, :3].flatten().tolist() == list(range(6))
+    out2 = T.kv_attend(c, 0, q, qoff, 2, flags=T.MASK_NONE)
+    assert torch.equal(out, out2)
+
+
+# ------------------------------------------------------------------------- streams, graphs
+def test_other_stream_and_repeated_calls_give_the_same_bits():
+    p = Pair(seqs=3, pages=60, blocks=32, H=2, D=64, seed=41)
+    p.grow([1500, 64, 190])
+    g = torch.Generator().manual_seed(42)
+    q = rows(g, 9, 4, 64)
+    off = torch.tensor([0, 3, 6, 9]).cuda()
+    want = T.kv_attend(p.gpu, 0, q, off, 3, flags=T.MASK_NONE)
+    wq, wk, wv = (rows(g, 333, h, 64) for h in (4, 2, 2))
+    o1, l1 = torch.zeros(1, dtype=torch.int64).cuda(), torch.tensor([333], dtype=torch.int32).cuda()
+    wwant = T.attend_window(wq, wk, wv, o1, l1, 333, window=50, sinks=1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [T.kv_attend(p.gpu, 0, q, off, 3, flags=T.MASK_NONE, stream=side) for _ in range(3)]
+    wgot = T.attend_window(wq, wk, wv, o1, l1, 333, window=50, sinks=1, stream=side)
+    side.synchronize()
+    assert all(torch.equal(want, x) for x in got) and torch.equal(wwant, wgot)
+
+
+def test_graph_of_a_decode_step():
+    """extend + append + attend + trim captured once and replayed: every replay is a step of its own
+    on the cache's state, with eager work between."""
+    H, D, steps = 2, 64, 70
+    p = Pair(seqs=2, pages=30, blocks=12, H=H, D=D, seed=51)
+    p.grow([250, 60])
+    kv = torch.empty(2, 2 * H, D, dtype=BF, device="cuda")
+    q = torch.empty(2, H, D, dtype=BF, device="cuda")
+    out = torch.empty(2, H, D, dtype=BF, device="cuda")
+    lse = torch.empty(2, H, device="cuda")
+    one = torch.ones(2, dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 1, 2]).cuda()
+    ws = T.Workspace()
+
+    def step():
+        T.kv_extend(p.gpu, one)
+        T.kv_append(p.gpu, 0, kv[:, :H], kv[:, H:], off, 1)
+        T.kv_attend(p.gpu, 0, q, off, 1, out=out, lse=lse, window=200, sinks=2, ws=ws)
+        T.kv_trim(p.gpu, 200, 2)
+
+    g = torch.Generator().manual_seed(52)
+    graph = None
+    for i in range(steps):
+        kv.copy_(rows(g, 2, 2 * H, D))
+        q.copy_(rows(g, 2, H, D))
+        if i == 1:
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                step()
+        if graph is None:
+            step()
+        else:
+            graph.replay()
+        p.ref.extend([1, 1])
+        h = kv.double().cpu().numpy()[None]
+        p.ref.append(h[:, :, :H], h[:, :, H:], [0, 1])
+        if i % 8 == 1 or i > steps - 3:
+            torch.cuda.synchronize()
+            for s in range(2):
+                want = p.ref.attend(s, 0, q[s:s + 1].double().cpu().numpy(), True, 200, 2)
+                check(out[s:s + 1], lse[s:s + 1], want, D, BF, p.ref.len[s])
+        p.ref.trim(200, 2)
+    p.same()
