@@ -8,9 +8,10 @@
 // or two 16-byte loads where V lies by feature.  No lane exchanges but the joining of the two
 // halves' maxima.
 //
-// The softmax's reference m is raised only where a score passes it by more than 2^8
-// (RAISE): the weights stay below 2^8 and the sums are fp32, so any reference within that
-// gives the same quotient, and raising it is rare after a query's first keys.
+// The softmax's reference m is raised only where a weight would pass 2^RAISE, and then to where the
+// largest is 2^ROOM: any reference gives the same quotient, the sums are fp32, and raising it is rare
+// after a query's first keys.  The room is for weights in fp16, whose least step is 2^-24: 2^-30 of
+// the largest weight.
 #pragma once
 
 #include <float.h>
@@ -19,9 +20,20 @@
 
 namespace tav2 {
 
-constexpr float RAISE = 8.f;       // in powers of two
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
+
+constexpr float RAISE = 14.f, ROOM = 6.f;
+
+__device__ __forceinline__ f32x16 mfma32(const f16x8& a, const f16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t pack2h(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, f16x2));
+}
 
 // Row of a 32-key tile that lane l % 32 = m loads, so that register r is key 16h + r.
 __device__ __forceinline__ int key_row(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
@@ -53,8 +65,8 @@ struct AttSeen {
   int sinks;
 };
 
-// s: this lane's 16 scores of query tile q before scaling (c > 0 turns them into powers of two);
-// key0: position of its first key.  Returns the weights, times 2^lv, in s; inv = 2^-lv.
+// s: this lane's 16 scores of query tile q; c s (c > 0) are powers of two; the values' scale is 2^lv =
+// 1 / inv; key0: position of the first key.  Leaves in s the weights times 2^lv, against m.
 template <int D, int QT>
 __device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16& s, float c, float lv,
                                             float inv, bool masked, const AttSeen<QT>& seen, int key0) {
@@ -69,9 +81,9 @@ __device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16& 
   float top = s[0];
 #pragma unroll
   for (int r = 1; r < 16; ++r) top = vmax(top, s[r]);
-  top = xmax32(top) * c;
+  top = __builtin_fmaf(xmax32(top), c, lv);
   if (__any(top > st.m[q] + RAISE)) {
-    const float m = top > st.m[q] ? top : st.m[q];
+    const float m = top - ROOM > st.m[q] ? top - ROOM : st.m[q];
     const float f = __builtin_amdgcn_exp2f(st.m[q] - m);
     st.m[q] = m;
     st.l[q] *= f;
@@ -97,14 +109,21 @@ __device__ __forceinline__ void att_operands(const f32x16& p, bf16x8 (&f)[2]) {
     f[t] = as_bf16x8(make_uint4(pack2(p[8 * t], p[8 * t + 1]), pack2(p[8 * t + 2], p[8 * t + 3]),
                                 pack2(p[8 * t + 4], p[8 * t + 5]), pack2(p[8 * t + 6], p[8 * t + 7])));
 }
+__device__ __forceinline__ void att_operands(const f32x16& p, f16x8 (&f)[2]) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    f[t] = __builtin_bit_cast(
+        f16x8, make_uint4(pack2h(p[8 * t], p[8 * t + 1]), pack2h(p[8 * t + 2], p[8 * t + 3]),
+                          pack2h(p[8 * t + 4], p[8 * t + 5]), pack2h(p[8 * t + 6], p[8 * t + 7])));
+}
 
 // kf[t]: the key row's features h D / 2 + 8t ..; qf the queries' likewise; vf[d][t]: feature
-// 32 d + l % 32, keys 16h + 8t ...
-template <int D, int QT>
-__device__ __forceinline__ void att_step(AttState<D, QT>& st, const bf16x8 (&kf)[D / 16],
-                                         const bf16x8 (&vf)[D / 32][2],
-                                         const bf16x8 (&qf)[QT][D / 16], float c, float lv,
-                                         float inv, bool masked, const AttSeen<QT>& seen, int key0) {
+// 32 d + l % 32, keys 16h + 8t ..; c: a lane's queries' factors.
+template <class V, int D, int QT>
+__device__ __forceinline__ void att_step(AttState<D, QT>& st, const V (&kf)[D / 16],
+                                         const V (&vf)[D / 32][2], const V (&qf)[QT][D / 16],
+                                         const float (&c)[QT], float lv, float inv, bool masked,
+                                         const AttSeen<QT>& seen, int key0) {
   f32x16 s[QT];
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
@@ -115,8 +134,8 @@ __device__ __forceinline__ void att_step(AttState<D, QT>& st, const bf16x8 (&kf)
   }
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
-    att_softmax<D, QT>(st, q, s[q], c, lv, inv, masked, seen, key0);
-    bf16x8 pf[2];
+    att_softmax<D, QT>(st, q, s[q], c[q], lv, inv, masked, seen, key0);
+    V pf[2];
     att_operands(s[q], pf);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)

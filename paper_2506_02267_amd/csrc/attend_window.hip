@@ -154,7 +154,9 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_bf16(Windo
 
   AttState<D, QT> st;
   st.clear();
-  const float c = w.scale * LOG2E;
+  float c[QT];
+#pragma unroll
+  for (int q = 0; q < QT; ++q) c[q] = w.scale * LOG2E;
   const int n = tiles.count();
   load(tiles.at(0) * TK);
   store(0);
@@ -180,7 +182,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_bf16(Windo
             vf[d][t] = as_bf16x8(*reinterpret_cast<const uint4*>(
                 lv[buf] + f * TK * 2 + ((4 * u + 2 * half + t) ^ swz_v(f)) * 16));
           }
-        att_step<D, QT>(st, kf, vf, qf, c, 0.f, 1.f, see == 1, seen, k0 + 32 * u + 16 * half);
+        att_step<bf16x8, D, QT>(st, kf, vf, qf, c, 0.f, 1.f, see == 1, seen, k0 + 32 * u + 16 * half);
       }
     }
     if (i + 1 < n) store(buf ^ 1);

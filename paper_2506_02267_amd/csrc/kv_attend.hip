@@ -4,15 +4,19 @@
 // share of the pages they see; its four waves take the pages in turn, each turning a page's codes
 // into matrix operands in its own registers, once for all 32 QT queries, and meet in LDS at
 // the end.  Nothing is staged: a lane's operand of K is half a key's codes, of V^T 16 keys of
-// one feature, both read straight from the page.  Codes are exact as bf16; a page's key scale
-// multiplies the fp32 scores, its value scale enters the weights as a power of two added to the
-// exponent.  Where queries are few, the pages are split over more workgroups, whose partial results
-// a second launch joins in a fixed order.
+// one feature, both read straight from the page, the next page's while this one is multiplied.
+// Operands are fp16, which holds codes exactly and the weights to 11 bits; a query is scaled by a
+// power of two first so that its largest feature lies in [2^14, 2^15) (features below 2^-28 of
+// that lose bits that fp32 sums would lose as well).  A page's key scale multiplies the fp32
+// scores, its value scale enters the weights as a power of two added to the exponent.  Where queries are
+// few, the pages are split over more workgroups, whose partial results a second launch joins
+// in a fixed order.
 #include <algorithm>
 
 #include "attend_core.h"
 #include "internal.h"
 #include "kv_common.h"
+#include "token_source.h"
 
 namespace tav2 {
 
@@ -52,8 +56,47 @@ __device__ __forceinline__ PageList pages_seen(int len, int64_t lo, int64_t hi, 
   return p;
 }
 
+// Codes as fp16: a byte biased to 0 .. 255 is 1024 and that much as the low bits of 0x6400.
+__device__ __forceinline__ uint32_t codes2h(uint32_t biased, uint32_t sel) {
+  const uint32_t w = __builtin_amdgcn_perm(0x64646464u, biased, sel);
+  const f16x2 x = __builtin_bit_cast(f16x2, w) - (f16x2){(_Float16)1152.f, (_Float16)1152.f};
+  return __builtin_bit_cast(uint32_t, x);
+}
+__device__ __forceinline__ f16x8 codes8h(uint32_t x, uint32_t y) {
+  x ^= 0x80808080u;
+  y ^= 0x80808080u;
+  return __builtin_bit_cast(f16x8, make_uint4(codes2h(x, 0x04010400u), codes2h(x, 0x04030402u),
+                                              codes2h(y, 0x04010400u), codes2h(y, 0x04030402u)));
+}
+
+// 8 bf16 values times f (a power of two) as fp16.
+__device__ __forceinline__ f16x8 scaled8h(const uint4& w, float f) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  uint32_t y[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    y[e] = pack2h(__uint_as_float(x[e] << 16) * f, __uint_as_float(x[e] & 0xFFFF0000u) * f);
+  return __builtin_bit_cast(f16x8, make_uint4(y[0], y[1], y[2], y[3]));
+}
+__device__ __forceinline__ float max8(const uint4& w, float m) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    m = fmaxf(m, fmaxf(__builtin_fabsf(__uint_as_float(x[e] << 16)),
+                       __builtin_fabsf(__uint_as_float(x[e] & 0xFFFF0000u))));
+  return m;
+}
+// The power of two that takes top into [2^14, 2^15), as a factor and back (tops below 2^-86 like
+// 2^-86: the factor back is a weight's, and sums of those over it stay finite).
+__device__ __forceinline__ void into_half(float top, float* f, float* back) {
+  uint32_t ex = __float_as_uint(top) >> 23;
+  ex = ex < 41 ? 41 : ex > 254 ? 254 : ex;
+  *f = __uint_as_float((268 - ex) << 23);
+  *back = __uint_as_float((ex - 14) << 23);
+}
+
 template <int D, int QT>
-__global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void kv_attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
   constexpr int KB = D / 2;   // bytes of a key's codes per lane
   __shared__ __align__(16) float mo[2][QT][D / 32][16][WAVE];
   __shared__ float mm[2][QT][2][WAVE];
@@ -75,24 +118,63 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void kv_attend_kernel(AttendA
   const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
   const int m = lane % 32, half = lane / 32;
 
-  // this lane's queries: operands, and what they see
-  bf16x8 qf[QT][D / 16];
-  AttSeen<QT> seen;
-  seen.sinks = a.q.sinks;
+  // which pages, and which of them this wave takes: every fourth of the workgroup's share
   const int64_t first_pos = a.causal ? int64_t(len) - nq : len;
   const int last_row = min(row0 + 32 * QT, rows) - 1;
   const int64_t lo_pos = a.causal ? first_pos + row0 / G : first_pos;
   const int64_t hi_pos = a.causal ? first_pos + last_row / G : first_pos;
+  const PageList list = pages_seen(len, lo_pos, hi_pos, a.q.window, a.q.sinks);
+  const int n = list.count(), chunk = (n + a.splits - 1) / a.splits;
+  const int i0 = split * chunk + wave, i1 = min(n, (split + 1) * chunk);
+  const int full = len / KVP;
+  const int32_t* table = c.table + int64_t(s) * c.max_blocks;
+  // a page that ends inside the list is the open block
+  auto page_of = [&](int i) {   // -1: released, or none
+    if (i >= i1) return -1;
+    const int b = list.at(i);
+    if (b >= full) return -1;
+    const int p = ld_meta(table + b);
+    return p < c.pages ? p : -1;
+  };
+  uint4 rk[2][D / 32], rv[2][D / 32];   // a page's codes: halves of keys, 16 keys of features
+  auto load = [&](int page, int u) {
+    const int64_t at = kv_unit(c, a.layer, page < 0 ? 0 : page, h) * KVP * D;
+    const int8_t* kp = c.k + at;
+    const int8_t* vp = c.v + at;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+      rk[u][t] = *reinterpret_cast<const uint4*>(kp + (32 * u + key_row(m)) * D + half * KB + 16 * t);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+      rv[u][d] = *reinterpret_cast<const uint4*>(vp + (32 * d + m) * KVP + 32 * u + 16 * half);
+  };
+  int page = page_of(i0);
+  load(page, 0);
+  load(page, 1);
+
+  // this lane's queries: operands, and what they see
+  f16x8 qf[QT][D / 16];
+  float cq[QT];
+  AttSeen<QT> seen;
+  seen.sinks = a.q.sinks;
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
     const int row = min(row0 + 32 * q + m, rows - 1);
     const int i = row / G, g = row % G;
     const bf16_t* p = static_cast<const bf16_t*>(a.q.q) + (q0 + i) * a.q.ld + (h * G + g) * D + half * KB;
+    uint4 w[D / 16];
+    float top = 0.f, f, back;
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) qf[q][t] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 8 * t));
+    for (int t = 0; t < D / 16; ++t) w[t] = *reinterpret_cast<const uint4*>(p + 8 * t);
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) top = max8(w[t], top);
+    into_half(xmax32(top), &f, &back);
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) qf[q][t] = scaled8h(w[t], f);
+    cq[q] = a.scale * LOG2E * back;
     const int64_t pos = a.causal ? first_pos + i : first_pos;
-    const int64_t top = pos + 1 < len ? pos + 1 : len;
-    seen.hi[q] = int(top > 0 ? top : 0);
+    const int64_t end = pos + 1 < len ? pos + 1 : len;
+    seen.hi[q] = int(end > 0 ? end : 0);
     const int64_t low = pos - a.q.window + 1;
     seen.lo[q] = a.q.window > 0 && low > 0 ? int(low) : 0;
   }
@@ -100,70 +182,105 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void kv_attend_kernel(AttendA
   // first one (or lies among the sinks)
   const int64_t all_hi = lo_pos + 1 < len ? lo_pos + 1 : len;
   const int64_t all_lo = a.q.window > 0 ? hi_pos - a.q.window + 1 : 0;
+  auto part_seen = [&](int b) {
+    return int64_t(b + 1) * KVP > all_hi ||
+           (int64_t(b) * KVP < all_lo && int64_t(b + 1) * KVP > a.q.sinks);
+  };
 
   AttState<D, QT> st;
   st.clear();
-  const PageList list = pages_seen(len, lo_pos, hi_pos, a.q.window, a.q.sinks);
-  const int n = list.count(), chunk = (n + a.splits - 1) / a.splits;
-  const int i1 = min(n, (split + 1) * chunk);
-  const int full = len / KVP;
-  const int64_t table0 = int64_t(s) * c.max_blocks;
-  const float scale = a.scale * LOG2E;
-  for (int i = split * chunk + wave; i < i1; i += 4) {
+  bool open = false;
+  for (int i = i0; i < i1; i += 4) {
     const int b = list.at(i);
-    const bool open = b >= full;   // the tail
-    int page = 0;
-    if (!open) {
-      page = c.table[table0 + b];
-      if (page < 0 || page >= c.pages) continue;   // released
+    open |= b >= full;
+    const int next = page_of(i + 4);
+    const int64_t at = kv_unit(c, a.layer, page < 0 ? 0 : page, h);
+    const float ks = ld_meta(c.k_scale + at), vs = ld_meta(c.v_scale + at);
+    const bool masked = part_seen(b);
+    float lv = __builtin_amdgcn_logf(vs), inv = 1.f / vs, cs[QT];
+#pragma unroll
+    for (int q = 0; q < QT; ++q) cs[q] = cq[q] * ks;
+    if (vs == 1.f) {   // a block of zeros, perhaps: as if at the smallest scale, so that its
+                       // weights do not raise the reference over those of small values
+      uint32_t any = 0;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) any |= rv[u][d].x | rv[u][d].y | rv[u][d].z | rv[u][d].w;
+      if (!__any(any != 0)) {
+        lv = -100.f;
+        inv = 0x1p100f;
+      }
     }
-    const int64_t at = kv_unit(c, a.layer, page, h);
-    const float cs = open ? scale : scale * c.k_scale[at];
-    const float vs = open ? 1.f : c.v_scale[at];
-    const float lv = open ? 0.f : __builtin_amdgcn_logf(vs), inv = open ? 1.f : 1.f / vs;
-    const bool masked = int64_t(b + 1) * KVP > all_hi ||
-                        (int64_t(b) * KVP < all_lo && int64_t(b + 1) * KVP > a.q.sinks);
-    const int8_t* kp = c.k + at * KVP * D;
-    const int8_t* vp = c.v + at * KVP * D;
-    const int64_t tail = kv_tail(c, a.layer, s, h);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      bf16x8 kf[D / 16], vf[D / 32][2];
-      const int kr = 32 * u + key_row(m), k0 = 32 * u + 16 * half;
-      if (!open) {
+      f16x8 kf[D / 16], vf[D / 32][2];
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t) {
-          const uint4 w = *reinterpret_cast<const uint4*>(kp + kr * D + half * KB + 16 * t);
-          kf[2 * t] = codes8(w.x, w.y);
-          kf[2 * t + 1] = codes8(w.z, w.w);
-        }
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) {
-          const uint4 w = *reinterpret_cast<const uint4*>(vp + (32 * d + m) * KVP + k0);
-          vf[d][0] = codes8(w.x, w.y);
-          vf[d][1] = codes8(w.z, w.w);
-        }
-      } else {   // bf16; what lies behind the last token is not read as numbers
-        const bf16_t* kt = c.k_tail + tail + kr * D + half * KB;
-#pragma unroll
-        for (int t = 0; t < D / 16; ++t) kf[t] = as_bf16x8(*reinterpret_cast<const uint4*>(kt + 8 * t));
-        const int held = len - b * KVP - k0;   // tokens from key k0 on
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const uint4 w =
-                *reinterpret_cast<const uint4*>(c.v_tail + tail + (32 * d + m) * KVP + k0 + 8 * t);
-            uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (8 * t + 2 * e >= held) x[e] = 0;
-              else if (8 * t + 2 * e + 1 >= held) x[e] &= 0xFFFFu;
-            }
-            vf[d][t] = as_bf16x8(make_uint4(x[0], x[1], x[2], x[3]));
-          }
+      for (int t = 0; t < D / 32; ++t) {
+        kf[2 * t] = codes8h(rk[u][t].x, rk[u][t].y);
+        kf[2 * t + 1] = codes8h(rk[u][t].z, rk[u][t].w);
       }
-      att_step<D, QT>(st, kf, vf, qf, cs, lv, inv, masked, seen, b * KVP + k0);
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) {
+        vf[d][0] = codes8h(rv[u][d].x, rv[u][d].y);
+        vf[d][1] = codes8h(rv[u][d].z, rv[u][d].w);
+      }
+      load(next, u);
+      if (page >= 0)
+        att_step<f16x8, D, QT>(st, kf, vf, qf, cs, lv, inv, masked, seen,
+                               b * KVP + 32 * u + 16 * half);
+    }
+    page = next;
+  }
+  if (open) {   // the open block, in bf16: scaled into fp16's range; what lies behind the last token is
+                // taken as zeros
+    const int64_t tail = kv_tail(c, a.layer, s, h);
+    const bool masked = part_seen(full);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int kr = 32 * u + key_row(m), k0 = 32 * u + 16 * half, held = len - full * KVP;
+      uint4 wk[D / 16], wv[D / 32][2];
+      float kt = 0.f, vt = 0.f, f, back, cs[QT];
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) {
+        wk[t] = make_uint4(0, 0, 0, 0);
+        if (kr < held)
+          wk[t] = *reinterpret_cast<const uint4*>(c.k_tail + tail + kr * D + half * KB + 8 * t);
+        kt = max8(wk[t], kt);
+      }
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const uint4 w =
+              *reinterpret_cast<const uint4*>(c.v_tail + tail + (32 * d + m) * KVP + k0 + 8 * t);
+          uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (k0 + 8 * t + 2 * e >= held) x[e] = 0;
+            else if (k0 + 8 * t + 2 * e + 1 >= held) x[e] &= 0xFFFFu;
+          }
+          wv[d][t] = make_uint4(x[0], x[1], x[2], x[3]);
+          vt = max8(wv[d][t], vt);
+        }
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) {
+        kt = fmaxf(kt, __shfl_xor(kt, o, WAVE));
+        vt = fmaxf(vt, __shfl_xor(vt, o, WAVE));
+      }
+      into_half(kt, &f, &back);
+      f16x8 kf[D / 16], vf[D / 32][2];
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) kf[t] = scaled8h(wk[t], f);
+#pragma unroll
+      for (int q = 0; q < QT; ++q) cs[q] = cq[q] * back;
+      into_half(vt, &f, &back);
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) vf[d][t] = scaled8h(wv[d][t], f);
+      att_step<f16x8, D, QT>(st, kf, vf, qf, cs, __builtin_amdgcn_logf(back), f, masked, seen,
+                             full * KVP + k0);
     }
   }
 
@@ -236,44 +353,55 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void kv_attend_kernel(AttendA
   }
 }
 
-// One wave per (query, head): the splits' parts in order, a lane two features (D 128), one, or
-// half of the lanes one.
-__global__ __launch_bounds__(64) void kv_merge_kernel(AttendArgs a, int D) {
+// A workgroup per (query, head): D features by 256 / D groups of splits, the groups joined in LDS.
+template <int D>
+__global__ __launch_bounds__(256) void kv_merge_kernel(AttendArgs a) {
+  constexpr int NG = 256 / D;
+  __shared__ float lo[NG][D], ll[NG];
   const int64_t at = blockIdx.x, n = a.q.total * a.q.heads;
-  const int lane = threadIdx.x;
+  const int tid = threadIdx.x, f = tid % D, g = tid / D;
   float M = -FLT_MAX;
-  for (int s = lane; s < a.splits; s += WAVE) M = fmaxf(M, a.part_ml[2 * (s * n + at)]);
+  for (int s = tid % WAVE; s < a.splits; s += WAVE) M = fmaxf(M, a.part_ml[2 * (s * n + at)]);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, WAVE));
-  float l = 0.f, x0 = 0.f, x1 = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
+  float l = 0.f, x = 0.f;
+#pragma unroll 4
+  for (int s = g; s < a.splits; s += NG) {
     const int64_t p = s * n + at;
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * p] - M);
-    l += a.part_ml[2 * p + 1] * f;
-    if (lane < D) x0 += a.part_o[p * D + lane] * f;
-    if (lane + WAVE < D) x1 += a.part_o[p * D + lane + WAVE] * f;
+    const float w = __builtin_amdgcn_exp2f(a.part_ml[2 * p] - M);
+    l += a.part_ml[2 * p + 1] * w;
+    x += a.part_o[p * D + f] * w;
+  }
+  lo[g][f] = x;
+  if (f == 0) ll[g] = l;
+  __syncthreads();
+  if (g) return;
+#pragma unroll
+  for (int j = 1; j < NG; ++j) {
+    x += lo[j][f];
+    l += ll[j];
   }
   const bool some = l > 0.f || l != l;
-  const float inv = some ? 1.f / l : 0.f;
-  if (lane < D) a.out[at * D + lane] = f2bf(x0 * inv);
-  if (lane + WAVE < D) a.out[at * D + lane + WAVE] = f2bf(x1 * inv);
-  if (a.lse && lane == 0) a.lse[at] = some ? (M + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
+  a.out[at * D + f] = f2bf(some ? x / l : 0.f);
+  if (a.lse && f == 0) a.lse[at] = some ? (M + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
 }
 
 int query_tiles(const tav2_kv& c, const tav2_kv_queries& q) {
   return int64_t(q.max_count) * (q.heads / c.kv_heads) > 32 && c.head_dim <= 64 ? 2 : 1;
 }
 
-// Shares of a sequence's pages: enough workgroups for two per CU, no share below one page
-// per wave.
+// Shares of a sequence's pages: enough workgroups to fill the CUs and to even out sequences of
+// different lengths, but no share so small that its partial results (4 bytes a feature, written and
+// read) come near the pages it reads (2 bytes a feature of 64 tokens).
 int key_splits(const tav2_kv& c, const tav2_kv_queries& q) {
   const int64_t rows = int64_t(q.max_count) * (q.heads / c.kv_heads);
   const int64_t seqs = q.total < c.num_seqs ? q.total : c.num_seqs;
   const int64_t groups = seqs * c.kv_heads * cdiv(rows, 32 * query_tiles(c, q));
   int64_t tokens = c.max_len;
   if (q.window > 0) tokens = std::min(tokens, int64_t(q.window) + q.max_count + q.sinks + 2 * KVP);
-  const int64_t most = std::max<int64_t>(1, tokens / (4 * KVP));
-  return int(std::max<int64_t>(1, std::min(most, 512 / std::max<int64_t>(1, groups))));
+  const int64_t least = std::max<int64_t>(4, std::min<int64_t>(rows, 32 * query_tiles(c, q)) / 2);
+  const int64_t most = std::max<int64_t>(1, tokens / (least * KVP));
+  return int(std::max<int64_t>(1, std::min(most, 1024 / std::max<int64_t>(1, groups))));
 }
 
 }  // namespace
@@ -321,7 +449,10 @@ hipError_t launch_kv_attend(const tav2_kv& c, int layer, const tav2_kv_queries& 
   }
   if (a.splits > 1) {
     ProfScope prof("kv_merge", st);
-    kv_merge_kernel<<<unsigned(q.total * q.heads), 64, 0, st>>>(a, c.head_dim);
+    const unsigned n = unsigned(q.total * q.heads);
+    if (c.head_dim == 32) kv_merge_kernel<32><<<n, 256, 0, st>>>(a);
+    else if (c.head_dim == 64) kv_merge_kernel<64><<<n, 256, 0, st>>>(a);
+    else kv_merge_kernel<128><<<n, 256, 0, st>>>(a);
   }
   return hipGetLastError();
 }

@@ -8,7 +8,12 @@ size = sum of weights times |v|:  |error| <= B |o| + B size + what fp32 adds.  A
 product of D terms is off by at most d = (D + 4) 2^-24 reach (reach: scale * sum |q k|), and its
 exponent's argument by 2^-23 of its magnitude, which reach bounds too; both move a weight by that
 relative amount, and the normalising sum again: 2 (d + 2 reach 2^-23) size.  Sums of n weights in
-fp32 add at most n 2^-24, exponentials and reciprocals a few 2^-23."""
+fp32 add at most n 2^-24, exponentials and reciprocals a few 2^-23.
+
+The cache's weights are fp16 (times the values' scale, against a reference that keeps the largest
+such product at 2^6 or more): off by at most 2^-11 of the weight, or by half the least step, 2^-25,
+which is 2^-31 of the largest product.  A key's code is at most 127, and 127 times the largest
+product's scale is at most the largest |v|, so the latter adds at most n 2^-31 max|v|."""
 import numpy as np
 import pytest
 import torch
@@ -22,21 +27,26 @@ BF, F32 = torch.bfloat16, torch.float32
 P = T.KV_PAGE
 
 
-def bound(out, size, reach, n, D, dtype):
+HALF = "fp16 weights"
+
+
+def bound(out, size, reach, n, D, dtype, vmax=0.0):
     """(bound of the outputs' error, of lse's)."""
     d = (D + 4) * 2.0 ** -24 * reach + 2 * 2.0 ** -23 * reach
     fp = 2 * d + (n + 40) * 2.0 ** -23
-    half = 2.0 ** -8 if dtype == BF else 2.0 ** -24
-    weights = 2.0 ** -8 if dtype == BF else 0.0
+    half = 2.0 ** -24 if dtype == F32 else 2.0 ** -8
+    weights = {BF: 2.0 ** -8, HALF: 2.0 ** -11, F32: 0.0}[dtype]
     tol = half * np.abs(out) + (weights + fp[..., None]) * size * (1 + 2.0 ** -7) + 1e-38
+    if dtype == HALF:
+        tol = tol + n * 2.0 ** -31 * vmax
     return tol, d + (n + 40) * 2.0 ** -23 + 2.0 ** -22 * reach
 
 
-def check(got, lse, want, D, dtype, n):
+def check(got, lse, want, D, dtype, n, vmax=0.0):
     out, ref_lse, size, reach = want
     g = got.double().cpu().numpy()
     assert np.isfinite(g).all()
-    tol, ltol = bound(out, size, reach, n, D, dtype)
+    tol, ltol = bound(out, size, reach, n, D, dtype, vmax)
     bad = np.argwhere(np.abs(g - out) > tol)
     assert bad.size == 0, (f"{len(bad)} of {g.size} values off, worst "
                            f"{np.max(np.abs(g - out) / tol):.2f} of its bound, first {bad[:4].tolist()}")
@@ -203,6 +213,9 @@ class Pair:
     def compact(self):
         used = T.kv_compact(self.gpu)
         assert int(used) == self.ref.compact()
+
+    def vmax(self, s, layer):
+        return max((float(np.abs(t[layer]).max()) for t in self.ref.v[s]), default=0.0)
 
     def same(self, content=True):
         """The whole state: tables, lengths, counts, and what pages and tails hold, exactly."""
@@ -389,7 +402,7 @@ def attend_pair(p, n, heads, causal, window=0, sinks=0, layer=0, scale=0.0, max_
             continue
         want = p.ref.attend(s, layer, q[sl].double().cpu().numpy(), causal, window, sinks,
                             scale if scale else None)
-        check(out[sl], lse[sl], want, p.D, BF, p.ref.len[s])
+        check(out[sl], lse[sl], want, p.D, HALF, p.ref.len[s], p.vmax(s, layer))
     return q, out, lse
 
 
@@ -497,7 +510,8 @@ def test_offsets_past_32_bits():
     ref.append(h[:, :, :H], h[:, :, H:], [0, 200])
     for s in range(2):
         want = ref.attend(s, 0, q[2 * s:2 * s + 2].double().cpu().numpy(), False)
-        check(out[2 * s:2 * s + 2], lse[2 * s:2 * s + 2], want, D, BF, 200)
+        check(out[2 * s:2 * s + 2], lse[2 * s:2 * s + 2], want, D, HALF, 200,
+              float(kv.abs().max()))
     c.refs.zero_()
     c.refs[c.table[c.table >= 0].long()] = 1
     assert int(T.kv_compact(c)) == 6      # from the end to the front
@@ -566,6 +580,6 @@ def test_graph_of_a_decode_step():
             torch.cuda.synchronize()
             for s in range(2):
                 want = p.ref.attend(s, 0, q[s:s + 1].double().cpu().numpy(), True, 200, 2)
-                check(out[s:s + 1], lse[s:s + 1], want, D, BF, p.ref.len[s])
+                check(out[s:s + 1], lse[s:s + 1], want, D, HALF, p.ref.len[s], p.vmax(s, 0))
         p.ref.trim(200, 2)
     p.same()
