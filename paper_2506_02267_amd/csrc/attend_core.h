@@ -71,12 +71,10 @@ template <int D, int QT>
 __device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16& s, float c, float lv,
                                             float inv, bool masked, const AttSeen<QT>& seen, int key0) {
   if (masked) {
+    // against register numbers: nothing for each key is left to be prepared where nothing is masked
+    const int hi = seen.hi[q] - key0, lo = seen.lo[q] - key0, sinks = seen.sinks - key0;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int key = key0 + r;
-      const bool see = key < seen.hi[q] && (key >= seen.lo[q] || key < seen.sinks);
-      s[r] = see ? s[r] : -INFINITY;
-    }
+    for (int r = 0; r < 16; ++r) s[r] = r < hi && (r >= lo || r < sinks) ? s[r] : -INFINITY;
   }
   float top = s[0];
 #pragma unroll

@@ -115,8 +115,8 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
   const int rows = int(nq) * G, row0 = tile * 32 * QT;
   if (row0 >= rows) return;
   const int len = kv_len(c, s);
-  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
-  const int m = lane % 32, half = lane / 32;
+  const int lane = threadIdx.x % WAVE, m = lane % 32, half = lane / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);   // (scalar page arithmetic)
 
   // which pages, and which of them this wave takes: every fourth of the workgroup's share
   const int64_t first_pos = a.causal ? int64_t(len) - nq : len;
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
     const int64_t at = kv_unit(c, a.layer, page < 0 ? 0 : page, h);
     const float ks = ld_meta(c.k_scale + at), vs = ld_meta(c.v_scale + at);
     const bool masked = part_seen(b);
-    float lv = __builtin_amdgcn_logf(vs), inv = 1.f / vs, cs[QT];
+    float lv = __builtin_amdgcn_logf(vs), inv = __builtin_amdgcn_rcpf(vs), cs[QT];
 #pragma unroll
     for (int q = 0; q < QT; ++q) cs[q] = cq[q] * ks;
     if (vs == 1.f) {   // a block of zeros, perhaps: as if at the smallest scale, so that its
@@ -401,7 +401,7 @@ int key_splits(const tav2_kv& c, const tav2_kv_queries& q) {
   if (q.window > 0) tokens = std::min(tokens, int64_t(q.window) + q.max_count + q.sinks + 2 * KVP);
   const int64_t least = std::max<int64_t>(4, std::min<int64_t>(rows, 32 * query_tiles(c, q)) / 2);
   const int64_t most = std::max<int64_t>(1, tokens / (least * KVP));
-  return int(std::max<int64_t>(1, std::min(most, 1024 / std::max<int64_t>(1, groups))));
+  return int(std::max<int64_t>(1, std::min(most, 2048 / std::max<int64_t>(1, groups))));
 }
 
 }  // namespace
