@@ -115,31 +115,38 @@ __device__ __forceinline__ void att_operands(const f32x16& p, f16x8 (&f)[2]) {
                           pack2h(p[8 * t + 4], p[8 * t + 5]), pack2h(p[8 * t + 6], p[8 * t + 7])));
 }
 
-// kf[t]: the key row's features h D / 2 + 8t ..; qf the queries' likewise; vf[d][t]: feature
-// 32 d + l % 32, keys 16h + 8t ..; c: a lane's queries' factors.
-template <class V, int D, int QT>
-__device__ __forceinline__ void att_step(AttState<D, QT>& st, const V (&kf)[D / 16],
-                                         const V (&vf)[D / 32][2], const V (&qf)[QT][D / 16],
-                                         const float (&c)[QT], float lv, float inv, bool masked,
-                                         const AttSeen<QT>& seen, int key0) {
+// keys(kf) sets kf[t]: operand of the key row's features h D / 2 + 8t ..; qf the queries' likewise; values(vf) sets
+// vf[d][t]: feature 32 d + l % 32, keys 16h + 8t ..; c: a lane's queries' factors.
+template <class V, int D, int QT, class Keys, class Values>
+__device__ __forceinline__ void att_step(AttState<D, QT>& st, Keys keys, Values values,
+                                         const V (&qf)[QT][D / 16], const float (&c)[QT], float lv,
+                                         float inv, bool masked, const AttSeen<QT>& seen, int key0) {
   f32x16 s[QT];
+  {
+    V kf[D / 16];
+    keys(kf);
 #pragma unroll
-  for (int q = 0; q < QT; ++q) {
+    for (int q = 0; q < QT; ++q) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[q][r] = 0.f;
+      for (int r = 0; r < 16; ++r) s[q][r] = 0.f;
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) s[q] = mfma32(kf[t], qf[q][t], s[q]);
+      for (int t = 0; t < D / 16; ++t) s[q] = mfma32(kf[t], qf[q][t], s[q]);
+    }
   }
+  V pf[QT][2];
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
     att_softmax<D, QT>(st, q, s[q], c[q], lv, inv, masked, seen, key0);
-    V pf[2];
-    att_operands(s[q], pf);
+    att_operands(s[q], pf[q]);
+  }
+  V vf[D / 32][2];
+  values(vf);
+#pragma unroll
+  for (int q = 0; q < QT; ++q)
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) st.o[d][q] = mfma32(vf[d][t], pf[t], st.o[d][q]);
-  }
+      for (int t = 0; t < 2; ++t) st.o[d][q] = mfma32(vf[d][t], pf[q][t], st.o[d][q]);
 }
 
 }  // namespace tav2

@@ -168,21 +168,25 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_bf16(Windo
     if (see) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        bf16x8 kf[D / 16], vf[D / 32][2];
-        const int row = 32 * u + key_row(m);
+        auto keys = [&](bf16x8(&kf)[D / 16]) {
+          const int row = 32 * u + key_row(m);
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t)
-          kf[t] = as_bf16x8(*reinterpret_cast<const uint4*>(
-              lk[buf] + row * D * 2 + ((half * (D / 16) + t) ^ swz_k<D>(row)) * 16));
+          for (int t = 0; t < D / 16; ++t)
+            kf[t] = as_bf16x8(*reinterpret_cast<const uint4*>(
+                lk[buf] + row * D * 2 + ((half * (D / 16) + t) ^ swz_k<D>(row)) * 16));
+        };
+        auto values = [&](bf16x8(&vf)[D / 32][2]) {
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d)
+          for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const int f = 32 * d + m;
-            vf[d][t] = as_bf16x8(*reinterpret_cast<const uint4*>(
-                lv[buf] + f * TK * 2 + ((4 * u + 2 * half + t) ^ swz_v(f)) * 16));
-          }
-        att_step<bf16x8, D, QT>(st, kf, vf, qf, c, 0.f, 1.f, see == 1, seen, k0 + 32 * u + 16 * half);
+            for (int t = 0; t < 2; ++t) {
+              const int f = 32 * d + m;
+              vf[d][t] = as_bf16x8(*reinterpret_cast<const uint4*>(
+                  lv[buf] + f * TK * 2 + ((4 * u + 2 * half + t) ^ swz_v(f)) * 16));
+            }
+        };
+        att_step<bf16x8, D, QT>(st, keys, values, qf, c, 0.f, 1.f, see == 1, seen,
+                                k0 + 32 * u + 16 * half);
       }
     }
     if (i + 1 < n) store(buf ^ 1);

@@ -3,8 +3,11 @@
 // A workgroup takes 32 QT queries of one kv head (the heads that share it count as queries) and a
 // share of the pages they see; its four waves take the pages in turn, each turning a page's codes
 // into matrix operands in its own registers, once for all 32 QT queries, and meet in LDS at
-// the end.  Nothing is staged: a lane's operand of K is half a key's codes, of V^T 16 keys of
-// one feature, both read straight from the page, the next page's while this one is multiplied.
+// the end.  A wave reads a page as it lies, a kilobyte a load, into registers (the next page's
+// loads are in flight while this one is multiplied), and passes it through its own part of LDS,
+// where a lane then reads its operands: half a key's codes, and 16 keys of one feature of V^T.  (Each
+// lane reading its operands from the page itself took 115 cycles of the address path a load: 44 us
+// for 64 users' new actions.)
 // Operands are fp16, which holds codes exactly and the weights to 11 bits; a query is scaled by a
 // power of two first so that its largest feature lies in [2^14, 2^15) (features below 2^-28 of
 // that lose bits that fp32 sums would lose as well).  A page's key scale multiplies the fp32
@@ -22,6 +25,8 @@ namespace tav2 {
 
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 struct AttendArgs {
   tav2_kv c;
   int layer;
@@ -33,9 +38,11 @@ struct AttendArgs {
   float* part_o;     // [splits, total, heads, D], with splits > 1
   float* part_ml;    // [splits, total, heads, 2]: reference and sum
   int tiles;         // query tiles per (sequence, kv head)
-  int splits;
+  int splits, chunk; // shares of a sequence's pages, and pages to a share
   int units;         // (sequence, kv head, split) groups, padded to a multiple of 8
 };
+
+constexpr int SHARES = 2048;   // workgroups that a launch is divided into, about
 
 // The pages that a tile's queries see: [0, sink) and [first, last), counted through.
 struct PageList {
@@ -69,6 +76,16 @@ __device__ __forceinline__ f16x8 codes8h(uint32_t x, uint32_t y) {
                                               codes2h(y, 0x04010400u), codes2h(y, 0x04030402u)));
 }
 
+// Places of a row's 16-byte pieces in LDS, xor'ed: the rows that 8 or 16 neighbouring lanes read
+// (key_row: 0 .. 3, 16 .. 19, 4 .. 7, 20 .. 23, and on; features: one after the other) lie in
+// different banks.
+template <int D>
+__device__ __forceinline__ int swz_key(int r) {
+  const int b0 = r & 1, b1 = (r >> 1) & 1, b2 = (r >> 2) & 1, b4 = (r >> 4) & 1;
+  return D == 32 ? b4 : D == 64 ? (b1 ^ b2) | b4 << 1 : (b0 ^ b2) | b1 << 1 | b4 << 2;
+}
+__device__ __forceinline__ int swz_feature(int d) { return ((d >> 2) & 1) | (((d >> 1) ^ (d >> 3)) & 1) << 1; }
+
 // 8 bf16 values times f (a power of two) as fp16.
 __device__ __forceinline__ f16x8 scaled8h(const uint4& w, float f) {
   const uint32_t x[4] = {w.x, w.y, w.z, w.w};
@@ -98,8 +115,11 @@ __device__ __forceinline__ void into_half(float top, float* f, float* back) {
 template <int D, int QT>
 __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
   constexpr int KB = D / 2;   // bytes of a key's codes per lane
-  __shared__ __align__(16) float mo[2][QT][D / 32][16][WAVE];
-  __shared__ float mm[2][QT][2][WAVE];
+  // a wave's page on its way, then its state
+  constexpr int STAGE = QT * D / 32 * 4 * WAVE;   // 16-byte pieces; a page has 8 D of them
+  static_assert(STAGE >= 8 * D, "a page fits");
+  __shared__ u32x4 stage[4][STAGE];
+  __shared__ float mm[4][QT][2][WAVE];
   const tav2_kv& c = a.c;
   const int H = c.kv_heads, G = a.q.heads / H;
   // units (which share K and V) on one XCD: a unit's query tiles are 8 apart, and so on
@@ -124,33 +144,59 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
   const int64_t lo_pos = a.causal ? first_pos + row0 / G : first_pos;
   const int64_t hi_pos = a.causal ? first_pos + last_row / G : first_pos;
   const PageList list = pages_seen(len, lo_pos, hi_pos, a.q.window, a.q.sinks);
-  const int n = list.count(), chunk = (n + a.splits - 1) / a.splits;
+  const int n = list.count();
+  // shares of one size, so that a long sequence has more of them (larger ones where it is
+  // longer than the host's estimate)
+  const int chunk = max(a.chunk, (n + a.splits - 1) / a.splits);
+  if (a.splits > 1 && split * chunk >= n) {   // an empty share: no sum, and kv_merge reads no more of it
+    const int row = row0 + int(threadIdx.x);
+    if (threadIdx.x < 32 * QT && row < rows) {
+      const int64_t part = int64_t(split) * a.q.total * a.q.heads + (q0 + row / G) * a.q.heads +
+                           h * G + row % G;
+      a.part_ml[2 * part] = -FLT_MAX;
+      a.part_ml[2 * part + 1] = 0.f;
+    }
+    return;
+  }
   const int i0 = split * chunk + wave, i1 = min(n, (split + 1) * chunk);
   const int full = len / KVP;
   const int32_t* table = c.table + int64_t(s) * c.max_blocks;
-  // a page that ends inside the list is the open block
-  auto page_of = [&](int i) {   // -1: released, or none
-    if (i >= i1) return -1;
-    const int b = list.at(i);
-    if (b >= full) return -1;
-    const int p = ld_meta(table + b);
-    return p < c.pages ? p : -1;
+  // this wave's next 64 pages, one a lane: number (-1: released, or the open block), key scale, and
+  // the value scale as a power of two and reciprocal.  Read once, so that no page waits for
+  // a chain of small loads.
+  int ids = -1;
+  float kss = 1.f, lvs = 0.f, invs = 1.f;
+  auto look_up = [&](int base) {
+    const int i = base + 4 * lane;
+    const int b = i < i1 ? list.at(i) : full;
+    ids = b < full ? table[b] : -1;
+    if (ids >= c.pages) ids = -1;
+    if (ids < 0) return;
+    const int64_t at = kv_unit(c, a.layer, ids, h);
+    const float vs = c.v_scale[at];
+    kss = c.k_scale[at];
+    lvs = __builtin_amdgcn_logf(vs);
+    invs = __builtin_amdgcn_rcpf(vs);
   };
-  uint4 rk[2][D / 32], rv[2][D / 32];   // a page's codes: halves of keys, 16 keys of features
-  auto load = [&](int page, int u) {
+  auto lane_f = [](float v, int t) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), t));
+  };
+  u32x4 rk[D / 16], rv[D / 16];   // a page's codes as they lie
+  auto load = [&](int page) {
     const int64_t at = kv_unit(c, a.layer, page < 0 ? 0 : page, h) * KVP * D;
-    const int8_t* kp = c.k + at;
-    const int8_t* vp = c.v + at;
+    const u32x4* kp = reinterpret_cast<const u32x4*>(c.k + at) + lane;
+    const u32x4* vp = reinterpret_cast<const u32x4*>(c.v + at) + lane;
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t)
-      rk[u][t] = *reinterpret_cast<const uint4*>(kp + (32 * u + key_row(m)) * D + half * KB + 16 * t);
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-      rv[u][d] = *reinterpret_cast<const uint4*>(vp + (32 * d + m) * KVP + 32 * u + 16 * half);
+    for (int i = 0; i < D / 16; ++i) {
+      rk[i] = kp[i * WAVE];
+      rv[i] = vp[i * WAVE];
+    }
   };
-  int page = page_of(i0);
-  load(page, 0);
-  load(page, 1);
+  u32x4* const my = stage[wave];
+  constexpr int KC = D / 16, VC = KVP / 16;   // pieces of a key, and of a feature's 64 keys
+  look_up(i0);
+  int page = __builtin_amdgcn_readlane(ids, 0);
+  load(page);
 
   // this lane's queries: operands, and what they see
   f16x8 qf[QT][D / 16];
@@ -190,45 +236,65 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
   AttState<D, QT> st;
   st.clear();
   bool open = false;
-  for (int i = i0; i < i1; i += 4) {
+  for (int i = i0, t = 0; i < i1; i += 4, ++t) {
+    if (t == WAVE) {
+      t = 0;
+      look_up(i);
+      page = __builtin_amdgcn_readlane(ids, 0);
+      load(page);
+    }
     const int b = list.at(i);
     open |= b >= full;
-    const int next = page_of(i + 4);
-    const int64_t at = kv_unit(c, a.layer, page < 0 ? 0 : page, h);
-    const float ks = ld_meta(c.k_scale + at), vs = ld_meta(c.v_scale + at);
+    const int next = t + 1 < WAVE ? __builtin_amdgcn_readlane(ids, t + 1) : -1;
     const bool masked = part_seen(b);
-    float lv = __builtin_amdgcn_logf(vs), inv = __builtin_amdgcn_rcpf(vs), cs[QT];
+    const float ks = lane_f(kss, t);
+    float lv = lane_f(lvs, t), inv = lane_f(invs, t), cs[QT];
 #pragma unroll
     for (int q = 0; q < QT; ++q) cs[q] = cq[q] * ks;
-    if (vs == 1.f) {   // a block of zeros, perhaps: as if at the smallest scale, so that its
-                       // weights do not raise the reference over those of small values
+    if (lv == 0.f) {   // scale 1: a block of zeros, perhaps: taken as if at the smallest
+                       // scale, so that its weights do not raise the reference over small values
       uint32_t any = 0;
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) any |= rv[u][d].x | rv[u][d].y | rv[u][d].z | rv[u][d].w;
+      for (int e = 0; e < D / 16; ++e) any |= rv[e].x | rv[e].y | rv[e].z | rv[e].w;
       if (!__any(any != 0)) {
         lv = -100.f;
         inv = 0x1p100f;
       }
     }
+    // (a wave's LDS operations are done in order; the barriers keep the compiler to it)
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f16x8 kf[D / 16], vf[D / 32][2];
+    for (int e = 0; e < D / 16; ++e) {
+      const int i = e * WAVE + lane, kr = i / KC, vr = i / VC;
+      my[kr * KC + ((i % KC) ^ swz_key<D>(kr))] = rk[e];
+      my[4 * D + vr * VC + ((i % VC) ^ swz_feature(vr))] = rv[e];
+    }
+    __builtin_amdgcn_wave_barrier();
+    load(next);
+    if (page >= 0) {
+#pragma unroll 1   // (both halves at once take too many registers)
+      for (int u = 0; u < 2; ++u) {
+        auto keys = [&](f16x8(&kf)[D / 16]) {
+          const int kr = 32 * u + key_row(m);
 #pragma unroll
-      for (int t = 0; t < D / 32; ++t) {
-        kf[2 * t] = codes8h(rk[u][t].x, rk[u][t].y);
-        kf[2 * t + 1] = codes8h(rk[u][t].z, rk[u][t].w);
-      }
+          for (int t = 0; t < D / 32; ++t) {
+            const u32x4 w = my[kr * KC + ((half * (D / 32) + t) ^ swz_key<D>(key_row(m)))];
+            kf[2 * t] = codes8h(w.x, w.y);
+            kf[2 * t + 1] = codes8h(w.z, w.w);
+          }
+        };
+        auto values = [&](f16x8(&vf)[D / 32][2]) {
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d) {
-        vf[d][0] = codes8h(rv[u][d].x, rv[u][d].y);
-        vf[d][1] = codes8h(rv[u][d].z, rv[u][d].w);
-      }
-      load(next, u);
-      if (page >= 0)
-        att_step<f16x8, D, QT>(st, kf, vf, qf, cs, lv, inv, masked, seen,
+          for (int d = 0; d < D / 32; ++d) {
+            const int vr = 32 * d + m;
+            const u32x4 w = my[4 * D + vr * VC + ((2 * u + half) ^ swz_feature(m))];
+            vf[d][0] = codes8h(w.x, w.y);
+            vf[d][1] = codes8h(w.z, w.w);
+          }
+        };
+        att_step<f16x8, D, QT>(st, keys, values, qf, cs, lv, inv, masked, seen,
                                b * KVP + 32 * u + 16 * half);
+      }
     }
     page = next;
   }
@@ -236,7 +302,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
                 // taken as zeros
     const int64_t tail = kv_tail(c, a.layer, s, h);
     const bool masked = part_seen(full);
-#pragma unroll
+#pragma unroll 1
     for (int u = 0; u < 2; ++u) {
       const int kr = 32 * u + key_row(m), k0 = 32 * u + 16 * half, held = len - full * KVP;
       uint4 wk[D / 16], wv[D / 32][2];
@@ -269,87 +335,84 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
         vt = fmaxf(vt, __shfl_xor(vt, o, WAVE));
       }
       into_half(kt, &f, &back);
-      f16x8 kf[D / 16], vf[D / 32][2];
-#pragma unroll
-      for (int t = 0; t < D / 16; ++t) kf[t] = scaled8h(wk[t], f);
+      float fv, backv;
+      into_half(vt, &fv, &backv);
 #pragma unroll
       for (int q = 0; q < QT; ++q) cs[q] = cq[q] * back;
-      into_half(vt, &f, &back);
+      auto keys = [&](f16x8(&kf)[D / 16]) {
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d)
+        for (int t = 0; t < D / 16; ++t) kf[t] = scaled8h(wk[t], f);
+      };
+      auto values = [&](f16x8(&vf)[D / 32][2]) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) vf[d][t] = scaled8h(wv[d][t], f);
-      att_step<f16x8, D, QT>(st, kf, vf, qf, cs, __builtin_amdgcn_logf(back), f, masked, seen,
-                             full * KVP + k0);
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) vf[d][t] = scaled8h(wv[d][t], fv);
+      };
+      att_step<f16x8, D, QT>(st, keys, values, qf, cs, __builtin_amdgcn_logf(backv), fv, masked,
+                             seen, full * KVP + k0);
     }
   }
 
-  // the four waves' states joined, two at a time: waves 2 and 3 into 0 and 1, then 1 into 0
-#pragma unroll
-  for (int q = 0; q < QT; ++q) st.l[q] = xsum32(st.l[q]);
-#pragma unroll
-  for (int step = 2; step >= 1; step /= 2) {
-    if (wave >= step && wave < 2 * step) {
-#pragma unroll
-      for (int q = 0; q < QT; ++q) {
-        mm[wave - step][q][0][lane] = st.m[q];
-        mm[wave - step][q][1][lane] = st.l[q];
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) mo[wave - step][q][d][r][lane] = st.o[d][q][r];
-      }
-    }
-    __syncthreads();
-    if (wave < step) {
-#pragma unroll
-      for (int q = 0; q < QT; ++q) {
-        const float m2 = mm[wave][q][0][lane], l2 = mm[wave][q][1][lane];
-        const float M = m2 > st.m[q] ? m2 : st.m[q];
-        const float f1 = __builtin_amdgcn_exp2f(st.m[q] - M), f2 = __builtin_amdgcn_exp2f(m2 - M);
-        st.m[q] = M;
-        st.l[q] = st.l[q] * f1 + l2 * f2;
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            st.o[d][q][r] = st.o[d][q][r] * f1 + mo[wave][q][d][r][lane] * f2;
-      }
-    }
-    __syncthreads();
-  }
-  if (wave != 0) return;
+  __builtin_amdgcn_wave_barrier();
+  // the four waves' states meet in LDS; wave w then joins registers 4w .. 4w + 3 of each tile (in the
+  // order of the waves), features 8w + 4 half .. of it
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
-    const int row = row0 + 32 * q + m;
-    if (row >= rows) continue;
-    const int64_t at = (q0 + row / G) * a.q.heads + h * G + row % G;
-    const float l = st.l[q];
-    if (a.splits > 1) {
-      const int64_t p = int64_t(split) * a.q.total * a.q.heads + at;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          *reinterpret_cast<float4*>(a.part_o + p * D + 32 * d + 8 * j + 4 * half) =
-              make_float4(st.o[d][q][4 * j], st.o[d][q][4 * j + 1], st.o[d][q][4 * j + 2],
-                          st.o[d][q][4 * j + 3]);
-      if (half == 0) {
-        a.part_ml[2 * p] = st.m[q];
-        a.part_ml[2 * p + 1] = l;
-      }
-      continue;
-    }
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;   // nothing seen: zeros
+    mm[wave][q][0][lane] = st.m[q];
+    mm[wave][q][1][lane] = xsum32(st.l[q]);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<uint2*>(a.out + at * D + 32 * d + 8 * j + 4 * half) =
-            make_uint2(pack2(st.o[d][q][4 * j] * inv, st.o[d][q][4 * j + 1] * inv),
-                       pack2(st.o[d][q][4 * j + 2] * inv, st.o[d][q][4 * j + 3] * inv));
-    if (a.lse && half == 0)
-      a.lse[at] = l > 0.f || l != l ? (st.m[q] + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
+        my[((q * (D / 32) + d) * 4 + j) * WAVE + lane] = __builtin_bit_cast(
+            u32x4, (f32x4){st.o[d][q][4 * j], st.o[d][q][4 * j + 1], st.o[d][q][4 * j + 2],
+                           st.o[d][q][4 * j + 3]});
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < QT; ++q) {
+    const int row = row0 + 32 * q + m;
+    if (row >= rows) continue;
+    float M = -FLT_MAX, l = 0.f, f[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) M = vmax(M, mm[w][q][0][lane]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      f[w] = __builtin_amdgcn_exp2f(mm[w][q][0][lane] - M);
+      l += mm[w][q][1][lane] * f[w];
+    }
+    const int64_t at = (q0 + row / G) * a.q.heads + h * G + row % G;
+    const int64_t part = int64_t(split) * a.q.total * a.q.heads + at;
+    const bool some = l > 0.f || l != l;   // nothing seen: zeros
+    const float inv = a.splits > 1 ? 1.f : some ? 1.f / l : 0.f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const f32x4 x = __builtin_bit_cast(
+            f32x4, stage[w][((q * (D / 32) + d) * 4 + wave) * WAVE + lane]);
+        o.x = __builtin_fmaf(x.x, f[w], o.x);
+        o.y = __builtin_fmaf(x.y, f[w], o.y);
+        o.z = __builtin_fmaf(x.z, f[w], o.z);
+        o.w = __builtin_fmaf(x.w, f[w], o.w);
+      }
+      const int feature = 32 * d + 8 * wave + 4 * half;
+      if (a.splits > 1)
+        *reinterpret_cast<float4*>(a.part_o + part * D + feature) = o;
+      else
+        *reinterpret_cast<uint2*>(a.out + at * D + feature) =
+            make_uint2(pack2(o.x * inv, o.y * inv), pack2(o.z * inv, o.w * inv));
+    }
+    if (wave == 0 && half == 0) {
+      if (a.splits > 1) {
+        a.part_ml[2 * part] = M;
+        a.part_ml[2 * part + 1] = l;
+      } else if (a.lse) {
+        a.lse[at] = some ? (M + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
+      }
+    }
   }
 }
 
@@ -368,8 +431,10 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(AttendArgs a) {
 #pragma unroll 4
   for (int s = g; s < a.splits; s += NG) {
     const int64_t p = s * n + at;
+    const float lp = a.part_ml[2 * p + 1];
+    if (lp == 0.f) continue;   // an empty share (its features are not written), or nothing seen
     const float w = __builtin_amdgcn_exp2f(a.part_ml[2 * p] - M);
-    l += a.part_ml[2 * p + 1] * w;
+    l += lp * w;
     x += a.part_o[p * D + f] * w;
   }
   lo[g][f] = x;
@@ -390,18 +455,26 @@ int query_tiles(const tav2_kv& c, const tav2_kv_queries& q) {
   return int64_t(q.max_count) * (q.heads / c.kv_heads) > 32 && c.head_dim <= 64 ? 2 : 1;
 }
 
-// Shares of a sequence's pages: enough workgroups to fill the CUs and to even out sequences of
-// different lengths, but no share so small that its partial results (4 bytes a feature, written and
-// read) come near the pages it reads (2 bytes a feature of 64 tokens).
-int key_splits(const tav2_kv& c, const tav2_kv_queries& q) {
-  const int64_t rows = int64_t(q.max_count) * (q.heads / c.kv_heads);
-  const int64_t seqs = q.total < c.num_seqs ? q.total : c.num_seqs;
-  const int64_t groups = seqs * c.kv_heads * cdiv(rows, 32 * query_tiles(c, q));
+// Pages that a query tile of the longest sequence sees, by the host's estimate.
+int64_t most_pages(const tav2_kv& c, const tav2_kv_queries& q) {
   int64_t tokens = c.max_len;
   if (q.window > 0) tokens = std::min(tokens, int64_t(q.window) + q.max_count + q.sinks + 2 * KVP);
-  const int64_t least = std::max<int64_t>(4, std::min<int64_t>(rows, 32 * query_tiles(c, q)) / 2);
-  const int64_t most = std::max<int64_t>(1, tokens / (least * KVP));
-  return int(std::max<int64_t>(1, std::min(most, 2048 / std::max<int64_t>(1, groups))));
+  return std::max<int64_t>(1, cdiv(tokens, KVP));
+}
+
+// Pages to a workgroup's share: such that there are workgroups enough to fill the CUs and to even out
+// sequences of different lengths, but no share so small that its partial results (4 bytes a feature,
+// written and read) come near the pages it reads (2 bytes a feature of 64 tokens).
+int share_pages(const tav2_kv& c, const tav2_kv_queries& q) {
+  const int64_t rows = int64_t(q.max_count) * (q.heads / c.kv_heads);
+  const int64_t seqs = q.total < c.num_seqs ? q.total : c.num_seqs;
+  const int64_t tile = 32 * query_tiles(c, q);
+  const int64_t groups = seqs * c.kv_heads * cdiv(rows, tile);
+  const int64_t least = std::max<int64_t>(4, std::min<int64_t>(rows, tile) / 2);
+  return int(std::max<int64_t>(least, cdiv(groups * most_pages(c, q), SHARES)));
+}
+int key_splits(const tav2_kv& c, const tav2_kv_queries& q) {
+  return int(cdiv(most_pages(c, q), share_pages(c, q)));
 }
 
 }  // namespace
@@ -430,6 +503,7 @@ hipError_t launch_kv_attend(const tav2_kv& c, int layer, const tav2_kv_queries& 
   a.lse = lse;
   const int QT = query_tiles(c, q);
   a.splits = key_splits(c, q);
+  a.chunk = share_pages(c, q);
   a.tiles = int(cdiv(int64_t(q.max_count) * (q.heads / c.kv_heads), 32 * QT));
   a.units = int((int64_t(c.num_seqs) * c.kv_heads * a.splits + 7) / 8 * 8);
   a.part_o = static_cast<float*>(ws);

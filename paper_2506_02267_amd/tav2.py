@@ -532,32 +532,32 @@ def _heads(name: str, x: torch.Tensor, dtype) -> int:
     """Elements from a row of x [rows, heads, head_dim] to the next (heads packed in a row)."""
     if x.dim() != 3 or x.dtype != dtype:
         raise ValueError(f"{name}: expected {dtype} [rows, heads, head_dim]")
-    if x.shape[0] > 0 and (x.stride(2) != 1 or x.stride(1) != x.shape[2]):
+    rows, heads, D = x.shape
+    ld, per_head, one = x.stride()
+    if rows > 0 and (one != 1 or (per_head != D and heads > 1)):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
-    width = x.shape[1] * x.shape[2]
-    return x.stride(0) if x.shape[0] > 1 else width
+    return ld if rows > 1 else heads * D
 
 
 def _dense(name: str, x: Optional[torch.Tensor], shape, dtype):
-    if x is not None and (tuple(x.shape) != tuple(shape) or x.dtype != dtype
-                          or not x.is_contiguous()):
+    if x is not None and (x.shape != shape or x.dtype != dtype or not x.is_contiguous()):
         raise ValueError(f"{name}: expected contiguous {dtype} {list(shape)}")
 
 
-def _run(fn: str, dev: torch.device, stream, args, *used):
-    """Call entry point `fn` with `args` and the stream, on the device that holds the tensors
-    (`used`: all of them), whichever device is current."""
-    if dev.type != "cuda":
+def _run(fn: str, device: int, stream: Optional[torch.cuda.Stream], args, *used):
+    """Call entry point `fn` with `args` and the stream (by default the current one of that device)
+    on GPU number `device`, whichever device is current; `used`: the tensors it takes."""
+    if device < 0:
         raise ValueError(f"{fn}: expected tensors on a GPU")
     for t in used:
-        if t is not None and t.device != dev:
-            raise ValueError(f"{fn}: tensors on {t.device} and {dev}")
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{fn}: a tensor is not on GPU {device}")
     call = getattr(load_library(), fn)
-    if dev.index != torch.cuda.current_device():
-        with torch.cuda.device(dev):
-            _check(fn, call(*args, _stream_handle(stream)))
-            _used_on(stream, *used)
-    else:
+    if stream is None and device == torch.cuda.current_device():
+        # (the handle alone: building a Stream object takes longer than the launch)
+        _check(fn, call(*args, torch._C._cuda_getCurrentRawStream(device)))
+        return
+    with torch.cuda.device(device):
         _check(fn, call(*args, _stream_handle(stream)))
         _used_on(stream, *used)
 
@@ -572,7 +572,7 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offset: tor
     one projection; offset int64 [R], length int32 [R].  window 0: none; the first `sinks` tokens
     stay visible.  lse (optional, fp32 [rows, heads]) receives the log of the sums."""
     dt = torch.float32 if q.dtype == torch.float32 else torch.bfloat16
-    lds = [_heads(n, x, dt) for n, x in (("q", q), ("k", k), ("v", v))]
+    lds = _heads("q", q, dt), _heads("k", k, dt), _heads("v", v, dt)
     rows, heads, D = q.shape
     if k.shape != v.shape or k.shape[0] != rows or k.shape[2] != D:
         raise ValueError("k, v: expected [rows, kv_heads, head_dim] of q's rows and head_dim")
@@ -583,14 +583,12 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offset: tor
         out = torch.empty((rows, heads, D), dtype=dt, device=q.device)
     _dense("out", out, (rows, heads, D), dt)
     _dense("lse", lse, (rows, heads), torch.float32)
-    a = Window(q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), q_ld=lds[0], k_ld=lds[1],
-               v_ld=lds[2], out=out.data_ptr(), lse=None if lse is None else lse.data_ptr(),
-               offset=offset.data_ptr(), len=length.data_ptr(), num_requests=R, max_len=max_len,
-               heads=heads, kv_heads=k.shape[1], head_dim=D,
-               dtype=F32 if dt == torch.float32 else BF16, window=window, sinks=sinks,
-               scale=scale, reserved=0)
-    _run("tav2_attend_window", q.device, stream, (ctypes.byref(a),), q, k, v, offset, length, out,
-         lse)
+    a = Window(q.data_ptr(), k.data_ptr(), v.data_ptr(), *lds, out.data_ptr(),
+               None if lse is None else lse.data_ptr(), offset.data_ptr(), length.data_ptr(), R,
+               max_len, heads, k.shape[1], D, F32 if dt == torch.float32 else BF16, window, sinks,
+               scale, 0)
+    _run("tav2_attend_window", q.get_device(), stream, (ctypes.byref(a),), q, k, v, offset, length,
+         out, lse)
     return out
 
 
@@ -620,15 +618,17 @@ class KvCache:
             _dense(name, x, shape, dt)
             if x.device != k.device:
                 raise ValueError(f"{name}: on {x.device}, k on {k.device}")
-        self.device = k.device
+        self.device, self.index = k.device, k.get_device()
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.k_tail, self.v_tail, self.table = k_tail, v_tail, table
         self.length, self.fresh, self.refs = length, fresh, refs
+        self.seqs = seqs
         self.s = Kv(k=k.data_ptr(), v=v.data_ptr(), k_scale=k_scale.data_ptr(),
                     v_scale=v_scale.data_ptr(), k_tail=k_tail.data_ptr(), v_tail=v_tail.data_ptr(),
                     table=table.data_ptr(), len=length.data_ptr(), fresh=fresh.data_ptr(),
                     refs=refs.data_ptr(), num_seqs=seqs, layers=layers, pages=pages,
                     max_blocks=blocks, kv_heads=heads, head_dim=D, max_len=max_len, reserved=0)
+        self.ref, self.row = ctypes.byref(self.s), (heads, D)
 
     @classmethod
     def create(cls, layers: int, pages: int, seqs: int, max_blocks: int, kv_heads: int,
@@ -655,16 +655,13 @@ class KvCache:
     def max_len(self, n: int):
         self.s.max_len = n
 
-    @property
-    def seqs(self) -> int:
-        return self.s.num_seqs
 
 
 def kv_extend(cache: KvCache, count: torch.Tensor, stream=None):
     """tav2_kv_extend: room for count[s] (int32 [seqs]) new tokens of every sequence;
     cache.fresh says what was granted."""
     _dense("count", count, (cache.seqs,), torch.int32)
-    _run("tav2_kv_extend", cache.device, stream, (ctypes.byref(cache.s), count.data_ptr()), count)
+    _run("tav2_kv_extend", cache.index, stream, (cache.ref, count.data_ptr()), count)
 
 
 def kv_append(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, offset: torch.Tensor,
@@ -672,15 +669,14 @@ def kv_append(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, offs
     """tav2_kv_append: one layer's keys and values (bf16 [rows, kv_heads, head_dim], possibly slices
     of one projection) of the tokens that the last kv_extend granted; sequence s's begin at row
     offset[s] (int64 [seqs] or longer)."""
-    ld = [_heads(n, x, torch.bfloat16) for n, x in (("k", k), ("v", v))]
-    for n, x in (("k", k), ("v", v)):
-        if x.shape[1] != cache.s.kv_heads or x.shape[2] != cache.s.head_dim:
-            raise ValueError(f"{n}: expected [rows, kv_heads, head_dim] of the cache's sizes")
+    k_ld, v_ld = _heads("k", k, torch.bfloat16), _heads("v", v, torch.bfloat16)
+    if k.shape[1:] != cache.row or v.shape[1:] != cache.row:
+        raise ValueError("k, v: expected [rows, kv_heads, head_dim] of the cache's sizes")
     if offset.dtype != torch.int64 or offset.dim() != 1 or offset.shape[0] < cache.seqs \
             or not offset.is_contiguous():
         raise ValueError("offset: expected contiguous int64 [seqs] or longer")
-    _run("tav2_kv_append", cache.device, stream,
-         (ctypes.byref(cache.s), layer, k.data_ptr(), ld[0], v.data_ptr(), ld[1],
+    _run("tav2_kv_append", cache.index, stream,
+         (cache.ref, layer, k.data_ptr(), k_ld, v.data_ptr(), v_ld,
           offset.data_ptr(), max_count), k, v, offset)
 
 
@@ -700,14 +696,12 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, offset: torch.Tensor,
         out = torch.empty((total, heads, D), dtype=torch.bfloat16, device=q.device)
     _dense("out", out, (total, heads, D), torch.bfloat16)
     _dense("lse", lse, (total, heads), torch.float32)
-    a = KvQueries(q=q.data_ptr(), offset=offset.data_ptr(), total=total, ld=ld,
-                  max_count=max_count, heads=heads, window=window, sinks=sinks, scale=scale,
-                  reserved=0)
+    a = ctypes.byref(KvQueries(q.data_ptr(), offset.data_ptr(), total, ld, max_count, heads, window,
+                               sinks, scale, 0))
     ws = ws or Workspace(q.device)
-    need = load_library().tav2_kv_attend_workspace(ctypes.byref(cache.s), ctypes.byref(a))
-    wp, wb = ws.get(need)
-    _run("tav2_kv_attend", cache.device, stream,
-         (ctypes.byref(cache.s), layer, ctypes.byref(a), flags, out.data_ptr(),
+    wp, wb = ws.get(load_library().tav2_kv_attend_workspace(cache.ref, a))
+    _run("tav2_kv_attend", cache.index, stream,
+         (cache.ref, layer, a, flags, out.data_ptr(),
           None if lse is None else lse.data_ptr(), wp, wb), q, offset, out, lse, ws.buf)
     return out
 
@@ -716,19 +710,19 @@ def kv_fork(cache: KvCache, parent: torch.Tensor, stream=None):
     """tav2_kv_fork: empty sequences s become continuations of sequence parent[s] (int32 [seqs],
     -1: not)."""
     _dense("parent", parent, (cache.seqs,), torch.int32)
-    _run("tav2_kv_fork", cache.device, stream, (ctypes.byref(cache.s), parent.data_ptr()), parent)
+    _run("tav2_kv_fork", cache.index, stream, (cache.ref, parent.data_ptr()), parent)
 
 
 def kv_free(cache: KvCache, drop: torch.Tensor, stream=None):
     """tav2_kv_free: sequences with drop[s] != 0 (uint8 [seqs]) give up their pages."""
     _dense("drop", drop, (cache.seqs,), torch.uint8)
-    _run("tav2_kv_free", cache.device, stream, (ctypes.byref(cache.s), drop.data_ptr()), drop)
+    _run("tav2_kv_free", cache.index, stream, (cache.ref, drop.data_ptr()), drop)
 
 
 def kv_trim(cache: KvCache, window: int, sinks: int = 0, stream=None):
     """tav2_kv_trim: every sequence gives up the pages that this window and these sinks no longer
     see."""
-    _run("tav2_kv_trim", cache.device, stream, (ctypes.byref(cache.s), window, sinks))
+    _run("tav2_kv_trim", cache.index, stream, (cache.ref, window, sinks))
 
 
 def kv_compact(cache: KvCache, used: Optional[torch.Tensor] = None,
@@ -739,9 +733,9 @@ def kv_compact(cache: KvCache, used: Optional[torch.Tensor] = None,
         used = torch.empty(1, dtype=torch.int32, device=cache.device)
     _dense("used", used, (1,), torch.int32)
     ws = ws or Workspace(cache.device)
-    wp, wb = ws.get(load_library().tav2_kv_compact_workspace(ctypes.byref(cache.s)))
-    _run("tav2_kv_compact", cache.device, stream,
-         (ctypes.byref(cache.s), used.data_ptr(), wp, wb), used, ws.buf)
+    wp, wb = ws.get(load_library().tav2_kv_compact_workspace(cache.ref))
+    _run("tav2_kv_compact", cache.index, stream,
+         (cache.ref, used.data_ptr(), wp, wb), used, ws.buf)
     return used
 
 
