@@ -39,10 +39,13 @@ struct AttendArgs {
   float* part_ml;    // [splits, total, heads, 2]: reference and sum
   int tiles;         // query tiles per (sequence, kv head)
   int splits, chunk; // shares of a sequence's pages, and pages to a share
-  int units;         // (sequence, kv head, split) groups, padded to a multiple of 8
+  int near;          // sequences of a block (my_job)
+  int units;         // (sequence, kv head, share) triples, padded
+  int group;         // neighbouring sequences whose rows fit one tile together
 };
 
-constexpr int SHARES = 2048;   // workgroups that a launch is divided into, about
+constexpr int SHARES = 512;      // workgroups that a launch is divided into, about
+constexpr int SHARE_MOST = 64;   // pages to a share, at most
 
 // The pages that a tile's queries see: [0, sink) and [first, last), counted through.
 struct PageList {
@@ -86,17 +89,23 @@ __device__ __forceinline__ int swz_key(int r) {
 }
 __device__ __forceinline__ int swz_feature(int d) { return ((d >> 2) & 1) | (((d >> 1) ^ (d >> 3)) & 1) << 1; }
 
+// 8 bf16 values of which the first n are kept and the others (whatever they hold) become zeros: by
+// selects, so that the loads before it stay together.
+__device__ __forceinline__ u32x4 first_of8(u32x4 w, int n) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] &= n > 2 * e + 1 ? 0xFFFFFFFFu : n > 2 * e ? 0xFFFFu : 0u;
+  return w;
+}
+
 // 8 bf16 values times f (a power of two) as fp16.
-__device__ __forceinline__ f16x8 scaled8h(const uint4& w, float f) {
-  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ f16x8 scaled8h(const u32x4& x, float f) {
   uint32_t y[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     y[e] = pack2h(__uint_as_float(x[e] << 16) * f, __uint_as_float(x[e] & 0xFFFF0000u) * f);
   return __builtin_bit_cast(f16x8, make_uint4(y[0], y[1], y[2], y[3]));
 }
-__device__ __forceinline__ float max8(const uint4& w, float m) {
-  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ float max8(const u32x4& x, float m) {
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     m = fmaxf(m, fmaxf(__builtin_fabsf(__uint_as_float(x[e] << 16)),
@@ -112,6 +121,143 @@ __device__ __forceinline__ void into_half(float top, float* f, float* back) {
   *back = __uint_as_float((ex - 14) << 23);
 }
 
+// A workgroup's share: `cap` query rows of a kv head of a sequence, entries [c0, c1) of their pages.
+struct Job {
+  int s, h, split, row0, G, rows;   // rows: the sequence's, (query, head) pairs
+  int64_t q0, nq, first_pos;        // its queries, and the first one's position
+  int64_t lo_pos, hi_pos;           // positions of this tile's first and last row
+  int len, chunk, n, c0, c1;
+  PageList list;
+  const int32_t* table;
+};
+
+__device__ __forceinline__ int64_t query_count(const AttendArgs& a, int s) {
+  const int64_t n = a.q.offset[s + 1] - a.q.offset[s];
+  return n < 0 ? 0 : n > a.q.max_count ? a.q.max_count : n;
+}
+
+// Queries and pages of sequence s; false: none, or out of the arguments' range.
+__device__ __forceinline__ bool job_of(const AttendArgs& a, int s, int row0, int cap, Job& j) {
+  const tav2_kv& c = a.c;
+  j.s = s;
+  j.row0 = row0;
+  j.G = a.q.heads / c.kv_heads;
+  j.q0 = a.q.offset[s];
+  j.nq = query_count(a, s);
+  if (j.q0 < 0 || j.q0 + j.nq > a.q.total) return false;
+  j.rows = int(j.nq) * j.G;
+  if (row0 >= j.rows) return false;
+  j.len = kv_len(c, s);
+  j.first_pos = a.causal ? int64_t(j.len) - j.nq : j.len;
+  const int last_row = min(row0 + cap, j.rows) - 1;
+  j.lo_pos = a.causal ? j.first_pos + row0 / j.G : j.first_pos;
+  j.hi_pos = a.causal ? j.first_pos + last_row / j.G : j.first_pos;
+  j.list = pages_seen(j.len, j.lo_pos, j.hi_pos, a.q.window, a.q.sinks);
+  j.n = j.list.count();
+  // shares of one size, so that a long sequence has more of them (larger ones where it is
+  // longer than the host's estimate)
+  j.chunk = max(a.chunk, (j.n + a.splits - 1) / a.splits);
+  j.table = c.table + int64_t(s) * c.max_blocks;
+  return true;
+}
+
+// The same for this workgroup, with its split.  An empty share of several leaves no sum, and kv_merge
+// reads no more of it.
+__device__ __forceinline__ bool my_job(const AttendArgs& a, int cap, Job& j) {
+  // Units (sequence, head, share) in the order (share, block of sequences, head), each on one XCD
+  // (workgroups go to the 8 in turn) with the block's sequences one after the other, since
+  // neighbours may be copies that read the same pages, and so the query tiles of each.  First shares come
+  // first, the later ones, which short sequences lack, at the end.
+  const int unit = int(blockIdx.x % unsigned(a.units));
+  const int tile = int(blockIdx.x / unsigned(a.units));
+  const int block = unit / (8 * a.near) * 8 + unit % 8;
+  const int blocks = (a.c.num_seqs + a.near - 1) / a.near * a.c.kv_heads;   // of a share
+  const int s = block % blocks / a.c.kv_heads * a.near + unit / 8 % a.near;
+  j.split = block / blocks;
+  if (j.split >= a.splits || s >= a.c.num_seqs || !job_of(a, s, tile * cap, cap, j)) return false;
+  j.h = block % a.c.kv_heads;
+  j.c0 = j.split * j.chunk;
+  j.c1 = min(j.n, j.c0 + j.chunk);
+  if (a.splits > 1 && j.c0 >= j.n) {
+    const int row = j.row0 + int(threadIdx.x);
+    if (int(threadIdx.x) < cap && row < j.rows) {
+      const int64_t part = int64_t(j.split) * a.q.total * a.q.heads +
+                           (j.q0 + row / j.G) * a.q.heads + j.h * j.G + row % j.G;
+      a.part_ml[2 * part] = -FLT_MAX;
+      a.part_ml[2 * part + 1] = 0.f;
+    }
+    return false;
+  }
+  return true;
+}
+
+// A wave's pages: every fourth entry of the share from c0 + wave on.
+template <int D>
+struct Feed {
+  // the next 64, one a lane: number (-1: released, or the open block), key scale, and the value
+  // scale as a power of two and reciprocal.  Read once, so that no page waits for a chain of
+  // small loads.
+  int ids;
+  float kss, lvs, invs;
+  u32x4 rk[D / 16], rv[D / 16];   // a page's codes as they lie
+
+  __device__ __forceinline__ void look_up(const AttendArgs& a, const Job& j, int base) {
+    const int full = j.len / KVP, i = base + 4 * (threadIdx.x % WAVE);
+    const int b = i < j.c1 ? j.list.at(i) : full;
+    ids = b < full ? j.table[b] : -1;
+    if (ids >= a.c.pages) ids = -1;
+    const int64_t at = kv_unit(a.c, a.layer, ids < 0 ? 0 : ids, j.h);
+    const float vs = a.c.v_scale[at];
+    kss = a.c.k_scale[at];
+    lvs = __builtin_amdgcn_logf(vs);
+    invs = __builtin_amdgcn_rcpf(vs);
+  }
+  __device__ __forceinline__ int page(int t) const { return __builtin_amdgcn_readlane(ids, t); }
+  static __device__ __forceinline__ float lane_f(float v, int t) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), t));
+  }
+  __device__ __forceinline__ void load(const AttendArgs& a, const Job& j, int page) {
+    const int lane = threadIdx.x % WAVE;
+    const int64_t at = kv_unit(a.c, a.layer, page < 0 ? 0 : page, j.h) * KVP * D;
+    const u32x4* kp = reinterpret_cast<const u32x4*>(a.c.k + at) + lane;
+    const u32x4* vp = reinterpret_cast<const u32x4*>(a.c.v + at) + lane;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      rk[i] = kp[i * WAVE];
+      rv[i] = vp[i * WAVE];
+    }
+  }
+  // Factors of entry t.  Scale 1 may be a block of zeros, which is taken as if at the smallest scale,
+  // so that its weights do not raise the reference over small values.
+  __device__ __forceinline__ void factors(int t, float* ks, float* lv, float* inv) const {
+    *ks = lane_f(kss, t);
+    *lv = lane_f(lvs, t);
+    *inv = lane_f(invs, t);
+    if (*lv == 0.f) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) any |= rv[e].x | rv[e].y | rv[e].z | rv[e].w;
+      if (!__any(any != 0)) {
+        *lv = -100.f;
+        *inv = 0x1p100f;
+      }
+    }
+  }
+  // The page into the wave's part of LDS: keys' pieces from 0, features' from 4 D (KC and VC pieces a
+  // row).  A wave's LDS operations are done in order; the barriers keep the compiler to it.
+  static constexpr int KC = D / 16, VC = KVP / 16;
+  __device__ __forceinline__ void put(u32x4* my) const {
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) {
+      const int i = e * WAVE + threadIdx.x % WAVE, kr = i / KC, vr = i / VC;
+      my[kr * KC + ((i % KC) ^ swz_key<D>(kr))] = rk[e];
+      my[4 * D + vr * VC + ((i % VC) ^ swz_feature(vr))] = rv[e];
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+};
+
 template <int D, int QT>
 __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
   constexpr int KB = D / 2;   // bytes of a key's codes per lane
@@ -121,82 +267,17 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
   __shared__ u32x4 stage[4][STAGE];
   __shared__ float mm[4][QT][2][WAVE];
   const tav2_kv& c = a.c;
-  const int H = c.kv_heads, G = a.q.heads / H;
-  // units (which share K and V) on one XCD: a unit's query tiles are 8 apart, and so on
-  const int unit = int(blockIdx.x % unsigned(a.units));
-  const int tile = int(blockIdx.x / unsigned(a.units));
-  const int split = unit % a.splits, sh = unit / a.splits;
-  const int s = sh / H, h = sh % H;
-  if (s >= c.num_seqs) return;
-  const int64_t q0 = a.q.offset[s];
-  int64_t nq = a.q.offset[s + 1] - q0;
-  nq = nq < 0 ? 0 : nq > a.q.max_count ? a.q.max_count : nq;
-  if (q0 < 0 || q0 + nq > a.q.total) return;
-  const int rows = int(nq) * G, row0 = tile * 32 * QT;
-  if (row0 >= rows) return;
-  const int len = kv_len(c, s);
+  Job j;
+  if (!my_job(a, 32 * QT, j)) return;
+  const int G = j.G, h = j.h, len = j.len, rows = j.rows, row0 = j.row0, full = len / KVP;
+  const int64_t q0 = j.q0;
   const int lane = threadIdx.x % WAVE, m = lane % 32, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);   // (scalar page arithmetic)
-
-  // which pages, and which of them this wave takes: every fourth of the workgroup's share
-  const int64_t first_pos = a.causal ? int64_t(len) - nq : len;
-  const int last_row = min(row0 + 32 * QT, rows) - 1;
-  const int64_t lo_pos = a.causal ? first_pos + row0 / G : first_pos;
-  const int64_t hi_pos = a.causal ? first_pos + last_row / G : first_pos;
-  const PageList list = pages_seen(len, lo_pos, hi_pos, a.q.window, a.q.sinks);
-  const int n = list.count();
-  // shares of one size, so that a long sequence has more of them (larger ones where it is
-  // longer than the host's estimate)
-  const int chunk = max(a.chunk, (n + a.splits - 1) / a.splits);
-  if (a.splits > 1 && split * chunk >= n) {   // an empty share: no sum, and kv_merge reads no more of it
-    const int row = row0 + int(threadIdx.x);
-    if (threadIdx.x < 32 * QT && row < rows) {
-      const int64_t part = int64_t(split) * a.q.total * a.q.heads + (q0 + row / G) * a.q.heads +
-                           h * G + row % G;
-      a.part_ml[2 * part] = -FLT_MAX;
-      a.part_ml[2 * part + 1] = 0.f;
-    }
-    return;
-  }
-  const int i0 = split * chunk + wave, i1 = min(n, (split + 1) * chunk);
-  const int full = len / KVP;
-  const int32_t* table = c.table + int64_t(s) * c.max_blocks;
-  // this wave's next 64 pages, one a lane: number (-1: released, or the open block), key scale, and
-  // the value scale as a power of two and reciprocal.  Read once, so that no page waits for
-  // a chain of small loads.
-  int ids = -1;
-  float kss = 1.f, lvs = 0.f, invs = 1.f;
-  auto look_up = [&](int base) {
-    const int i = base + 4 * lane;
-    const int b = i < i1 ? list.at(i) : full;
-    ids = b < full ? table[b] : -1;
-    if (ids >= c.pages) ids = -1;
-    if (ids < 0) return;
-    const int64_t at = kv_unit(c, a.layer, ids, h);
-    const float vs = c.v_scale[at];
-    kss = c.k_scale[at];
-    lvs = __builtin_amdgcn_logf(vs);
-    invs = __builtin_amdgcn_rcpf(vs);
-  };
-  auto lane_f = [](float v, int t) {
-    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), t));
-  };
-  u32x4 rk[D / 16], rv[D / 16];   // a page's codes as they lie
-  auto load = [&](int page) {
-    const int64_t at = kv_unit(c, a.layer, page < 0 ? 0 : page, h) * KVP * D;
-    const u32x4* kp = reinterpret_cast<const u32x4*>(c.k + at) + lane;
-    const u32x4* vp = reinterpret_cast<const u32x4*>(c.v + at) + lane;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      rk[i] = kp[i * WAVE];
-      rv[i] = vp[i * WAVE];
-    }
-  };
   u32x4* const my = stage[wave];
-  constexpr int KC = D / 16, VC = KVP / 16;   // pieces of a key, and of a feature's 64 keys
-  look_up(i0);
-  int page = __builtin_amdgcn_readlane(ids, 0);
-  load(page);
+  Feed<D> feed;
+  feed.look_up(a, j, j.c0 + wave);
+  int page = feed.page(0);
+  feed.load(a, j, page);
 
   // this lane's queries: operands, and what they see
   f16x8 qf[QT][D / 16];
@@ -208,17 +289,17 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
     const int row = min(row0 + 32 * q + m, rows - 1);
     const int i = row / G, g = row % G;
     const bf16_t* p = static_cast<const bf16_t*>(a.q.q) + (q0 + i) * a.q.ld + (h * G + g) * D + half * KB;
-    uint4 w[D / 16];
+    u32x4 w[D / 16];
     float top = 0.f, f, back;
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) w[t] = *reinterpret_cast<const uint4*>(p + 8 * t);
+    for (int t = 0; t < D / 16; ++t) w[t] = *reinterpret_cast<const u32x4*>(p + 8 * t);
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) top = max8(w[t], top);
     into_half(xmax32(top), &f, &back);
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) qf[q][t] = scaled8h(w[t], f);
     cq[q] = a.scale * LOG2E * back;
-    const int64_t pos = a.causal ? first_pos + i : first_pos;
+    const int64_t pos = a.causal ? j.first_pos + i : j.first_pos;
     const int64_t end = pos + 1 < len ? pos + 1 : len;
     seen.hi[q] = int(end > 0 ? end : 0);
     const int64_t low = pos - a.q.window + 1;
@@ -226,8 +307,8 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
   }
   // a page is seen whole by all of them where it ends by the first's last key and starts at the last's
   // first one (or lies among the sinks)
-  const int64_t all_hi = lo_pos + 1 < len ? lo_pos + 1 : len;
-  const int64_t all_lo = a.q.window > 0 ? hi_pos - a.q.window + 1 : 0;
+  const int64_t all_hi = j.lo_pos + 1 < len ? j.lo_pos + 1 : len;
+  const int64_t all_lo = a.q.window > 0 ? j.hi_pos - a.q.window + 1 : 0;
   auto part_seen = [&](int b) {
     return int64_t(b + 1) * KVP > all_hi ||
            (int64_t(b) * KVP < all_lo && int64_t(b + 1) * KVP > a.q.sinks);
@@ -236,41 +317,23 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
   AttState<D, QT> st;
   st.clear();
   bool open = false;
-  for (int i = i0, t = 0; i < i1; i += 4, ++t) {
+  for (int i = j.c0 + wave, t = 0; i < j.c1; i += 4, ++t) {
     if (t == WAVE) {
       t = 0;
-      look_up(i);
-      page = __builtin_amdgcn_readlane(ids, 0);
-      load(page);
+      feed.look_up(a, j, i);
+      page = feed.page(0);
+      feed.load(a, j, page);
     }
-    const int b = list.at(i);
+    const int b = j.list.at(i);
     open |= b >= full;
-    const int next = t + 1 < WAVE ? __builtin_amdgcn_readlane(ids, t + 1) : -1;
+    const int next = t + 1 < WAVE ? feed.page(t + 1) : -1;
     const bool masked = part_seen(b);
-    const float ks = lane_f(kss, t);
-    float lv = lane_f(lvs, t), inv = lane_f(invs, t), cs[QT];
+    float ks, lv, inv, cs[QT];
+    feed.factors(t, &ks, &lv, &inv);
 #pragma unroll
     for (int q = 0; q < QT; ++q) cs[q] = cq[q] * ks;
-    if (lv == 0.f) {   // scale 1: a block of zeros, perhaps: taken as if at the smallest
-                       // scale, so that its weights do not raise the reference over small values
-      uint32_t any = 0;
-#pragma unroll
-      for (int e = 0; e < D / 16; ++e) any |= rv[e].x | rv[e].y | rv[e].z | rv[e].w;
-      if (!__any(any != 0)) {
-        lv = -100.f;
-        inv = 0x1p100f;
-      }
-    }
-    // (a wave's LDS operations are done in order; the barriers keep the compiler to it)
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int e = 0; e < D / 16; ++e) {
-      const int i = e * WAVE + lane, kr = i / KC, vr = i / VC;
-      my[kr * KC + ((i % KC) ^ swz_key<D>(kr))] = rk[e];
-      my[4 * D + vr * VC + ((i % VC) ^ swz_feature(vr))] = rv[e];
-    }
-    __builtin_amdgcn_wave_barrier();
-    load(next);
+    feed.put(my);
+    feed.load(a, j, next);
     if (page >= 0) {
 #pragma unroll 1   // (both halves at once take too many registers)
       for (int u = 0; u < 2; ++u) {
@@ -278,7 +341,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
           const int kr = 32 * u + key_row(m);
 #pragma unroll
           for (int t = 0; t < D / 32; ++t) {
-            const u32x4 w = my[kr * KC + ((half * (D / 32) + t) ^ swz_key<D>(key_row(m)))];
+            const u32x4 w = my[kr * Feed<D>::KC + ((half * (D / 32) + t) ^ swz_key<D>(key_row(m)))];
             kf[2 * t] = codes8h(w.x, w.y);
             kf[2 * t + 1] = codes8h(w.z, w.w);
           }
@@ -287,7 +350,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
 #pragma unroll
           for (int d = 0; d < D / 32; ++d) {
             const int vr = 32 * d + m;
-            const u32x4 w = my[4 * D + vr * VC + ((2 * u + half) ^ swz_feature(m))];
+            const u32x4 w = my[4 * D + vr * Feed<D>::VC + ((2 * u + half) ^ swz_feature(m))];
             vf[d][0] = codes8h(w.x, w.y);
             vf[d][1] = codes8h(w.z, w.w);
           }
@@ -300,35 +363,29 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
   }
   if (open) {   // the open block, in bf16: scaled into fp16's range; what lies behind the last token is
                 // taken as zeros
-    const int64_t tail = kv_tail(c, a.layer, s, h);
+    const int64_t tail = kv_tail(c, a.layer, j.s, h);
     const bool masked = part_seen(full);
 #pragma unroll 1
     for (int u = 0; u < 2; ++u) {
       const int kr = 32 * u + key_row(m), k0 = 32 * u + 16 * half, held = len - full * KVP;
-      uint4 wk[D / 16], wv[D / 32][2];
       float kt = 0.f, vt = 0.f, f, back, cs[QT];
+      auto raw_key = [&](int t) {
+        return first_of8(*reinterpret_cast<const u32x4*>(c.k_tail + tail + kr * D + half * KB + 8 * t),
+                         kr < held ? 8 : 0);
+      };
+      auto raw_value = [&](int d, int t) {
+        return first_of8(*reinterpret_cast<const u32x4*>(c.v_tail + tail + (32 * d + m) * KVP + k0 + 8 * t),
+                         held - k0 - 8 * t);
+      };
+      // (read twice, the second time from the cache: the scales come first, and the registers do not
+      // hold it all)
 #pragma unroll
-      for (int t = 0; t < D / 16; ++t) {
-        wk[t] = make_uint4(0, 0, 0, 0);
-        if (kr < held)
-          wk[t] = *reinterpret_cast<const uint4*>(c.k_tail + tail + kr * D + half * KB + 8 * t);
-        kt = max8(wk[t], kt);
-      }
+      for (int t = 0; t < D / 16; ++t) kt = max8(raw_key(t), kt);
 #pragma unroll
       for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const uint4 w =
-              *reinterpret_cast<const uint4*>(c.v_tail + tail + (32 * d + m) * KVP + k0 + 8 * t);
-          uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (k0 + 8 * t + 2 * e >= held) x[e] = 0;
-            else if (k0 + 8 * t + 2 * e + 1 >= held) x[e] &= 0xFFFFu;
-          }
-          wv[d][t] = make_uint4(x[0], x[1], x[2], x[3]);
-          vt = max8(wv[d][t], vt);
-        }
+        for (int t = 0; t < 2; ++t) vt = max8(raw_value(d, t), vt);
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int o = 32; o >= 1; o >>= 1) {
         kt = fmaxf(kt, __shfl_xor(kt, o, WAVE));
@@ -341,13 +398,13 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
       for (int q = 0; q < QT; ++q) cs[q] = cq[q] * back;
       auto keys = [&](f16x8(&kf)[D / 16]) {
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t) kf[t] = scaled8h(wk[t], f);
+        for (int t = 0; t < D / 16; ++t) kf[t] = scaled8h(raw_key(t), f);
       };
       auto values = [&](f16x8(&vf)[D / 32][2]) {
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-          for (int t = 0; t < 2; ++t) vf[d][t] = scaled8h(wv[d][t], fv);
+          for (int t = 0; t < 2; ++t) vf[d][t] = scaled8h(raw_value(d, t), fv);
       };
       att_step<f16x8, D, QT>(st, keys, values, qf, cs, __builtin_amdgcn_logf(backv), fv, masked,
                              seen, full * KVP + k0);
@@ -383,7 +440,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
       l += mm[w][q][1][lane] * f[w];
     }
     const int64_t at = (q0 + row / G) * a.q.heads + h * G + row % G;
-    const int64_t part = int64_t(split) * a.q.total * a.q.heads + at;
+    const int64_t part = int64_t(j.split) * a.q.total * a.q.heads + at;
     const bool some = l > 0.f || l != l;   // nothing seen: zeros
     const float inv = a.splits > 1 ? 1.f : some ? 1.f / l : 0.f;
 #pragma unroll
@@ -412,6 +469,295 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
       } else if (a.lse) {
         a.lse[at] = some ? (M + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
       }
+    }
+  }
+}
+
+// Sequences that hold the same pages in this share (copies of one another) are read once: of a window
+// of `a.group` neighbouring sequences, whose rows fit one tile together, the first of each set
+// takes the rows of all, and the others leave.  Returns the set as bits of the window (its own
+// alone where the share's first page has one holder), 0: leave.
+__device__ __forceinline__ uint32_t shared_set(const AttendArgs& a, const Job& j) {
+  __shared__ uint32_t differ;
+  const int base = j.s / a.group * a.group, me = j.s - base;
+  const int b0 = j.list.at(j.c0), last = j.list.at(j.c1 - 1);
+  int holders = 0;
+  if (last < j.len / KVP) {
+    const int p = j.table[b0];
+    if (p >= 0 && p < a.c.pages) holders = a.c.refs[p];
+  }
+  if (holders < 2) return 1u << me;
+  if (threadIdx.x == 0) differ = 0;
+  __syncthreads();
+  const int k = threadIdx.x / 16;   // 16 threads a candidate
+  if (k < a.group && k != me) {
+    Job o;
+    bool same = base + k < a.c.num_seqs && job_of(a, base + k, 0, 16, o) &&
+                o.list.sink == j.list.sink && o.list.first == j.list.first && o.chunk == j.chunk &&
+                o.n >= j.c1 && last < o.len / KVP;
+    if (same)
+      for (int i = j.c0 + threadIdx.x % 16; i < j.c1; i += 16)
+        same &= o.table[j.list.at(i)] == j.table[j.list.at(i)];
+    if (!same) atomicOr(&differ, 1u << k);
+  }
+  __syncthreads();
+  const uint32_t set = ~differ & ((1u << a.group) - 1);
+  return (set & ((1u << me) - 1)) ? 0 : set;
+}
+
+// At most 16 query rows: on the 16x16x32 instructions, a page's 64 keys at once.  S^T comes in four tiles
+// of 16 keys, in the order that makes a lane's 16 scores its quarter's 16 consecutive keys
+// (16 g + 4 i + r in register r of tile i, g = l / 16), again the operand of O^T = V^T P^T as they
+// stand.  Half the vector work of a 32-row tile.
+template <int D>
+__global__ __launch_bounds__(256, 3) void kv_attend16_kernel(AttendArgs a) {
+  constexpr int F = D / 4;           // features of a lane's quarter
+  constexpr int NK = D / 32;         // products over the features
+  constexpr int ND = D / 16;         // tiles of O^T
+  __shared__ u32x4 stage[4][8 * D];  // a wave's page on its way, then its state (D / 16 x 64)
+  __shared__ float mm[4][2][16];
+  const tav2_kv& c = a.c;
+  Job j;
+  if (!my_job(a, 16, j)) return;
+  const int lane = threadIdx.x % WAVE, m = lane % 16, g = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int full = j.len / KVP;
+  u32x4* const my = stage[wave];
+  Feed<D> feed;
+  feed.look_up(a, j, j.c0 + wave);
+  int page = feed.page(0);
+  feed.load(a, j, page);
+
+  // this lane's row: which (query, head) of which sequence, and what it sees
+  int row = min(j.row0 + m, j.rows - 1), count = j.rows - j.row0, slot = j.s;
+  if (a.group > 1) {
+    const uint32_t set = shared_set(a, j);
+    if (set == 0) return;
+    if (set & (set - 1)) {
+      const int base = j.s / a.group * a.group;
+      count = 0;
+      for (int k = 0; k < a.group; ++k) {
+        if (!(set >> k & 1)) continue;
+        const int n = int(query_count(a, base + k)) * j.G;
+        if (m >= count && m < count + n) {
+          slot = base + k;
+          row = m - count;
+        }
+        count += n;
+      }
+      if (m >= count) row = 0;   // padding: this sequence's first
+    }
+  }
+  const bool valid = m < count;
+  const int64_t q0 = a.q.offset[slot];
+  const int len = kv_len(c, slot), i_q = row / j.G;
+  const int64_t pos = a.causal ? int64_t(len) - query_count(a, slot) + i_q : len;
+  const int64_t qi = q0 + i_q, at = qi * a.q.heads + j.h * j.G + row % j.G;
+  const int64_t end = pos + 1 < len ? pos + 1 : len, low = pos - a.q.window + 1;
+  const int hi = int(end > 0 ? end : 0), lo = a.q.window > 0 && low > 0 ? int(low) : 0;
+  int all_hi = hi, all_lo = lo;   // what all rows see: from the last one's first key to the first's last
+#pragma unroll
+  for (int o = 8; o >= 1; o >>= 1) {
+    all_hi = min(all_hi, __shfl_xor(all_hi, o, WAVE));
+    all_lo = max(all_lo, __shfl_xor(all_lo, o, WAVE));
+  }
+  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  f16x8 qf[NK];
+  float cq;
+  {
+    const bf16_t* p = static_cast<const bf16_t*>(a.q.q) + qi * a.q.ld + (j.h * j.G + row % j.G) * D + g * F;
+    u32x4 w[NK];
+    float top = 0.f, f, back;
+#pragma unroll
+    for (int t = 0; t < NK; ++t) w[t] = *reinterpret_cast<const u32x4*>(p + 8 * t);
+#pragma unroll
+    for (int t = 0; t < NK; ++t) top = max8(w[t], top);
+    into_half(xmax32(xmax16(top)), &f, &back);
+#pragma unroll
+    for (int t = 0; t < NK; ++t) qf[t] = scaled8h(w[t], f);
+    cq = a.scale * LOG2E * back;
+  }
+
+  f32x4 o[ND];
+  float ref = -FLT_MAX, sum = 0.f;
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
+
+  // one page: keys(i, kf) sets the operands of S^T's tile i, values(d, vf) those of O^T's tile d
+  auto step = [&](auto keys, auto values, float cs, float lv, float inv, int key0) {
+    f32x4 s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f16x8 kf[NK];
+      keys(i, kf);
+      s[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < NK; ++t) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[t], qf[t], s[i], 0, 0, 0);
+    }
+    if (key0 + KVP > all_hi || (key0 < all_lo && key0 + KVP > a.q.sinks)) {
+      const int k0 = key0 + 16 * g, hi_ = hi - k0, lo_ = lo - k0, sinks = a.q.sinks - k0;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        s[r / 4][r % 4] = r < hi_ && (r >= lo_ || r < sinks) ? s[r / 4][r % 4] : -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = vmax(top, s[r / 4][r % 4]);
+    top = __builtin_fmaf(xmax32(xmax16(top)), cs, lv);
+    if (__any(top > ref + RAISE)) {
+      const float to = top - ROOM > ref ? top - ROOM : ref;
+      const float f = __builtin_amdgcn_exp2f(ref - to);
+      ref = to;
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= f;
+    }
+    const float b = lv - ref;
+    float part = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / 4][r % 4], cs, b));
+      s[r / 4][r % 4] = x;
+      part += x;
+    }
+    sum = __builtin_fmaf(part, inv, sum);
+    f16x8 pf[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      pf[t] = __builtin_bit_cast(
+          f16x8, make_uint4(pack2h(s[2 * t][0], s[2 * t][1]), pack2h(s[2 * t][2], s[2 * t][3]),
+                            pack2h(s[2 * t + 1][0], s[2 * t + 1][1]),
+                            pack2h(s[2 * t + 1][2], s[2 * t + 1][3])));
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      f16x8 vf[2];
+      values(d, vf);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[t], pf[t], o[d], 0, 0, 0);
+    }
+  };
+  const int krow = 16 * (m / 4) + m % 4;   // + 4 i: the key of tile i that this lane's row is
+  bool open = false;
+  for (int i = j.c0 + wave, t = 0; i < j.c1; i += 4, ++t) {
+    if (t == WAVE) {
+      t = 0;
+      feed.look_up(a, j, i);
+      page = feed.page(0);
+      feed.load(a, j, page);
+    }
+    const int b = j.list.at(i);
+    open |= b >= full;
+    const int next = t + 1 < WAVE ? feed.page(t + 1) : -1;
+    float ks, lv, inv;
+    feed.factors(t, &ks, &lv, &inv);
+    feed.put(my);
+    feed.load(a, j, next);
+    if (page >= 0) {
+      auto keys = [&](int i, f16x8(&kf)[NK]) {
+        const int kr = krow + 4 * i;
+        if constexpr (D == 32) {   // 8 bytes: half a piece
+          const uint2 w = reinterpret_cast<const uint2*>(my)[2 * (kr * 2 + ((g / 2) ^ swz_key<D>(kr))) + g % 2];
+          kf[0] = codes8h(w.x, w.y);
+        } else {
+#pragma unroll
+          for (int p = 0; p < D / 64; ++p) {
+            const u32x4 w = my[kr * Feed<D>::KC + ((g * (D / 64) + p) ^ swz_key<D>(kr))];
+            kf[2 * p] = codes8h(w.x, w.y);
+            kf[2 * p + 1] = codes8h(w.z, w.w);
+          }
+        }
+      };
+      auto values = [&](int d, f16x8(&vf)[2]) {
+        const int vr = 16 * d + m;
+        const u32x4 w = my[4 * D + vr * Feed<D>::VC + (g ^ swz_feature(m))];
+        vf[0] = codes8h(w.x, w.y);
+        vf[1] = codes8h(w.z, w.w);
+      };
+      step(keys, values, cq * ks, lv, inv, b * KVP);
+    }
+    page = next;
+  }
+  if (open) {   // the open block, in bf16 (as in the kernel above)
+    const int64_t tail = kv_tail(c, a.layer, j.s, j.h);
+    const int held = j.len - full * KVP;
+    float kt = 0.f, vt = 0.f, fk, backk, fv, backv;
+    auto raw_key = [&](int i, int t) {
+      return first_of8(*reinterpret_cast<const u32x4*>(c.k_tail + tail + (krow + 4 * i) * D + g * F + 8 * t),
+                       krow + 4 * i < held ? 8 : 0);
+    };
+    auto raw_value = [&](int d, int t) {
+      return first_of8(*reinterpret_cast<const u32x4*>(c.v_tail + tail + (16 * d + m) * KVP + 16 * g + 8 * t),
+                       held - 16 * g - 8 * t);
+    };
+    // (read twice, as above)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < NK; ++t) kt = max8(raw_key(i, t), kt);
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) vt = max8(raw_value(d, t), vt);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int x = 32; x >= 1; x >>= 1) {
+      kt = fmaxf(kt, __shfl_xor(kt, x, WAVE));
+      vt = fmaxf(vt, __shfl_xor(vt, x, WAVE));
+    }
+    into_half(kt, &fk, &backk);
+    into_half(vt, &fv, &backv);
+    auto keys = [&](int i, f16x8(&kf)[NK]) {
+#pragma unroll
+      for (int t = 0; t < NK; ++t) kf[t] = scaled8h(raw_key(i, t), fk);
+    };
+    auto values = [&](int d, f16x8(&vf)[2]) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) vf[t] = scaled8h(raw_value(d, t), fv);
+    };
+    step(keys, values, cq * backk, __builtin_amdgcn_logf(backv), fv, full * KVP);
+  }
+
+  // the four waves' states meet in LDS; wave w joins every fourth tile of O^T, in the order of the waves
+  __builtin_amdgcn_wave_barrier();
+  sum = xsum32(xsum16(sum));
+  if (g == 0) {
+    mm[wave][0][m] = ref;
+    mm[wave][1][m] = sum;
+  }
+#pragma unroll
+  for (int d = 0; d < ND; ++d) my[d * WAVE + lane] = __builtin_bit_cast(u32x4, o[d]);
+  __syncthreads();
+  if (!valid) return;
+  float M = -FLT_MAX, l = 0.f, f[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) M = vmax(M, mm[w][0][m]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    f[w] = __builtin_amdgcn_exp2f(mm[w][0][m] - M);
+    l += mm[w][1][m] * f[w];
+  }
+  const int64_t part = int64_t(j.split) * a.q.total * a.q.heads + at;
+  const bool some = l > 0.f || l != l;
+  const float inv = some ? 1.f / l : 0.f;
+  for (int d = wave; d < ND; d += 4) {
+    f32x4 x = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) x += __builtin_bit_cast(f32x4, stage[w][d * WAVE + lane]) * f[w];
+    const int feature = 16 * d + 4 * g;
+    if (a.splits > 1)
+      *reinterpret_cast<f32x4*>(a.part_o + part * D + feature) = x;
+    else
+      *reinterpret_cast<uint2*>(a.out + at * D + feature) =
+          make_uint2(pack2(x[0] * inv, x[1] * inv), pack2(x[2] * inv, x[3] * inv));
+  }
+  if (wave == 0 && g == 0) {
+    if (a.splits > 1) {
+      a.part_ml[2 * part] = M;
+      a.part_ml[2 * part + 1] = l;
+    } else if (a.lse) {
+      a.lse[at] = some ? (M + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
     }
   }
 }
@@ -451,8 +797,10 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(AttendArgs a) {
   if (a.lse && f == 0) a.lse[at] = some ? (M + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
 }
 
-int query_tiles(const tav2_kv& c, const tav2_kv_queries& q) {
-  return int64_t(q.max_count) * (q.heads / c.kv_heads) > 32 && c.head_dim <= 64 ? 2 : 1;
+// Query rows of a workgroup: 16, 32, or (64 features at most: registers) 64.
+int tile_rows(const tav2_kv& c, const tav2_kv_queries& q) {
+  const int64_t rows = int64_t(q.max_count) * (q.heads / c.kv_heads);
+  return rows <= 16 ? 16 : rows > 32 && c.head_dim <= 64 ? 64 : 32;
 }
 
 // Pages that a query tile of the longest sequence sees, by the host's estimate.
@@ -468,21 +816,26 @@ int64_t most_pages(const tav2_kv& c, const tav2_kv_queries& q) {
 int share_pages(const tav2_kv& c, const tav2_kv_queries& q) {
   const int64_t rows = int64_t(q.max_count) * (q.heads / c.kv_heads);
   const int64_t seqs = q.total < c.num_seqs ? q.total : c.num_seqs;
-  const int64_t tile = 32 * query_tiles(c, q);
+  const int64_t tile = tile_rows(c, q);
   const int64_t groups = seqs * c.kv_heads * cdiv(rows, tile);
   const int64_t least = std::max<int64_t>(4, std::min<int64_t>(rows, tile) / 2);
-  return int(std::max<int64_t>(least, cdiv(groups * most_pages(c, q), SHARES)));
+  return int(std::max(least, std::min<int64_t>(SHARE_MOST, cdiv(groups * most_pages(c, q), SHARES))));
 }
 int key_splits(const tav2_kv& c, const tav2_kv_queries& q) {
   return int(cdiv(most_pages(c, q), share_pages(c, q)));
+}
+
+int near_seqs(const tav2_kv& c) { return c.num_seqs < 8 ? c.num_seqs : 8; }
+int64_t query_units(const tav2_kv& c, int splits) {
+  const int near = near_seqs(c);
+  return cdiv(splits * cdiv(c.num_seqs, near) * c.kv_heads, 8) * 8 * near;
 }
 
 }  // namespace
 
 int64_t kv_attend_groups(const tav2_kv& c, const tav2_kv_queries& q) {
   const int64_t rows = int64_t(q.max_count) * (q.heads / c.kv_heads);
-  const int64_t units = (int64_t(c.num_seqs) * c.kv_heads * key_splits(c, q) + 7) / 8 * 8;
-  return units * cdiv(rows, 32 * query_tiles(c, q));
+  return query_units(c, key_splits(c, q)) * cdiv(rows, tile_rows(c, q));
 }
 
 size_t kv_attend_bytes(const tav2_kv& c, const tav2_kv_queries& q) {
@@ -501,24 +854,29 @@ hipError_t launch_kv_attend(const tav2_kv& c, int layer, const tav2_kv_queries& 
   a.scale = q.scale > 0.f ? q.scale : 1.f / sqrtf(float(c.head_dim));
   a.out = static_cast<bf16_t*>(out);
   a.lse = lse;
-  const int QT = query_tiles(c, q);
+  const int tile = tile_rows(c, q), rows = q.max_count * (q.heads / c.kv_heads);
   a.splits = key_splits(c, q);
   a.chunk = share_pages(c, q);
-  a.tiles = int(cdiv(int64_t(q.max_count) * (q.heads / c.kv_heads), 32 * QT));
-  a.units = int((int64_t(c.num_seqs) * c.kv_heads * a.splits + 7) / 8 * 8);
+  a.tiles = int(cdiv(rows, tile));
+  a.group = tile == 16 && a.splits > 1 ? 16 / rows : 1;
+  a.near = near_seqs(c);
+  a.units = int(query_units(c, a.splits));
   a.part_o = static_cast<float*>(ws);
   if (a.splits > 1) a.part_ml = a.part_o + size_t(a.splits) * q.total * q.heads * c.head_dim;
   const unsigned grid = unsigned(a.units) * unsigned(a.tiles);
   {
     ProfScope prof("kv_attend", st);
     if (c.head_dim == 32) {
-      if (QT == 1) kv_attend_kernel<32, 1><<<grid, 256, 0, st>>>(a);
+      if (tile == 16) kv_attend16_kernel<32><<<grid, 256, 0, st>>>(a);
+      else if (tile == 32) kv_attend_kernel<32, 1><<<grid, 256, 0, st>>>(a);
       else kv_attend_kernel<32, 2><<<grid, 256, 0, st>>>(a);
     } else if (c.head_dim == 64) {
-      if (QT == 1) kv_attend_kernel<64, 1><<<grid, 256, 0, st>>>(a);
+      if (tile == 16) kv_attend16_kernel<64><<<grid, 256, 0, st>>>(a);
+      else if (tile == 32) kv_attend_kernel<64, 1><<<grid, 256, 0, st>>>(a);
       else kv_attend_kernel<64, 2><<<grid, 256, 0, st>>>(a);
     } else {
-      kv_attend_kernel<128, 1><<<grid, 256, 0, st>>>(a);
+      if (tile == 16) kv_attend16_kernel<128><<<grid, 256, 0, st>>>(a);
+      else kv_attend_kernel<128, 1><<<grid, 256, 0, st>>>(a);
     }
   }
   if (a.splits > 1) {
