@@ -17,6 +17,8 @@ namespace tav2 {
 
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int TK = 64;   // keys of a tile (bf16)
 
 struct WindowArgs {
@@ -78,7 +80,7 @@ __device__ __forceinline__ int swz_k(int row) {
 template <int D, int QT>
 __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_bf16(WindowArgs w) {
   constexpr int CH = D / 8;                       // 16-byte pieces of a row
-  constexpr int NK = (TK * CH + 255) / 256;       // pieces of K per thread
+  constexpr int NK = TK * CH / 256;               // pieces of K per thread
   constexpr int NV = (TK / 2 * CH + 255) / 256;   // pairs of pieces of V per thread
   __shared__ __align__(16) uint8_t lk[2][TK * D * 2], lv[2][D * TK * 2];
   Rows r;
@@ -108,44 +110,36 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_bf16(Windo
   const bool idle = wrow0 >= r.rows;
   const int wlo = wrow0 / r.G, whi = min(wrow0 + 32 * QT - 1, r.rows - 1) / r.G;
 
-  uint4 gk[NK], gv[NV][2];
+  u32x4 gk[NK], gv[NV][2];
   auto load = [&](int k0) {
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
-      const int e = tid + 256 * i;
-      if (TK * CH % 256 && e >= TK * CH) continue;
-      const int row = min(k0 + e / CH, r.len - 1);
-      gk[i] = *reinterpret_cast<const uint4*>(kb + int64_t(row) * a.k_ld + e % CH * 8);
+      const int e = tid + 256 * i, row = min(k0 + e / CH, r.len - 1);
+      gk[i] = *reinterpret_cast<const u32x4*>(kb + int64_t(row) * a.k_ld + e % CH * 8);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int e = tid + 256 * i;
-      if (TK / 2 * CH % 256 && e >= TK / 2 * CH) continue;
-      const int row = k0 + e / CH * 2;
+      const int e = (tid + 256 * i) % (TK / 2 * CH);   // (32 features: the second half again)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        gv[i][j] = *reinterpret_cast<const uint4*>(vb + int64_t(min(row + j, r.len - 1)) * a.v_ld +
-                                                   e % CH * 8);
+      for (int j = 0; j < 2; ++j) {
+        const int row = min(k0 + e / CH * 2 + j, r.len - 1);
+        gv[i][j] = *reinterpret_cast<const u32x4*>(vb + int64_t(row) * a.v_ld + e % CH * 8);
+      }
     }
   };
   auto store = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
-      const int e = tid + 256 * i;
-      if (TK * CH % 256 && e >= TK * CH) continue;
-      const int row = e / CH, ch = e % CH;
-      *reinterpret_cast<uint4*>(lk[buf] + row * D * 2 + (ch ^ swz_k<D>(row)) * 16) = gk[i];
+      const int e = tid + 256 * i, row = e / CH, ch = e % CH;
+      *reinterpret_cast<u32x4*>(lk[buf] + row * D * 2 + (ch ^ swz_k<D>(row)) * 16) = gk[i];
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int e = tid + 256 * i;
-      if (TK / 2 * CH % 256 && e >= TK / 2 * CH) continue;
-      const int kp = e / CH, d0 = e % CH * 8;
-      const uint32_t x[4] = {gv[i][0].x, gv[i][0].y, gv[i][0].z, gv[i][0].w};
-      const uint32_t y[4] = {gv[i][1].x, gv[i][1].y, gv[i][1].z, gv[i][1].w};
+      const int e = (tid + 256 * i) % (TK / 2 * CH), kp = e / CH, d0 = e % CH * 8;
 #pragma unroll
       for (int f = 0; f < 8; ++f) {
-        const uint32_t word = __builtin_amdgcn_perm(y[f / 2], x[f / 2], f % 2 ? 0x07060302u : 0x05040100u);
+        const uint32_t word = __builtin_amdgcn_perm(gv[i][1][f / 2], gv[i][0][f / 2],
+                                                    f % 2 ? 0x07060302u : 0x05040100u);
         const int d = d0 + f;
         *reinterpret_cast<uint32_t*>(lv[buf] + d * TK * 2 + ((kp / 4) ^ swz_v(d)) * 16 + kp % 4 * 4) = word;
       }
@@ -166,7 +160,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_bf16(Windo
     if (i + 1 < n) load(tiles.at(i + 1) * TK);
     const int see = idle ? 0 : tile_seen(k0, TK, wlo, whi, a.window, a.sinks);
     if (see) {
-#pragma unroll
+#pragma unroll 1   // (both halves at once take too many registers)
       for (int u = 0; u < 2; ++u) {
         auto keys = [&](bf16x8(&kf)[D / 16]) {
           const int row = 32 * u + key_row(m);
@@ -227,7 +221,7 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
   const int wrow0 = r.row0 + wave * 32;
   const float* kb = static_cast<const float*>(a.k) + r.off * a.k_ld + r.h * D;
   const float* vb = static_cast<const float*>(a.v) + r.off * a.v_ld + r.h * D;
-  float4 qf[D / 8];
+  f32x4 qf[D / 8];
   AttSeen<1> seen;
   seen.sinks = a.sinks;
   {
@@ -235,7 +229,7 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
     const float* p = static_cast<const float*>(a.q) + (r.off + pos) * a.q_ld +
                      (r.h * r.G + row % r.G) * D + half * (D / 2);
 #pragma unroll
-    for (int t = 0; t < D / 8; ++t) qf[t] = *reinterpret_cast<const float4*>(p + 4 * t);
+    for (int t = 0; t < D / 8; ++t) qf[t] = *reinterpret_cast<const f32x4*>(p + 4 * t);
     seen.hi[0] = pos + 1;
     seen.lo[0] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
   }
@@ -243,13 +237,13 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
   const Tiles tiles = tiles_seen(r.row0 / r.G, last_row / r.G, a.window, a.sinks, TF);
   const bool idle = wrow0 >= r.rows;
   const int wlo = wrow0 / r.G, whi = min(wrow0 + 31, r.rows - 1) / r.G;
-  float4 gk[NC], gv[NC];
+  f32x4 gk[NC], gv[NC];
   auto load = [&](int k0) {
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       const int e = tid + 256 * i, row = min(k0 + e / CH, r.len - 1), ch = e % CH * 4;
-      gk[i] = *reinterpret_cast<const float4*>(kb + int64_t(row) * a.k_ld + ch);
-      gv[i] = *reinterpret_cast<const float4*>(vb + int64_t(row) * a.v_ld + ch);
+      gk[i] = *reinterpret_cast<const f32x4*>(kb + int64_t(row) * a.k_ld + ch);
+      gv[i] = *reinterpret_cast<const f32x4*>(vb + int64_t(row) * a.v_ld + ch);
     }
   };
   AttState<D, 1> st;
@@ -263,7 +257,7 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
       const int e = tid + 256 * j, row = e / CH, ch = e % CH * 4;
-      *reinterpret_cast<float4*>(lk + row * KS + ch) = gk[j];
+      *reinterpret_cast<f32x4*>(lk + row * KS + ch) = gk[j];
       lv[(ch + 0) * VS + row] = gv[j].x;
       lv[(ch + 1) * VS + row] = gv[j].y;
       lv[(ch + 2) * VS + row] = gv[j].z;
@@ -279,7 +273,7 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
     const float* kr = lk + key_row(m) * KS + half * (D / 2);
 #pragma unroll
     for (int t = 0; t < D / 8; ++t) {
-      const float4 k4 = *reinterpret_cast<const float4*>(kr + 4 * t);
+      const f32x4 k4 = *reinterpret_cast<const f32x4*>(kr + 4 * t);
       s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.x, qf[t].x, s, 0, 0, 0);
       s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.y, qf[t].y, s, 0, 0, 0);
       s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.z, qf[t].z, s, 0, 0, 0);
@@ -291,7 +285,7 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
       const float* vr = lv + (32 * d + m) * VS + 16 * half;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const float4 v4 = *reinterpret_cast<const float4*>(vr + 4 * t);
+        const f32x4 v4 = *reinterpret_cast<const f32x4*>(vr + 4 * t);
         st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v4.x, s[4 * t], st.o[d][0], 0, 0, 0);
         st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v4.y, s[4 * t + 1], st.o[d][0], 0, 0, 0);
         st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v4.z, s[4 * t + 2], st.o[d][0], 0, 0, 0);
