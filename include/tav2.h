@@ -346,8 +346,8 @@ typedef struct tav2_window {
   const void*    q;            /* device, rows of [heads, head_dim], dtype; values finite */
   const void*    k;            /* device, rows of [kv_heads, head_dim], dtype; values finite */
   const void*    v;            /* device, rows of [kv_heads, head_dim], dtype; values finite */
-  int64_t q_ld, k_ld, v_ld;    /* elements from a row to the next: at least a row, multiples of
-                                  8 (bf16) or 4 (fp32) */
+  int64_t q_ld, k_ld, v_ld;    /* elements from a row to the next: at least a row, at most 2^24,
+                                  multiples of 8 (bf16) or 4 (fp32) */
   void*          out;          /* device [rows, heads, head_dim], dtype: token i's row i */
   float*         lse;          /* device [rows, heads], or NULL */
   const int64_t* offset;       /* device [R]: first row of each sequence */
@@ -418,7 +418,7 @@ tav2_status tav2_kv_extend(const tav2_kv* c, const int32_t* count, void* stream)
 /*
  * The keys and values of the tokens that the last tav2_kv_extend granted, for one layer
  * (once per layer and extension): sequence s's fresh[s] tokens are rows offset[s].. of k and v
- * (bf16 rows of [kv_heads, head_dim], row strides k_ld and v_ld elements, multiples of 8; 16-byte
+ * (bf16 rows of [kv_heads, head_dim], row strides k_ld and v_ld elements as in tav2_window; 16-byte
  * aligned; values finite).  Blocks that are full now go to their pages, the rest to the tail.
  *   offset    device int64 [num_seqs]
  *   max_count host-side bound of fresh[s]; tokens of a sequence past it are not written
@@ -444,7 +444,7 @@ typedef struct tav2_kv_queries {
   const void*    q;            /* device bf16: query i's head h at q + i * ld + h * head_dim */
   const int64_t* offset;       /* device [num_seqs + 1]; offset[0] = 0, offset[num_seqs] = total */
   int64_t total;               /* host: number of queries (>= 0) */
-  int64_t ld;                  /* elements between queries: a multiple of 8 */
+  int64_t ld;                  /* elements between queries, as in tav2_window */
   int32_t max_count;           /* host-side bound of a sequence's queries */
   int32_t heads;               /* a multiple of kv_heads */
   int32_t window, sinks;       /* >= 0 */

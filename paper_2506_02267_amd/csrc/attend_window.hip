@@ -20,6 +20,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int TK = 64;   // keys of a tile (bf16)
+constexpr int ROWS_256 = 1000000;   // workgroups of 256 rows, at least
 
 struct WindowArgs {
   tav2_window a;
@@ -35,10 +36,13 @@ struct Rows {
 
 __device__ __forceinline__ bool rows_of(const WindowArgs& w, int per, Rows& r) {
   const tav2_window& a = w.a;
-  int64_t u = blockIdx.x;
-  const int units = a.num_requests * a.kv_heads;
-  const int unit = int(u % units);
-  const int tile = w.tiles - 1 - int(u / units);   // the longest rows first
+  // The rows with the most keys first.  Workgroups go to the 8 XCDs in turn: a sequence's tiles are put
+  // one place further each time, since with its tiles all on one XCD some of these ended long after
+  // the others (32 sequences of 203 - 4000 tokens: 287 us, and now see below).
+  const int64_t units = int64_t(a.num_requests) * a.kv_heads;
+  const int64_t turn = blockIdx.x / units;
+  const int unit = int((blockIdx.x + turn) % units);
+  const int tile = w.tiles - 1 - int(turn);
   const int s = unit / a.kv_heads;
   r.h = unit % a.kv_heads;
   r.G = a.heads / a.kv_heads;
@@ -78,7 +82,7 @@ __device__ __forceinline__ int swz_k(int row) {
 }
 
 template <int D, int QT>
-__global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_bf16(WindowArgs w) {
+__global__ __launch_bounds__(256, 2) void attend_window_bf16(WindowArgs w) {
   constexpr int CH = D / 8;                       // 16-byte pieces of a row
   constexpr int NK = TK * CH / 256;               // pieces of K per thread
   constexpr int NV = (TK / 2 * CH + 255) / 256;   // pairs of pieces of V per thread
@@ -110,22 +114,35 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_bf16(Windo
   const bool idle = wrow0 >= r.rows;
   const int wlo = wrow0 / r.G, whi = min(wrow0 + 32 * QT - 1, r.rows - 1) / r.G;
 
+  // A thread's pieces of a tile, as byte offsets from the tile's first row: fixed but for a sequence's
+  // last tile, where rows past the end become its last one (their weights are 0).
   u32x4 gk[NK], gv[NV][2];
-  auto load = [&](int k0) {
+  uint32_t ok[NK], ov[NV][2];
+  auto offsets = [&](int last) {
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
-      const int e = tid + 256 * i, row = min(k0 + e / CH, r.len - 1);
-      gk[i] = *reinterpret_cast<const u32x4*>(kb + int64_t(row) * a.k_ld + e % CH * 8);
+      const int e = tid + 256 * i;
+      ok[i] = (uint32_t(min(e / CH, last)) * uint32_t(a.k_ld) + e % CH * 8) * 2;
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int e = (tid + 256 * i) % (TK / 2 * CH);   // (32 features: the second half again)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int row = min(k0 + e / CH * 2 + j, r.len - 1);
-        gv[i][j] = *reinterpret_cast<const u32x4*>(vb + int64_t(row) * a.v_ld + e % CH * 8);
-      }
+      for (int j = 0; j < 2; ++j)
+        ov[i][j] = (uint32_t(min(e / CH * 2 + j, last)) * uint32_t(a.v_ld) + e % CH * 8) * 2;
     }
+  };
+  offsets(TK - 1);
+  auto load = [&](int k0) {
+    if (k0 + TK > r.len) offsets(r.len - 1 - k0);   // (the last tile visited)
+    const char* kt = reinterpret_cast<const char*>(kb + int64_t(k0) * a.k_ld);
+    const char* vt = reinterpret_cast<const char*>(vb + int64_t(k0) * a.v_ld);
+#pragma unroll
+    for (int i = 0; i < NK; ++i) gk[i] = *reinterpret_cast<const u32x4*>(kt + ok[i]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) gv[i][j] = *reinterpret_cast<const u32x4*>(vt + ov[i][j]);
   };
   auto store = [&](int buf) {
 #pragma unroll
@@ -146,6 +163,15 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_bf16(Windo
     }
   };
 
+  // where this lane reads its operands of a tile's first half: key row, features; feature row, keys (32
+  // keys on are 64 bytes on; 32 features on the permutation is another by 4 pieces, 64 bytes)
+  uint32_t ak[D / 16], av[2];
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t)
+    ak[t] = key_row(m) * D * 2 + ((half * (D / 16) + t) ^ swz_k<D>(key_row(m))) * 16;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) av[t] = m * TK * 2 + ((2 * half + t) ^ swz_v(m)) * 16;
+
   AttState<D, QT> st;
   st.clear();
   float c[QT];
@@ -160,24 +186,21 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_bf16(Windo
     if (i + 1 < n) load(tiles.at(i + 1) * TK);
     const int see = idle ? 0 : tile_seen(k0, TK, wlo, whi, a.window, a.sinks);
     if (see) {
-#pragma unroll 1   // (both halves at once take too many registers)
+      const uint8_t* const kl = lk[buf];
+      const uint8_t* const vl = lv[buf];
+#pragma unroll QT == 1 && D <= 64 ? 2 : 1   // (both halves at once take too many registers elsewhere)
       for (int u = 0; u < 2; ++u) {
         auto keys = [&](bf16x8(&kf)[D / 16]) {
-          const int row = 32 * u + key_row(m);
 #pragma unroll
           for (int t = 0; t < D / 16; ++t)
-            kf[t] = as_bf16x8(*reinterpret_cast<const uint4*>(
-                lk[buf] + row * D * 2 + ((half * (D / 16) + t) ^ swz_k<D>(row)) * 16));
+            kf[t] = as_bf16x8(*reinterpret_cast<const uint4*>(kl + 32 * u * D * 2 + ak[t]));
         };
         auto values = [&](bf16x8(&vf)[D / 32][2]) {
 #pragma unroll
           for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              const int f = 32 * d + m;
-              vf[d][t] = as_bf16x8(*reinterpret_cast<const uint4*>(
-                  lv[buf] + f * TK * 2 + ((4 * u + 2 * half + t) ^ swz_v(f)) * 16));
-            }
+            for (int t = 0; t < 2; ++t)
+              vf[d][t] = as_bf16x8(*reinterpret_cast<const uint4*>(vl + 32 * d * TK * 2 + (av[t] ^ (64 * (u ^ (d & 1))))));
         };
         att_step<bf16x8, D, QT>(st, keys, values, qf, c, 0.f, 1.f, see == 1, seen,
                                 k0 + 32 * u + 16 * half);
@@ -309,9 +332,12 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
   if (a.lse && half == 0) a.lse[at] = (st.m[0] + __builtin_amdgcn_logf(l)) * LN2;
 }
 
+// Rows of a workgroup: 128, or 256 where that leaves enough of them (and 64 features at most:
+// registers).
 int rows_per_group(const tav2_window& a) {
   if (a.dtype == TAV2_F32 || a.head_dim == 128) return 128;
-  return 256;
+  const int64_t rows = int64_t(a.max_len) * (a.heads / a.kv_heads);
+  return int64_t(a.num_requests) * a.kv_heads * cdiv(rows, 256) >= ROWS_256 ? 256 : 128;
 }
 
 }  // namespace
@@ -333,8 +359,11 @@ hipError_t launch_attend_window(const tav2_window& a, hipStream_t st) {
     else if (a.head_dim == 64) attend_window_f32<64><<<grid, 256, 0, st>>>(w);
     else attend_window_f32<128><<<grid, 256, 0, st>>>(w);
   } else {
-    if (a.head_dim == 32) attend_window_bf16<32, 2><<<grid, 256, 0, st>>>(w);
-    else if (a.head_dim == 64) attend_window_bf16<64, 2><<<grid, 256, 0, st>>>(w);
+    const bool two = rows_per_group(a) == 256;
+    if (a.head_dim == 32 && two) attend_window_bf16<32, 2><<<grid, 256, 0, st>>>(w);
+    else if (a.head_dim == 32) attend_window_bf16<32, 1><<<grid, 256, 0, st>>>(w);
+    else if (a.head_dim == 64 && two) attend_window_bf16<64, 2><<<grid, 256, 0, st>>>(w);
+    else if (a.head_dim == 64) attend_window_bf16<64, 1><<<grid, 256, 0, st>>>(w);
     else attend_window_bf16<128, 1><<<grid, 256, 0, st>>>(w);
   }
   return hipGetLastError();

@@ -22,7 +22,7 @@ bool scale_ok(float s) { return s >= 0.f && s <= 3.0e38f; }
 
 // Rows of `heads` heads at least, `per` elements in 16 bytes.
 bool stride_ok(int64_t ld, int heads, int head_dim, int per) {
-  return ld >= int64_t(heads) * head_dim && ld % per == 0 && ld <= (int64_t(1) << 40);
+  return ld >= int64_t(heads) * head_dim && ld % per == 0 && ld <= (1 << 24);
 }
 
 tav2_status check_kv(const tav2_kv* c) {
