@@ -90,7 +90,8 @@ __global__ __launch_bounds__(256, 2) void attend_window_bf16(WindowArgs w) {
   Rows r;
   if (!rows_of(w, 128 * QT, r)) return;
   const tav2_window& a = w.a;
-  const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE, m = lane % 32, half = lane / 32;
+  const int tid = threadIdx.x, lane = tid % WAVE, m = lane % 32, half = lane / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);   // (scalar branches)
   const int wrow0 = r.row0 + wave * 32 * QT;
   const bf16_t* kb = static_cast<const bf16_t*>(a.k) + r.off * a.k_ld + r.h * D;
   const bf16_t* vb = static_cast<const bf16_t*>(a.v) + r.off * a.v_ld + r.h * D;
@@ -144,12 +145,16 @@ __global__ __launch_bounds__(256, 2) void attend_window_bf16(WindowArgs w) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) gv[i][j] = *reinterpret_cast<const u32x4*>(vt + ov[i][j]);
   };
+  // and its places in LDS
+  uint32_t sk[NK];
+#pragma unroll
+  for (int i = 0; i < NK; ++i) {
+    const int e = tid + 256 * i, row = e / CH;
+    sk[i] = row * D * 2 + ((e % CH) ^ swz_k<D>(row)) * 16;
+  }
   auto store = [&](int buf) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const int e = tid + 256 * i, row = e / CH, ch = e % CH;
-      *reinterpret_cast<u32x4*>(lk[buf] + row * D * 2 + (ch ^ swz_k<D>(row)) * 16) = gk[i];
-    }
+    for (int i = 0; i < NK; ++i) *reinterpret_cast<u32x4*>(lk[buf] + sk[i]) = gk[i];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int e = (tid + 256 * i) % (TK / 2 * CH), kp = e / CH, d0 = e % CH * 8;
@@ -240,7 +245,8 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
   Rows r;
   if (!rows_of(w, 128, r)) return;
   const tav2_window& a = w.a;
-  const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE, m = lane % 32, half = lane / 32;
+  const int tid = threadIdx.x, lane = tid % WAVE, m = lane % 32, half = lane / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);   // (scalar branches)
   const int wrow0 = r.row0 + wave * 32;
   const float* kb = static_cast<const float*>(a.k) + r.off * a.k_ld + r.h * D;
   const float* vb = static_cast<const float*>(a.v) + r.off * a.v_ld + r.h * D;
