@@ -2,9 +2,8 @@
 //
 // A workgroup takes 4 x 32 QT consecutive (position, head) rows of one kv head of a sequence; its
 // four waves share each 64-key tile through LDS: keys as rows, values by feature (two keys a 32-bit
-// word, turned while they are written), both in 16-byte pieces whose places are permuted so that
-// neither the writes nor the operand reads meet in a bank.  The next tile's loads are in flight while
-// the present one is multiplied, one barrier a tile.  Tiles that no row of the workgroup sees are not
+// word, turned while they are written).  The next tile's loads are in flight while the present one is
+// multiplied, one barrier a tile.  Tiles that no row of the workgroup sees are not
 // visited, and a wave skips those that none of its own sees, so the work is that of the window.
 // Bound by the vector units: an exponential, a scaling, a maximum, a sum and a rounding for each
 // score, beside 4 D matrix operations.
@@ -75,18 +74,20 @@ __device__ __forceinline__ int tile_seen(int k0, int tk, int lo, int hi, int win
   return low && k0 + tk - 1 <= lo ? 2 : 1;
 }
 
-__device__ __forceinline__ int swz_v(int d) { return (d & 7) ^ ((d >> 3) & 7); }
-template <int D>
-__device__ __forceinline__ int swz_k(int row) {
-  return D == 32 ? ((row >> 1) & 1) | ((row >> 4) & 1) << 1 : (row & 3) | ((row >> 4) & 1) << 2;
-}
+// The row of a half tile's operand that key k is (key_row's inverse).
+__device__ __forceinline__ int operand_row(int k) { return 8 * ((k >> 2) & 3) + 4 * (k >> 4 & 1) + (k & 3); }
 
 template <int D, int QT>
 __global__ __launch_bounds__(256, 2) void attend_window_bf16(WindowArgs w) {
   constexpr int CH = D / 8;                       // 16-byte pieces of a row
   constexpr int NK = TK * CH / 256;               // pieces of K per thread
   constexpr int NV = (TK / 2 * CH + 255) / 256;   // pairs of pieces of V per thread
-  __shared__ __align__(16) uint8_t lk[2][TK * D * 2], lv[2][D * TK * 2];
+  // Rows of 16 bytes more than their numbers take, so that the 8 neighbouring rows that lanes read together
+  // begin 4 banks apart; keys in the order of the operand's rows; a feature's 16-byte pieces of
+  // keys xor'ed by feature / 8, so that the writes of 8 features by 8 lanes do not meet either.
+  // Addresses are fixed and constants.
+  constexpr int KS = D * 2 + 16, VS = TK * 2 + 16;
+  __shared__ __align__(16) uint8_t lk[2][TK * KS], lv[2][D * VS];
   Rows r;
   if (!rows_of(w, 128 * QT, r)) return;
   const tav2_window& a = w.a;
@@ -146,36 +147,34 @@ __global__ __launch_bounds__(256, 2) void attend_window_bf16(WindowArgs w) {
       for (int j = 0; j < 2; ++j) gv[i][j] = *reinterpret_cast<const u32x4*>(vt + ov[i][j]);
   };
   // and its places in LDS
-  uint32_t sk[NK];
+  uint32_t sk[NK], sv[NV];
 #pragma unroll
   for (int i = 0; i < NK; ++i) {
-    const int e = tid + 256 * i, row = e / CH;
-    sk[i] = row * D * 2 + ((e % CH) ^ swz_k<D>(row)) * 16;
+    const int e = tid + 256 * i, k = e / CH;
+    sk[i] = (k / 32 * 32 + operand_row(k % 32)) * KS + e % CH * 16;
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int e = (tid + 256 * i) % (TK / 2 * CH);
+    sv[i] = e % CH * 8 * VS + (((e / CH) / 4) ^ (e % CH % 8)) * 16 + (e / CH) % 4 * 4;
   }
   auto store = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < NK; ++i) *reinterpret_cast<u32x4*>(lk[buf] + sk[i]) = gk[i];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int e = (tid + 256 * i) % (TK / 2 * CH), kp = e / CH, d0 = e % CH * 8;
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int f = 0; f < 8; ++f) {
-        const uint32_t word = __builtin_amdgcn_perm(gv[i][1][f / 2], gv[i][0][f / 2],
-                                                    f % 2 ? 0x07060302u : 0x05040100u);
-        const int d = d0 + f;
-        *reinterpret_cast<uint32_t*>(lv[buf] + d * TK * 2 + ((kp / 4) ^ swz_v(d)) * 16 + kp % 4 * 4) = word;
-      }
-    }
+      for (int f = 0; f < 8; ++f)
+        *reinterpret_cast<uint32_t*>(lv[buf] + sv[i] + f * VS) = __builtin_amdgcn_perm(
+            gv[i][1][f / 2], gv[i][0][f / 2], f % 2 ? 0x07060302u : 0x05040100u);
   };
-
-  // where this lane reads its operands of a tile's first half: key row, features; feature row, keys (32
-  // keys on are 64 bytes on; 32 features on the permutation is another by 4 pieces, 64 bytes)
-  uint32_t ak[D / 16], av[2];
+  // where this lane reads its operands: key row, features; feature row, keys
+  const uint32_t ak = m * KS + half * D;
+  uint32_t av[2][2];   // [keys' half, xor features' parity of 32][keys 8 t ..]
 #pragma unroll
-  for (int t = 0; t < D / 16; ++t)
-    ak[t] = key_row(m) * D * 2 + ((half * (D / 16) + t) ^ swz_k<D>(key_row(m))) * 16;
+  for (int x = 0; x < 2; ++x)
 #pragma unroll
-  for (int t = 0; t < 2; ++t) av[t] = m * TK * 2 + ((2 * half + t) ^ swz_v(m)) * 16;
+    for (int t = 0; t < 2; ++t) av[x][t] = m * VS + ((4 * x + 2 * half + t) ^ (m / 8)) * 16;
 
   AttState<D, QT> st;
   st.clear();
@@ -191,21 +190,21 @@ __global__ __launch_bounds__(256, 2) void attend_window_bf16(WindowArgs w) {
     if (i + 1 < n) load(tiles.at(i + 1) * TK);
     const int see = idle ? 0 : tile_seen(k0, TK, wlo, whi, a.window, a.sinks);
     if (see) {
-      const uint8_t* const kl = lk[buf];
+      const uint8_t* const kl = lk[buf] + ak;
       const uint8_t* const vl = lv[buf];
 #pragma unroll QT == 1 && D <= 64 ? 2 : 1   // (both halves at once take too many registers elsewhere)
       for (int u = 0; u < 2; ++u) {
         auto keys = [&](bf16x8(&kf)[D / 16]) {
 #pragma unroll
           for (int t = 0; t < D / 16; ++t)
-            kf[t] = as_bf16x8(*reinterpret_cast<const uint4*>(kl + 32 * u * D * 2 + ak[t]));
+            kf[t] = as_bf16x8(*reinterpret_cast<const uint4*>(kl + 32 * u * KS + 16 * t));
         };
         auto values = [&](bf16x8(&vf)[D / 32][2]) {
 #pragma unroll
           for (int d = 0; d < D / 32; ++d)
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-              vf[d][t] = as_bf16x8(*reinterpret_cast<const uint4*>(vl + 32 * d * TK * 2 + (av[t] ^ (64 * (u ^ (d & 1))))));
+              vf[d][t] = as_bf16x8(*reinterpret_cast<const uint4*>(vl + 32 * d * VS + av[u ^ (d & 1)][t]));
         };
         att_step<bf16x8, D, QT>(st, keys, values, qf, c, 0.f, 1.f, see == 1, seen,
                                 k0 + 32 * u + 16 * half);

@@ -510,7 +510,7 @@ __device__ __forceinline__ uint32_t shared_set(const AttendArgs& a, const Job& j
 // (16 g + 4 i + r in register r of tile i, g = l / 16), again the operand of O^T = V^T P^T as they
 // stand.  Half the vector work of a 32-row tile.
 template <int D>
-__global__ __launch_bounds__(256, 3) void kv_attend16_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(AttendArgs a) {
   constexpr int F = D / 4;           // features of a lane's quarter
   constexpr int NK = D / 32;         // products over the features
   constexpr int ND = D / 16;         // tiles of O^T
@@ -797,17 +797,25 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(AttendArgs a) {
   if (a.lse && f == 0) a.lse[at] = some ? (M + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
 }
 
-// Query rows of a workgroup: 16, 32, or (64 features at most: registers) 64.
-int tile_rows(const tav2_kv& c, const tav2_kv_queries& q) {
-  const int64_t rows = int64_t(q.max_count) * (q.heads / c.kv_heads);
-  return rows <= 16 ? 16 : rows > 32 && c.head_dim <= 64 ? 64 : 32;
-}
-
 // Pages that a query tile of the longest sequence sees, by the host's estimate.
 int64_t most_pages(const tav2_kv& c, const tav2_kv_queries& q) {
   int64_t tokens = c.max_len;
   if (q.window > 0) tokens = std::min(tokens, int64_t(q.window) + q.max_count + q.sinks + 2 * KVP);
   return std::max<int64_t>(1, cdiv(tokens, KVP));
+}
+
+// Query rows of a workgroup: 16, 32, or, where there are pages enough to fill the CUs with tiles of twice
+// the work, 64 (which turn a page's codes into operands once for twice the queries, but start and
+// end later; 64 features at most: registers).  Both sides, us a call, 4 heads of 64, one history
+// of 16384 tokens: 64 candidates 14.1 with 32 rows and 24.5 with 64, 200: 18.4 and 25.4, 500: 26.1 and 26.7,
+// 600 (10240 tiles x pages): 36.7 and 37.3, 800: 44.6 and 38.7, 1000: 42.2 and 40.1; 32 histories of 4096 - 16384
+// tokens, 64 candidates each: 79 and 66.
+int tile_rows(const tav2_kv& c, const tav2_kv_queries& q) {
+  const int64_t rows = int64_t(q.max_count) * (q.heads / c.kv_heads);
+  if (rows <= 16) return 16;
+  const int64_t seqs = std::min<int64_t>(q.total, c.num_seqs);
+  const int64_t work = seqs * c.kv_heads * cdiv(rows, 64) * most_pages(c, q);
+  return rows > 32 && c.head_dim <= 64 && work > 10240 ? 64 : 32;
 }
 
 // Pages to a workgroup's share: such that there are workgroups enough to fill the CUs and to even out
