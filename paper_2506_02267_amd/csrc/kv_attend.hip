@@ -475,15 +475,18 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
 
 // Sequences that hold the same pages in this share (copies of one another) are read once: of a window
 // of `a.group` neighbouring sequences, whose rows fit one tile together, the first of each set
-// takes the rows of all, and the others leave.  Returns the set as bits of the window (its own
-// alone where the share's first page has one holder), 0: leave.
+// takes the rows of all, and the others leave.  A share may end with the open block, which is each
+// sequence's own.  Returns the set as bits of the window (its own alone where the share's first
+// page has one holder), 0: leave.
 __device__ __forceinline__ uint32_t shared_set(const AttendArgs& a, const Job& j) {
   __shared__ uint32_t differ;
   const int base = j.s / a.group * a.group, me = j.s - base;
-  const int b0 = j.list.at(j.c0), last = j.list.at(j.c1 - 1);
+  const int full = j.len / KVP, last = j.list.at(j.c1 - 1);
+  const bool ends_open = last >= full;
+  const int p1 = j.c1 - (ends_open ? 1 : 0);   // the share's pages: [c0, p1)
   int holders = 0;
-  if (last < j.len / KVP) {
-    const int p = j.table[b0];
+  if (p1 > j.c0) {
+    const int p = j.table[j.list.at(j.c0)];
     if (p >= 0 && p < a.c.pages) holders = a.c.refs[p];
   }
   if (holders < 2) return 1u << me;
@@ -493,10 +496,11 @@ __device__ __forceinline__ uint32_t shared_set(const AttendArgs& a, const Job& j
   if (k < a.group && k != me) {
     Job o;
     bool same = base + k < a.c.num_seqs && job_of(a, base + k, 0, 16, o) &&
-                o.list.sink == j.list.sink && o.list.first == j.list.first && o.chunk == j.chunk &&
-                o.n >= j.c1 && last < o.len / KVP;
+                o.list.sink == j.list.sink && o.list.first == j.list.first &&
+                o.chunk == j.chunk && min(o.n, j.c0 + o.chunk) == j.c1 &&
+                (ends_open ? o.len / KVP == full : o.len / KVP > last);
     if (same)
-      for (int i = j.c0 + threadIdx.x % 16; i < j.c1; i += 16)
+      for (int i = j.c0 + threadIdx.x % 16; i < p1; i += 16)
         same &= o.table[j.list.at(i)] == j.table[j.list.at(i)];
     if (!same) atomicOr(&differ, 1u << k);
   }
@@ -530,8 +534,9 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
 
   // this lane's row: which (query, head) of which sequence, and what it sees
   int row = min(j.row0 + m, j.rows - 1), count = j.rows - j.row0, slot = j.s;
+  uint32_t set = 0;   // sequences taken together, if several
   if (a.group > 1) {
-    const uint32_t set = shared_set(a, j);
+    set = shared_set(a, j);
     if (set == 0) return;
     if (set & (set - 1)) {
       const int base = j.s / a.group * a.group;
@@ -554,7 +559,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
   const int64_t pos = a.causal ? int64_t(len) - query_count(a, slot) + i_q : len;
   const int64_t qi = q0 + i_q, at = qi * a.q.heads + j.h * j.G + row % j.G;
   const int64_t end = pos + 1 < len ? pos + 1 : len, low = pos - a.q.window + 1;
-  const int hi = int(end > 0 ? end : 0), lo = a.q.window > 0 && low > 0 ? int(low) : 0;
+  int hi = int(end > 0 ? end : 0);
+  const int lo = a.q.window > 0 && low > 0 ? int(low) : 0;
   int all_hi = hi, all_lo = lo;   // what all rows see: from the last one's first key to the first's last
 #pragma unroll
   for (int o = 8; o >= 1; o >>= 1) {
@@ -639,7 +645,6 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
     }
   };
   const int krow = 16 * (m / 4) + m % 4;   // + 4 i: the key of tile i that this lane's row is
-  bool open = false;
   for (int i = j.c0 + wave, t = 0; i < j.c1; i += 4, ++t) {
     if (t == WAVE) {
       t = 0;
@@ -648,7 +653,6 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
       feed.load(a, j, page);
     }
     const int b = j.list.at(i);
-    open |= b >= full;
     const int next = t + 1 < WAVE ? feed.page(t + 1) : -1;
     float ks, lv, inv;
     feed.factors(t, &ks, &lv, &inv);
@@ -679,9 +683,11 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
     }
     page = next;
   }
-  if (open) {   // the open block, in bf16 (as in the kernel above)
-    const int64_t tail = kv_tail(c, a.layer, j.s, j.h);
-    const int held = j.len - full * KVP;
+  // the open block, in bf16 (as in the kernel above): this sequence's, or, of several taken together,
+  // each one's, which its own rows alone see, by the waves in turn
+  auto open_block = [&](int of) {
+    const int64_t tail = kv_tail(c, a.layer, of, j.h);
+    const int held = kv_len(c, of) - full * KVP;
     float kt = 0.f, vt = 0.f, fk, backk, fv, backv;
     auto raw_key = [&](int i, int t) {
       return first_of8(*reinterpret_cast<const u32x4*>(c.k_tail + tail + (krow + 4 * i) * D + g * F + 8 * t),
@@ -717,6 +723,17 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
       for (int t = 0; t < 2; ++t) vf[t] = scaled8h(raw_value(d, t), fv);
     };
     step(keys, values, cq * backk, __builtin_amdgcn_logf(backv), fv, full * KVP);
+  };
+  if (j.list.at(j.c1 - 1) >= full) {
+    const int mine = hi, base = j.s / a.group * a.group;
+    if (set == 0) set = 1u << (j.s - base);
+    int turn = j.c1 - 1 - j.c0;   // (the wave whose turn it is takes a single one)
+    while (set) {
+      const int of = base + __builtin_ctz(set);
+      set &= set - 1;
+      hi = slot == of ? mine : 0;
+      if (turn++ % 4 == wave) open_block(of);
+    }
   }
 
   // the four waves' states meet in LDS; wave w joins every fourth tile of O^T, in the order of the waves
