@@ -110,8 +110,8 @@ class Cache:
             x = np.stack([r[layer] for r in rows])
             for a in range(0, len(rows) // PAGE * PAGE, PAGE):
                 for h in range(x.shape[1]):
-                    c, scale = quantise(x[a:a + PAGE, h])
-                    x[a:a + PAGE, h] = c * scale
+                    codes, scale = quantise(x[a:a + PAGE, h])
+                    x[a:a + PAGE, h] = codes * scale
             out.append(x)
         held = np.ones(self.len[s], dtype=bool)
         for b, p in enumerate(self.table[s]):

@@ -402,7 +402,7 @@ def attend_pair(p, n, heads, causal, window=0, sinks=0, layer=0, scale=0.0, max_
             continue
         want = p.ref.attend(s, layer, q[sl].double().cpu().numpy(), causal, window, sinks,
                             scale if scale else None)
-        check(out[sl], lse[sl], want, p.D, HALF, p.ref.len[s], p.vmax(s, layer))
+        check(out[sl], lse[sl], want, p.D, HALF, max(p.ref.len[s], 1), p.vmax(s, layer))
     return q, out, lse
 
 
@@ -453,6 +453,62 @@ def test_kv_attend_trimmed_pages_are_not_seen():
     attend_pair(p, [4, 4, 4], 2, False, 0, 0)         # the whole: what is gone is not seen
     p.trim(1, 0)
     attend_pair(p, [2, 70, 3], 2, False, 0, 0)        # a sequence with nothing left sees nothing
+
+
+@pytest.mark.parametrize("D,Hkv,heads,causal,window,sinks", [
+    (64, 2, 4, False, 0, 0), (64, 1, 1, True, 0, 0), (32, 1, 2, True, 900, 70),
+    (128, 1, 4, False, 1500, 1), (64, 4, 4, True, 3000, 0)])
+def test_kv_attend_copies_of_one_sequence(D, Hkv, heads, causal, window, sinks):
+    """Forks, whose common pages are read once for several of them: next to each other and apart,
+    with other sequences between, of different query counts, grown apart by a few tokens, by a block,
+    trimmed, and with parents that are gone."""
+    print(f"copies: D {D} heads {heads}/{Hkv} causal {causal} window {window} sinks {sinks}", flush=True)
+    p = Pair(seqs=19, pages=400, blocks=60, H=Hkv, D=D, seed=D + heads)
+    p.grow([2500, 2496, 1300] + [0] * 16)
+    #          3..10 of the first, one of the third among them, 12.. of the second
+    p.fork([-1] * 3 + [0, 0, 0, 0, 2, 0, 0, 0, -1, 1, 1, 1, 1, 1, -1, 0])
+    g = np.random.default_rng(heads)
+    most = max(1, 16 * Hkv // heads // 3)
+    for step in range(3):
+        n = [0, 1, 0] + [int(x) for x in g.integers(0, most + 1, size=16)]
+        n[4], n[5] = most, most
+        n = [min(x, p.ref.len[s]) if causal else x for s, x in enumerate(n)]
+        attend_pair(p, n, heads, causal, window, sinks, seed=step)
+        attend_pair(p, [1] * 19, heads, causal, window, sinks, seed=step + 50)
+        if step == 0:      # different open blocks, one that fills, one that is left
+            p.grow([0, 3, 0, 1, 0, 5, 60, 2, 1, 1, 70, 0, 4, 64, 1, 1, 1, 0, 0])
+        elif step == 1:    # the parents go, the copies keep their pages; other sequences take their places
+            p.free([1, 1, 0] + [0] * 8 + [1] + [0] * 4 + [1, 0, 0])
+            p.grow([100, 2500, 0] + [0] * 16)
+            if window:
+                p.trim(window, sinks)
+    p.same()
+
+
+def test_kv_attend_copies_give_the_bits_of_sequences_of_their_own():
+    """Reading common pages once changes no result: a fork's attention is its parent's."""
+    p = Pair(seqs=9, pages=200, blocks=60, H=2, D=64, seed=77)
+    p.grow([3333] + [0] * 8)
+    p.fork([-1] + [0] * 8)
+    g = torch.Generator().manual_seed(5)
+    q1 = rows(g, 2, 4, 64)
+    one = torch.tensor([0, 2] + [2] * 8).cuda()
+    want = T.kv_attend(p.gpu, 0, q1, one, 2, flags=T.MASK_NONE)
+    each = torch.arange(10).cuda() * 2
+    got = T.kv_attend(p.gpu, 0, q1.repeat(9, 1, 1), each, 2, flags=T.MASK_NONE)
+    err = (got.float().view(9, 2, 4, 64) - want.float()).abs().max()
+    # (shares divided otherwise: sums of other halves; a rounding to bf16 apart at most)
+    assert float(err) <= float(want.float().abs().max()) * 2.0 ** -7
+    assert all(torch.equal(got[:2], got[2 * i:2 * i + 2]) for i in range(9))
+
+
+@pytest.mark.parametrize("n", [1, 16, 17, 33, 64, 65, 130, 700])
+def test_kv_attend_every_tile_size(n):
+    """16, 32 and 64 query rows a workgroup, and rows beside the last tile."""
+    p = Pair(seqs=3, pages=1200, blocks=400, H=4, D=64, seed=n)
+    p.grow([16400, 200, 0])
+    attend_pair(p, [n, min(n, 3), 1], 4, False, seed=n)
+    attend_pair(p, [min(n, 200), min(n, 50), 2], 8, True, 5000, 100, seed=n + 1)
 
 
 def test_kv_attend_extreme_scales():
