@@ -5,6 +5,8 @@
 // state and its arguments only: no list whose order would follow the order of atomics.  Page numbers and
 // lengths are clamped before they index anything, so a corrupted table cannot make a kernel leave its
 // buffers.
+#include <atomic>
+
 #include "common.h"
 #include "internal.h"
 #include "kv_common.h"
@@ -162,7 +164,7 @@ __global__ __launch_bounds__(256) void kv_trim_kernel(tav2_kv c, int window, int
   const int s = blockIdx.x;
   const int len = kv_len(c, s);
   const int last = len - window + 1;   // the first position that stays visible
-  release(c, s, (sinks + KVP - 1) / KVP, last > 0 ? last / KVP : 0);
+  release(c, s, sinks / KVP + (sinks % KVP != 0), last > 0 ? last / KVP : 0);
 }
 
 // Whether this call makes sequence s a copy, and of which one.
@@ -298,6 +300,18 @@ __global__ __launch_bounds__(256) void kv_compact_kernel(tav2_kv c, KvPlan plan)
 
 hipError_t launch_kv_extend(const tav2_kv& c, const int32_t* count, hipStream_t st) {
   static_assert(TAV2_KV_SEQS_MAX * 4 <= 128 * 1024, "the prefix sums fit LDS");
+  if (c.num_seqs > 8192) {   // more LDS than a kernel has without asking
+    static std::atomic<bool> done[64] = {};
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev < 0 || dev >= 64 || !done[dev].load(std::memory_order_acquire)) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kv_extend_kernel),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, TAV2_KV_SEQS_MAX * 4);
+      if (e != hipSuccess) return e;
+      if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
+    }
+  }
   ProfScope prof("kv_extend", st);
   kv_extend_kernel<<<1, EXT_NT, size_t(c.num_seqs) * 4, st>>>(c, count);
   return hipGetLastError();

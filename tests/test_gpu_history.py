@@ -150,6 +150,27 @@ def test_attend_window_extreme_scores(dtype, D):
         check(out, lse, want, D, dtype, L)
 
 
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (70, 2 ** 31 - 1),
+                                          (0, 2 ** 31 - 1)])
+def test_largest_window_and_sinks_are_none(window, sinks):
+    L, D = 500, 64
+    g = torch.Generator().manual_seed(13)
+    q, k, v = (rows(g, L, 2, D) for _ in range(3))
+    off, length = torch.zeros(1, dtype=torch.int64).cuda(), torch.tensor([L], dtype=torch.int32).cuda()
+    want = T.attend_window(q, k, v, off, length, L)
+    got = T.attend_window(q, k, v, off, length, L, window=window, sinks=sinks)
+    assert torch.equal(want, got)
+    p = Pair(seqs=1, pages=9, blocks=9, H=2, D=D, seed=1)
+    p.grow([L])
+    q = rows(g, 40, 2, D)
+    o2 = torch.tensor([0, 40]).cuda()
+    for flags in (T.MASK_NONE, T.MASK_CAUSAL):
+        want = T.kv_attend(p.gpu, 0, q, o2, 40, flags=flags)
+        got = T.kv_attend(p.gpu, 0, q, o2, 40, flags=flags, window=window, sinks=sinks)
+        # (a window may divide the work otherwise)
+        assert float((want.float() - got.float()).abs().max()) <= 2.0 ** -7 * float(want.abs().max())
+
+
 def test_attend_window_does_not_see_the_future():
     """NaN and infinities in later tokens' tiles do not reach the rows of earlier tiles."""
     L, H, D = 600, 2, 64
@@ -320,6 +341,23 @@ def test_extend_many_sequences_and_pages():
         assert table[s, :len(ref.table[s])].tolist() == ref.table[s]
 
 
+def test_the_most_sequences():
+    n = T.KV_SEQS_MAX
+    c = new_cache(n, 50000, 4, 1, 32, dirty=False)
+    ref = history.Cache(n, 50000, 4)
+    g = np.random.default_rng(8)
+    for step in range(2):
+        count = g.integers(0, 140, size=n)
+        T.kv_extend(c, torch.from_numpy(count.astype(np.int32)).cuda())
+        ref.extend([int(x) for x in count])
+        assert c.fresh.tolist() == ref.fresh and c.refs.tolist() == ref.refs
+    table = c.table.cpu().numpy()
+    assert all(table[s, :len(ref.table[s])].tolist() == ref.table[s] for s in range(n))
+    T.kv_trim(c, 2 ** 31 - 1, 2 ** 31 - 1)      # nothing to release, at the largest arguments
+    T.kv_free(c, torch.ones(n, dtype=torch.uint8, device="cuda"))
+    assert int(c.refs.abs().sum()) == 0 and int((c.table != -1).sum()) == 0
+
+
 def test_fork_shares_pages_and_copies_tails():
     p = Pair(seqs=8, pages=30, blocks=6, H=2, D=64, layers=2, seed=7)
     p.grow([130, 64, 5, 0, 0, 0, 0, 0])
@@ -342,6 +380,8 @@ def test_trim_and_compact():
     p.grow([1000, 64, 63, 640])
     p.fork([-1, -1, -1, -1])
     p.trim(2000, 0)
+    p.same()
+    p.trim(10, 2 ** 31 - 1)
     p.same()
     p.trim(300, 65)
     p.same()

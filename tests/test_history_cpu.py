@@ -50,7 +50,7 @@ def fake_window(**kw):
     (dict(num_requests=-1), -2), (dict(max_len=-1), -2), (dict(heads=0), -2), (dict(heads=3), -2),
     (dict(kv_heads=0), -2), (dict(window=-1), -2), (dict(sinks=-1), -2), (dict(scale=-1.0), -2),
     (dict(scale=float("nan")), -2), (dict(scale=float("inf")), -2),
-    (dict(q_ld=255), -2), (dict(q_ld=248), -2), (dict(k_ld=120), -2), (dict(v_ld=132), -2),
+    (dict(q_ld=255), -2), (dict(q_ld=248), -2), (dict(q_ld=(1 << 24) + 8), -2), (dict(k_ld=120), -2), (dict(v_ld=132), -2),
     (dict(q=FAKE + 8), -2), (dict(k=FAKE + 2), -2), (dict(v=FAKE + 4), -2), (dict(out=FAKE + 8), -2),
     (dict(head_dim=48, q_ld=192, k_ld=96, v_ld=96), -4), (dict(head_dim=256, q_ld=1024), -4),
     (dict(max_len=1 << 30), -4), (dict(num_requests=1 << 30, max_len=1 << 20), -4),
