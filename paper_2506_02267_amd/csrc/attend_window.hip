@@ -1,7 +1,7 @@
 // Causal attention of packed sequences with a window and sink tokens.
 //
-// A workgroup takes 4 x 32 QT consecutive (position, head) rows of one kv head of a sequence; its
-// four waves share each 64-key tile through LDS: keys as rows, values by feature (two keys a 32-bit
+// A workgroup takes 128 consecutive (position, head) rows of one kv head of a sequence; its four waves
+// (or eight, below) share each 64-key tile through LDS: keys as rows, values by feature (two keys a 32-bit
 // word, turned while they are written).  The next tile's loads are in flight while the present one is
 // multiplied, one barrier a tile.  Tiles that no row of the workgroup sees are not
 // visited, and a wave skips those that none of its own sees, so the work is that of the window.
@@ -19,7 +19,12 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int TK = 64;   // keys of a tile (bf16)
-constexpr int ROWS_256 = 1000000;   // workgroups of 256 rows, at least
+constexpr int ROWS = 128;   // rows of a workgroup, 32 a wave
+// Workgroups up to which a second four waves take the other half of each tile's keys: few ones leave
+// SIMDs idle.  Both sides, us: 512 workgroups, 16384 tokens whole 227 and 291, with a window of 1024 35.0
+// and 38.4, 4 x 4096 62.8 and 78.5; 1024, 8 x 4096 108.7 and 104; some 2000 (32 histories of 203 - 4000 tokens)
+// 155 and 147; 4096, 64 x 2048 with a window of 512 151 and 136.
+constexpr int64_t SPLIT_GROUPS = 768;
 
 struct WindowArgs {
   tav2_window a;
@@ -33,7 +38,7 @@ struct Rows {
   int len, rows, row0, h, G;
 };
 
-__device__ __forceinline__ bool rows_of(const WindowArgs& w, int per, Rows& r) {
+__device__ __forceinline__ bool rows_of(const WindowArgs& w, Rows& r) {
   const tav2_window& a = w.a;
   // The rows with the most keys first.  Workgroups go to the 8 XCDs in turn: a sequence's tiles are put
   // one place further each time, since with its tiles all on one XCD some of these ended long after
@@ -48,7 +53,7 @@ __device__ __forceinline__ bool rows_of(const WindowArgs& w, int per, Rows& r) {
   r.off = a.offset[s];
   r.len = a.len[s] < a.max_len ? a.len[s] : a.max_len;
   r.rows = r.len * r.G;
-  r.row0 = tile * per;
+  r.row0 = tile * ROWS;
   return r.row0 < r.rows;
 }
 
@@ -77,8 +82,8 @@ __device__ __forceinline__ int tile_seen(int k0, int tk, int lo, int hi, int win
 // The row of a half tile's operand that key k is (key_row's inverse).
 __device__ __forceinline__ int operand_row(int k) { return 8 * ((k >> 2) & 3) + 4 * (k >> 4 & 1) + (k & 3); }
 
-template <int D, int QT>
-__global__ __launch_bounds__(256, 2) void attend_window_bf16(WindowArgs w) {
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(SPLIT ? 512 : 256, SPLIT && D <= 64 ? 4 : 2) void attend_window_bf16(WindowArgs w) {
   constexpr int CH = D / 8;                       // 16-byte pieces of a row
   constexpr int NK = TK * CH / 256;               // pieces of K per thread
   constexpr int NV = (TK / 2 * CH + 255) / 256;   // pairs of pieces of V per thread
@@ -87,51 +92,59 @@ __global__ __launch_bounds__(256, 2) void attend_window_bf16(WindowArgs w) {
   // keys xor'ed by feature / 8, so that the writes of 8 features by 8 lanes do not meet either.
   // Addresses are fixed and constants.
   constexpr int KS = D * 2 + 16, VS = TK * 2 + 16;
-  __shared__ __align__(16) uint8_t lk[2][TK * KS], lv[2][D * VS];
+  __shared__ __align__(16) uint8_t lds[2 * (TK * KS + D * VS)];
+  auto lk = [&](int buf) { return lds + buf * (TK * KS); };
+  auto lv = [&](int buf) { return lds + 2 * TK * KS + buf * (D * VS); };
   Rows r;
-  if (!rows_of(w, 128 * QT, r)) return;
+  if (!rows_of(w, r)) return;
   const tav2_window& a = w.a;
   const int tid = threadIdx.x, lane = tid % WAVE, m = lane % 32, half = lane / 32;
-  const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);   // (scalar branches)
-  const int wrow0 = r.row0 + wave * 32 * QT;
+  // (scalar, for scalar branches; with SPLIT the second four waves take the same rows, and each four
+  // one half of a tile's keys)
+  const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE) % 4;
+  const int part = SPLIT ? __builtin_amdgcn_readfirstlane(tid / 256) : 0;
+  const int wrow0 = r.row0 + wave * 32;
   const bf16_t* kb = static_cast<const bf16_t*>(a.k) + r.off * a.k_ld + r.h * D;
   const bf16_t* vb = static_cast<const bf16_t*>(a.v) + r.off * a.v_ld + r.h * D;
 
-  bf16x8 qf[QT][D / 16];
-  AttSeen<QT> seen;
+  bf16x8 qf[1][D / 16];
+  AttSeen<1> seen;
   seen.sinks = a.sinks;
-#pragma unroll
-  for (int q = 0; q < QT; ++q) {
-    const int row = min(wrow0 + 32 * q + m, r.rows - 1);
+  {
+    const int row = min(wrow0 + m, r.rows - 1);
     const int pos = row / r.G;
     const bf16_t* p = static_cast<const bf16_t*>(a.q) + (r.off + pos) * a.q_ld +
                       (r.h * r.G + row % r.G) * D + half * (D / 2);
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) qf[q][t] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 8 * t));
-    seen.hi[q] = pos + 1;
-    seen.lo[q] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+    for (int t = 0; t < D / 16; ++t) qf[0][t] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 8 * t));
+    seen.hi[0] = pos + 1;
+    seen.lo[0] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
   }
-  const int last_row = min(r.row0 + 128 * QT, r.rows) - 1;
+  const int last_row = min(r.row0 + ROWS, r.rows) - 1;
   const Tiles tiles = tiles_seen(r.row0 / r.G, last_row / r.G, a.window, a.sinks, TK);
   const bool idle = wrow0 >= r.rows;
-  const int wlo = wrow0 / r.G, whi = min(wrow0 + 32 * QT - 1, r.rows - 1) / r.G;
+  const int wlo = wrow0 / r.G, whi = min(wrow0 + 31, r.rows - 1) / r.G;
 
   // A thread's pieces of a tile, as byte offsets from the tile's first row: fixed but for a sequence's
-  // last tile, where rows past the end become its last one (their weights are 0).
-  u32x4 gk[NK], gv[NV][2];
-  uint32_t ok[NK], ov[NV][2];
+  // last tile, where rows past the end become its last one (their weights are 0).  With SPLIT the first
+  // four waves bring the values, the others the keys.
+  constexpr int NP = SPLIT ? 2 * NV : NK + 2 * NV;
+  constexpr int VP = SPLIT ? 0 : NK;   // the first of the values' pieces
+  const int t256 = tid % 256;
+  u32x4 piece[NP];
+  uint32_t from[NP];
   auto offsets = [&](int last) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const int e = tid + 256 * i;
-      ok[i] = (uint32_t(min(e / CH, last)) * uint32_t(a.k_ld) + e % CH * 8) * 2;
+    for (int i = 0; i < (SPLIT ? NP : NK); ++i) {
+      if (SPLIT && part == 0) break;
+      const int e = (t256 + 256 * i) % (TK * CH);
+      from[i] = (uint32_t(min(e / CH, last)) * uint32_t(a.k_ld) + e % CH * 8) * 2;
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int e = (tid + 256 * i) % (TK / 2 * CH);   // (32 features: the second half again)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        ov[i][j] = (uint32_t(min(e / CH * 2 + j, last)) * uint32_t(a.v_ld) + e % CH * 8) * 2;
+    for (int i = 0; i < 2 * NV; ++i) {
+      if (SPLIT && part == 1) break;
+      const int e = (t256 + 256 * (i / 2)) % (TK / 2 * CH);   // (32 features: the second half again)
+      from[VP + i] = (uint32_t(min(e / CH * 2 + i % 2, last)) * uint32_t(a.v_ld) + e % CH * 8) * 2;
     }
   };
   offsets(TK - 1);
@@ -139,48 +152,50 @@ __global__ __launch_bounds__(256, 2) void attend_window_bf16(WindowArgs w) {
     if (k0 + TK > r.len) offsets(r.len - 1 - k0);   // (the last tile visited)
     const char* kt = reinterpret_cast<const char*>(kb + int64_t(k0) * a.k_ld);
     const char* vt = reinterpret_cast<const char*>(vb + int64_t(k0) * a.v_ld);
+    if (SPLIT && part == 0) kt = vt;
 #pragma unroll
-    for (int i = 0; i < NK; ++i) gk[i] = *reinterpret_cast<const u32x4*>(kt + ok[i]);
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) gv[i][j] = *reinterpret_cast<const u32x4*>(vt + ov[i][j]);
+    for (int i = 0; i < NP; ++i)
+      piece[i] = *reinterpret_cast<const u32x4*>((SPLIT || i < NK ? kt : vt) + from[i]);
   };
   // and its places in LDS
-  uint32_t sk[NK], sv[NV];
+  uint32_t sk[SPLIT ? NP : NK], sv[NV];
 #pragma unroll
-  for (int i = 0; i < NK; ++i) {
-    const int e = tid + 256 * i, k = e / CH;
+  for (int i = 0; i < (SPLIT ? NP : NK); ++i) {
+    const int e = (t256 + 256 * i) % (TK * CH), k = e / CH;
     sk[i] = (k / 32 * 32 + operand_row(k % 32)) * KS + e % CH * 16;
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int e = (tid + 256 * i) % (TK / 2 * CH);
+    const int e = (t256 + 256 * i) % (TK / 2 * CH);
     sv[i] = e % CH * 8 * VS + (((e / CH) / 4) ^ (e % CH % 8)) * 16 + (e / CH) % 4 * 4;
   }
   auto store = [&](int buf) {
+    if (!SPLIT || part == 1) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) *reinterpret_cast<u32x4*>(lk[buf] + sk[i]) = gk[i];
+      for (int i = 0; i < (SPLIT ? NP : NK); ++i) *reinterpret_cast<u32x4*>(lk(buf) + sk[i]) = piece[i];
+    }
+    if (!SPLIT || part == 0) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+      for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int f = 0; f < 8; ++f)
-        *reinterpret_cast<uint32_t*>(lv[buf] + sv[i] + f * VS) = __builtin_amdgcn_perm(
-            gv[i][1][f / 2], gv[i][0][f / 2], f % 2 ? 0x07060302u : 0x05040100u);
+        for (int f = 0; f < 8; ++f)
+          *reinterpret_cast<uint32_t*>(lv(buf) + sv[i] + f * VS) =
+              __builtin_amdgcn_perm(piece[VP + 2 * i + 1][f / 2], piece[VP + 2 * i][f / 2],
+                                    f % 2 ? 0x07060302u : 0x05040100u);
+    }
   };
   // where this lane reads its operands: key row, features; feature row, keys
-  const uint32_t ak = m * KS + half * D;
+  // (with SPLIT, of the wave's half)
+  const uint32_t ak = (32 * part + m) * KS + half * D;
   uint32_t av[2][2];   // [keys' half, xor features' parity of 32][keys 8 t ..]
 #pragma unroll
   for (int x = 0; x < 2; ++x)
 #pragma unroll
-    for (int t = 0; t < 2; ++t) av[x][t] = m * VS + ((4 * x + 2 * half + t) ^ (m / 8)) * 16;
+    for (int t = 0; t < 2; ++t) av[x][t] = m * VS + ((4 * (x ^ part) + 2 * half + t) ^ (m / 8)) * 16;
 
-  AttState<D, QT> st;
+  AttState<D, 1> st;
   st.clear();
-  float c[QT];
-#pragma unroll
-  for (int q = 0; q < QT; ++q) c[q] = w.scale * LOG2E;
+  const float c[1] = {w.scale * LOG2E};
   const int n = tiles.count();
   load(tiles.at(0) * TK);
   store(0);
@@ -190,10 +205,10 @@ __global__ __launch_bounds__(256, 2) void attend_window_bf16(WindowArgs w) {
     if (i + 1 < n) load(tiles.at(i + 1) * TK);
     const int see = idle ? 0 : tile_seen(k0, TK, wlo, whi, a.window, a.sinks);
     if (see) {
-      const uint8_t* const kl = lk[buf] + ak;
-      const uint8_t* const vl = lv[buf];
-#pragma unroll QT == 1 && D <= 64 ? 2 : 1   // (both halves at once take too many registers elsewhere)
-      for (int u = 0; u < 2; ++u) {
+      const uint8_t* const kl = lk(buf) + ak;
+      const uint8_t* const vl = lv(buf);
+#pragma unroll D <= 64 ? 2 : 1   // (128 features: both halves at once take too many registers)
+      for (int u = 0; u < (SPLIT ? 1 : 2); ++u) {
         auto keys = [&](bf16x8(&kf)[D / 16]) {
 #pragma unroll
           for (int t = 0; t < D / 16; ++t)
@@ -206,30 +221,50 @@ __global__ __launch_bounds__(256, 2) void attend_window_bf16(WindowArgs w) {
             for (int t = 0; t < 2; ++t)
               vf[d][t] = as_bf16x8(*reinterpret_cast<const uint4*>(vl + 32 * d * VS + av[u ^ (d & 1)][t]));
         };
-        att_step<bf16x8, D, QT>(st, keys, values, qf, c, 0.f, 1.f, see == 1, seen,
-                                k0 + 32 * u + 16 * half);
+        att_step<bf16x8, D, 1>(st, keys, values, qf, c, 0.f, 1.f, see == 1, seen,
+                                k0 + 32 * (u + part) + 16 * half);
       }
     }
     if (i + 1 < n) store(buf ^ 1);
     __syncthreads();
   }
+  if constexpr (SPLIT) {   // the second halves' states, through the tiles' LDS, into the first's
+    static_assert(4 * (D / 32) * 16 * WAVE * 4 <= int(sizeof(lds)), "they fit");
+    __shared__ float ml[4][2][WAVE];
+    float* const their = reinterpret_cast<float*>(lds) + wave * (D / 32) * 16 * WAVE + lane;
+    if (part == 1) {
+      ml[wave][0][lane] = st.m[0];
+      ml[wave][1][lane] = st.l[0];
 #pragma unroll
-  for (int q = 0; q < QT; ++q) {
-    const int row = wrow0 + 32 * q + m;
-    const float l = xsum32(st.l[q]);
-    if (row >= r.rows) continue;
-    const int64_t at = (r.off + row / r.G) * a.heads + r.h * r.G + row % r.G;
-    const float inv = 1.f / l;   // a row sees itself: l > 0
-    bf16_t* out = static_cast<bf16_t*>(a.out) + at * D + 4 * half;
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) their[(d * 16 + e) * WAVE] = st.o[d][0][e];
+    }
+    __syncthreads();
+    if (part == 1) return;
+    const float m2 = ml[wave][0][lane], M = m2 > st.m[0] ? m2 : st.m[0];
+    const float f1 = __builtin_amdgcn_exp2f(st.m[0] - M), f2 = __builtin_amdgcn_exp2f(m2 - M);
+    st.m[0] = M;
+    st.l[0] = st.l[0] * f1 + ml[wave][1][lane] * f2;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<uint2*>(out + 32 * d + 8 * j) =
-            make_uint2(pack2(st.o[d][q][4 * j] * inv, st.o[d][q][4 * j + 1] * inv),
-                       pack2(st.o[d][q][4 * j + 2] * inv, st.o[d][q][4 * j + 3] * inv));
-    if (a.lse && half == 0) a.lse[at] = (st.m[q] + __builtin_amdgcn_logf(l)) * LN2;
+      for (int e = 0; e < 16; ++e) st.o[d][0][e] = st.o[d][0][e] * f1 + their[(d * 16 + e) * WAVE] * f2;
   }
+  const int row = wrow0 + m;
+  const float l = xsum32(st.l[0]);
+  if (row >= r.rows) return;
+  const int64_t at = (r.off + row / r.G) * a.heads + r.h * r.G + row % r.G;
+  const float inv = 1.f / l;   // a row sees itself: l > 0
+  bf16_t* out = static_cast<bf16_t*>(a.out) + at * D + 4 * half;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<uint2*>(out + 32 * d + 8 * j) =
+          make_uint2(pack2(st.o[d][0][4 * j] * inv, st.o[d][0][4 * j + 1] * inv),
+                     pack2(st.o[d][0][4 * j + 2] * inv, st.o[d][0][4 * j + 3] * inv));
+  if (a.lse && half == 0) a.lse[at] = (st.m[0] + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 // fp32: the same on 32x32x2 fp32 products, 32 keys a tile; the weights are operands as they
@@ -242,7 +277,7 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
   constexpr int CH = D / 4, NC = TF * CH / 256;
   __shared__ __align__(16) float lk[TF * KS], lv[D * VS];
   Rows r;
-  if (!rows_of(w, 128, r)) return;
+  if (!rows_of(w, r)) return;
   const tav2_window& a = w.a;
   const int tid = threadIdx.x, lane = tid % WAVE, m = lane % 32, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);   // (scalar branches)
@@ -261,7 +296,7 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
     seen.hi[0] = pos + 1;
     seen.lo[0] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
   }
-  const int last_row = min(r.row0 + 128, r.rows) - 1;
+  const int last_row = min(r.row0 + ROWS, r.rows) - 1;
   const Tiles tiles = tiles_seen(r.row0 / r.G, last_row / r.G, a.window, a.sinks, TF);
   const bool idle = wrow0 >= r.rows;
   const int wlo = wrow0 / r.G, whi = min(wrow0 + 31, r.rows - 1) / r.G;
@@ -337,26 +372,18 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
   if (a.lse && half == 0) a.lse[at] = (st.m[0] + __builtin_amdgcn_logf(l)) * LN2;
 }
 
-// Rows of a workgroup: 128, or 256 where that leaves enough of them (and 64 features at most:
-// registers).
-int rows_per_group(const tav2_window& a) {
-  if (a.dtype == TAV2_F32 || a.head_dim == 128) return 128;
-  const int64_t rows = int64_t(a.max_len) * (a.heads / a.kv_heads);
-  return int64_t(a.num_requests) * a.kv_heads * cdiv(rows, 256) >= ROWS_256 ? 256 : 128;
-}
-
 }  // namespace
 
 int64_t attend_window_groups(const tav2_window& a) {
   return int64_t(a.num_requests) * a.kv_heads *
-         cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), rows_per_group(a));
+         cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), ROWS);
 }
 
 hipError_t launch_attend_window(const tav2_window& a, hipStream_t st) {
   WindowArgs w;
   w.a = a;
   w.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf(float(a.head_dim));
-  w.tiles = int(cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), rows_per_group(a)));
+  w.tiles = int(cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), ROWS));
   const unsigned grid = unsigned(attend_window_groups(a));
   ProfScope prof("attend_window", st);
   if (a.dtype == TAV2_F32) {
@@ -364,12 +391,13 @@ hipError_t launch_attend_window(const tav2_window& a, hipStream_t st) {
     else if (a.head_dim == 64) attend_window_f32<64><<<grid, 256, 0, st>>>(w);
     else attend_window_f32<128><<<grid, 256, 0, st>>>(w);
   } else {
-    const bool two = rows_per_group(a) == 256;
-    if (a.head_dim == 32 && two) attend_window_bf16<32, 2><<<grid, 256, 0, st>>>(w);
-    else if (a.head_dim == 32) attend_window_bf16<32, 1><<<grid, 256, 0, st>>>(w);
-    else if (a.head_dim == 64 && two) attend_window_bf16<64, 2><<<grid, 256, 0, st>>>(w);
-    else if (a.head_dim == 64) attend_window_bf16<64, 1><<<grid, 256, 0, st>>>(w);
-    else attend_window_bf16<128, 1><<<grid, 256, 0, st>>>(w);
+    const bool split = int64_t(grid) <= SPLIT_GROUPS;
+    if (a.head_dim == 32 && split) attend_window_bf16<32, true><<<grid, 512, 0, st>>>(w);
+    else if (a.head_dim == 32) attend_window_bf16<32, false><<<grid, 256, 0, st>>>(w);
+    else if (a.head_dim == 64 && split) attend_window_bf16<64, true><<<grid, 512, 0, st>>>(w);
+    else if (a.head_dim == 64) attend_window_bf16<64, false><<<grid, 256, 0, st>>>(w);
+    else if (split) attend_window_bf16<128, true><<<grid, 512, 0, st>>>(w);
+    else attend_window_bf16<128, false><<<grid, 256, 0, st>>>(w);
   }
   return hipGetLastError();
 }
