@@ -226,33 +226,37 @@ __global__ __launch_bounds__(EXT_NT) void kv_plan_kernel(tav2_kv c, int32_t* __r
   __shared__ int sums[EXT_NW], cnt[SCAN * EXT_NW];
   const int tid = threadIdx.x;
   int mine = 0;
+#pragma unroll 8
   for (int64_t p = tid; p < c.pages; p += EXT_NT) mine += c.refs[p] > 0;
   int U;
   block_scan(mine, sums, &U);
   int holes = 0, moves = 0;
   for (int64_t p0 = 0; p0 < c.pages; p0 += SCAN * EXT_NT) {
-    bool flag[SCAN];
+    bool held[SCAN], flag[SCAN];
     int rank[SCAN];
 #pragma unroll
     for (int j = 0; j < SCAN; ++j) {
       const int64_t p = p0 + j * EXT_NT + tid;
-      flag[j] = p < U && !(c.refs[p] > 0);
+      held[j] = c.refs[p < c.pages ? p : 0] > 0 && p < c.pages;
     }
-    int n = block_rank(flag, rank, cnt);
+    if (p0 < U) {
 #pragma unroll
-    for (int j = 0; j < SCAN; ++j)
-      if (flag[j]) plan.hole[holes + rank[j]] = int(p0 + j * EXT_NT + tid);
-    holes += n;
+      for (int j = 0; j < SCAN; ++j) flag[j] = p0 + j * EXT_NT + tid < U && !held[j];
+      const int n = block_rank(flag, rank, cnt);
 #pragma unroll
-    for (int j = 0; j < SCAN; ++j) {
-      const int64_t p = p0 + j * EXT_NT + tid;
-      flag[j] = p >= U && p < c.pages && c.refs[p] > 0;
+      for (int j = 0; j < SCAN; ++j)
+        if (flag[j]) plan.hole[holes + rank[j]] = int(p0 + j * EXT_NT + tid);
+      holes += n;
     }
-    n = block_rank(flag, rank, cnt);
+    if (p0 + SCAN * EXT_NT > U) {
 #pragma unroll
-    for (int j = 0; j < SCAN; ++j)
-      if (flag[j]) plan.from[moves + rank[j]] = int(p0 + j * EXT_NT + tid);
-    moves += n;
+      for (int j = 0; j < SCAN; ++j) flag[j] = p0 + j * EXT_NT + tid >= U && held[j];
+      const int n = block_rank(flag, rank, cnt);
+#pragma unroll
+      for (int j = 0; j < SCAN; ++j)
+        if (flag[j]) plan.from[moves + rank[j]] = int(p0 + j * EXT_NT + tid);
+      moves += n;
+    }
   }
   __threadfence_block();
   __syncthreads();   // the lists are whole (as many holes as moves, by counting)
