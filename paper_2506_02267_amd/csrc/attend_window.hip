@@ -38,7 +38,7 @@ struct Rows {
   int len, rows, row0, h, G;
 };
 
-__device__ __forceinline__ bool rows_of(const WindowArgs& w, Rows& r) {
+__device__ __forceinline__ bool rows_of(const WindowArgs& w, int per, Rows& r) {
   const tav2_window& a = w.a;
   // The rows with the most keys first.  Workgroups go to the 8 XCDs in turn: a sequence's tiles are put
   // one place further each time, since with its tiles all on one XCD some of these ended long after
@@ -53,7 +53,7 @@ __device__ __forceinline__ bool rows_of(const WindowArgs& w, Rows& r) {
   r.off = a.offset[s];
   r.len = a.len[s] < a.max_len ? a.len[s] : a.max_len;
   r.rows = r.len * r.G;
-  r.row0 = tile * ROWS;
+  r.row0 = tile * per;
   return r.row0 < r.rows;
 }
 
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(SPLIT ? 512 : 256, SPLIT && D <= 64 ? 4 : 2) void a
   auto lk = [&](int buf) { return lds + buf * (TK * KS); };
   auto lv = [&](int buf) { return lds + 2 * TK * KS + buf * (D * VS); };
   Rows r;
-  if (!rows_of(w, r)) return;
+  if (!rows_of(w, ROWS, r)) return;
   const tav2_window& a = w.a;
   const int tid = threadIdx.x, lane = tid % WAVE, m = lane % 32, half = lane / 32;
   // (scalar, for scalar branches; with SPLIT the second four waves take the same rows, and each four
@@ -267,28 +267,32 @@ __global__ __launch_bounds__(SPLIT ? 512 : 256, SPLIT && D <= 64 ? 4 : 2) void a
   if (a.lse && half == 0) a.lse[at] = (st.m[0] + __builtin_amdgcn_logf(l)) * LN2;
 }
 
-// fp32: the same on 32x32x2 fp32 products, 32 keys a tile; the weights are operands as they
-// are.
+// fp32, on 32x32x2 fp32 products (the weights are operands as they are), which bound it: a workgroup
+// takes 32 rows, and its four waves take the 32-key tiles in turn, each through its own part of LDS, so
+// that no wave waits for another until their states meet at the end.
 constexpr int TF = 32;
+constexpr int ROWS_F32 = 32;
 
 template <int D>
-__global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
-  constexpr int KS = D + 4, VS = TF + 4;   // LDS rows (floats)
-  constexpr int CH = D / 4, NC = TF * CH / 256;
-  __shared__ __align__(16) float lk[TF * KS], lv[D * VS];
+__global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_f32(WindowArgs w) {
+  constexpr int LS = D + 4;                 // an LDS row (floats)
+  constexpr int CH = D / 4, NC = TF * CH / WAVE;
+  __shared__ __align__(16) float lds[4][2 * TF * LS];
+  __shared__ float ml[4][2][WAVE];
   Rows r;
-  if (!rows_of(w, r)) return;
+  if (!rows_of(w, ROWS_F32, r)) return;
   const tav2_window& a = w.a;
   const int tid = threadIdx.x, lane = tid % WAVE, m = lane % 32, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);   // (scalar branches)
-  const int wrow0 = r.row0 + wave * 32;
+  float* const lk = lds[wave];              // keys in the order of the operand's rows
+  float* const lv = lk + TF * LS;           // values as they lie
   const float* kb = static_cast<const float*>(a.k) + r.off * a.k_ld + r.h * D;
   const float* vb = static_cast<const float*>(a.v) + r.off * a.v_ld + r.h * D;
+  const int row = min(r.row0 + m, r.rows - 1), pos = row / r.G;
   f32x4 qf[D / 8];
   AttSeen<1> seen;
   seen.sinks = a.sinks;
   {
-    const int row = min(wrow0 + m, r.rows - 1), pos = row / r.G;
     const float* p = static_cast<const float*>(a.q) + (r.off + pos) * a.q_ld +
                      (r.h * r.G + row % r.G) * D + half * (D / 2);
 #pragma unroll
@@ -296,94 +300,102 @@ __global__ __launch_bounds__(256) void attend_window_f32(WindowArgs w) {
     seen.hi[0] = pos + 1;
     seen.lo[0] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
   }
-  const int last_row = min(r.row0 + ROWS, r.rows) - 1;
-  const Tiles tiles = tiles_seen(r.row0 / r.G, last_row / r.G, a.window, a.sinks, TF);
-  const bool idle = wrow0 >= r.rows;
-  const int wlo = wrow0 / r.G, whi = min(wrow0 + 31, r.rows - 1) / r.G;
+  const int lo = r.row0 / r.G, hi = (min(r.row0 + ROWS_F32, r.rows) - 1) / r.G;
+  const Tiles tiles = tiles_seen(lo, hi, a.window, a.sinks, TF);
   f32x4 gk[NC], gv[NC];
   auto load = [&](int k0) {
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      const int e = tid + 256 * i, row = min(k0 + e / CH, r.len - 1), ch = e % CH * 4;
-      gk[i] = *reinterpret_cast<const f32x4*>(kb + int64_t(row) * a.k_ld + ch);
-      gv[i] = *reinterpret_cast<const f32x4*>(vb + int64_t(row) * a.v_ld + ch);
+      const int e = lane + WAVE * i, key = min(k0 + e / CH, r.len - 1), ch = e % CH * 4;
+      gk[i] = *reinterpret_cast<const f32x4*>(kb + int64_t(key) * a.k_ld + ch);
+      gv[i] = *reinterpret_cast<const f32x4*>(vb + int64_t(key) * a.v_ld + ch);
     }
   };
   AttState<D, 1> st;
   st.clear();
   const float c = w.scale * LOG2E;
   const int n = tiles.count();
-  load(tiles.at(0) * TF);
-  for (int i = 0; i < n; ++i) {
+  if (wave < n) load(tiles.at(wave) * TF);
+  for (int i = wave; i < n; i += 4) {
     const int k0 = tiles.at(i) * TF;
-    if (i) __syncthreads();   // the last tile has been read
+    // (a wave's LDS operations are done in order; the barriers keep the compiler to it)
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-      const int e = tid + 256 * j, row = e / CH, ch = e % CH * 4;
-      *reinterpret_cast<f32x4*>(lk + row * KS + ch) = gk[j];
-      lv[(ch + 0) * VS + row] = gv[j].x;
-      lv[(ch + 1) * VS + row] = gv[j].y;
-      lv[(ch + 2) * VS + row] = gv[j].z;
-      lv[(ch + 3) * VS + row] = gv[j].w;
+      const int e = lane + WAVE * j, key = e / CH, ch = e % CH * 4;
+      *reinterpret_cast<f32x4*>(lk + operand_row(key) * LS + ch) = gk[j];
+      *reinterpret_cast<f32x4*>(lv + key * LS + ch) = gv[j];
     }
-    __syncthreads();
-    if (i + 1 < n) load(tiles.at(i + 1) * TF);
-    const int see = idle ? 0 : tile_seen(k0, TF, wlo, whi, a.window, a.sinks);
-    if (!see) continue;
+    __builtin_amdgcn_wave_barrier();
+    if (i + 4 < n) load(tiles.at(i + 4) * TF);
     f32x16 s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
-    const float* kr = lk + key_row(m) * KS + half * (D / 2);
+    const float* kr = lk + m * LS + half * (D / 2);
 #pragma unroll
     for (int t = 0; t < D / 8; ++t) {
       const f32x4 k4 = *reinterpret_cast<const f32x4*>(kr + 4 * t);
-      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.x, qf[t].x, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.y, qf[t].y, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.z, qf[t].z, s, 0, 0, 0);
-      s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.w, qf[t].w, s, 0, 0, 0);
-    }
-    att_softmax<D, 1>(st, 0, s, c, 0.f, 1.f, see == 1, seen, k0 + 16 * half);
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d) {
-      const float* vr = lv + (32 * d + m) * VS + 16 * half;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const f32x4 v4 = *reinterpret_cast<const f32x4*>(vr + 4 * t);
-        st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v4.x, s[4 * t], st.o[d][0], 0, 0, 0);
-        st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v4.y, s[4 * t + 1], st.o[d][0], 0, 0, 0);
-        st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v4.z, s[4 * t + 2], st.o[d][0], 0, 0, 0);
-        st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v4.w, s[4 * t + 3], st.o[d][0], 0, 0, 0);
-      }
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4[e], qf[t][e], s, 0, 0, 0);
     }
+    att_softmax<D, 1>(st, 0, s, c, 0.f, 1.f, tile_seen(k0, TF, lo, hi, a.window, a.sinks) != 2, seen,
+                      k0 + 16 * half);
+    const float* vr = lv + 16 * half * LS + m;
+#pragma unroll
+    for (int t = 0; t < 16; ++t)
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+        st.o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(vr[t * LS + 32 * d], s[t], st.o[d][0], 0, 0, 0);
   }
-  const int row = wrow0 + m;
-  const float l = xsum32(st.l[0]);
-  if (row >= r.rows) return;
-  const int64_t at = (r.off + row / r.G) * a.heads + r.h * r.G + row % r.G;
-  const float inv = 1.f / l;
-  float* out = static_cast<float*>(a.out) + at * D + 4 * half;
+  // the waves' states meet in LDS; wave w joins registers 4w .. 4w + 3 of each tile, in the order of the
+  // waves: features 8w + 4 half .. of it
+  __builtin_amdgcn_wave_barrier();
+  static_assert(D / 32 * 16 * WAVE <= 2 * TF * LS, "a state fits");
+  ml[wave][0][lane] = st.m[0];
+  ml[wave][1][lane] = xsum32(st.l[0]);
 #pragma unroll
   for (int d = 0; d < D / 32; ++d)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<float4*>(out + 32 * d + 8 * j) =
-          make_float4(st.o[d][0][4 * j] * inv, st.o[d][0][4 * j + 1] * inv,
-                      st.o[d][0][4 * j + 2] * inv, st.o[d][0][4 * j + 3] * inv);
-  if (a.lse && half == 0) a.lse[at] = (st.m[0] + __builtin_amdgcn_logf(l)) * LN2;
+      reinterpret_cast<f32x4*>(lds[wave])[(d * 4 + j) * WAVE + lane] =
+          (f32x4){st.o[d][0][4 * j], st.o[d][0][4 * j + 1], st.o[d][0][4 * j + 2], st.o[d][0][4 * j + 3]};
+  __syncthreads();
+  if (r.row0 + m >= r.rows) return;
+  float M = -FLT_MAX, l = 0.f, f[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) M = vmax(M, ml[x][0][lane]);
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    f[x] = __builtin_amdgcn_exp2f(ml[x][0][lane] - M);
+    l += ml[x][1][lane] * f[x];
+  }
+  const int64_t at = (r.off + pos) * a.heads + r.h * r.G + row % r.G;
+  const float inv = 1.f / l;   // a row sees itself: l > 0
+  float* out = static_cast<float*>(a.out) + at * D + 8 * wave + 4 * half;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) {
+    f32x4 o = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) o += reinterpret_cast<const f32x4*>(lds[x])[(d * 4 + wave) * WAVE + lane] * f[x];
+    *reinterpret_cast<f32x4*>(out + 32 * d) = o * inv;
+  }
+  if (a.lse && wave == 0 && half == 0) a.lse[at] = (M + __builtin_amdgcn_logf(l)) * LN2;
 }
+
+int rows_per_group(const tav2_window& a) { return a.dtype == TAV2_F32 ? ROWS_F32 : ROWS; }
 
 }  // namespace
 
 int64_t attend_window_groups(const tav2_window& a) {
   return int64_t(a.num_requests) * a.kv_heads *
-         cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), ROWS);
+         cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), rows_per_group(a));
 }
 
 hipError_t launch_attend_window(const tav2_window& a, hipStream_t st) {
   WindowArgs w;
   w.a = a;
   w.scale = a.scale > 0.f ? a.scale : 1.f / sqrtf(float(a.head_dim));
-  w.tiles = int(cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), ROWS));
+  w.tiles = int(cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), rows_per_group(a)));
   const unsigned grid = unsigned(attend_window_groups(a));
   ProfScope prof("attend_window", st);
   if (a.dtype == TAV2_F32) {
