@@ -791,14 +791,15 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(AttendArgs a) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, WAVE));
   float l = 0.f, x = 0.f;
-#pragma unroll 4
+  // An empty share's features are not written: read all the same, so that no load waits for the sum
+  // that says so, and dropped.
+#pragma unroll 8
   for (int s = g; s < a.splits; s += NG) {
     const int64_t p = s * n + at;
-    const float lp = a.part_ml[2 * p + 1];
-    if (lp == 0.f) continue;   // an empty share (its features are not written), or nothing seen
+    const float lp = a.part_ml[2 * p + 1], o = a.part_o[p * D + f];
     const float w = __builtin_amdgcn_exp2f(a.part_ml[2 * p] - M);
     l += lp * w;
-    x += a.part_o[p * D + f] * w;
+    x += lp != 0.f ? o * w : 0.f;
   }
   lo[g][f] = x;
   if (f == 0) ll[g] = l;
