@@ -122,18 +122,24 @@ __global__ __launch_bounds__(EXT_NT) void kv_extend_kernel(tav2_kv c, const int3
   }
   if (found > want) found = want;
   __syncthreads();
+  if (found < want) {   // the pages of the sequence that got only some of them
+    int lo = 0, hi = S - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (upto[mid] > found) hi = mid; else lo = mid + 1;
+    }
+    const int before = lo ? upto[lo - 1] : 0;
+    int32_t* e = c.table + int64_t(lo) * c.max_blocks + kv_len(c, lo) / KVP;
+    for (int r = tid; r < found - before; r += EXT_NT) {
+      c.refs[e[r]] = 0;
+      e[r] = -1;
+    }
+    __syncthreads();   // the lengths are read no more
+  }
   for (int s = tid; s < S; s += EXT_NT) {
     const int old = kv_len(c, s), n = count[s];
     const bool fits = n > 0 && (int64_t(old) + n) / KVP <= c.max_blocks;
-    const int before = s ? upto[s - 1] : 0;
     const bool granted = fits && upto[s] <= found;
-    if (fits && !granted) {   // the pages of a sequence that got only some of them
-      for (int r = before; r < found; ++r) {
-        int32_t* e = c.table + int64_t(s) * c.max_blocks + old / KVP + (r - before);
-        c.refs[*e] = 0;
-        *e = -1;
-      }
-    }
     c.fresh[s] = granted ? n : 0;
     if (granted) c.len[s] = old + n;
   }
