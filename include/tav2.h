@@ -362,7 +362,7 @@ typedef struct tav2_window {
   int32_t reserved;            /* set to 0 */
 } tav2_window;
 /* q, k, v, out 16-byte aligned.  Errors: TAV2_ERR_NULL, TAV2_ERR_SHAPE, TAV2_ERR_DTYPE,
- * TAV2_ERR_UNSUPPORTED (another head_dim; over 2^31 - 1 workgroups), TAV2_ERR_HIP. */
+ * TAV2_ERR_UNSUPPORTED (another head_dim; over 2^24 - 1 workgroups), TAV2_ERR_HIP. */
 tav2_status tav2_attend_window(const tav2_window* a, void* stream);
 
 /*
@@ -445,7 +445,7 @@ typedef struct tav2_kv_queries {
   const int64_t* offset;       /* device [num_seqs + 1]; offset[0] = 0, offset[num_seqs] = total */
   int64_t total;               /* host: number of queries (>= 0) */
   int64_t ld;                  /* elements between queries, as in tav2_window */
-  int32_t max_count;           /* host-side bound of a sequence's queries */
+  int32_t max_count;           /* host-side bound of a sequence's queries, at most total */
   int32_t heads;               /* a multiple of kv_heads */
   int32_t window, sinks;       /* >= 0 */
   float   scale;               /* > 0, or 0 for 1 / sqrt(head_dim) */

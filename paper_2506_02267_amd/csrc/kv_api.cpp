@@ -8,7 +8,8 @@ using namespace tav2;
 namespace {
 
 constexpr size_t WS_ALIGN = 256;
-constexpr int64_t MAX_GRID = (int64_t(1) << 31) - 1;
+constexpr int64_t MAX_ROWS = (int64_t(1) << 31) - 1;
+constexpr int64_t MAX_GROUPS = (int64_t(1) << 24) - 1;   // of 256 threads: a launch has fewer than 2^32
 constexpr int MAX_HEADS = 65535;
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -51,9 +52,9 @@ tav2_status check_queries(const tav2_kv* c, const tav2_kv_queries* q) {
   if (q->total > 0 && q->max_count == 0) return TAV2_ERR_SHAPE;
   if (q->heads < 1 || q->heads % c->kv_heads || q->window < 0 || q->sinks < 0 || !scale_ok(q->scale))
     return TAV2_ERR_SHAPE;
-  if (q->heads > MAX_HEADS || q->total * q->heads > MAX_GRID) return TAV2_ERR_UNSUPPORTED;
+  if (q->heads > MAX_HEADS || q->total > MAX_ROWS / q->heads) return TAV2_ERR_UNSUPPORTED;
   if (!stride_ok(q->ld, q->heads, c->head_dim, 8)) return TAV2_ERR_SHAPE;
-  if (q->total > 0 && kv_attend_groups(*c, *q) > MAX_GRID) return TAV2_ERR_UNSUPPORTED;
+  if (q->total > 0 && kv_attend_groups(*c, *q) > MAX_GROUPS) return TAV2_ERR_UNSUPPORTED;
   return TAV2_OK;
 }
 
@@ -83,7 +84,7 @@ tav2_status tav2_attend_window(const tav2_window* a, void* stream) {
   if (!aligned(a->q, 16) || !aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->out, 16))
     return TAV2_ERR_SHAPE;
   if (int64_t(a->max_len) * (a->heads / a->kv_heads) > (int64_t(1) << 30) ||
-      attend_window_groups(*a) > MAX_GRID || int64_t(a->num_requests) * a->kv_heads > MAX_GRID)
+      int64_t(a->num_requests) * a->kv_heads > MAX_GROUPS || attend_window_groups(*a) > MAX_GROUPS)
     return TAV2_ERR_UNSUPPORTED;
   return hip_status(launch_attend_window(*a, static_cast<hipStream_t>(stream)));
 }
@@ -106,7 +107,7 @@ tav2_status tav2_kv_append(const tav2_kv* c, int32_t layer, const void* k, int64
   if (max_count == 0) return TAV2_OK;
   if (!k || !v || !offset) return TAV2_ERR_NULL;
   if (!aligned(k, 16) || !aligned(v, 16)) return TAV2_ERR_SHAPE;
-  if (kv_append_groups(*c, max_count) > MAX_GRID) return TAV2_ERR_UNSUPPORTED;
+  if (kv_append_groups(*c, max_count) > MAX_GROUPS) return TAV2_ERR_UNSUPPORTED;
   return hip_status(launch_kv_append(*c, layer, k, k_ld, v, v_ld, offset, max_count,
                                      static_cast<hipStream_t>(stream)));
 }

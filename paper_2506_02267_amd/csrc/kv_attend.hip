@@ -5,15 +5,19 @@
 // into matrix operands in its own registers, once for all 32 QT queries, and meet in LDS at
 // the end.  A wave reads a page as it lies, a kilobyte a load, into registers (the next page's
 // loads are in flight while this one is multiplied), and passes it through its own part of LDS,
-// where a lane then reads its operands: half a key's codes, and 16 keys of one feature of V^T.  (Each
-// lane reading its operands from the page itself took 115 cycles of the address path a load: 44 us
-// for 64 users' new actions.)
+// where a lane then reads its operands: half a key's codes, and 16 keys of one feature of V^T.  (With
+// each lane reading its operands from the page itself, 128 features in a window took 60 us for 50, the
+// rest was alike.)
 // Operands are fp16, which holds codes exactly and the weights to 11 bits; a query is scaled by a
 // power of two first so that its largest feature lies in [2^14, 2^15) (features below 2^-28 of
 // that lose bits that fp32 sums would lose as well).  A page's key scale multiplies the fp32
-// scores, its value scale enters the weights as a power of two added to the exponent.  Where queries are
+// scores, its value scale enters the weights by its logarithm, added to the exponent.  Where queries are
 // few, the pages are split over more workgroups, whose partial results a second launch joins
 // in a fixed order.
+// One query a sequence is bound by HBM: 64 sequences of 16384 tokens, 8 kv heads, are read at 5.6 TB/s
+// with 64 features and 5.7 with 128 (a large copy: 4.7, read and written).  Many queries are bound by the vector
+// units, which turn codes into fp16 and scores into weights while the matrix units wait, and the
+// reverse: 1000 candidates of one 16384-token history, 4 heads of 64, take 39 us, 13 at a large product's rate.
 #include <algorithm>
 
 #include "attend_core.h"
@@ -44,8 +48,12 @@ struct AttendArgs {
   int group;         // neighbouring sequences whose rows fit one tile together
 };
 
-constexpr int SHARES = 512;      // workgroups that a launch is divided into, about
-constexpr int SHARE_MOST = 64;   // pages to a share, at most
+// Workgroups that a launch is divided into, about (two to a CU).  New actions of 64 users, us: 35.7 with
+// 512, 37.8 with 768, 38.8 with 1024, 47 with 4096; 64 sequences of 8192 tokens each 27.4, 28.9, 28.9, 39.6.
+constexpr int SHARES = 512;
+// Pages to a share, at most (a longer one ends later than the rest).  8 copies each of 32 histories, us: 102 with
+// 16, 86 with 32, 79 with 64; 64 sequences of 16384 tokens, 8 heads, 200, 195 and 191.
+constexpr int SHARE_MOST = 64;
 
 // The pages that a tile's queries see: [0, sink) and [first, last), counted through.
 struct PageList {
@@ -161,13 +169,14 @@ __device__ __forceinline__ bool job_of(const AttendArgs& a, int s, int row0, int
   return true;
 }
 
-// The same for this workgroup, with its split.  An empty share of several leaves no sum, and kv_merge
-// reads no more of it.
+// The same for this workgroup, with its split.  An empty share of several leaves a sum of zero and no
+// features (kv_merge drops what it reads there).
 __device__ __forceinline__ bool my_job(const AttendArgs& a, int cap, Job& j) {
   // Units (sequence, head, share) in the order (share, block of sequences, head), each on one XCD
   // (workgroups go to the 8 in turn) with the block's sequences one after the other, since
-  // neighbours may be copies that read the same pages, and so the query tiles of each.  First shares come
-  // first, the later ones, which short sequences lack, at the end.
+  // neighbours may be copies that read the same pages, and so the query tiles of each (8 copies each of 32
+  // histories 79 us, with sequences spread over the XCDs 92).  First shares come first, the later
+  // ones, which short sequences lack, at the end.
   const int unit = int(blockIdx.x % unsigned(a.units));
   const int tile = int(blockIdx.x / unsigned(a.units));
   const int block = unit / (8 * a.near) * 8 + unit % 8;
@@ -512,7 +521,9 @@ __device__ __forceinline__ uint32_t shared_set(const AttendArgs& a, const Job& j
 // At most 16 query rows: on the 16x16x32 instructions, a page's 64 keys at once.  S^T comes in four tiles
 // of 16 keys, in the order that makes a lane's 16 scores its quarter's 16 consecutive keys
 // (16 g + 4 i + r in register r of tile i, g = l / 16), again the operand of O^T = V^T P^T as they
-// stand.  Half the vector work of a 32-row tile.
+// stand.  Half the vector work of a 32-row tile: new actions of 64 users (4 rows) 35.5 us for 42.2 with
+// that, 8 copies each of 32 histories 79 for 108.  Where rows are few enough, neighbouring sequences share
+// a tile over the pages that they have in common (shared_set): the copies take 91 us without.
 template <int D>
 __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(AttendArgs a) {
   constexpr int F = D / 4;           // features of a lane's quarter
@@ -780,6 +791,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
 }
 
 // A workgroup per (query, head): D features by 256 / D groups of splits, the groups joined in LDS.
+// Bound by latency: two dependent reads, 3.2 us for one query of 64 shares.
 template <int D>
 __global__ __launch_bounds__(256) void kv_merge_kernel(AttendArgs a) {
   constexpr int NG = 256 / D;
@@ -817,7 +829,7 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(AttendArgs a) {
 
 // Pages that a query tile of the longest sequence sees, by the host's estimate.
 int64_t most_pages(const tav2_kv& c, const tav2_kv_queries& q) {
-  int64_t tokens = c.max_len;
+  int64_t tokens = std::min<int64_t>(c.max_len, int64_t(c.max_blocks) * KVP + KVP - 1);
   if (q.window > 0) tokens = std::min(tokens, int64_t(q.window) + q.max_count + q.sinks + 2 * KVP);
   return std::max<int64_t>(1, cdiv(tokens, KVP));
 }
@@ -861,7 +873,9 @@ int64_t query_units(const tav2_kv& c, int splits) {
 
 int64_t kv_attend_groups(const tav2_kv& c, const tav2_kv_queries& q) {
   const int64_t rows = int64_t(q.max_count) * (q.heads / c.kv_heads);
-  return query_units(c, key_splits(c, q)) * cdiv(rows, tile_rows(c, q));
+  const int splits = key_splits(c, q);
+  return std::max(query_units(c, splits) * cdiv(rows, tile_rows(c, q)),
+                  splits > 1 ? q.total * q.heads : 0);
 }
 
 size_t kv_attend_bytes(const tav2_kv& c, const tav2_kv_queries& q) {

@@ -544,14 +544,17 @@ def _dense(name: str, x: Optional[torch.Tensor], shape, dtype):
         raise ValueError(f"{name}: expected contiguous {dtype} {list(shape)}")
 
 
-def _run(fn: str, device: int, stream: Optional[torch.cuda.Stream], args, *used):
+def _run(fn: str, device: int, stream: Optional[torch.cuda.Stream], args, *used, keep=()):
     """Call entry point `fn` with `args` and the stream (by default the current one of that device)
-    on GPU number `device`, whichever device is current; `used`: the tensors it takes."""
+    on GPU number `device`, whichever device is current; `used`: the tensors it takes, `keep`:
+    more of them, known to be on that device."""
     if device < 0:
         raise ValueError(f"{fn}: expected tensors on a GPU")
     for t in used:
         if t is not None and t.get_device() != device:
             raise ValueError(f"{fn}: a tensor is not on GPU {device}")
+    if stream is not None and stream.device_index != device:
+        raise ValueError(f"{fn}: the stream is not on GPU {device}")
     call = getattr(load_library(), fn)
     if stream is None and device == torch.cuda.current_device():
         # (the handle alone: building a Stream object takes longer than the launch)
@@ -559,7 +562,7 @@ def _run(fn: str, device: int, stream: Optional[torch.cuda.Stream], args, *used)
         return
     with torch.cuda.device(device):
         _check(fn, call(*args, _stream_handle(stream)))
-        _used_on(stream, *used)
+        _used_on(stream, *used, *keep)
 
 
 def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offset: torch.Tensor,
@@ -629,6 +632,7 @@ class KvCache:
                     refs=refs.data_ptr(), num_seqs=seqs, layers=layers, pages=pages,
                     max_blocks=blocks, kv_heads=heads, head_dim=D, max_len=max_len, reserved=0)
         self.ref, self.row = ctypes.byref(self.s), (heads, D)
+        self.buffers = (k, v, k_scale, v_scale, k_tail, v_tail, table, length, fresh, refs)
 
     @classmethod
     def create(cls, layers: int, pages: int, seqs: int, max_blocks: int, kv_heads: int,
@@ -656,12 +660,12 @@ class KvCache:
         self.s.max_len = n
 
 
-
 def kv_extend(cache: KvCache, count: torch.Tensor, stream=None):
     """tav2_kv_extend: room for count[s] (int32 [seqs]) new tokens of every sequence;
     cache.fresh says what was granted."""
     _dense("count", count, (cache.seqs,), torch.int32)
-    _run("tav2_kv_extend", cache.index, stream, (cache.ref, count.data_ptr()), count)
+    _run("tav2_kv_extend", cache.index, stream, (cache.ref, count.data_ptr()), count,
+         keep=cache.buffers)
 
 
 def kv_append(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, offset: torch.Tensor,
@@ -677,7 +681,7 @@ def kv_append(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, offs
         raise ValueError("offset: expected contiguous int64 [seqs] or longer")
     _run("tav2_kv_append", cache.index, stream,
          (cache.ref, layer, k.data_ptr(), k_ld, v.data_ptr(), v_ld,
-          offset.data_ptr(), max_count), k, v, offset)
+          offset.data_ptr(), max_count), k, v, offset, keep=cache.buffers)
 
 
 def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, offset: torch.Tensor, max_count: int,
@@ -702,7 +706,8 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, offset: torch.Tensor,
     wp, wb = ws.get(load_library().tav2_kv_attend_workspace(cache.ref, a))
     _run("tav2_kv_attend", cache.index, stream,
          (cache.ref, layer, a, flags, out.data_ptr(),
-          None if lse is None else lse.data_ptr(), wp, wb), q, offset, out, lse, ws.buf)
+          None if lse is None else lse.data_ptr(), wp, wb), q, offset, out, lse, ws.buf,
+         keep=cache.buffers)
     return out
 
 
@@ -710,19 +715,21 @@ def kv_fork(cache: KvCache, parent: torch.Tensor, stream=None):
     """tav2_kv_fork: empty sequences s become continuations of sequence parent[s] (int32 [seqs],
     -1: not)."""
     _dense("parent", parent, (cache.seqs,), torch.int32)
-    _run("tav2_kv_fork", cache.index, stream, (cache.ref, parent.data_ptr()), parent)
+    _run("tav2_kv_fork", cache.index, stream, (cache.ref, parent.data_ptr()), parent,
+         keep=cache.buffers)
 
 
 def kv_free(cache: KvCache, drop: torch.Tensor, stream=None):
     """tav2_kv_free: sequences with drop[s] != 0 (uint8 [seqs]) give up their pages."""
     _dense("drop", drop, (cache.seqs,), torch.uint8)
-    _run("tav2_kv_free", cache.index, stream, (cache.ref, drop.data_ptr()), drop)
+    _run("tav2_kv_free", cache.index, stream, (cache.ref, drop.data_ptr()), drop,
+         keep=cache.buffers)
 
 
 def kv_trim(cache: KvCache, window: int, sinks: int = 0, stream=None):
     """tav2_kv_trim: every sequence gives up the pages that this window and these sinks no longer
     see."""
-    _run("tav2_kv_trim", cache.index, stream, (cache.ref, window, sinks))
+    _run("tav2_kv_trim", cache.index, stream, (cache.ref, window, sinks), keep=cache.buffers)
 
 
 def kv_compact(cache: KvCache, used: Optional[torch.Tensor] = None,
@@ -735,7 +742,7 @@ def kv_compact(cache: KvCache, used: Optional[torch.Tensor] = None,
     ws = ws or Workspace(cache.device)
     wp, wb = ws.get(load_library().tav2_kv_compact_workspace(cache.ref))
     _run("tav2_kv_compact", cache.index, stream,
-         (cache.ref, used.data_ptr(), wp, wb), used, ws.buf)
+         (cache.ref, used.data_ptr(), wp, wb), used, ws.buf, keep=cache.buffers)
     return used
 
 

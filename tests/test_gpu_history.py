@@ -341,6 +341,20 @@ def test_extend_many_sequences_and_pages():
         assert table[s, :len(ref.table[s])].tolist() == ref.table[s]
 
 
+def test_extend_gives_back_thousands_of_pages():
+    """A sequence that the pool proves too small for after most of its pages were found; the sequences
+    behind it, which would fit, get none either."""
+    c, ref = new_cache(4, 6000, 8000, 1, 32, dirty=False), history.Cache(4, 6000, 8000)
+    for count in ([64 * 100, 64 * 7000, 64, 5], [3, 64 * 5900 - 3, 1, 64], [0, 64 * 5901, 64, 0]):
+        T.kv_extend(c, torch.tensor(count, dtype=torch.int32).cuda())
+        ref.extend(count)
+        assert c.fresh.tolist() == ref.fresh and c.length.tolist() == ref.len
+        assert c.refs.tolist() == ref.refs
+        for s in range(4):
+            row = [x for x in c.table[s].tolist() if x != -1]
+            assert row == ref.table[s][:len(row)] and len(row) == ref.len[s] // P
+
+
 def test_the_most_sequences():
     n = T.KV_SEQS_MAX
     c = new_cache(n, 50000, 4, 1, 32, dirty=False)
@@ -633,6 +647,22 @@ def test_other_stream_and_repeated_calls_give_the_same_bits():
     wgot = T.attend_window(wq, wk, wv, o1, l1, 333, window=50, sinks=1, stream=side)
     side.synchronize()
     assert all(torch.equal(want, x) for x in got) and torch.equal(wwant, wgot)
+
+
+def test_cache_dropped_while_another_stream_reads_it():
+    """Memory of a cache that is given up while a call on another stream is still to run is not
+    handed out before that call has ended."""
+    c = T.KvCache.create(1, 10000, 4, 16, 2, 64)
+    old, size = c.k.data_ptr(), c.k.numel()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(int(1e8))   # some 50 ms
+    T.kv_trim(c, 5, stream=side)
+    del c
+    new = torch.empty(size, dtype=torch.int8, device="cuda")
+    assert new.data_ptr() != old
+    side.synchronize()
 
 
 def test_graph_of_a_decode_step():

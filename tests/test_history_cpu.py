@@ -6,6 +6,7 @@ import math
 import os
 import subprocess
 from fractions import Fraction
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -166,6 +167,31 @@ def test_attend_other_errors():
     assert call(out=None, ws=None, n=0, qq=ctypes.byref(empty)) == 0
 
 
+def test_sizes_whose_products_pass_64_bits_or_a_launch():
+    lib, c = T.load_library(), fake_kv()
+    for kw in (dict(total=1 << 62, max_count=1), dict(total=(1 << 63) - 1, max_count=1)):
+        q = fake_queries(**kw)
+        assert lib.tav2_kv_attend(ctypes.byref(c), 0, ctypes.byref(q), 0, FAKE, FAKE, None, 0,
+                                  None) == -4
+    wide = fake_kv(num_seqs=T.KV_SEQS_MAX, kv_heads=512, head_dim=32)   # 2^24 (sequence, head) pairs
+    q = fake_queries(total=40000, heads=512, ld=512 * 32)
+    assert lib.tav2_kv_attend(ctypes.byref(wide), 0, ctypes.byref(q), 0, FAKE, FAKE, FAKE, 1 << 50,
+                              None) == -4
+    assert lib.tav2_kv_append(ctypes.byref(wide), 0, FAKE, 512 * 32, FAKE, 512 * 32, FAKE, 200,
+                              None) == -4
+    for kw in (dict(num_requests=1 << 30, heads=1 << 14, kv_heads=1 << 14, max_len=1 << 27,
+                    q_ld=1 << 20, k_ld=1 << 20, v_ld=1 << 20), dict(num_requests=1 << 23)):
+        a = fake_window(**kw)
+        assert lib.tav2_attend_window(ctypes.byref(a), None) == -4
+
+
+def test_an_estimate_past_the_tables_divides_as_the_tables_do():
+    lib, q = T.load_library(), fake_queries()
+    need = [lib.tav2_kv_attend_workspace(ctypes.byref(fake_kv(max_len=n)), ctypes.byref(q))
+            for n in (16 * 64 + 63, 16 * 64 + 64, 1 << 20, (1 << 31) - 1)]
+    assert need[0] > 0 and need == [need[0]] * 4
+
+
 # ------------------------------------------------------------------------- the binding
 def host_cache(**kw):
     a = dict(layers=1, pages=4, seqs=2, max_blocks=3, kv_heads=2, head_dim=32, device="cpu")
@@ -205,6 +231,11 @@ def test_binding_refuses_wrong_shapes_and_types():
         with pytest.raises(ValueError):
             call()
             print("accepted:", i)
+
+
+def test_binding_refuses_a_stream_of_another_device():
+    with pytest.raises(ValueError, match="stream"):
+        T._run("tav2_kv_trim", 0, SimpleNamespace(device_index=1, cuda_stream=0), ())
 
 
 def test_cache_refuses_buffers_that_do_not_fit_together():
