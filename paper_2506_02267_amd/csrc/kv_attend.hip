@@ -129,6 +129,11 @@ __device__ __forceinline__ void into_half(float top, float* f, float* back) {
   *back = __uint_as_float((ex - 14) << 23);
 }
 
+// A score's factor from the query's and the keys'.  One that fp32 cannot hold (queries of zeros, tiny scales)
+// is no zero, by which a masked -inf would become a NaN: scores are below 2^38, so 2^-126 adds at most
+// 2^-88 to an exponent that is nearer to zero still.
+__device__ __forceinline__ float score_factor(float q, float k) { return fmaxf(q * k, FLT_MIN); }
+
 // A workgroup's share: `cap` query rows of a kv head of a sequence, entries [c0, c1) of their pages.
 struct Job {
   int s, h, split, row0, G, rows;   // rows: the sequence's, (query, head) pairs
@@ -340,7 +345,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
     float ks, lv, inv, cs[QT];
     feed.factors(t, &ks, &lv, &inv);
 #pragma unroll
-    for (int q = 0; q < QT; ++q) cs[q] = cq[q] * ks;
+    for (int q = 0; q < QT; ++q) cs[q] = score_factor(cq[q], ks);
     feed.put(my);
     feed.load(a, j, next);
     if (page >= 0) {
@@ -404,7 +409,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
       float fv, backv;
       into_half(vt, &fv, &backv);
 #pragma unroll
-      for (int q = 0; q < QT; ++q) cs[q] = cq[q] * back;
+      for (int q = 0; q < QT; ++q) cs[q] = score_factor(cq[q], back);
       auto keys = [&](f16x8(&kf)[D / 16]) {
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) kf[t] = scaled8h(raw_key(t), f);
@@ -690,7 +695,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
         vf[0] = codes8h(w.x, w.y);
         vf[1] = codes8h(w.z, w.w);
       };
-      step(keys, values, cq * ks, lv, inv, b * KVP);
+      step(keys, values, score_factor(cq, ks), lv, inv, b * KVP);
     }
     page = next;
   }
@@ -733,7 +738,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
 #pragma unroll
       for (int t = 0; t < 2; ++t) vf[t] = scaled8h(raw_value(d, t), fv);
     };
-    step(keys, values, cq * backk, __builtin_amdgcn_logf(backv), fv, full * KVP);
+    step(keys, values, score_factor(cq, backk), __builtin_amdgcn_logf(backv), fv, full * KVP);
   };
   if (j.list.at(j.c1 - 1) >= full) {
     const int mine = hi, base = j.s / a.group * a.group;

@@ -150,6 +150,19 @@ def test_attend_window_extreme_scores(dtype, D):
         check(out, lse, want, D, dtype, L)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("spread,scale", [(0.0, 0.0), (2.0 ** -120, 0.0), (0.0, 1e-44), (1.0, 1e-40)])
+def test_attend_window_scores_below_fp32(dtype, spread, scale):
+    g = torch.Generator().manual_seed(12)
+    q, k = rows(g, 100, 2, 64, dtype, spread), rows(g, 100, 2, 64, dtype, spread)
+    v, lse = rows(g, 100, 2, 64, dtype), torch.empty(100, 2, device="cuda")
+    out = T.attend_window(q, k, v, torch.zeros(1, dtype=torch.int64).cuda(),
+                          torch.tensor([100], dtype=torch.int32).cuda(), 100, 30, 2, scale, lse=lse)
+    want = history.window_attention(*(x.double().cpu().numpy() for x in (q, k, v)), 30, 2,
+                                    scale if scale else None)
+    check(out, lse, want, 64, dtype, 100)
+
+
 @pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (70, 2 ** 31 - 1),
                                           (0, 2 ** 31 - 1)])
 def test_largest_window_and_sinks_are_none(window, sinks):
@@ -437,12 +450,13 @@ def test_random_walk():
 
 
 # ------------------------------------------------------------------------- kv_attend
-def attend_pair(p, n, heads, causal, window=0, sinks=0, layer=0, scale=0.0, max_len=None, seed=0):
+def attend_pair(p, n, heads, causal, window=0, sinks=0, layer=0, scale=0.0, max_len=None, seed=0,
+                spread=1.5):
     """kv_attend of n[s] queries for every sequence against the oracle."""
     g = torch.Generator().manual_seed(seed + 77)
     off = np.concatenate([[0], np.cumsum(n)])
     total = int(off[-1])
-    q = rows(g, total, heads + 1, p.D, scale=1.5)[:, 1:]      # a slice: rows lie further apart
+    q = rows(g, total, heads + 1, p.D, scale=spread)[:, 1:]      # a slice: rows lie further apart
     out = torch.full((total, heads, p.D), 9.0, dtype=BF, device="cuda")
     lse = torch.full((total, heads), 9.0, device="cuda")
     if max_len is not None:
@@ -574,6 +588,20 @@ def test_kv_attend_extreme_scales():
     attend_pair(p, [3], 1, False)
     attend_pair(p, [3], 1, False, scale=2.0)
     attend_pair(p, [70], 1, True, scale=1e-3)
+
+
+@pytest.mark.parametrize("n", [1, 20, 70])
+@pytest.mark.parametrize("spread,keys,scale", [
+    (0.0, 0.0, 0.0), (0.0, 2.0 ** -99, 0.0), (2.0 ** -100, 2.0 ** -50, 0.0), (0.0, 1.0, 1e-30),
+    (1.0, 1.0, 1e-40), (2.0 ** -120, 1.0, 1e-44)])
+def test_kv_attend_scores_below_fp32(n, spread, keys, scale):
+    """Queries of zeros or next to it (padding), keys and scales likewise: products of the factors that fp32
+    cannot hold are scores of zero, in blocks that are masked in part too."""
+    p = Pair(seqs=2, pages=20, blocks=10, H=1, D=64, seed=43)
+    p.grow([64, 130], keys)
+    p.grow([9, 64], keys)
+    attend_pair(p, [n, n], 1, True, spread=spread, scale=scale)
+    attend_pair(p, [n, n], 1, False, 100, 3, spread=spread, scale=scale)
 
 
 def test_steps_of_a_serving_loop():
