@@ -345,7 +345,8 @@ tav2_status tav2_select_encode_eq2(const tav2_seq* seq, const tav2_eq2* eq2,
 typedef struct tav2_window {
   const void*    q;            /* device, rows of [heads, head_dim], dtype; values finite */
   const void*    k;            /* device, rows of [kv_heads, head_dim], dtype; values finite */
-  const void*    v;            /* device, rows of [kv_heads, head_dim], dtype; values finite */
+  const void*    v;            /* device, rows of [kv_heads, head_dim], dtype; values finite,
+                                  magnitudes up to 2^90; scores within fp32's range */
   int64_t q_ld, k_ld, v_ld;    /* elements from a row to the next: at least a row, at most 2^24,
                                   multiples of 8 (bf16) or 4 (fp32) */
   void*          out;          /* device [rows, heads, head_dim], dtype: token i's row i */
@@ -419,7 +420,8 @@ tav2_status tav2_kv_extend(const tav2_kv* c, const int32_t* count, void* stream)
  * The keys and values of the tokens that the last tav2_kv_extend granted, for one layer
  * (once per layer and extension): sequence s's fresh[s] tokens are rows offset[s].. of k and v
  * (bf16 rows of [kv_heads, head_dim], row strides k_ld and v_ld elements as in tav2_window; 16-byte
- * aligned; values finite).  Blocks that are full now go to their pages, the rest to the tail.
+ * aligned; finite; v's magnitudes 0 or from 2^-80 to 2^50, beyond which tav2_kv_attend loses
+ * precision).  Blocks that are full now go to their pages, the rest to the tail.
  *   offset    device int64 [num_seqs]
  *   max_count host-side bound of fresh[s]; tokens of a sequence past it are not written
  */
@@ -436,7 +438,7 @@ tav2_status tav2_kv_append(const tav2_kv* c, int32_t layer, const void* k, int64
  *     every cached token.
  * window and sinks as for tav2_attend_window, counted from the query's position; blocks that were
  * released (tav2_kv_trim) are not seen.  out and lse as there; a query that sees nothing gets
- * zeros and -inf.  Queries and outputs are bf16; products take the codes exactly, the scales in fp32.
+ * zeros and -inf.  Queries (finite; scores within fp32's range) and outputs are bf16; products take the codes exactly, the scales in fp32.
  *   ws  device workspace of tav2_kv_attend_workspace() bytes, 256-byte aligned.
  * Errors: those above, TAV2_ERR_WORKSPACE.
  */

@@ -241,8 +241,9 @@ struct Feed {
       rv[i] = vp[i * WAVE];
     }
   }
-  // Factors of entry t.  Scale 1 may be a block of zeros, which is taken as if at the smallest scale,
-  // so that its weights do not raise the reference over small values.
+  // Factors of entry t.  Scale 1 may be a block of zeros, which is taken as if at the scale 2^-80: its
+  // weights then neither raise the reference over small values (down to 2^-90) nor vanish beside large
+  // ones (up to 2^50), and as many as there are tokens can be summed.
   __device__ __forceinline__ void factors(int t, float* ks, float* lv, float* inv) const {
     *ks = lane_f(kss, t);
     *lv = lane_f(lvs, t);
@@ -252,8 +253,8 @@ struct Feed {
 #pragma unroll
       for (int e = 0; e < D / 16; ++e) any |= rv[e].x | rv[e].y | rv[e].z | rv[e].w;
       if (!__any(any != 0)) {
-        *lv = -100.f;
-        *inv = 0x1p100f;
+        *lv = -80.f;
+        *inv = 0x1p80f;
       }
     }
   }

@@ -588,7 +588,7 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offset: tor
     _dense("lse", lse, (rows, heads), torch.float32)
     a = Window(q.data_ptr(), k.data_ptr(), v.data_ptr(), *lds, out.data_ptr(),
                None if lse is None else lse.data_ptr(), offset.data_ptr(), length.data_ptr(), R,
-               max_len, heads, k.shape[1], D, F32 if dt == torch.float32 else BF16, window, sinks,
+               max_len if rows else 0, heads, k.shape[1], D, F32 if dt == torch.float32 else BF16, window, sinks,
                scale, 0)
     _run("tav2_attend_window", q.get_device(), stream, (ctypes.byref(a),), q, k, v, offset, length,
          out, lse)
@@ -681,7 +681,7 @@ def kv_append(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, offs
         raise ValueError("offset: expected contiguous int64 [seqs] or longer")
     _run("tav2_kv_append", cache.index, stream,
          (cache.ref, layer, k.data_ptr(), k_ld, v.data_ptr(), v_ld,
-          offset.data_ptr(), max_count), k, v, offset, keep=cache.buffers)
+          offset.data_ptr(), max_count if k.shape[0] else 0), k, v, offset, keep=cache.buffers)
 
 
 def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, offset: torch.Tensor, max_count: int,

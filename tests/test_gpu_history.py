@@ -184,6 +184,19 @@ def test_largest_window_and_sinks_are_none(window, sinks):
         assert float((want.float() - got.float()).abs().max()) <= 2.0 ** -7 * float(want.abs().max())
 
 
+def test_batches_of_no_rows():
+    """Requests whose histories are all empty, and an extension by nothing."""
+    none = rows(torch.Generator().manual_seed(13), 0, 2, 64)
+    off, n = torch.zeros(3, dtype=torch.int64).cuda(), torch.zeros(3, dtype=torch.int32).cuda()
+    assert T.attend_window(none, none, none, off, n, 50).shape == (0, 2, 64)
+    c = T.KvCache.create(1, 4, 3, 2, 2, 64)
+    T.kv_extend(c, n)
+    T.kv_append(c, 0, none, none, off, 50)
+    assert T.kv_attend(c, 0, none, torch.zeros(4, dtype=torch.int64).cuda(), 0).shape == (0, 2, 64)
+    torch.cuda.synchronize()
+    assert c.length.tolist() == [0, 0, 0]
+
+
 def test_attend_window_does_not_see_the_future():
     """NaN and infinities in later tokens' tiles do not reach the rows of earlier tiles."""
     L, H, D = 600, 2, 64
@@ -602,6 +615,30 @@ def test_kv_attend_scores_below_fp32(n, spread, keys, scale):
     p.grow([9, 64], keys)
     attend_pair(p, [n, n], 1, True, spread=spread, scale=scale)
     attend_pair(p, [n, n], 1, False, 100, 3, spread=spread, scale=scale)
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_kv_attend_zero_blocks_beside_large_values_and_many(n):
+    """Blocks of zero values weigh as much as others: beside values of 2^45, and 40000 tokens of nothing
+    else, of which the later ones score higher (their sums pass the earlier reference by 2^13)."""
+    p = Pair(seqs=1, pages=10, blocks=10, H=1, D=64, seed=44)
+    for spread in (0.0, 2.0 ** 45, 0.0, 0.0, 0.0):
+        p.grow([64], spread)
+    attend_pair(p, [n], 1, False, spread=2.0 ** -60)
+
+    L, H, D = 40000, 1, 64
+    c = T.KvCache.create(1, L // P, 1, L // P, H, D)
+    k = torch.full((L, H, D), 1.171875, dtype=BF, device="cuda")
+    k[torch.arange(L) // P % 16 < 4] = 0
+    v, off = torch.zeros_like(k), torch.zeros(1, dtype=torch.int64).cuda()
+    T.kv_extend(c, torch.tensor([L], dtype=torch.int32).cuda())
+    T.kv_append(c, 0, k, v, off, L)
+    q, lse = torch.ones(n, H, D, dtype=BF, device="cuda"), torch.empty(n, H, device="cuda")
+    out = T.kv_attend(c, 0, q, torch.tensor([0, n]).cuda(), n, lse=lse, flags=T.MASK_NONE)
+    low = int((k[:, 0, 0] == 0).sum())
+    want = np.log(low + (L - low) * np.exp(8 * 1.171875))
+    tol = (L + 40) * 2.0 ** -23 + ((D + 4) * 2.0 ** -24 + 2.0 ** -22) * 9.4 + 2.0 ** -23 * want
+    assert (out == 0).all() and np.abs(lse.double().cpu().numpy() - want).max() <= tol
 
 
 def test_steps_of_a_serving_loop():
