@@ -27,6 +27,7 @@ constexpr int ROWS = 128;   // rows of a workgroup, 32 a wave
 // and 38.4, 4 x 4096 62.8 and 78.5; 1024, 8 x 4096 108.7 and 104; some 2000 (32 histories of 203 - 4000 tokens)
 // 155 and 147; 4096, 64 x 2048 with a window of 512 151 and 136.
 constexpr int64_t SPLIT_GROUPS = 768;
+constexpr int BUNDLE = 4;   // tiles of a sequence that are neighbours on an XCD (rows_of)
 
 struct WindowArgs {
   tav2_window a;
@@ -42,13 +43,16 @@ struct Rows {
 
 __device__ __forceinline__ bool rows_of(const WindowArgs& w, int per, Rows& r) {
   const tav2_window& a = w.a;
-  // The rows with the most keys first.  Workgroups go to the 8 XCDs in turn: a sequence's tiles are put
-  // one place further each time, since with its tiles all on one XCD some of these ended long after
-  // the others (32 sequences of 203 - 4000 tokens: 287 us for 168).
-  const int64_t units = int64_t(a.num_requests) * a.kv_heads;
-  const int64_t turn = blockIdx.x / units;
-  const int unit = int((blockIdx.x + turn) % units);
-  const int tile = w.tiles - 1 - int(turn);
+  // The rows with the most keys first.  Workgroups go to the 8 XCDs in turn: BUNDLE neighbouring tiles of
+  // a sequence go to the same one together, where they read the same keys at about the same time, the
+  // next of them to another.
+  const int units = a.num_requests * a.kv_heads;
+  const int slot = int(blockIdx.x) / 8;
+  const int bundle = slot / BUNDLE * 8 + int(blockIdx.x) % 8;
+  const int turn = bundle / units * BUNDLE + slot % BUNDLE;
+  const int unit = (bundle + bundle / units) % units;
+  const int tile = w.tiles - 1 - turn;
+  if (tile < 0) return false;
   const int s = unit / a.kv_heads;
   r.h = unit % a.kv_heads;
   r.G = a.heads / a.kv_heads;
@@ -391,8 +395,8 @@ int rows_per_group(const tav2_window& a) { return a.dtype == TAV2_F32 ? ROWS_F32
 }  // namespace
 
 int64_t attend_window_groups(const tav2_window& a) {
-  return int64_t(a.num_requests) * a.kv_heads *
-         cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), rows_per_group(a));
+  const int64_t tiles = cdiv(int64_t(a.max_len) * (a.heads / a.kv_heads), rows_per_group(a));
+  return cdiv(int64_t(a.num_requests) * a.kv_heads * cdiv(tiles, BUNDLE), 8) * 8 * BUNDLE;
 }
 
 hipError_t launch_attend_window(const tav2_window& a, hipStream_t st) {
@@ -407,7 +411,7 @@ hipError_t launch_attend_window(const tav2_window& a, hipStream_t st) {
     else if (a.head_dim == 64) attend_window_f32<64><<<grid, 256, 0, st>>>(w);
     else attend_window_f32<128><<<grid, 256, 0, st>>>(w);
   } else {
-    const bool split = int64_t(grid) <= SPLIT_GROUPS;
+    const bool split = int64_t(a.num_requests) * a.kv_heads * w.tiles <= SPLIT_GROUPS;
     if (a.head_dim == 32 && split) attend_window_bf16<32, true><<<grid, 512, 0, st>>>(w);
     else if (a.head_dim == 32) attend_window_bf16<32, false><<<grid, 256, 0, st>>>(w);
     else if (a.head_dim == 64 && split) attend_window_bf16<64, true><<<grid, 512, 0, st>>>(w);
