@@ -65,20 +65,26 @@ struct AttSeen {
   int sinks;
 };
 
-// s: this lane's 16 scores of query tile q; c s (c > 0) are powers of two; the values' scale is 2^lv =
-// 1 / inv; key0: position of the first key.  Leaves in s the weights times 2^lv, against m.
-template <int D, int QT>
-__device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16& s, float c, float lv,
+// s: this lane's scores of query tile q against NB blocks of 32 keys; c s (c > 0) are powers of two; the
+// values' scale is 2^lv = 1 / inv; key0: position of the first key.  Leaves in s the weights times 2^lv,
+// against m.
+template <int D, int QT, int NB>
+__device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16 (&s)[NB], float c, float lv,
                                             float inv, bool masked, const AttSeen<QT>& seen, int key0) {
   if (masked) {
     // against register numbers: nothing for each key is left to be prepared where nothing is masked
     const int hi = seen.hi[q] - key0, lo = seen.lo[q] - key0, sinks = seen.sinks - key0;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = r < hi && (r >= lo || r < sinks) ? s[r] : -INFINITY;
-  }
-  float top = s[0];
+    for (int u = 0; u < NB; ++u)
 #pragma unroll
-  for (int r = 1; r < 16; ++r) top = vmax(top, s[r]);
+      for (int r = 0; r < 16; ++r) {
+        const int k = 32 * u + r;
+        s[u][r] = k < hi && (k >= lo || k < sinks) ? s[u][r] : -INFINITY;
+      }
+  }
+  float top = s[0][0];
+#pragma unroll
+  for (int r = 1; r < 16 * NB; ++r) top = vmax(top, s[r / 16][r % 16]);
   top = __builtin_fmaf(xmax32(top), c, lv);
   if (__any(top > st.m[q] + RAISE)) {
     const float m = top - ROOM > st.m[q] ? top - ROOM : st.m[q];
@@ -93,9 +99,10 @@ __device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16& 
   const float b = lv - st.m[q];
   float sum = 0.f;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, b));
-    sum += s[r];
+  for (int r = 0; r < 16 * NB; ++r) {
+    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / 16][r % 16], c, b));
+    s[r / 16][r % 16] = p;
+    sum += p;
   }
   st.l[q] = __builtin_fmaf(sum, inv, st.l[q]);
 }
@@ -115,38 +122,44 @@ __device__ __forceinline__ void att_operands(const f32x16& p, f16x8 (&f)[2]) {
                           pack2h(p[8 * t + 4], p[8 * t + 5]), pack2h(p[8 * t + 6], p[8 * t + 7])));
 }
 
-// keys(kf) sets kf[t]: operand of the key row's features h D / 2 + 8t ..; qf the queries' likewise; values(vf) sets
-// vf[d][t]: feature 32 d + l % 32, keys 16h + 8t ..; c: a lane's queries' factors.
-template <class V, int D, int QT, class Keys, class Values>
+// NB blocks of 32 keys.  keys(u, kf) sets kf[t]: operand of block u's key row's features h D / 2 + 8t ..; qf the
+// queries' likewise; values(u, vf) sets vf[d][t]: feature 32 d + l % 32, keys 16h + 8t .. of block u; c: a
+// lane's queries' factors.
+template <class V, int NB, int D, int QT, class Keys, class Values>
 __device__ __forceinline__ void att_step(AttState<D, QT>& st, Keys keys, Values values,
                                          const V (&qf)[QT][D / 16], const float (&c)[QT], float lv,
                                          float inv, bool masked, const AttSeen<QT>& seen, int key0) {
-  f32x16 s[QT];
-  {
+  f32x16 s[QT][NB];
+#pragma unroll
+  for (int u = 0; u < NB; ++u) {
     V kf[D / 16];
-    keys(kf);
+    keys(u, kf);
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[q][r] = 0.f;
+      for (int r = 0; r < 16; ++r) s[q][u][r] = 0.f;
 #pragma unroll
-      for (int t = 0; t < D / 16; ++t) s[q] = mfma32(kf[t], qf[q][t], s[q]);
+      for (int t = 0; t < D / 16; ++t) s[q][u] = mfma32(kf[t], qf[q][t], s[q][u]);
     }
   }
-  V pf[QT][2];
+  V pf[QT][NB][2];
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
-    att_softmax<D, QT>(st, q, s[q], c[q], lv, inv, masked, seen, key0);
-    att_operands(s[q], pf[q]);
+    att_softmax<D, QT, NB>(st, q, s[q], c[q], lv, inv, masked, seen, key0);
+#pragma unroll
+    for (int u = 0; u < NB; ++u) att_operands(s[q][u], pf[q][u]);
   }
-  V vf[D / 32][2];
-  values(vf);
 #pragma unroll
-  for (int q = 0; q < QT; ++q)
+  for (int u = 0; u < NB; ++u) {
+    V vf[D / 32][2];
+    values(u, vf);
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
+    for (int q = 0; q < QT; ++q)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) st.o[d][q] = mfma32(vf[d][t], pf[q][t], st.o[d][q]);
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) st.o[d][q] = mfma32(vf[d][t], pf[q][u][t], st.o[d][q]);
+  }
 }
 
 }  // namespace tav2

@@ -206,34 +206,41 @@ __global__ __launch_bounds__(SPLIT ? 512 : 256, SPLIT && D <= 64 ? 4 : 2) void a
   load(tiles.at(0) * TK);
   store(0);
   __syncthreads();
-  for (int i = 0; i < n; ++i) {
+  int i = 0;
+  do {   // (a row sees itself: there is a tile)
     const int k0 = tiles.at(i) * TK, buf = i & 1;
     if (i + 1 < n) load(tiles.at(i + 1) * TK);
     const int see = idle ? 0 : tile_seen(k0, TK, wlo, whi, a.window, a.sinks);
     if (see) {
       const uint8_t* const kl = lk(buf) + ak;
       const uint8_t* const vl = lv(buf);
-#pragma unroll D <= 64 ? 2 : 1   // (128 features: both halves at once take too many registers)
-      for (int u = 0; u < (SPLIT ? 1 : 2); ++u) {
-        auto keys = [&](bf16x8(&kf)[D / 16]) {
+      // With 128 features both halves of the tile at once: one look at the reference for 64 keys, and longer
+      // runs of products (8 x 4096 tokens of 4 heads 176 us for 187); with fewer the halves in turn, in fewer
+      // registers (64 x 2048 tokens with a window of 512 128 us for 131; 32 features 133 for 139).
+      constexpr int NB = !SPLIT && D == 128 ? 2 : 1;
+#pragma unroll
+      for (int u0 = 0; u0 < (SPLIT ? 1 : 2); u0 += NB) {
+        auto keys = [&](int b, bf16x8(&kf)[D / 16]) {
+          const int u = u0 + b;
 #pragma unroll
           for (int t = 0; t < D / 16; ++t)
             kf[t] = as_bf16x8(*reinterpret_cast<const uint4*>(kl + 32 * u * KS + 16 * t));
         };
-        auto values = [&](bf16x8(&vf)[D / 32][2]) {
+        auto values = [&](int b, bf16x8(&vf)[D / 32][2]) {
+          const int u = u0 + b;
 #pragma unroll
           for (int d = 0; d < D / 32; ++d)
 #pragma unroll
             for (int t = 0; t < 2; ++t)
               vf[d][t] = as_bf16x8(*reinterpret_cast<const uint4*>(vl + 32 * d * VS + av[u ^ (d & 1)][t]));
         };
-        att_step<bf16x8, D, 1>(st, keys, values, qf, c, 0.f, 1.f, see == 1, seen,
-                                k0 + 32 * (u + part) + 16 * half);
+        att_step<bf16x8, NB, D, 1>(st, keys, values, qf, c, 0.f, 1.f, see == 1, seen,
+                                   k0 + 32 * (u0 + part) + 16 * half);
       }
     }
     if (i + 1 < n) store(buf ^ 1);
     __syncthreads();
-  }
+  } while (++i < n);
   if constexpr (SPLIT) {   // the second halves' states, through the tiles' LDS, into the first's
     static_assert(4 * (D / 32) * 16 * WAVE * 4 <= int(sizeof(lds)), "they fit");
     __shared__ float ml[4][2][WAVE];
@@ -336,7 +343,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_f32(Window
     }
     __builtin_amdgcn_wave_barrier();
     if (i + 4 < n) load(tiles.at(i + 4) * TF);
-    f32x16 s;
+    f32x16 sc[1], &s = sc[0];
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
     const float* kr = lk + m * LS + half * (D / 2);
@@ -346,8 +353,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_f32(Window
 #pragma unroll
       for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4[e], qf[t][e], s, 0, 0, 0);
     }
-    att_softmax<D, 1>(st, 0, s, c, 0.f, 1.f, tile_seen(k0, TF, lo, hi, a.window, a.sinks) != 2, seen,
-                      k0 + 16 * half);
+    att_softmax<D, 1, 1>(st, 0, sc, c, 0.f, 1.f, tile_seen(k0, TF, lo, hi, a.window, a.sinks) != 2, seen,
+                         k0 + 16 * half);
     const float* vr = lv + 16 * half * LS + m;
 #pragma unroll
     for (int t = 0; t < 16; ++t)
