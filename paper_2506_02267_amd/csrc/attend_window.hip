@@ -8,7 +8,7 @@
 // Bound by the vector units: an exponential, a scaling, a maximum, a sum and a rounding for each
 // score, beside 4 D matrix operations; the two add up, as two waves a SIMD seldom meet in different
 // ones.  16384 tokens with a window of 1024, 4 heads of 64: 34 us (13 at a large product's rate); 32 sequences
-// of 203 - 4000 tokens, 4 heads on 2: 142 us (73).
+// of 203 - 4000 tokens, 4 heads on 2: 134 us (73).
 #include <algorithm>
 
 #include "attend_core.h"
@@ -45,7 +45,9 @@ __device__ __forceinline__ bool rows_of(const WindowArgs& w, int per, Rows& r) {
   const tav2_window& a = w.a;
   // The rows with the most keys first.  Workgroups go to the 8 XCDs in turn: BUNDLE neighbouring tiles of
   // a sequence go to the same one together, where they read the same keys at about the same time, the
-  // next of them to another.
+  // next of them to another (with a sequence's tiles all on one, some XCDs ended long after the others: 32
+  // sequences of 203 - 4000 tokens 287 us for 168).  Bundles of 1, 2, 4, 8 and 16, us: 8 sequences in fp32 21.2,
+  // 20.0, 19.4, 19.8, 20.1; 8 x 4096 tokens in bf16 103.8, 99.9, 100.5, 105.8, 110.
   const int units = a.num_requests * a.kv_heads;
   const int slot = int(blockIdx.x) / 8;
   const int bundle = slot / BUNDLE * 8 + int(blockIdx.x) % 8;
@@ -283,7 +285,7 @@ __global__ __launch_bounds__(SPLIT ? 512 : 256, SPLIT && D <= 64 ? 4 : 2) void a
 // fp32, on 32x32x2 fp32 products (the weights are operands as they are): a workgroup takes 32 rows,
 // and its four waves take the 32-key tiles in turn, each through its own part of LDS, so that no wave
 // waits for another until their states meet at the end.  8 sequences of 57 - 1000 tokens, a window of 200, 8 heads
-// of 32: 21 us, the few tiles of a row one after the other (35 with 128 rows a workgroup); 4 x 2000 tokens of
+// of 32: 19 us, the few tiles of a row one after the other (35 with 128 rows a workgroup); 4 x 2000 tokens of
 // 64 features: 97 us for 160.
 constexpr int TF = 32;
 constexpr int ROWS_F32 = 32;

@@ -17,7 +17,7 @@
 // One query a sequence is bound by HBM: 64 sequences of 16384 tokens, 8 kv heads, are read at 5.6 TB/s
 // with 64 features and 5.7 with 128 (a large copy: 4.7, read and written).  Many queries are bound by the vector
 // units, which turn codes into fp16 and scores into weights while the matrix units wait, and the
-// reverse: 1000 candidates of one 16384-token history, 4 heads of 64, take 39 us, 13 at a large product's rate.
+// reverse: 1000 candidates of one 16384-token history, 4 heads of 64, take 36.7 us, 13 at a large product's rate.
 #include <algorithm>
 
 #include "attend_core.h"
@@ -860,9 +860,9 @@ int64_t most_pages(const tav2_kv& c, const tav2_kv_queries& q) {
 // Query rows of a workgroup: 16, 32, or, where there are pages enough to fill the CUs with tiles of twice
 // the work, 64 (which turn a page's codes into operands once for twice the queries, but start and
 // end later; 64 features at most: registers).  Both sides, us a call, 4 heads of 64, one history
-// of 16384 tokens: 64 candidates 14.1 with 32 rows and 24.5 with 64, 200: 18.4 and 25.4, 500: 26.1 and 26.7,
-// 600 (10240 tiles x pages): 36.7 and 37.3, 800: 44.6 and 38.7, 1000: 42.2 and 40.1; 32 histories of 4096 - 16384
-// tokens, 64 candidates each: 79 and 66.
+// of 16384 tokens: 64 candidates 12.9 with 32 rows and 24.5 with 64, 400: 28.1 and 24.8, 500: 24.2 and 25.3,
+// 600 (10240 tiles x pages): 36.7 and 34.7, with 32 features 26.4 and 28.3, 800: 44.6 and 35.8; 8 histories of
+// 4096 - 16384 tokens, 64 candidates each: 25.0 and 27.1, 32 of them: 79 and 66.
 int tile_rows(const tav2_kv& c, const tav2_kv_queries& q) {
   const int64_t rows = int64_t(q.max_count) * (q.heads / c.kv_heads);
   if (rows <= 16) return 16;
