@@ -774,3 +774,77 @@ def test_graph_of_a_decode_step():
                 check(out[s:s + 1], lse[s:s + 1], want, D, HALF, p.ref.len[s], p.vmax(s, 0))
         p.ref.trim(200, 2)
     p.same()
+
+
+def test_graph_of_a_slate_and_an_encoding():
+    """fork + extend + append + attend + free + compact and a windowed encoding captured once: every replay
+    gives the bits of the eager calls on a cache like it, with eager work between."""
+    H, D = 2, 64
+
+    def fresh():
+        p = Pair(seqs=4, pages=40, blocks=12, H=H, D=D, seed=61)
+        p.grow([250, 130, 0, 0])
+        return p.gpu
+
+    a, b = fresh(), fresh()
+    parent = torch.tensor([-1, -1, 0, 1], dtype=torch.int32).cuda()
+    count = torch.tensor([1, 0, 70, 5], dtype=torch.int32).cuda()
+    drop = torch.tensor([0, 0, 1, 1], dtype=torch.uint8).cuda()
+    kv = torch.empty(76, 2 * H, D, dtype=BF, device="cuda")
+    q = torch.empty(76, H, D, dtype=BF, device="cuda")
+    k_off, q_off = torch.tensor([0, 1, 1, 71]).cuda(), torch.tensor([0, 1, 1, 71, 76]).cuda()
+    w_off, w_len = torch.tensor([0, 50]).cuda(), torch.tensor([50, 26], dtype=torch.int32).cuda()
+
+    def outputs():
+        return [torch.empty(76, H, D, dtype=BF, device="cuda") for _ in range(2)] + [
+            torch.empty(1, dtype=torch.int32, device="cuda")]
+
+    def step(c, out, ws):
+        T.kv_fork(c, parent)
+        T.kv_extend(c, count)
+        T.kv_append(c, 0, kv[:, :H], kv[:, H:], k_off, 70)
+        T.kv_attend(c, 0, q, q_off, 70, out=out[0], ws=ws[0])
+        T.attend_window(q, kv[:, :H], kv[:, H:], w_off, w_len, 50, 20, 1, out=out[1])
+        T.kv_free(c, drop)
+        T.kv_compact(c, used=out[2], ws=ws[1])
+
+    g = torch.Generator().manual_seed(62)
+    ga, gb = outputs(), outputs()
+    wa, wb = [T.Workspace(), T.Workspace()], [T.Workspace(), T.Workspace()]
+    kv.copy_(rows(g, 76, 2 * H, D))
+    q.copy_(rows(g, 76, H, D))
+    for c, o, w in ((a, ga, wa), (b, gb, wb)):   # (workspaces and kernels' attributes, outside the capture)
+        step(c, o, w)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a, ga, wa)
+    for i in range(5):
+        kv.copy_(rows(g, 76, 2 * H, D))
+        q.copy_(rows(g, 76, H, D))
+        graph.replay()
+        torch.cuda.synchronize()
+        step(b, gb, wb)
+        assert all(torch.equal(x, y) for x, y in zip(ga, gb)), i
+        assert a.table.tolist() == b.table.tolist() and a.refs.tolist() == b.refs.tolist()
+        assert a.length.tolist() == b.length.tolist() == [252 + i, 130, 0, 0]
+
+
+def test_two_calls_at_once():
+    """Calls that only read the cache, on two streams with workspaces of their own."""
+    p = Pair(seqs=3, pages=200, blocks=64, H=2, D=64, seed=63)
+    p.grow([3500, 640, 2000])
+    g = torch.Generator().manual_seed(64)
+    qs = [rows(g, 3, 4, 64), rows(g, 3 * 90, 4, 64)]
+    offs = [torch.tensor([0, 1, 2, 3]).cuda(), torch.tensor([0, 90, 180, 270]).cuda()]
+    want = [T.kv_attend(p.gpu, 0, q, o, n, flags=T.MASK_NONE) for q, o, n in zip(qs, offs, (1, 90))]
+    streams, ws = [torch.cuda.Stream() for _ in qs], [T.Workspace() for _ in qs]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    outs = [[torch.empty_like(w) for _ in range(4)] for w in want]
+    for i in range(4):
+        for j in range(2):
+            T.kv_attend(p.gpu, 0, qs[j], offs[j], (1, 90)[j], out=outs[j][i], flags=T.MASK_NONE,
+                        ws=ws[j], stream=streams[j])
+    torch.cuda.synchronize()
+    for j in range(2):
+        assert all(torch.equal(want[j], x) for x in outs[j])
