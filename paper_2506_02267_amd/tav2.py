@@ -674,8 +674,9 @@ def kv_append(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, offs
     of one projection) of the tokens that the last kv_extend granted; sequence s's begin at row
     offset[s] (int64 [seqs] or longer)."""
     k_ld, v_ld = _heads("k", k, torch.bfloat16), _heads("v", v, torch.bfloat16)
-    if k.shape[1:] != cache.row or v.shape[1:] != cache.row:
-        raise ValueError("k, v: expected [rows, kv_heads, head_dim] of the cache's sizes")
+    if k.shape[1:] != cache.row or v.shape != k.shape:
+        raise ValueError("k, v: expected [rows, kv_heads, head_dim] of the cache's sizes, as many of "
+                         "each")
     if offset.dtype != torch.int64 or offset.dim() != 1 or offset.shape[0] < cache.seqs \
             or not offset.is_contiguous():
         raise ValueError("offset: expected contiguous int64 [seqs] or longer")

@@ -233,6 +233,15 @@ def test_binding_refuses_wrong_shapes_and_types():
             print("accepted:", i)
 
 
+def test_append_refuses_fewer_values_than_keys():
+    """(kv_append reads offset[s] + i rows of both.)"""
+    c = host_cache()
+    kv = [torch.zeros(n, 2, 32, dtype=torch.bfloat16) for n in (5, 4)]
+    for k, v in ((0, 1), (1, 0)):
+        with pytest.raises(ValueError, match="k, v"):
+            T.kv_append(c, 0, kv[k], kv[v], torch.zeros(2, dtype=torch.int64), 5)
+
+
 def test_binding_refuses_a_stream_of_another_device():
     with pytest.raises(ValueError, match="stream"):
         T._run("tav2_kv_trim", 0, SimpleNamespace(device_index=1, cuda_stream=0), ())
