@@ -359,7 +359,7 @@ typedef struct tav2_window {
   int32_t head_dim;            /* 32, 64 or 128 */
   int32_t dtype;               /* TAV2_F32 or TAV2_BF16 */
   int32_t window, sinks;       /* >= 0 */
-  float   scale;               /* > 0, or 0 for 1 / sqrt(head_dim) */
+  float   scale;               /* > 0, at most 2.3e38, or 0 for 1 / sqrt(head_dim) */
   int32_t reserved;            /* set to 0 */
 } tav2_window;
 /* q, k, v, out 16-byte aligned.  Errors: TAV2_ERR_NULL, TAV2_ERR_SHAPE, TAV2_ERR_DTYPE,
@@ -450,7 +450,7 @@ typedef struct tav2_kv_queries {
   int32_t max_count;           /* host-side bound of a sequence's queries, at most total */
   int32_t heads;               /* a multiple of kv_heads */
   int32_t window, sinks;       /* >= 0 */
-  float   scale;               /* > 0, or 0 for 1 / sqrt(head_dim) */
+  float   scale;               /* > 0, at most 2.3e38, or 0 for 1 / sqrt(head_dim) */
   int32_t reserved;            /* set to 0 */
 } tav2_kv_queries;
 size_t tav2_kv_attend_workspace(const tav2_kv* c, const tav2_kv_queries* q);

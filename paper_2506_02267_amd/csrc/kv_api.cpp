@@ -18,8 +18,9 @@ tav2_status hip_status(hipError_t e) { return e == hipSuccess ? TAV2_OK : TAV2_E
 
 bool head_dim_ok(int d) { return d == 32 || d == 64 || d == 128; }
 
-// A scale of 0 stands for 1 / sqrt(head_dim).
-bool scale_ok(float s) { return s >= 0.f && s <= 3.0e38f; }
+// A scale of 0 stands for 1 / sqrt(head_dim).  The kernels multiply by log2(e): the bound leaves that
+// finite.
+bool scale_ok(float s) { return s >= 0.f && s <= 2.3e38f; }
 
 // Rows of `heads` heads at least, `per` elements in 16 bytes.
 bool stride_ok(int64_t ld, int heads, int head_dim, int per) {

@@ -112,6 +112,16 @@ def test_every_cache_call_refuses_a_bad_cache(kw, status):
     assert lib.tav2_kv_compact_workspace(ctypes.byref(c)) == 0
 
 
+@pytest.mark.parametrize("scale,status", [(2.3e38, 0), (2.37e38, -2), (3.0e38, -2)])
+def test_scales_that_log2_e_takes_past_fp32(scale, status):
+    """Scores are taken in powers of two: with a scale past FLT_MAX / log2(e) = 2.36e38 a score of zero
+    would be 0 times infinity."""
+    lib, a, c = T.load_library(), fake_window(num_requests=0, scale=scale), fake_kv()
+    assert lib.tav2_attend_window(ctypes.byref(a), None) == status
+    q = fake_queries(q=None, offset=None, total=0, max_count=0, scale=scale)
+    assert lib.tav2_kv_attend(ctypes.byref(c), 0, ctypes.byref(q), 0, None, None, None, 0, None) == status
+
+
 def test_null_cache():
     assert set(kv_calls(None).values()) == {-1}
 
