@@ -420,8 +420,7 @@ tav2_status tav2_kv_extend(const tav2_kv* c, const int32_t* count, void* stream)
  * The keys and values of the tokens that the last tav2_kv_extend granted, for one layer
  * (once per layer and extension): sequence s's fresh[s] tokens are rows offset[s].. of k and v
  * (bf16 rows of [kv_heads, head_dim], row strides k_ld and v_ld elements as in tav2_window; 16-byte
- * aligned; finite; v's magnitudes 0 or from 2^-80 to 2^50, beyond which tav2_kv_attend loses
- * precision).  Blocks that are full now go to their pages, the rest to the tail.
+ * aligned; finite; v's magnitudes at most 2^80).  Blocks that are full now go to their pages, the rest to the tail.
  *   offset    device int64 [num_seqs]
  *   max_count host-side bound of fresh[s]; tokens of a sequence past it are not written
  */

@@ -12,6 +12,13 @@
 // largest is 2^ROOM: any reference gives the same quotient, the sums are fp32, and raising it is rare
 // after a query's first keys.  The room is for weights in fp16, whose least step is 2^-24: 2^-30 of
 // the largest weight.
+//
+// Values may come with a scale 2^lv of their own for each block of keys.  What is multiplied is then a weight
+// times 2^lv, against m; the weights' sum l has a reference of its own, n, since scales lie further apart
+// than fp32's powers of two reach.  A block's part of it comes from the same exponentials,
+// 2^(c s + lv - m): times 2^-lv 2^(m - n) = inv d.  A block whose products are all below 2^(m - FLOOR), or
+// whose values are zeros (lv = -inf), adds nothing to the features, its weights being zeros in fp16; its
+// exponentials are taken against its own largest score, for the sum alone.
 #pragma once
 
 #include <float.h>
@@ -26,7 +33,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 
-constexpr float RAISE = 14.f, ROOM = 6.f;
+constexpr float RAISE = 14.f, ROOM = 6.f, FLOOR = 32.f;
 
 __device__ __forceinline__ f32x16 mfma32(const f16x8& a, const f16x8& b, const f32x16& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
@@ -65,12 +72,29 @@ struct AttSeen {
   int sinks;
 };
 
-// s: this lane's scores of query tile q against NB blocks of 32 keys; c s (c > 0) are powers of two; the
-// values' scale is 2^lv = 1 / inv; key0: position of the first key.  Leaves in s the weights times 2^lv,
-// against m.
-template <int D, int QT, int NB>
-__device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16 (&s)[NB], float c, float lv,
-                                            float inv, bool masked, const AttSeen<QT>& seen, int key0) {
+// With scaled values: m refers to the products, n to the weights, d = 2^(m - n).
+template <int D, int QT>
+struct AttScaledState : AttState<D, QT> {
+  float n[QT], d[QT];
+  __device__ __forceinline__ void clear() {
+    AttState<D, QT>::clear();
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+      n[q] = -FLT_MAX;
+      d[q] = 1.f;
+    }
+  }
+};
+
+// What a block's values are to be multiplied by: nothing, or 2^lv = 1 / inv.
+struct AttNoScale {};
+struct AttScale {
+  float lv, inv;
+};
+
+// Scores of keys that are not seen become -inf; returns the largest of the others, of both halves.
+template <int QT, int NB>
+__device__ __forceinline__ float att_mask(f32x16 (&s)[NB], int q, bool masked, const AttSeen<QT>& seen, int key0) {
   if (masked) {
     // against register numbers: nothing for each key is left to be prepared where nothing is masked
     const int hi = seen.hi[q] - key0, lo = seen.lo[q] - key0, sinks = seen.sinks - key0;
@@ -85,7 +109,28 @@ __device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16 (
   float top = s[0][0];
 #pragma unroll
   for (int r = 1; r < 16 * NB; ++r) top = vmax(top, s[r / 16][r % 16]);
-  top = __builtin_fmaf(xmax32(top), c, lv);
+  return xmax32(top);
+}
+
+// s becomes 2^(c s + b); returns the sum.
+template <int NB>
+__device__ __forceinline__ float att_exp(f32x16 (&s)[NB], float c, float b) {
+  float sum = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16 * NB; ++r) {
+    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / 16][r % 16], c, b));
+    s[r / 16][r % 16] = p;
+    sum += p;
+  }
+  return sum;
+}
+
+// s: this lane's scores of query tile q against NB blocks of 32 keys; c s (c > 0) are powers of two; key0:
+// position of the first key.  Leaves in s the weights (times the values' scale), against m.
+template <int D, int QT, int NB>
+__device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16 (&s)[NB], float c, AttNoScale,
+                                            bool masked, const AttSeen<QT>& seen, int key0) {
+  const float top = att_mask(s, q, masked, seen, key0) * c;
   if (__any(top > st.m[q] + RAISE)) {
     const float m = top - ROOM > st.m[q] ? top - ROOM : st.m[q];
     const float f = __builtin_amdgcn_exp2f(st.m[q] - m);
@@ -96,15 +141,57 @@ __device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16 (
 #pragma unroll
       for (int r = 0; r < 16; ++r) st.o[d][q][r] *= f;
   }
-  const float b = lv - st.m[q];
-  float sum = 0.f;
-#pragma unroll
-  for (int r = 0; r < 16 * NB; ++r) {
-    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / 16][r % 16], c, b));
-    s[r / 16][r % 16] = p;
-    sum += p;
+  st.l[q] += att_exp(s, c, -st.m[q]);
+}
+
+// Where a block's largest score `top` passes the references, those that it does not: m, n and d, and the factors
+// of the features and of the sum so far.
+__device__ __forceinline__ void att_raise(float top, float lv, float& m, float& n, float& d, float* of, float* lf) {
+  const float over = top + lv;
+  const float m1 = over - ROOM > m ? over - ROOM : m;
+  const float n1 = top - ROOM > n ? top - ROOM : n;
+  *of = __builtin_amdgcn_exp2f(m - m1);
+  *lf = __builtin_amdgcn_exp2f(n - n1);
+  d = __builtin_amdgcn_exp2f(m1 - n1);
+  m = m1;
+  n = n1;
+}
+__device__ __forceinline__ bool att_passes(float top, float lv, float m, float n) {
+  return vmax(top + (lv - m), top - n) > RAISE;
+}
+
+// The exponentials' offset b and the factor e of their sum.
+__device__ __forceinline__ void att_offset(float top, AttScale v, float m, float n, float d, float* b, float* e) {
+  *b = v.lv - m;
+  *e = v.inv * d;
+  const bool low = top + *b < -FLOOR;
+  if (__any(low)) {
+    // (a score of 2^20 and more is itself rounded by 2^-24 of it: further below then.  Nothing seen: the
+    // exponentials are zeros whatever they are taken against)
+    const bool some = top > -FLT_MAX;
+    const float bl = some ? -FLOOR - top - __builtin_fabsf(top) * 0x1p-22f : 0.f;
+    const float el = some ? __builtin_amdgcn_exp2f(-bl - n) : 0.f;
+    *b = low ? bl : *b;
+    *e = low ? el : *e;
   }
-  st.l[q] = __builtin_fmaf(sum, inv, st.l[q]);
+}
+
+template <int D, int QT, int NB>
+__device__ __forceinline__ void att_softmax(AttScaledState<D, QT>& st, int q, f32x16 (&s)[NB], float c, AttScale v,
+                                            bool masked, const AttSeen<QT>& seen, int key0) {
+  const float top = att_mask(s, q, masked, seen, key0) * c;
+  if (__any(att_passes(top, v.lv, st.m[q], st.n[q]))) {
+    float of, lf;
+    att_raise(top, v.lv, st.m[q], st.n[q], st.d[q], &of, &lf);
+    st.l[q] *= lf;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st.o[d][q][r] *= of;
+  }
+  float b, e;
+  att_offset(top, v, st.m[q], st.n[q], st.d[q], &b, &e);
+  st.l[q] = __builtin_fmaf(att_exp(s, c, b), e, st.l[q]);
 }
 
 // 16 weights as the operands of two products.
@@ -125,10 +212,10 @@ __device__ __forceinline__ void att_operands(const f32x16& p, f16x8 (&f)[2]) {
 // NB blocks of 32 keys.  keys(u, kf) sets kf[t]: operand of block u's key row's features h D / 2 + 8t ..; qf the
 // queries' likewise; values(u, vf) sets vf[d][t]: feature 32 d + l % 32, keys 16h + 8t .. of block u; c: a
 // lane's queries' factors.
-template <class V, int NB, int D, int QT, class Keys, class Values>
-__device__ __forceinline__ void att_step(AttState<D, QT>& st, Keys keys, Values values,
-                                         const V (&qf)[QT][D / 16], const float (&c)[QT], float lv,
-                                         float inv, bool masked, const AttSeen<QT>& seen, int key0) {
+template <class V, int NB, int D, int QT, class State, class Keys, class Values, class Scale>
+__device__ __forceinline__ void att_step(State& st, Keys keys, Values values, const V (&qf)[QT][D / 16],
+                                         const float (&c)[QT], Scale scale, bool masked,
+                                         const AttSeen<QT>& seen, int key0) {
   f32x16 s[QT][NB];
 #pragma unroll
   for (int u = 0; u < NB; ++u) {
@@ -145,7 +232,7 @@ __device__ __forceinline__ void att_step(AttState<D, QT>& st, Keys keys, Values 
   V pf[QT][NB][2];
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
-    att_softmax<D, QT, NB>(st, q, s[q], c[q], lv, inv, masked, seen, key0);
+    att_softmax(st, q, s[q], c[q], scale, masked, seen, key0);
 #pragma unroll
     for (int u = 0; u < NB; ++u) att_operands(s[q][u], pf[q][u]);
   }

@@ -236,7 +236,7 @@ __global__ __launch_bounds__(SPLIT ? 512 : 256, SPLIT && D <= 64 ? 4 : 2) void a
             for (int t = 0; t < 2; ++t)
               vf[d][t] = as_bf16x8(*reinterpret_cast<const uint4*>(vl + 32 * d * VS + av[u ^ (d & 1)][t]));
         };
-        att_step<bf16x8, NB, D, 1>(st, keys, values, qf, c, 0.f, 1.f, see == 1, seen,
+        att_step<bf16x8, NB, D, 1>(st, keys, values, qf, c, AttNoScale(), see == 1, seen,
                                    k0 + 32 * (u0 + part) + 16 * half);
       }
     }
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void attend_window_f32(Window
 #pragma unroll
       for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k4[e], qf[t][e], s, 0, 0, 0);
     }
-    att_softmax<D, 1, 1>(st, 0, sc, c, 0.f, 1.f, tile_seen(k0, TF, lo, hi, a.window, a.sinks) != 2, seen,
+    att_softmax(st, 0, sc, c, AttNoScale(), tile_seen(k0, TF, lo, hi, a.window, a.sinks) != 2, seen,
                          k0 + 16 * half);
     const float* vr = lv + 16 * half * LS + m;
 #pragma unroll

@@ -121,13 +121,21 @@ __device__ __forceinline__ float max8(const u32x4& x, float m) {
   return m;
 }
 // The power of two that takes top into [2^14, 2^15), as a factor and back (tops below 2^-86 like
-// 2^-86: the factor back is a weight's, and sums of those over it stay finite).
+// 2^-86: both stay normal numbers).
 __device__ __forceinline__ void into_half(float top, float* f, float* back) {
   uint32_t ex = __float_as_uint(top) >> 23;
   ex = ex < 41 ? 41 : ex > 254 ? 254 : ex;
   *f = __uint_as_float((268 - ex) << 23);
   *back = __uint_as_float((ex - 14) << 23);
 }
+
+// The scale of an open block's values; of zeros none.
+__device__ __forceinline__ AttScale tail_scale(float top, float back, float f) {
+  return AttScale{top > 0.f ? __builtin_amdgcn_logf(back) : -INFINITY, f};
+}
+
+// 2^(x / 2), to be taken twice: a weight of 2^-127 and less may belong to a value as large beside the others.
+__device__ __forceinline__ float half_factor(float x) { return __builtin_amdgcn_exp2f(0.5f * x); }
 
 // A score's factor from the query's and the keys'.  One that fp32 cannot hold (queries of zeros, tiny scales)
 // is no zero, by which a masked -inf would become a NaN: scores are below 2^38, so 2^-126 adds at most
@@ -241,21 +249,16 @@ struct Feed {
       rv[i] = vp[i * WAVE];
     }
   }
-  // Factors of entry t.  Scale 1 may be a block of zeros, which is taken as if at the scale 2^-80: its
-  // weights then neither raise the reference over small values (down to 2^-90) nor vanish beside large
-  // ones (up to 2^50), and as many as there are tokens can be summed.
-  __device__ __forceinline__ void factors(int t, float* ks, float* lv, float* inv) const {
+  // Factors of entry t.  Scale 1 may be a block of zeros, whose scale counts as none.
+  __device__ __forceinline__ void factors(int t, float* ks, AttScale* v) const {
     *ks = lane_f(kss, t);
-    *lv = lane_f(lvs, t);
-    *inv = lane_f(invs, t);
-    if (*lv == 0.f) {
+    v->lv = lane_f(lvs, t);
+    v->inv = lane_f(invs, t);
+    if (v->lv == 0.f) {
       uint32_t any = 0;
 #pragma unroll
       for (int e = 0; e < D / 16; ++e) any |= rv[e].x | rv[e].y | rv[e].z | rv[e].w;
-      if (!__any(any != 0)) {
-        *lv = -80.f;
-        *inv = 0x1p80f;
-      }
+      if (!__any(any != 0)) v->lv = -INFINITY;
     }
   }
   // The page into the wave's part of LDS: keys' pieces from 0, features' from 4 D (KC and VC pieces a
@@ -329,7 +332,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
            (int64_t(b) * KVP < all_lo && int64_t(b + 1) * KVP > a.q.sinks);
   };
 
-  AttState<D, QT> st;
+  AttScaledState<D, QT> st;
   st.clear();
   bool open = false;
   int i = j.c0 + wave, t = 0;
@@ -344,8 +347,9 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
     open |= i < j.c1 && b >= full;
     const int next = t + 1 < WAVE ? feed.page(t + 1) : -1;
     const bool masked = part_seen(b);
-    float ks, lv, inv, cs[QT];
-    feed.factors(t, &ks, &lv, &inv);
+    float ks, cs[QT];
+    AttScale vs;
+    feed.factors(t, &ks, &vs);
 #pragma unroll
     for (int q = 0; q < QT; ++q) cs[q] = score_factor(cq[q], ks);
     feed.put(my);
@@ -377,7 +381,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
             vf[d][1] = codes8h(w.z, w.w);
           }
         };
-        att_step<f16x8, NB, D, QT>(st, keys, values, qf, cs, lv, inv, masked, seen,
+        att_step<f16x8, NB, D, QT>(st, keys, values, qf, cs, vs, masked, seen,
                                    b * KVP + 32 * u0 + 16 * half);
       }
     }
@@ -438,17 +442,17 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
 #pragma unroll
           for (int t = 0; t < 2; ++t) vf[d][t] = scaled8h(raw_value(d, t), fv);
       };
-      att_step<f16x8, 1, D, QT>(st, keys, values, qf, cs, __builtin_amdgcn_logf(backv), fv, masked,
-                                seen, full * KVP + k0);
+      att_step<f16x8, 1, D, QT>(st, keys, values, qf, cs, tail_scale(vt, backv, fv), masked, seen,
+                                full * KVP + k0);
     }
   }
 
   __builtin_amdgcn_wave_barrier();
-  // the four waves' states meet in LDS; wave w then joins registers 4w .. 4w + 3 of each tile (in the
-  // order of the waves), features 8w + 4 half .. of it
+  // the four waves' states meet in LDS, features against the weights' reference as their sums are; wave w
+  // then joins registers 4w .. 4w + 3 of each tile (in the order of the waves), features 8w + 4 half .. of it
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
-    mm[wave][q][0][lane] = st.m[q];
+    mm[wave][q][0][lane] = st.n[q];
     mm[wave][q][1][lane] = xsum32(st.l[q]);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -456,7 +460,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
       for (int j = 0; j < 4; ++j)
         my[((q * (D / 32) + d) * 4 + j) * WAVE + lane] = __builtin_bit_cast(
             u32x4, (f32x4){st.o[d][q][4 * j], st.o[d][q][4 * j + 1], st.o[d][q][4 * j + 2],
-                           st.o[d][q][4 * j + 3]});
+                           st.o[d][q][4 * j + 3]} * st.d[q]);
   }
   __syncthreads();
 #pragma unroll
@@ -468,8 +472,8 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
     for (int w = 0; w < 4; ++w) M = vmax(M, mm[w][q][0][lane]);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      f[w] = __builtin_amdgcn_exp2f(mm[w][q][0][lane] - M);
-      l += mm[w][q][1][lane] * f[w];
+      f[w] = half_factor(mm[w][q][0][lane] - M);
+      l += mm[w][q][1][lane] * f[w] * f[w];
     }
     const int64_t at = (q0 + row / G) * a.q.heads + h * G + row % G;
     const int64_t part = int64_t(j.split) * a.q.total * a.q.heads + at;
@@ -482,10 +486,10 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
       for (int w = 0; w < 4; ++w) {
         const f32x4 x = __builtin_bit_cast(
             f32x4, stage[w][((q * (D / 32) + d) * 4 + wave) * WAVE + lane]);
-        o.x = __builtin_fmaf(x.x, f[w], o.x);
-        o.y = __builtin_fmaf(x.y, f[w], o.y);
-        o.z = __builtin_fmaf(x.z, f[w], o.z);
-        o.w = __builtin_fmaf(x.w, f[w], o.w);
+        o.x = __builtin_fmaf(x.x * f[w], f[w], o.x);
+        o.y = __builtin_fmaf(x.y * f[w], f[w], o.y);
+        o.z = __builtin_fmaf(x.z * f[w], f[w], o.z);
+        o.w = __builtin_fmaf(x.w * f[w], f[w], o.w);
       }
       const int feature = 32 * d + 8 * wave + 4 * half;
       if (a.splits > 1)
@@ -620,12 +624,12 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
   }
 
   f32x4 o[ND];
-  float ref = -FLT_MAX, sum = 0.f;
+  float ref = -FLT_MAX, wref = -FLT_MAX, ratio = 1.f, sum = 0.f;   // (m, n, d, l of attend_core.h)
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
   // one page: keys(i, kf) sets the operands of S^T's tile i, values(d, vf) those of O^T's tile d
-  auto step = [&](auto keys, auto values, float cs, float lv, float inv, int key0) {
+  auto step = [&](auto keys, auto values, float cs, AttScale vs, int key0) {
     f32x4 s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -644,16 +648,16 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
     float top = s[0][0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = vmax(top, s[r / 4][r % 4]);
-    top = __builtin_fmaf(xmax32(xmax16(top)), cs, lv);
-    if (__any(top > ref + RAISE)) {
-      const float to = top - ROOM > ref ? top - ROOM : ref;
-      const float f = __builtin_amdgcn_exp2f(ref - to);
-      ref = to;
-      sum *= f;
+    top = xmax32(xmax16(top)) * cs;
+    if (__any(att_passes(top, vs.lv, ref, wref))) {
+      float of, lf;
+      att_raise(top, vs.lv, ref, wref, ratio, &of, &lf);
+      sum *= lf;
 #pragma unroll
-      for (int d = 0; d < ND; ++d) o[d] *= f;
+      for (int d = 0; d < ND; ++d) o[d] *= of;
     }
-    const float b = lv - ref;
+    float b, e;
+    att_offset(top, vs, ref, wref, ratio, &b, &e);
     float part = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -661,7 +665,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
       s[r / 4][r % 4] = x;
       part += x;
     }
-    sum = __builtin_fmaf(part, inv, sum);
+    sum = __builtin_fmaf(part, e, sum);
     f16x8 pf[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -688,8 +692,9 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
     }
     const int b = j.list.at(i);
     const int next = t + 1 < WAVE ? feed.page(t + 1) : -1;
-    float ks, lv, inv;
-    feed.factors(t, &ks, &lv, &inv);
+    float ks;
+    AttScale vs;
+    feed.factors(t, &ks, &vs);
     feed.put(my);
     feed.load(a, j, next);
     if (page >= 0) {
@@ -713,7 +718,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
         vf[0] = codes8h(w.x, w.y);
         vf[1] = codes8h(w.z, w.w);
       };
-      step(keys, values, score_factor(cq, ks), lv, inv, b * KVP);
+      step(keys, values, score_factor(cq, ks), vs, b * KVP);
     }
     page = next;
   }
@@ -756,7 +761,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
 #pragma unroll
       for (int t = 0; t < 2; ++t) vf[t] = scaled8h(raw_value(d, t), fv);
     };
-    step(keys, values, score_factor(cq, backk), __builtin_amdgcn_logf(backv), fv, full * KVP);
+    step(keys, values, score_factor(cq, backk), tail_scale(vt, backv, fv), full * KVP);
   };
   if (j.list.at(j.c1 - 1) >= full) {
     const int mine = hi, base = j.s / a.group * a.group;
@@ -774,11 +779,11 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
   __builtin_amdgcn_wave_barrier();
   sum = xsum32(xsum16(sum));
   if (g == 0) {
-    mm[wave][0][m] = ref;
+    mm[wave][0][m] = wref;
     mm[wave][1][m] = sum;
   }
 #pragma unroll
-  for (int d = 0; d < ND; ++d) my[d * WAVE + lane] = __builtin_bit_cast(u32x4, o[d]);
+  for (int d = 0; d < ND; ++d) my[d * WAVE + lane] = __builtin_bit_cast(u32x4, o[d] * ratio);
   __syncthreads();
   if (!valid) return;
   float M = -FLT_MAX, l = 0.f, f[4];
@@ -786,8 +791,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
   for (int w = 0; w < 4; ++w) M = vmax(M, mm[w][0][m]);
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    f[w] = __builtin_amdgcn_exp2f(mm[w][0][m] - M);
-    l += mm[w][1][m] * f[w];
+    f[w] = half_factor(mm[w][0][m] - M);
+    l += mm[w][1][m] * f[w] * f[w];
   }
   const int64_t part = int64_t(j.split) * a.q.total * a.q.heads + at;
   const bool some = l > 0.f || l != l;
@@ -795,7 +800,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
   for (int d = wave; d < ND; d += 4) {
     f32x4 x = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) x += __builtin_bit_cast(f32x4, stage[w][d * WAVE + lane]) * f[w];
+    for (int w = 0; w < 4; ++w) x += __builtin_bit_cast(f32x4, stage[w][d * WAVE + lane]) * f[w] * f[w];
     const int feature = 16 * d + 4 * g;
     if (a.splits > 1)
       *reinterpret_cast<f32x4*>(a.part_o + part * D + feature) = x;
@@ -832,9 +837,9 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(AttendArgs a) {
   for (int s = g; s < a.splits; s += NG) {
     const int64_t p = s * n + at;
     const float lp = a.part_ml[2 * p + 1], o = a.part_o[p * D + f];
-    const float w = __builtin_amdgcn_exp2f(a.part_ml[2 * p] - M);
-    l += lp * w;
-    x += lp != 0.f ? o * w : 0.f;
+    const float w = half_factor(a.part_ml[2 * p] - M);
+    l += lp * w * w;
+    x += lp != 0.f ? o * w * w : 0.f;
   }
   lo[g][f] = x;
   if (f == 0) ll[g] = l;

@@ -848,3 +848,60 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for j in range(2):
         assert all(torch.equal(want[j], x) for x in outs[j])
+
+
+# ------------------------------------------------------------------------- blocks of very different values
+def levels_cache(blocks, seed, copies):
+    """A sequence of blocks (tokens, score in nats, spread of the values) for queries of ones, and copies of it:
+    the blocks before the last fill pages, all keys of a block are alike."""
+    S = 1 + copies
+    p = Pair(seqs=S, pages=len(blocks), blocks=len(blocks), H=1, D=64, seed=seed)
+    off = torch.zeros(S, dtype=torch.int64).cuda()
+    for tokens, score, spread in blocks:
+        kv = torch.cat([torch.full((tokens, 1, 64), score / 8.0),
+                        torch.randn(tokens, 1, 64, generator=p.g) * spread], 1).to(BF)
+        x, count = kv.cuda(), [tokens] + [0] * copies
+        T.kv_extend(p.gpu, torch.tensor(count, dtype=torch.int32).cuda())
+        T.kv_append(p.gpu, 0, x[:, :1], x[:, 1:], off, tokens)
+        p.ref.extend(count)
+        h = kv.double().numpy()[None]
+        p.ref.append(h[:, :, :1], h[:, :, 1:], [0] * S)
+    p.fork([-1] + [0] * copies)
+    return p
+
+
+BIG, SMALL = 2.0 ** 77, 2.0 ** -80
+
+
+@pytest.mark.parametrize("n", [1, 20, 70])
+@pytest.mark.parametrize("blocks", [
+    [(64, 0.0, 0.0), (64, 0.0, BIG), (20, 0.0, 1.0)],
+    [(64, 0.0, BIG), (64, 3.0, 0.0), (20, 0.0, 1.0)],
+    [(64, -3.0, 0.0), (64, 0.0, 2.0 ** 45), (20, 0.0, 1.0)],
+    [(64, 0.0, 2.0 ** 45), (64, -3.0, 0.0), (20, 0.0, 1.0)],
+    [(64, 0.0, SMALL), (64, 0.0, BIG), (20, 0.0, SMALL)],
+    [(64, 0.0, BIG), (64, 2.0, SMALL), (20, 1.0, SMALL)],
+    [(64, -10.0, SMALL), (64, -6.0, 0.0), (64, -3.0, 1.0), (64, 0.0, BIG), (20, -3.0, 0.0)],
+    [(64, 0.0, BIG), (64, 3.0, 1.0), (64, 6.0, 0.0), (64, 10.0, SMALL), (20, 6.0, 0.0)],
+    [(64, 0.0, 2.0 ** 35), (20, 0.0, 0.0)],
+    [(64, 0.0, BIG), (20, -5.0, 0.0)],
+    [(64, 0.0, 0.0), (64, -4.0, SMALL), (20, 0.0, BIG)],
+    [(64, 0.0, 0.0), (20, 1.0, 0.0)],
+    [(64, 100.0, SMALL), (64, 0.0, BIG), (20, 50.0, 1.0)],
+])
+def test_kv_attend_weighs_blocks_whatever_their_values(blocks, n):
+    """Zero, tiny and huge values beside each other, in pages and in the open block, in either order and at
+    different scores: each token has the weight of its score.  Every block four times over, so that
+    a wave meets them one after the other; in one share, and split."""
+    print(f"{blocks} n {n}", flush=True)
+    copies = 2 if n == 1 else 0   # (rows few enough for copies to share a tile)
+    p = levels_cache([b for b in blocks[:-1] for _ in range(4)] + blocks[-1:], n, copies)
+    total = n * (1 + copies)
+    q, off = torch.ones(total, 1, 64, dtype=BF, device="cuda"), torch.arange(2 + copies).cuda() * n
+    want = p.ref.attend(0, 0, np.ones((n, 1, 64)), False)
+    for max_len in (0, 64 * 20):
+        p.gpu.max_len = max_len
+        lse = torch.empty(total, 1, device="cuda")
+        out = T.kv_attend(p.gpu, 0, q, off, n, flags=T.MASK_NONE, lse=lse)
+        for s in range(0, total, n):
+            check(out[s:s + n], lse[s:s + n], want, 64, HALF, p.ref.len[0], p.vmax(0, 0))
