@@ -401,7 +401,8 @@ typedef struct tav2_kv {
   int32_t kv_heads;    /* >= 1 */
   int32_t head_dim;    /* 32, 64 or 128 */
   int32_t max_len;     /* host-side estimate of the longest sequence: tav2_kv_attend divides
-                          its work by it (results do not depend on it) */
+                          its work by it (another estimate changes a result as another order of
+                          its sums does, no more) */
   int32_t reserved;    /* set to 0 */
 } tav2_kv;
 

@@ -9,9 +9,10 @@
 // halves' maxima.
 //
 // The softmax's reference m is raised only where a weight would pass 2^RAISE, and then to where the
-// largest is 2^ROOM: any reference gives the same quotient, the sums are fp32, and raising it is rare
-// after a query's first keys.  The room is for weights in fp16, whose least step is 2^-24: 2^-30 of
-// the largest weight.
+// largest is at least 2^ROOM: any reference gives the same quotient, the sums are fp32, and raising it is
+// rare after a query's first keys.  The room is for weights in fp16, whose least step is 2^-24: 2^-30 of
+// the largest weight.  References are whole numbers and each query's are its own scores' alone, so that a
+// weight's rounding to 16 bits depends neither on where its reference stands nor on the wave's other queries.
 //
 // Values may come with a scale 2^lv of their own for each block of keys.  What is multiplied is then a weight
 // times 2^lv, against m; the weights' sum l has a reference of its own, n, since scales lie further apart
@@ -132,7 +133,7 @@ __device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16 (
                                             bool masked, const AttSeen<QT>& seen, int key0) {
   const float top = att_mask(s, q, masked, seen, key0) * c;
   if (__any(top > st.m[q] + RAISE)) {
-    const float m = top - ROOM > st.m[q] ? top - ROOM : st.m[q];
+    const float m = top > st.m[q] + RAISE ? __builtin_floorf(top) - ROOM : st.m[q];
     const float f = __builtin_amdgcn_exp2f(st.m[q] - m);
     st.m[q] = m;
     st.l[q] *= f;
@@ -147,9 +148,8 @@ __device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16 (
 // Where a block's largest score `top` passes the references, those that it does not: m, n and d, and the factors
 // of the features and of the sum so far.
 __device__ __forceinline__ void att_raise(float top, float lv, float& m, float& n, float& d, float* of, float* lf) {
-  const float over = top + lv;
-  const float m1 = over - ROOM > m ? over - ROOM : m;
-  const float n1 = top - ROOM > n ? top - ROOM : n;
+  const float m1 = top + (lv - m) > RAISE ? __builtin_floorf(top + lv) - ROOM : m;
+  const float n1 = top - n > RAISE ? __builtin_floorf(top) - ROOM : n;
   *of = __builtin_amdgcn_exp2f(m - m1);
   *lf = __builtin_amdgcn_exp2f(n - n1);
   d = __builtin_amdgcn_exp2f(m1 - n1);

@@ -905,3 +905,81 @@ def test_kv_attend_weighs_blocks_whatever_their_values(blocks, n):
         out = T.kv_attend(p.gpu, 0, q, off, n, flags=T.MASK_NONE, lse=lse)
         for s in range(0, total, n):
             check(out[s:s + n], lse[s:s + n], want, 64, HALF, p.ref.len[0], p.vmax(0, 0))
+
+
+# ------------------------------------------------------------------------- what a row's bits depend on
+@pytest.mark.parametrize("lens,H,D,dtype,window", [
+    ([300], 2, 64, BF, 0), ([300], 2, 128, BF, 100), ([300], 4, 32, BF, 0), ([200], 2, 64, F32, 0),
+    ([130, 64, 200] * 70, 4, 64, BF, 0), ([70] * 400, 2, 128, BF, 0)])
+def test_attend_window_rows_do_not_depend_on_their_neighbours(lens, H, D, dtype, window):
+    """Other rows' queries, whose larger scores move their own references, leave a row's bits alone."""
+    g = torch.Generator().manual_seed(71)
+    total = sum(lens)
+    q, k, v = (rows(g, total, H, D, dtype) for _ in range(3))
+    k = (k.float() * torch.linspace(0.2, 3.0, total).view(-1, 1, 1).cuda()).to(dtype)
+    off = torch.tensor(np.concatenate([[0], np.cumsum(lens)])[:-1].astype(np.int64)).cuda()
+    length = torch.tensor(lens, dtype=torch.int32).cuda()
+    mine = torch.arange(total).cuda() % 3 == 1
+    got = []
+    for others in (1.0, 40.0):
+        qq = torch.where(mine[:, None, None], q, (q.float() * others).to(dtype))
+        lse = torch.empty(total, H, device="cuda")
+        got.append((T.attend_window(qq, k, v, off, length, max(lens), window=window, lse=lse), lse))
+    (a, la), (b, lb) = got
+    assert torch.equal(a[mine], b[mine]) and torch.equal(la[mine], lb[mine])
+
+
+@pytest.mark.parametrize("n,D", [(10, 64), (10, 128), (40, 32), (40, 64), (40, 128), (700, 64)])
+def test_kv_attend_rows_do_not_depend_on_their_neighbours(n, D):
+    g = torch.Generator().manual_seed(72)
+    p = Pair(seqs=1, pages=300, blocks=300, H=1, D=D, seed=73)
+    for spread in (0.2, 0.6, 1.0, 1.5, 2.0):   # later tokens score higher
+        p.grow([1000], spread)
+    p.grow([3])
+    q = rows(g, n, 1, D)
+    mine = torch.arange(n).cuda() % 3 == 1
+    got = []
+    for others in (1.0, 40.0):
+        qq = torch.where(mine[:, None, None], q, (q.float() * others).to(BF))
+        for max_len in (0, 5003):
+            p.gpu.max_len = max_len
+            lse = torch.empty(n, 1, device="cuda")
+            got.append((T.kv_attend(p.gpu, 0, qq, torch.tensor([0, n]).cuda(), n, lse=lse,
+                                    flags=T.MASK_NONE), lse))
+    for (a, la), (b, lb) in zip(got[:2], got[2:]):
+        assert torch.equal(a[mine], b[mine]) and torch.equal(la[mine], lb[mine])
+
+
+@pytest.mark.parametrize("n,heads", [(1, 1), (5, 2), (20, 1), (70, 1), (200, 2)])
+def test_kv_attend_weights_round_alike_however_the_work_is_divided(n, heads):
+    """A weight is rounded to fp16 against a power of two, so that estimates of the length, by which the pages
+    are divided and the references begin, leave its rounding alone.  Scores here are whole eighths of a
+    power of two and codes are small, so that the weights are known: fp16 of 2^(j/8), their sum not
+    rounded.  fp32's sums of 1000 terms move that quotient by at most 2^-17 of the values' size, and rounding
+    to bf16 keeps the order of numbers: an output lies between the roundings of the quotient's bounds."""
+    D, L = 64, 1000
+    g = np.random.default_rng(n)
+    k, v = np.zeros((L, 1, D)), g.integers(-3, 4, size=(L, 1, D)).astype(float)
+    j = g.integers(0, 40, size=L)
+    k[:, 0, 0], k[::P, 0, 1], v[::P, 0, D - 1] = j / 4.0, 127 / 4.0, 127.0    # key scale 1/4, value scale 1
+    c = new_cache(1, L // P, L // P, 1, D)
+    off = torch.zeros(1, dtype=torch.int64).cuda()
+    kv = torch.from_numpy(np.concatenate([k, v], 1)).to(BF).cuda()
+    T.kv_extend(c, torch.tensor([L], dtype=torch.int32).cuda())
+    T.kv_append(c, 0, kv[:, :1], kv[:, 1:], off, L)
+    q = torch.zeros(n, heads, D, dtype=BF, device="cuda")
+    q[:, :, 0] = torch.tensor([1.0, 0.5]).cuda()[torch.arange(n).cuda() % 2][:, None]
+    for max_len in (0, 300, 520, 1000, 10 ** 6):
+        c.max_len = max_len
+        out = T.kv_attend(c, 0, q, torch.tensor([0, n]).cuda(), n, flags=T.MASK_NONE, scale=float(np.log(2.0)))
+        for half in range(min(n, 2)):
+            w = 2.0 ** ((j / 8.0) if half else (j / 4.0))
+            mant, e = np.frexp(w)
+            hw = np.ldexp(mant.astype(np.float16).astype(float), e)
+            want = hw @ v[:, 0] / w.sum()
+            size = hw @ np.abs(v[:, 0]) / w.sum()
+            lo, hi = (torch.from_numpy(x).to(BF).double().numpy() for x in (want - 2.0 ** -17 * size,
+                                                                            want + 2.0 ** -17 * size))
+            got = out[half::2].double().cpu().numpy()
+            bad = (got < lo) | (got > hi)
+            assert not bad.any(), (max_len, half, int(bad.sum()), got.size)
