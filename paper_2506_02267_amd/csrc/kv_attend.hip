@@ -120,14 +120,18 @@ __device__ __forceinline__ float max8(const u32x4& x, float m) {
                        __builtin_fabsf(__uint_as_float(x[e] & 0xFFFF0000u))));
   return m;
 }
-// The power of two that takes top into [2^14, 2^15), as a factor and back (tops below 2^-86 like
-// 2^-86: both stay normal numbers).
+// The power of two that takes top into [2^TO, 2^(TO + 1)), as a factor and back (tops below 2^-86 like
+// 2^-86: both stay normal numbers).  Queries and keys go as high as fp16 has room for, the open block's values to
+// where codes are: next to a page's products theirs then begin as high, and their small weights keep as
+// many bits.
+template <int TO>
 __device__ __forceinline__ void into_half(float top, float* f, float* back) {
   uint32_t ex = __float_as_uint(top) >> 23;
   ex = ex < 41 ? 41 : ex > 254 ? 254 : ex;
-  *f = __uint_as_float((268 - ex) << 23);
-  *back = __uint_as_float((ex - 14) << 23);
+  *f = __uint_as_float((254 + TO - ex) << 23);
+  *back = __uint_as_float((ex - TO) << 23);
 }
+constexpr int TO_TOP = 14, TO_CODES = 6;
 
 // The scale of an open block's values; of zeros none.
 __device__ __forceinline__ AttScale tail_scale(float top, float back, float f) {
@@ -313,7 +317,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
     for (int t = 0; t < D / 16; ++t) w[t] = *reinterpret_cast<const u32x4*>(p + 8 * t);
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) top = max8(w[t], top);
-    into_half(xmax32(top), &f, &back);
+    into_half<TO_TOP>(xmax32(top), &f, &back);
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) qf[q][t] = scaled8h(w[t], f);
     cq[q] = a.scale * LOG2E * back;
@@ -427,9 +431,9 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
         kt = fmaxf(kt, __shfl_xor(kt, o, WAVE));
         vt = fmaxf(vt, __shfl_xor(vt, o, WAVE));
       }
-      into_half(kt, &f, &back);
+      into_half<TO_TOP>(kt, &f, &back);
       float fv, backv;
-      into_half(vt, &fv, &backv);
+      into_half<TO_CODES>(vt, &fv, &backv);
 #pragma unroll
       for (int q = 0; q < QT; ++q) cs[q] = score_factor(cq[q], back);
       auto keys = [&](int, f16x8(&kf)[D / 16]) {
@@ -617,7 +621,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
     for (int t = 0; t < NK; ++t) w[t] = *reinterpret_cast<const u32x4*>(p + 8 * t);
 #pragma unroll
     for (int t = 0; t < NK; ++t) top = max8(w[t], top);
-    into_half(xmax32(xmax16(top)), &f, &back);
+    into_half<TO_TOP>(xmax32(xmax16(top)), &f, &back);
 #pragma unroll
     for (int t = 0; t < NK; ++t) qf[t] = scaled8h(w[t], f);
     cq = a.scale * LOG2E * back;
@@ -751,8 +755,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
       kt = fmaxf(kt, __shfl_xor(kt, x, WAVE));
       vt = fmaxf(vt, __shfl_xor(vt, x, WAVE));
     }
-    into_half(kt, &fk, &backk);
-    into_half(vt, &fv, &backv);
+    into_half<TO_TOP>(kt, &fk, &backk);
+    into_half<TO_CODES>(vt, &fv, &backv);
     auto keys = [&](int i, f16x8(&kf)[NK]) {
 #pragma unroll
       for (int t = 0; t < NK; ++t) kf[t] = scaled8h(raw_key(i, t), fk);

@@ -983,3 +983,28 @@ def test_kv_attend_weights_round_alike_however_the_work_is_divided(n, heads):
             got = out[half::2].double().cpu().numpy()
             bad = (got < lo) | (got > hi)
             assert not bad.any(), (max_len, half, int(bad.sum()), got.size)
+
+
+@pytest.mark.parametrize("n", [1, 20, 70])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_kv_attend_small_weights_in_the_open_block(D, n):
+    """63 open tokens of weight 2^-22 beside one token of weight 1 in a page that its wave takes before:
+    in the features that the page lacks they are the whole output."""
+    p = Pair(seqs=1, pages=4, blocks=4, H=1, D=D, seed=5)
+    L = 4 * P + 63
+    kv = torch.zeros(L, 2, D)
+    unit = D ** -0.5   # a key of x unit scores x against ones
+    kv[:4 * P, 0], kv[0, 0], kv[4 * P:, 0] = -40 * unit, 0.0, -15.5 * unit
+    kv[0, 1, 0], kv[4 * P:, 1, 1:] = 1.0, 1.0
+    kv = kv.to(BF)
+    T.kv_extend(p.gpu, torch.tensor([L], dtype=torch.int32).cuda())
+    x = kv.cuda()
+    T.kv_append(p.gpu, 0, x[:, :1], x[:, 1:], torch.zeros(1, dtype=torch.int64).cuda(), L)
+    p.ref.extend([L])
+    h = kv.double().numpy()[None]
+    p.ref.append(h[:, :, :1], h[:, :, 1:], [0])
+    p.gpu.max_len = 0
+    lse = torch.empty(n, 1, device="cuda")
+    out = T.kv_attend(p.gpu, 0, torch.ones(n, 1, D, dtype=BF, device="cuda"), torch.tensor([0, n]).cuda(),
+                      n, flags=T.MASK_NONE, lse=lse)
+    check(out, lse, p.ref.attend(0, 0, np.ones((n, 1, D)), False), D, HALF, L, 1.0)
