@@ -346,7 +346,7 @@ typedef struct tav2_window {
   const void*    q;            /* device, rows of [heads, head_dim], dtype; values finite */
   const void*    k;            /* device, rows of [kv_heads, head_dim], dtype; values finite */
   const void*    v;            /* device, rows of [kv_heads, head_dim], dtype; values finite,
-                                  magnitudes up to 2^90; scores within fp32's range */
+                                  magnitudes up to 2^90; <q,k> and scores up to 2^125 */
   int64_t q_ld, k_ld, v_ld;    /* elements from a row to the next: at least a row, at most 2^24,
                                   multiples of 8 (bf16) or 4 (fp32) */
   void*          out;          /* device [rows, heads, head_dim], dtype: token i's row i */
@@ -438,7 +438,7 @@ tav2_status tav2_kv_append(const tav2_kv* c, int32_t layer, const void* k, int64
  *     every cached token.
  * window and sinks as for tav2_attend_window, counted from the query's position; blocks that were
  * released (tav2_kv_trim) are not seen.  out and lse as there; a query that sees nothing gets
- * zeros and -inf.  Queries (finite; scores within fp32's range) and outputs are bf16; products take the codes exactly, the scales in fp32.
+ * zeros and -inf.  Queries (finite; scores up to 2^125) and outputs are bf16; products take the codes exactly, the scales in fp32.
  *   ws  device workspace of tav2_kv_attend_workspace() bytes, 256-byte aligned.
  * Errors: those above, TAV2_ERR_WORKSPACE.
  */

@@ -36,7 +36,8 @@ struct AttendArgs {
   int layer;
   tav2_kv_queries q;
   bool causal;
-  float scale;
+  float scale;       // times log2(e), as scale * 2^scale_e, in [1/2, 1)
+  int scale_e;
   bf16_t* out;
   float* lse;        // nullable
   float* part_o;     // [splits, total, heads, D], with splits > 1
@@ -141,10 +142,14 @@ __device__ __forceinline__ AttScale tail_scale(float top, float back, float f) {
 // 2^(x / 2), to be taken twice: a weight of 2^-127 and less may belong to a value as large beside the others.
 __device__ __forceinline__ float half_factor(float x) { return __builtin_amdgcn_exp2f(0.5f * x); }
 
-// A score's factor from the query's and the keys'.  One that fp32 cannot hold (queries of zeros, tiny scales)
-// is no zero, by which a masked -inf would become a NaN: scores are below 2^38, so 2^-126 adds at most
-// 2^-88 to an exponent that is nearer to zero still.
-__device__ __forceinline__ float score_factor(float q, float k) { return fmaxf(q * k, FLT_MIN); }
+// A score's factor: the scale times the keys' (k), and the power of two (e) that takes the query's and the
+// scale's back, apart, since their product alone may leave fp32's range.  One that leaves it with the keys
+// (queries of zeros, tiny scales) is no zero, by which a masked -inf would become a NaN, and not
+// infinite, by which a zero would: scores are below 2^38, so 2^-126 adds at most 2^-88 to an exponent that is
+// nearer to zero still.
+__device__ __forceinline__ float score_factor(float k, int e) {
+  return __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(k, e), FLT_MIN, FLT_MAX);
+}
 
 // A workgroup's share: `cap` query rows of a kv head of a sequence, entries [c0, c1) of their pages.
 struct Job {
@@ -303,7 +308,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
 
   // this lane's queries: operands, and what they see
   f16x8 qf[QT][D / 16];
-  float cq[QT];
+  int cq[QT];   // powers of two
   AttSeen<QT> seen;
   seen.sinks = a.q.sinks;
 #pragma unroll
@@ -320,7 +325,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
     into_half<TO_TOP>(xmax32(top), &f, &back);
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) qf[q][t] = scaled8h(w[t], f);
-    cq[q] = a.scale * LOG2E * back;
+    cq[q] = a.scale_e + __builtin_amdgcn_frexp_expf(back) - 1;
     const int64_t pos = a.causal ? j.first_pos + i : j.first_pos;
     const int64_t end = pos + 1 < len ? pos + 1 : len;
     seen.hi[q] = int(end > 0 ? end : 0);
@@ -355,7 +360,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
     AttScale vs;
     feed.factors(t, &ks, &vs);
 #pragma unroll
-    for (int q = 0; q < QT; ++q) cs[q] = score_factor(cq[q], ks);
+    for (int q = 0; q < QT; ++q) cs[q] = score_factor(a.scale * ks, cq[q]);
     feed.put(my);
     feed.load(a, j, next);
     if (page >= 0) {
@@ -435,7 +440,7 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
       float fv, backv;
       into_half<TO_CODES>(vt, &fv, &backv);
 #pragma unroll
-      for (int q = 0; q < QT; ++q) cs[q] = score_factor(cq[q], back);
+      for (int q = 0; q < QT; ++q) cs[q] = score_factor(a.scale * back, cq[q]);
       auto keys = [&](int, f16x8(&kf)[D / 16]) {
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) kf[t] = scaled8h(raw_key(t), f);
@@ -612,7 +617,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
   all_hi = __builtin_amdgcn_readfirstlane(all_hi);
   all_lo = __builtin_amdgcn_readfirstlane(all_lo);
   f16x8 qf[NK];
-  float cq;
+  int cq;   // a power of two
   {
     const bf16_t* p = static_cast<const bf16_t*>(a.q.q) + qi * a.q.ld + (j.h * j.G + row % j.G) * D + g * F;
     u32x4 w[NK];
@@ -624,7 +629,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
     into_half<TO_TOP>(xmax32(xmax16(top)), &f, &back);
 #pragma unroll
     for (int t = 0; t < NK; ++t) qf[t] = scaled8h(w[t], f);
-    cq = a.scale * LOG2E * back;
+    cq = a.scale_e + __builtin_amdgcn_frexp_expf(back) - 1;
   }
 
   f32x4 o[ND];
@@ -722,7 +727,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
         vf[0] = codes8h(w.x, w.y);
         vf[1] = codes8h(w.z, w.w);
       };
-      step(keys, values, score_factor(cq, ks), vs, b * KVP);
+      step(keys, values, score_factor(a.scale * ks, cq), vs, b * KVP);
     }
     page = next;
   }
@@ -765,7 +770,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(Atten
 #pragma unroll
       for (int t = 0; t < 2; ++t) vf[t] = scaled8h(raw_value(d, t), fv);
     };
-    step(keys, values, score_factor(cq, backk), tail_scale(vt, backv, fv), full * KVP);
+    step(keys, values, score_factor(a.scale * backk, cq), tail_scale(vt, backv, fv), full * KVP);
   };
   if (j.list.at(j.c1 - 1) >= full) {
     const int mine = hi, base = j.s / a.group * a.group;
@@ -923,7 +928,7 @@ hipError_t launch_kv_attend(const tav2_kv& c, int layer, const tav2_kv_queries& 
   a.layer = layer;
   a.q = q;
   a.causal = causal;
-  a.scale = q.scale > 0.f ? q.scale : 1.f / sqrtf(float(c.head_dim));
+  a.scale = frexpf((q.scale > 0.f ? q.scale : 1.f / sqrtf(float(c.head_dim))) * LOG2E, &a.scale_e);
   a.out = static_cast<bf16_t*>(out);
   a.lse = lse;
   const int tile = tile_rows(c, q), rows = q.max_count * (q.heads / c.kv_heads);

@@ -1008,3 +1008,45 @@ def test_kv_attend_small_weights_in_the_open_block(D, n):
     out = T.kv_attend(p.gpu, 0, torch.ones(n, 1, D, dtype=BF, device="cuda"), torch.tensor([0, n]).cuda(),
                       n, flags=T.MASK_NONE, lse=lse)
     check(out, lse, p.ref.attend(0, 0, np.ones((n, 1, D)), False), D, HALF, L, 1.0)
+
+
+@pytest.mark.parametrize("n", [1, 20, 70])
+@pytest.mark.parametrize("scale,queries,keys", [
+    (2.0 ** -90, 2.0 ** -33, 2.0 ** 120), (2.0 ** -120, 1.0, 2.0 ** 117), (2.0 ** 90, 2.0 ** -100, 2.0 ** 6),
+    (2.0 ** 120, 2.0 ** -30, 2.0 ** -93), (2.0 ** -126, 2.0 ** 100, 2.0 ** 24)])
+def test_kv_attend_scores_of_factors_that_lie_far_apart(n, scale, queries, keys):
+    """Scores of ordinary size, whatever the sizes of scale, queries and keys that they come from."""
+    p = Pair(seqs=1, pages=10, blocks=10, H=1, D=64, seed=47)
+    kv = torch.randn(333, 2, 64, generator=p.g)
+    kv[:, 0] *= keys
+    kv = kv.to(BF)
+    x = kv.cuda()
+    T.kv_extend(p.gpu, torch.tensor([333], dtype=torch.int32).cuda())
+    T.kv_append(p.gpu, 0, x[:, :1], x[:, 1:], torch.zeros(1, dtype=torch.int64).cuda(), 333)
+    p.ref.extend([333])
+    h = kv.double().numpy()[None]
+    p.ref.append(h[:, :, :1], h[:, :, 1:], [0])
+    attend_pair(p, [n], 1, True, scale=scale, spread=queries)
+
+
+@pytest.mark.parametrize("n", [1, 20, 70])
+@pytest.mark.parametrize("query,key,scale", [
+    ([2.0 ** 100] + [0.0] * 63, [0.0, 2.0 ** 60] + [0.0] * 62, 1e30),     # at right angles
+    ([2.0 ** -33] * 64, [2.0 ** 126] * 64, 2.0 ** -100)])                # scores of 1/2
+def test_kv_attend_factors_that_fp32_cannot_hold(query, key, scale, n):
+    """The scale and the query's size alone leave fp32's range, above or below; with the keys scores are
+    ordinary."""
+    p = Pair(seqs=1, pages=4, blocks=4, H=1, D=64, seed=48)
+    kv = torch.randn(100, 2, 64, generator=p.g)
+    kv[:, 0] = torch.tensor(key)
+    kv = kv.to(BF)
+    x = kv.cuda()
+    T.kv_extend(p.gpu, torch.tensor([100], dtype=torch.int32).cuda())
+    T.kv_append(p.gpu, 0, x[:, :1], x[:, 1:], torch.zeros(1, dtype=torch.int64).cuda(), 100)
+    p.ref.extend([100])
+    h = kv.double().numpy()[None]
+    p.ref.append(h[:, :, :1], h[:, :, 1:], [0])
+    q = torch.tensor(query).to(BF).repeat(n, 1, 1)
+    lse = torch.empty(n, 1, device="cuda")
+    out = T.kv_attend(p.gpu, 0, q.cuda(), torch.tensor([0, n]).cuda(), n, flags=T.MASK_NONE, scale=scale, lse=lse)
+    check(out, lse, p.ref.attend(0, 0, q.double().numpy(), False, scale=scale), 64, HALF, 100, p.vmax(0, 0))
