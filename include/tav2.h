@@ -444,8 +444,9 @@ tav2_status tav2_kv_append(const tav2_kv* c, int32_t layer, const void* k, int64
  */
 typedef struct tav2_kv_queries {
   const void*    q;            /* device bf16: query i's head h at q + i * ld + h * head_dim */
-  const int64_t* offset;       /* device [num_seqs + 1]; offset[0] = 0, offset[num_seqs] = total */
-  int64_t total;               /* host: number of queries (>= 0) */
+  const int64_t* offset;       /* device [num_seqs + 1], not descending, from 0 to at most total */
+  int64_t total;               /* host: queries there is room for (>= 0); those before offset[0] and
+                                  from offset[num_seqs] on are left as they are in out and lse */
   int64_t ld;                  /* elements between queries, as in tav2_window */
   int32_t max_count;           /* host-side bound of a sequence's queries, at most total */
   int32_t heads;               /* a multiple of kv_heads */

@@ -835,6 +835,8 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(AttendArgs a) {
   __shared__ float lo[NG][D], ll[NG];
   const int64_t at = blockIdx.x, n = a.q.total * a.q.heads;
   const int tid = threadIdx.x, f = tid % D, g = tid / D;
+  // queries of no sequence (their part of the workspace is not written): left as they were
+  const int64_t r0 = a.q.offset[0] * a.q.heads, r1 = a.q.offset[a.c.num_seqs] * a.q.heads;
   float M = -FLT_MAX;
   for (int s = tid % WAVE; s < a.splits; s += WAVE) M = fmaxf(M, a.part_ml[2 * (s * n + at)]);
 #pragma unroll
@@ -859,6 +861,7 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(AttendArgs a) {
     x += lo[j][f];
     l += ll[j];
   }
+  if (at < r0 || at >= r1) return;
   const bool some = l > 0.f || l != l;
   a.out[at * D + f] = f2bf(some ? x / l : 0.f);
   if (a.lse && f == 0) a.lse[at] = some ? (M + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;

@@ -690,7 +690,8 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, offset: torch.Tensor,
               flags: int = MASK_CAUSAL, window: int = 0, sinks: int = 0, scale: float = 0.0,
               ws: Optional[Workspace] = None, stream=None) -> torch.Tensor:
     """tav2_kv_attend: queries q (bf16 [total, heads, head_dim]) over one layer of the cache; sequence
-    s has the queries offset[s] .. offset[s+1] (int64 [seqs + 1]), at most max_count.
+    s has the queries offset[s] .. offset[s+1] (int64 [seqs + 1]), at most max_count; rows of no
+    sequence (a padded batch) are left as they are.
     MASK_CAUSAL: its last tokens; MASK_NONE: candidates to follow it."""
     ld = _heads("q", q, torch.bfloat16)
     total, heads, D = q.shape

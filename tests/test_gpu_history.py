@@ -1050,3 +1050,32 @@ def test_kv_attend_factors_that_fp32_cannot_hold(query, key, scale, n):
     lse = torch.empty(n, 1, device="cuda")
     out = T.kv_attend(p.gpu, 0, q.cuda(), torch.tensor([0, n]).cuda(), n, flags=T.MASK_NONE, scale=scale, lse=lse)
     check(out, lse, p.ref.attend(0, 0, q.double().numpy(), False, scale=scale), 64, HALF, 100, p.vmax(0, 0))
+
+
+@pytest.mark.parametrize("n", [1, 3, 20, 70])
+def test_kv_attend_leaves_the_rows_of_no_sequence(n):
+    """A padded batch: rows before the first sequence's and behind the last one's stay as they were, with
+    the pages split over workgroups and not."""
+    p = Pair(seqs=3, pages=60, blocks=60, H=1, D=64, seed=49)
+    p.grow([1500, 64, 130])
+    g = torch.Generator().manual_seed(50)
+    for before, behind in ((0, 5), (2, 9)):
+        counts = [n, 0, n]
+        off = np.concatenate([[0], np.cumsum(counts)]) + before
+        total = int(off[-1]) + behind
+        q = rows(g, total, 2, 64)
+        for max_len in (0, 2000):
+            p.gpu.max_len = max_len
+            out = torch.full((total, 2, 64), 9.0, dtype=BF, device="cuda")
+            lse = torch.full((total, 2), 9.0, device="cuda")
+            ws = T.Workspace()
+            ws.get(1 << 20)
+            ws.buf.fill_(255)      # (NaN)
+            T.kv_attend(p.gpu, 0, q, torch.from_numpy(off).cuda(), n, out=out, lse=lse,
+                        flags=T.MASK_NONE, ws=ws)
+            for s in (0, 2):
+                sl = slice(int(off[s]), int(off[s + 1]))
+                want = p.ref.attend(s, 0, q[sl].double().cpu().numpy(), False)
+                check(out[sl], lse[sl], want, 64, HALF, 1500, p.vmax(s, 0))
+            for x in (out, lse):
+                assert (x[:before] == 9.0).all() and (x[int(off[-1]):] == 9.0).all()
