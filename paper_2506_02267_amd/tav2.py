@@ -341,17 +341,27 @@ class DeviceWeights:
 
 
 class Workspace:
-    """A reusable, 256-byte-aligned device buffer (allocated outside the hot path)."""
+    """A reusable, 256-byte-aligned device buffer (allocated outside the hot path), grown to the largest
+    call's need.  For calls that follow one another: those that may run at the same time, graphs' replays
+    among them, need workspaces of their own."""
 
     def __init__(self, device="cuda"):
         self.device = device
+        self.gpu = torch.device(device).type == "cuda"
         self.buf: Optional[torch.Tensor] = None
+        self.captured = False                # the buffer's address is part of a graph
+        self.kept: List[torch.Tensor] = []   # outgrown buffers that graphs still write to
 
     def get(self, nbytes: int):
         if nbytes == 0:
             return None, 0
         if self.buf is None or self.buf.numel() < nbytes + 256:
+            if self.captured:
+                self.kept.append(self.buf)
+                self.captured = False
             self.buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        if self.gpu and not self.captured:
+            self.captured = torch.cuda.is_current_stream_capturing()
         p = self.buf.data_ptr()
         off = (-p) % 256
         return ctypes.c_void_p(p + off), self.buf.numel() - off

@@ -1079,3 +1079,28 @@ def test_kv_attend_leaves_the_rows_of_no_sequence(n):
                 check(out[sl], lse[sl], want, 64, HALF, 1500, p.vmax(s, 0))
             for x in (out, lse):
                 assert (x[:before] == 9.0).all() and (x[int(off[-1]):] == 9.0).all()
+
+
+def test_workspace_that_grows_after_a_capture():
+    """A captured call's workspace stays its own when a larger call takes the same Workspace afterwards."""
+    p = Pair(seqs=1, pages=40, blocks=40, H=1, D=64, seed=51)
+    p.grow([2000])
+    g = torch.Generator().manual_seed(52)
+    q, big = rows(g, 1, 2, 64), rows(g, 90, 2, 64)
+    off, off_big = torch.tensor([0, 1]).cuda(), torch.tensor([0, 90]).cuda()
+    want = T.kv_attend(p.gpu, 0, q, off, 1, flags=T.MASK_NONE)
+    ws, out = T.Workspace(), torch.empty_like(q)
+    T.kv_attend(p.gpu, 0, q, off, 1, out=out, flags=T.MASK_NONE, ws=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        T.kv_attend(p.gpu, 0, q, off, 1, out=out, flags=T.MASK_NONE, ws=ws)
+    small = ws.buf.numel()
+    T.kv_attend(p.gpu, 0, big, off_big, 90, flags=T.MASK_NONE, ws=ws)
+    assert ws.buf.numel() > small
+    other = [torch.full((small,), 77, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all((x == 77).all() for x in other)

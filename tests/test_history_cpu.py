@@ -5,6 +5,7 @@ import ctypes
 import math
 import os
 import subprocess
+import weakref
 from fractions import Fraction
 from types import SimpleNamespace
 
@@ -255,6 +256,24 @@ def test_append_refuses_fewer_values_than_keys():
 def test_binding_refuses_a_stream_of_another_device():
     with pytest.raises(ValueError, match="stream"):
         T._run("tav2_kv_trim", 0, SimpleNamespace(device_index=1, cuda_stream=0), ())
+
+
+def test_workspace_keeps_what_a_graph_writes_to(monkeypatch):
+    """A buffer used in a capture outlives the workspace's growth: replays write to its address.  Others
+    are given back."""
+    ws = T.Workspace("cpu")
+    ws.gpu, capturing = True, [False]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    ws.get(1000)
+    first = weakref.ref(ws.buf)
+    capturing[0] = True
+    ws.get(500)
+    capturing[0] = False
+    ws.get(800)
+    ws.get(5000)
+    second = weakref.ref(ws.buf)
+    ws.get(50000)
+    assert first() is not None and second() is None and ws.buf.numel() >= 50000
 
 
 def test_cache_refuses_buffers_that_do_not_fit_together():
