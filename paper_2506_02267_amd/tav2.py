@@ -554,6 +554,19 @@ def _dense(name: str, x: Optional[torch.Tensor], shape, dtype):
         raise ValueError(f"{name}: expected contiguous {dtype} {list(shape)}")
 
 
+def _whole(**sizes):
+    """Refuse what the C ABI's 32 bits do not hold (ctypes would drop the upper ones)."""
+    for name, n in sizes.items():
+        if not -2 ** 31 <= n < 2 ** 31:
+            raise ValueError(f"{name}: {n} is past 32 bits")
+
+
+def _scale(scale: float) -> float:
+    if scale != 0 and ctypes.c_float(scale).value == 0:
+        raise ValueError(f"scale: {scale} is 0 in fp32, which stands for 1 / sqrt(head_dim)")
+    return scale
+
+
 def _run(fn: str, device: int, stream: Optional[torch.cuda.Stream], args, *used, keep=()):
     """Call entry point `fn` with `args` and the stream (by default the current one of that device)
     on GPU number `device`, whichever device is current; `used`: the tensors it takes, `keep`:
@@ -584,6 +597,7 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offset: tor
     q [rows, heads, head_dim], k and v [rows, kv_heads, head_dim], bf16 or fp32, may be slices of
     one projection; offset int64 [R], length int32 [R].  window 0: none; the first `sinks` tokens
     stay visible.  lse (optional, fp32 [rows, heads]) receives the log of the sums."""
+    _whole(max_len=max_len, window=window, sinks=sinks)
     dt = torch.float32 if q.dtype == torch.float32 else torch.bfloat16
     lds = _heads("q", q, dt), _heads("k", k, dt), _heads("v", v, dt)
     rows, heads, D = q.shape
@@ -599,7 +613,7 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offset: tor
     a = Window(q.data_ptr(), k.data_ptr(), v.data_ptr(), *lds, out.data_ptr(),
                None if lse is None else lse.data_ptr(), offset.data_ptr(), length.data_ptr(), R,
                max_len if rows else 0, heads, k.shape[1], D, F32 if dt == torch.float32 else BF16, window, sinks,
-               scale, 0)
+               _scale(scale), 0)
     _run("tav2_attend_window", q.get_device(), stream, (ctypes.byref(a),), q, k, v, offset, length,
          out, lse)
     return out
@@ -631,6 +645,7 @@ class KvCache:
             _dense(name, x, shape, dt)
             if x.device != k.device:
                 raise ValueError(f"{name}: on {x.device}, k on {k.device}")
+        _whole(max_len=max_len)
         self.device, self.index = k.device, k.get_device()
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.k_tail, self.v_tail, self.table = k_tail, v_tail, table
@@ -667,6 +682,7 @@ class KvCache:
 
     @max_len.setter
     def max_len(self, n: int):
+        _whole(max_len=n)
         self.s.max_len = n
 
 
@@ -683,6 +699,7 @@ def kv_append(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, offs
     """tav2_kv_append: one layer's keys and values (bf16 [rows, kv_heads, head_dim], possibly slices
     of one projection) of the tokens that the last kv_extend granted; sequence s's begin at row
     offset[s] (int64 [seqs] or longer)."""
+    _whole(layer=layer, max_count=max_count)
     k_ld, v_ld = _heads("k", k, torch.bfloat16), _heads("v", v, torch.bfloat16)
     if k.shape[1:] != cache.row or v.shape != k.shape:
         raise ValueError("k, v: expected [rows, kv_heads, head_dim] of the cache's sizes, as many of "
@@ -703,6 +720,7 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, offset: torch.Tensor,
     s has the queries offset[s] .. offset[s+1] (int64 [seqs + 1]), at most max_count; rows of no
     sequence (a padded batch) are left as they are.
     MASK_CAUSAL: its last tokens; MASK_NONE: candidates to follow it."""
+    _whole(layer=layer, max_count=max_count, window=window, sinks=sinks, flags=flags)
     ld = _heads("q", q, torch.bfloat16)
     total, heads, D = q.shape
     if D != cache.s.head_dim:
@@ -713,7 +731,7 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, offset: torch.Tensor,
     _dense("out", out, (total, heads, D), torch.bfloat16)
     _dense("lse", lse, (total, heads), torch.float32)
     a = ctypes.byref(KvQueries(q.data_ptr(), offset.data_ptr(), total, ld, max_count, heads, window,
-                               sinks, scale, 0))
+                               sinks, _scale(scale), 0))
     ws = ws or Workspace(q.device)
     wp, wb = ws.get(load_library().tav2_kv_attend_workspace(cache.ref, a))
     _run("tav2_kv_attend", cache.index, stream,
@@ -741,6 +759,7 @@ def kv_free(cache: KvCache, drop: torch.Tensor, stream=None):
 def kv_trim(cache: KvCache, window: int, sinks: int = 0, stream=None):
     """tav2_kv_trim: every sequence gives up the pages that this window and these sinks no longer
     see."""
+    _whole(window=window, sinks=sinks)
     _run("tav2_kv_trim", cache.index, stream, (cache.ref, window, sinks), keep=cache.buffers)
 
 

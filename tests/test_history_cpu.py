@@ -258,6 +258,32 @@ def test_binding_refuses_a_stream_of_another_device():
         T._run("tav2_kv_trim", 0, SimpleNamespace(device_index=1, cuda_stream=0), ())
 
 
+def test_binding_refuses_numbers_that_the_abi_does_not_hold(monkeypatch):
+    """A window of 2^32 + 5 would be one of 5, sinks of 2^32 none, a scale of 1e-50 the default one."""
+    c = host_cache()
+    bf, i64, i32 = torch.zeros(5, 2, 32, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int64), torch.zeros(
+        3, dtype=torch.int32)
+    monkeypatch.setattr(T, "_run", lambda *a, **k: None)
+    calls = {"window": lambda **k: T.attend_window(bf, bf, bf, i64, i32, **{"max_len": 5, **k}),
+             "append": lambda **k: T.kv_append(c, **{"layer": 0, "k": bf, "v": bf, "offset": i64, "max_count": 5, **k}),
+             "attend": lambda **k: T.kv_attend(c, **{"layer": 0, "q": bf, "offset": i64, "max_count": 5, **k}),
+             "trim": lambda **k: T.kv_trim(c, **{"window": 5, **k}),
+             "max_len": lambda max_len: setattr(c, "max_len", max_len)}
+    for name, what in (("window", ("max_len", "window", "sinks")), ("append", ("layer", "max_count")),
+                       ("attend", ("layer", "max_count", "window", "sinks")), ("trim", ("window", "sinks")),
+                       ("max_len", ("max_len",))):
+        for key in what:
+            calls[name](**{key: 2 ** 31 - 1 if key != "max_count" else 5})
+            for bad in (2 ** 32 + 5, 2 ** 32, 2 ** 31, -2 ** 31 - 1):
+                with pytest.raises(ValueError, match="32 bits"):
+                    calls[name](**{key: bad})
+    for name in ("window", "attend"):
+        calls[name](scale=1e-44)
+        for bad in (1e-50, -1e-60):
+            with pytest.raises(ValueError, match="scale"):
+                calls[name](scale=bad)
+
+
 def test_workspace_keeps_what_a_graph_writes_to(monkeypatch):
     """A buffer used in a capture outlives the workspace's growth: replays write to its address.  Others
     are given back."""
