@@ -1104,3 +1104,89 @@ def test_workspace_that_grows_after_a_capture():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and all((x == 77).all() for x in other)
+
+
+# ------------------------------------------------------------------------- kernels that large batches take
+# (tokens of the longer sequences, heads, kv_heads, D, window, sinks); 200 sequences, so that there are more
+# workgroups than the kernel with eight waves takes (768)
+@pytest.mark.parametrize("long,H,Hkv,D,window,sinks", [
+    ([700, 1000], 4, 4, 32, 0, 0), ([700, 1000], 8, 4, 32, 100, 3), ([700, 1000], 4, 4, 64, 0, 0),
+    ([513, 900], 8, 4, 64, 65, 70), ([700, 1000], 4, 4, 128, 0, 0), ([700, 899], 6, 3, 128, 200, 5)])
+def test_attend_window_large_batches(long, H, Hkv, D, window, sinks):
+    """Many short ragged sequences, empty ones among them, and some of several tiles."""
+    print(f"{long} heads {H}/{Hkv} D {D} window {window} sinks {sinks}", flush=True)
+    g = np.random.default_rng(D + window)
+    lens = [int(x) for x in g.integers(1, 131, size=200)]
+    for i in range(0, 200, 37):
+        lens[i] = 0
+    lens[5], lens[120] = long
+    assert len(lens) * Hkv * -(-max(lens) * (H // Hkv) // 128) > 768
+    gt = torch.Generator().manual_seed(D)
+    total = sum(lens)
+    q, k, v = (rows(gt, total, h, D) for h in (H, Hkv, Hkv))
+    off = np.concatenate([[0], np.cumsum(lens)])
+    lse = torch.full((total, H), 7.0, device="cuda")
+    out = T.attend_window(q, k, v, torch.from_numpy(off[:-1].astype(np.int64)).cuda(),
+                          torch.tensor(lens, dtype=torch.int32).cuda(), max(lens), window=window, sinks=sinks, lse=lse)
+    host = [x.double().cpu().numpy() for x in (q, k, v)]
+    for a, L in zip(off, lens):
+        sl = slice(int(a), int(a) + L)
+        check(out[sl], lse[sl], history.window_attention(*(x[sl] for x in host), window, sinks), D, BF, max(L, 1))
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("seqs", [96, 97])
+def test_attend_window_either_side_of_the_split(seqs, D):
+    """768 workgroups, the most that take eight waves, and the next number: the same bits but for the order in
+    which halves are joined."""
+    H, L = 8, 100
+    g = torch.Generator().manual_seed(seqs)
+    q, k, v = (rows(g, seqs * L, H, D) for _ in range(3))
+    lse = torch.empty(seqs * L, H, device="cuda")
+    out = T.attend_window(q, k, v, torch.arange(seqs).cuda() * L,
+                          torch.full((seqs,), L, dtype=torch.int32).cuda(), L, window=40, sinks=2, lse=lse)
+    for s in (0, 1, seqs // 2, seqs - 1):
+        sl = slice(s * L, s * L + L)
+        want = history.window_attention(*(x[sl].double().cpu().numpy() for x in (q, k, v)), 40, 2)
+        check(out[sl], lse[sl], want, D, BF, L)
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("n", [1, 20, 70])
+def test_kv_attend_shares_of_many_pages(n, D):
+    """An estimate far too small: shares of hundreds of pages, whose numbers a wave looks up 64 at a time."""
+    L = 40003
+    p = Pair(seqs=2, pages=L // P, blocks=L // P, H=1, D=D, seed=n)
+    g = torch.Generator().manual_seed(n)
+    kv = rows(g, L, 2, D)
+    T.kv_extend(p.gpu, torch.tensor([L, 0], dtype=torch.int32).cuda())
+    T.kv_append(p.gpu, 0, kv[:, :1], kv[:, 1:], torch.zeros(2, dtype=torch.int64).cuda(), L)
+    T.kv_fork(p.gpu, torch.tensor([-1, 0], dtype=torch.int32).cuda())
+    p.ref.extend([L, 0])
+    h = kv.double().cpu().numpy()
+    p.ref.k[0], p.ref.v[0] = [h[i:i + 1, :1] for i in range(L)], [h[i:i + 1, 1:] for i in range(L)]
+    p.ref.fork([-1, 0])
+    q = rows(g, 2 * n, 1, D)
+    q[n:] = q[:n]
+    want = p.ref.attend(0, 0, q[:n].double().cpu().numpy(), False, 30000, 9000)
+    bits = []
+    for max_len in (0, 1, 10 ** 6):
+        p.gpu.max_len = max_len
+        lse = torch.empty(2 * n, 1, device="cuda")
+        out = T.kv_attend(p.gpu, 0, q, torch.tensor([0, n, 2 * n]).cuda(), n, flags=T.MASK_NONE, window=30000,
+                          sinks=9000, lse=lse)
+        for s in (0, n):
+            check(out[s:s + n], lse[s:s + n], want, D, HALF, L, p.vmax(0, 0))
+        bits.append(out)
+    assert torch.equal(bits[0], bits[1]) and torch.equal(bits[0][:n], bits[0][n:])
+
+
+@pytest.mark.parametrize("n", [1, 16, 17, 33, 65, 700, 1300])
+@pytest.mark.parametrize("D", [32, 128])
+def test_kv_attend_every_tile_size_and_width(n, D):
+    """As test_kv_attend_every_tile_size, for the other widths, and sizes at which 64 rows a workgroup are
+    taken where there are such kernels."""
+    p = Pair(seqs=3, pages=1200, blocks=400, H=2, D=D, seed=n)
+    p.grow([16400, 200, 0])
+    attend_pair(p, [n, min(n, 3), 1], 2, False, seed=n)
+    attend_pair(p, [min(n, 200), min(n, 50), 2], 4, True, 5000, 100, seed=n + 1)
