@@ -876,16 +876,19 @@ int64_t most_pages(const tav2_kv& c, const tav2_kv_queries& q) {
 
 // Query rows of a workgroup: 16, 32, or, where there are pages enough to fill the CUs with tiles of twice
 // the work, 64 (which turn a page's codes into operands once for twice the queries, but start and
-// end later; 64 features at most: registers).  Both sides, us a call, 4 heads of 64, one history
-// of 16384 tokens: 64 candidates 12.9 with 32 rows and 24.5 with 64, 400: 28.1 and 24.8, 500: 24.2 and 25.3,
-// 600 (10240 tiles x pages): 36.7 and 34.7, with 32 features 26.4 and 28.3, 800: 44.6 and 35.8; 8 histories of
-// 4096 - 16384 tokens, 64 candidates each: 25.0 and 27.1, 32 of them: 79 and 66.
+// end later; 64 features at most: registers; with 32 the turning is the smaller part).  By the number of 64-row tiles
+// times pages; us a call with 32 and 64 rows, 4 heads.  64 features: one history of 16384 tokens, 64 candidates
+// (1024) 13.3 and 24.4, 300 (5120) 24.5 and 25.4, 400 (7168) 28.8 and 25.9, 500 (8192) 24.6 and 26.4, 600 (10240)
+// 37.5 and 36.1, 800 (13312) 45.1 and 37.5; 8 histories of 4096 - 16384, 64 candidates each (8192) 25.5 and 28.3,
+// 100 (16384) 38.5 and 37.8, 500 125 and 119; 16 of them, 1000 each, 473 and 407.  32 features: 800 (13312) 32.4 and
+// 30.3, 2000 (32768) 50.3 and 51.6; 8 x 200 (32768) 48.4 and 50.2, 8 x 500 (65536) 88.1 and 90.2; 16 x 1000
+// (262144) 309 and 297.
 int tile_rows(const tav2_kv& c, const tav2_kv_queries& q) {
   const int64_t rows = int64_t(q.max_count) * (q.heads / c.kv_heads);
   if (rows <= 16) return 16;
   const int64_t seqs = std::min<int64_t>(q.total, c.num_seqs);
   const int64_t work = seqs * c.kv_heads * cdiv(rows, 64) * most_pages(c, q);
-  return rows > 32 && c.head_dim <= 64 && work > 10240 ? 64 : 32;
+  return rows > 32 && c.head_dim <= 64 && work > (c.head_dim == 64 ? 9000 : 100000) ? 64 : 32;
 }
 
 // Pages to a workgroup's share: such that there are workgroups enough to fill the CUs and to even out

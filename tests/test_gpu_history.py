@@ -1186,7 +1186,7 @@ def test_kv_attend_shares_of_many_pages(n, D):
 def test_kv_attend_every_tile_size_and_width(n, D):
     """As test_kv_attend_every_tile_size, for the other widths, and sizes at which 64 rows a workgroup are
     taken where there are such kernels."""
-    p = Pair(seqs=3, pages=1200, blocks=400, H=2, D=D, seed=n)
+    p = Pair(seqs=3, pages=1200, blocks=1300, H=2, D=D, seed=n)
     p.grow([16400, 200, 0])
     attend_pair(p, [n, min(n, 3), 1], 2, False, seed=n)
     attend_pair(p, [min(n, 200), min(n, 50), 2], 4, True, 5000, 100, seed=n + 1)
