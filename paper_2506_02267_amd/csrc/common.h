@@ -75,20 +75,6 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, bf16x2_t));
 }
 
-// Eight int8 codes as bf16: at most 8 significant bits, so the upper half of the float is
-// exact.
-__device__ __forceinline__ bf16x8 codes8(uint32_t x, uint32_t y) {
-  uint32_t p[4];
-#pragma unroll
-  for (int j = 0; j < 8; j += 2) {
-    const uint32_t w = j < 4 ? x : y;
-    const uint32_t a = __float_as_uint(float(int8_t((w >> (8 * (j & 3))) & 0xFF)));
-    const uint32_t b = __float_as_uint(float(int8_t((w >> (8 * (j & 3) + 8)) & 0xFF)));
-    p[j / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-  }
-  return as_bf16x8(make_uint4(p[0], p[1], p[2], p[3]));
-}
-
 // Order-preserving 32-bit key of an fp32 score: larger score <=> larger key,
 // -0.0 maps to the key of +0.0.  Key 0 lies below every finite score and -inf.
 __device__ __forceinline__ uint32_t score_key(float s) {

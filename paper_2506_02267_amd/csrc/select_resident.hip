@@ -43,6 +43,19 @@ constexpr int GROUPS = 4;    // groups of a thread's rows
 constexpr int LIST = 2048;   // rows that may be among the k best, at most
 static_assert(NBINS == NT && GROUPS * NT >= TAV2_K_MAX, "one bin per thread; enough groups");
 
+// Eight codes as bf16: at most 8 significant bits, so the upper half of the float is exact.
+__device__ __forceinline__ bf16x8 codes(uint32_t x, uint32_t y) {
+  uint32_t p[4];
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    const uint32_t w = j < 4 ? x : y;
+    const uint32_t a = __float_as_uint(float(int8_t((w >> (8 * (j & 3))) & 0xFF)));
+    const uint32_t b = __float_as_uint(float(int8_t((w >> (8 * (j & 3) + 8)) & 0xFF)));
+    p[j / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  }
+  return as_bf16x8(make_uint4(p[0], p[1], p[2], p[3]));
+}
+
 // The kk best of the workgroup's keys (key[j]: row j NT + thread, 0: none), the kk-th of
 // which lies in [tlo, thi] and is found bit by bit below the bits these have in common:
 // every key above it, placed by counting, then the lowest rows equal to it, in row order.
@@ -214,8 +227,8 @@ __global__ __launch_bounds__(NT) void select_resident_kernel(Args A) {
         t1[i] = y[1];
       }
       if constexpr (I8) {
-        acc[0] = mfma32(cf[kb], codes8(t0[0], t0[1]), acc[0]);
-        acc[1] = mfma32(cf[kb], codes8(t1[0], t1[1]), acc[1]);
+        acc[0] = mfma32(cf[kb], codes(t0[0], t0[1]), acc[0]);
+        acc[1] = mfma32(cf[kb], codes(t1[0], t1[1]), acc[1]);
       } else {
         acc[0] = mfma32(cf[kb], as_bf16x8(make_uint4(t0[0], t0[1], t0[2], t0[3])), acc[0]);
         acc[1] = mfma32(cf[kb], as_bf16x8(make_uint4(t1[0], t1[1], t1[2], t1[3])), acc[1]);
