@@ -337,7 +337,7 @@ tav2_status tav2_select_encode_eq2(const tav2_seq* seq, const tav2_eq2* eq2,
  *     the positions j <= p with window == 0, p - j < window or j < sinks;
  *   out = sum_j softmax(s)_j v_j,g ;  lse = log sum_j exp(s_j)  (natural logarithm).
  * The softmax's statistics and every sum are fp32; bf16: its weights are rounded to bf16 as
- * operands of the matrix product (at most 2^-9 of a weight).
+ * operands of the matrix product (by at most 2^-8 of a weight).
  * q, k and v are rows of heads: token i's head h starts at q + i * q_ld + h * head_dim
  * (elements), so that all three can be slices of one projection's output.  Sequence r owns rows
  * [offset[r], offset[r] + len[r]); rows of no sequence are neither read nor written.
@@ -412,7 +412,9 @@ typedef struct tav2_kv {
  * that would pass max_blocks is not extended; from the first one that the free pages do not
  * suffice for on, none is.  fresh[s] says what was granted (count[s] or 0).  The tokens' keys and values
  * are written afterwards, layer by layer, by tav2_kv_append; until then the sequence is not to be
- * forked, trimmed or attended to in the layers that lack them.
+ * forked, trimmed or attended to in the layers that lack them.  The tokens of a sequence that was not
+ * extended are not there: a tav2_kv_attend with TAV2_MASK_CAUSAL takes the sequence's last tokens for
+ * theirs, and its rows for them mean nothing.
  * Errors (of all tav2_kv_ calls): TAV2_ERR_NULL, TAV2_ERR_SHAPE, TAV2_ERR_UNSUPPORTED, TAV2_ERR_HIP.
  */
 tav2_status tav2_kv_extend(const tav2_kv* c, const int32_t* count, void* stream);
