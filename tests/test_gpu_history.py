@@ -1190,3 +1190,27 @@ def test_kv_attend_every_tile_size_and_width(n, D):
     p.grow([16400, 200, 0])
     attend_pair(p, [n, min(n, 3), 1], 2, False, seed=n)
     attend_pair(p, [min(n, 200), min(n, 50), 2], 4, True, 5000, 100, seed=n + 1)
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Two captured calls of different sizes on one Workspace, replayed in turn with eager work between."""
+    p = Pair(seqs=2, pages=80, blocks=60, H=2, D=64, seed=53)
+    p.grow([3000, 700])
+    g = torch.Generator().manual_seed(54)
+    qs = [rows(g, 2, 4, 64), rows(g, 80, 4, 64)]
+    offs = [torch.tensor([0, 1, 2]).cuda(), torch.tensor([0, 40, 80]).cuda()]
+    want = [T.kv_attend(p.gpu, 0, q, o, n, flags=T.MASK_NONE) for q, o, n in zip(qs, offs, (1, 40))]
+    outs, ws, graphs = [torch.empty_like(w) for w in want], T.Workspace(), []
+    for i in (0, 1):
+        T.kv_attend(p.gpu, 0, qs[i], offs[i], (1, 40)[i], out=outs[i], flags=T.MASK_NONE, ws=ws)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            T.kv_attend(p.gpu, 0, qs[i], offs[i], (1, 40)[i], out=outs[i], flags=T.MASK_NONE, ws=ws)
+    for step in range(4):
+        for i in ((0, 1), (1, 0))[step % 2]:
+            outs[i].zero_()
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i], want[i]), (step, i)
+        T.kv_trim(p.gpu, 2 ** 31 - 1)
