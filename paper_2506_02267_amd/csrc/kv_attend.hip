@@ -17,7 +17,7 @@
 // One query a sequence is bound by HBM: 64 sequences of 16384 tokens, 8 kv heads, are read at 5.6 TB/s
 // with 64 features and 5.7 with 128 (a large copy: 4.7, read and written).  Many queries are bound by the vector
 // units, which turn codes into fp16 and scores into weights while the matrix units wait, and the
-// reverse: 1000 candidates of one 16384-token history, 4 heads of 64, take 36.7 us, 13 at a large product's rate.
+// reverse: 1000 candidates of one 16384-token history, 4 heads of 64, take 38 us, 13 at a large product's rate.
 #include <algorithm>
 
 #include "attend_core.h"
@@ -49,11 +49,11 @@ struct AttendArgs {
   int group;         // neighbouring sequences whose rows fit one tile together
 };
 
-// Workgroups that a launch is divided into, about (two to a CU).  New actions of 64 users, us: 35.7 with
-// 512, 37.8 with 768, 38.8 with 1024, 47 with 4096; 64 sequences of 8192 tokens each 27.4, 28.9, 28.9, 39.6.
+// Workgroups that a launch is divided into, about (two to a CU).  New actions of 64 users, us: 35.5 with
+// 512, 37.0 with 768, 34.3 with 1024, 44.1 with 4096; 64 sequences of 8192 tokens each 27.5, 28.5, 28.9, 38.0.
 constexpr int SHARES = 512;
-// Pages to a share, at most (a longer one ends later than the rest).  8 copies each of 32 histories, us: 102 with
-// 16, 86 with 32, 79 with 64; 64 sequences of 16384 tokens, 8 heads, 200, 195 and 191.
+// Pages to a share, at most (a longer one ends later than the rest).  8 copies each of 16 histories, us: 102 with
+// 16, 86 with 32, 80 with 64; 64 sequences of 16384 tokens, 8 heads, 200, 195 and 191.
 constexpr int SHARE_MOST = 64;
 
 // The pages that a tile's queries see: [0, sink) and [first, last), counted through.
@@ -196,8 +196,8 @@ __device__ __forceinline__ bool job_of(const AttendArgs& a, int s, int row0, int
 __device__ __forceinline__ bool my_job(const AttendArgs& a, int cap, Job& j) {
   // Units (sequence, head, share) in the order (share, block of sequences, head), each on one XCD
   // (workgroups go to the 8 in turn) with the block's sequences one after the other, since
-  // neighbours may be copies that read the same pages, and so the query tiles of each (8 copies each of 32
-  // histories 79 us, with sequences spread over the XCDs 92).  First shares come first, the later
+  // neighbours may be copies that read the same pages, and so the query tiles of each (8 copies each of 16
+  // histories 79 us, with sequences spread over the XCDs 93).  First shares come first, the later
   // ones, which short sequences lack, at the end.
   const int unit = int(blockIdx.x % unsigned(a.units));
   const int tile = int(blockIdx.x / unsigned(a.units));
@@ -364,9 +364,9 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
     feed.put(my);
     feed.load(a, j, next);
     if (page >= 0) {
-      // Both halves of a page at once where the registers suffice: one look at the reference for 64 keys.  One
-      // history of 16384 tokens, us: 64 candidates 12.9 for 13.8, 200: 17.2 for 17.5, 400: 28.3 for 27.2 (fewer waves
-      // fit), 500: 24.6 for 25.7.
+      // Both halves of a page at once where the registers suffice: one look at the references for 64 keys.  One
+      // history of 16384 tokens, us: 64 candidates 13.3 for 14.0, 200: 17.3 for 17.9, 400: 29.2 for 27.9 (fewer waves
+      // fit), 500: 24.9 for 26.3.
       constexpr int NB = QT == 1 && D <= 64 ? 2 : 1;
 #pragma unroll 1
       for (int u0 = 0; u0 < 2; u0 += NB) {
@@ -398,10 +398,10 @@ __global__ __launch_bounds__(256, 2) void kv_attend_kernel(AttendArgs a) {
     ++t;
     i += 4;
   };
-  // With 64 rows a wave without a page passes once, with page -1: the state then lies in one set of registers,
-  // with no copies to another at each page's end (1000 candidates 36.7 us for 39.0); with 32, whose
-  // state is half of that, such waves go on at once (64 candidates 12.9 us for 13.2).
-  if constexpr (QT > 1) {
+  // With 64 rows of 32 features a wave without a page passes once, with page -1: the state then lies in one set
+  // of registers, with no copies to another at each page's end (16 histories, 1000 candidates each, 295 us for 326).
+  // Elsewhere such waves go on at once (64 features, 1000 candidates of one history 39.0 us for 39.3).
+  if constexpr (QT > 1 && D == 32) {
     do visit(); while (i < j.c1);
   } else {
     while (i < j.c1) visit();
@@ -557,9 +557,9 @@ __device__ __forceinline__ uint32_t shared_set(const AttendArgs& a, const Job& j
 // At most 16 query rows: on the 16x16x32 instructions, a page's 64 keys at once.  S^T comes in four tiles
 // of 16 keys, in the order that makes a lane's 16 scores its quarter's 16 consecutive keys
 // (16 g + 4 i + r in register r of tile i, g = l / 16), again the operand of O^T = V^T P^T as they
-// stand.  Half the vector work of a 32-row tile: new actions of 64 users (4 rows) 35.5 us for 42.2 with
-// that, 8 copies each of 32 histories 79 for 108.  Where rows are few enough, neighbouring sequences share
-// a tile over the pages that they have in common (shared_set): the copies take 91 us without.
+// stand.  Half the vector work of a 32-row tile: new actions of 64 users (4 rows) 35.4 us for 40.2 with
+// that, 8 copies each of 16 histories 79 for 109.  Where rows are few enough, neighbouring sequences share
+// a tile over the pages that they have in common (shared_set): the copies take 92 us without.
 template <int D>
 __global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_attend16_kernel(AttendArgs a) {
   constexpr int F = D / 4;           // features of a lane's quarter
