@@ -6,8 +6,8 @@
 // multiplied, one barrier a tile.  Tiles that no row of the workgroup sees are not
 // visited, and a wave skips those that none of its own sees, so the work is that of the window.
 // Bound by the vector units: an exponential, a scaling, a maximum, a sum and a rounding for each
-// score, beside 4 D matrix operations; the two add up, as two waves a SIMD seldom meet in different
-// ones.  16384 tokens with a window of 1024, 4 heads of 64: 34 us (13 at a large product's rate); 32 sequences
+// score, beside 4 D matrix operations; the two add up, as the three waves a SIMD (four with the kernel of
+// eight waves) seldom meet in different ones.  16384 tokens with a window of 1024, 4 heads of 64: 34 us (13 at a large product's rate); 32 sequences
 // of 203 - 4000 tokens, 4 heads on 2: 134 us (73).
 #include <algorithm>
 
@@ -35,7 +35,7 @@ struct WindowArgs {
   int tiles;   // row tiles per (sequence, kv head)
 };
 
-// Rows of this workgroup: positions lo .. hi of a sequence of len tokens.
+// Rows of this workgroup, (position, head) pairs: from row0 on of a sequence's `rows`; `len` tokens from row `off`.
 struct Rows {
   int64_t off;
   int len, rows, row0, h, G;
@@ -286,7 +286,8 @@ __global__ __launch_bounds__(SPLIT ? 512 : 256, SPLIT && D <= 64 ? 4 : 2) void a
 // and its four waves take the 32-key tiles in turn, each through its own part of LDS, so that no wave
 // waits for another until their states meet at the end.  8 sequences of 57 - 1000 tokens, a window of 200, 8 heads
 // of 32: 19 us, the few tiles of a row one after the other (35 with 128 rows a workgroup); 4 x 2000 tokens of
-// 64 features: 97 us for 160.
+// 64 features: 98 us for 160.  With 128 features a workgroup's LDS and registers fill a CU: 4 x 1000 - 2000 tokens, 4 heads
+// on 2, 140 us.
 constexpr int TF = 32;
 constexpr int ROWS_F32 = 32;
 
