@@ -194,7 +194,9 @@ __device__ __forceinline__ void att_softmax(AttScaledState<D, QT>& st, int q, f3
   st.l[q] = __builtin_fmaf(att_exp(s, c, b), e, st.l[q]);
 }
 
-// 16 weights as the operands of two products.
+// 16 weights as the operands of two products, which take both in one type: bf16 where the values are bf16 (a
+// weight is off by at most 2^-8, as each value may be already; fp16 would not hold the values), fp16 (2^-11)
+// where they are codes.
 __device__ __forceinline__ void att_operands(const f32x16& p, bf16x8 (&f)[2]) {
 #pragma unroll
   for (int t = 0; t < 2; ++t)
