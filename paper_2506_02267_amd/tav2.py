@@ -554,11 +554,11 @@ def _dense(name: str, x: Optional[torch.Tensor], shape, dtype):
         raise ValueError(f"{name}: expected contiguous {dtype} {list(shape)}")
 
 
-def _whole(**sizes):
-    """Refuse what the C ABI's 32 bits do not hold (ctypes would drop the upper ones)."""
-    for name, n in sizes.items():
-        if not -2 ** 31 <= n < 2 ** 31:
-            raise ValueError(f"{name}: {n} is past 32 bits")
+def _whole(sizes: int):
+    """Refuse what the C ABI's 32 bits do not hold (ctypes would drop the upper ones): `sizes` is several
+    or'ed together, past 32 bits where one is, unless another is negative, which the call refuses."""
+    if not -2 ** 31 <= sizes < 2 ** 31:
+        raise ValueError("a size, window or index is past 32 bits")
 
 
 def _scale(scale: float) -> float:
@@ -597,7 +597,7 @@ def attend_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offset: tor
     q [rows, heads, head_dim], k and v [rows, kv_heads, head_dim], bf16 or fp32, may be slices of
     one projection; offset int64 [R], length int32 [R].  window 0: none; the first `sinks` tokens
     stay visible.  lse (optional, fp32 [rows, heads]) receives the log of the sums."""
-    _whole(max_len=max_len, window=window, sinks=sinks)
+    _whole(max_len | window | sinks)
     dt = torch.float32 if q.dtype == torch.float32 else torch.bfloat16
     lds = _heads("q", q, dt), _heads("k", k, dt), _heads("v", v, dt)
     rows, heads, D = q.shape
@@ -645,7 +645,7 @@ class KvCache:
             _dense(name, x, shape, dt)
             if x.device != k.device:
                 raise ValueError(f"{name}: on {x.device}, k on {k.device}")
-        _whole(max_len=max_len)
+        _whole(max_len)
         self.device, self.index = k.device, k.get_device()
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.k_tail, self.v_tail, self.table = k_tail, v_tail, table
@@ -682,7 +682,7 @@ class KvCache:
 
     @max_len.setter
     def max_len(self, n: int):
-        _whole(max_len=n)
+        _whole(n)
         self.s.max_len = n
 
 
@@ -699,7 +699,7 @@ def kv_append(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, offs
     """tav2_kv_append: one layer's keys and values (bf16 [rows, kv_heads, head_dim], possibly slices
     of one projection) of the tokens that the last kv_extend granted; sequence s's begin at row
     offset[s] (int64 [seqs] or longer)."""
-    _whole(layer=layer, max_count=max_count)
+    _whole(layer | max_count)
     k_ld, v_ld = _heads("k", k, torch.bfloat16), _heads("v", v, torch.bfloat16)
     if k.shape[1:] != cache.row or v.shape != k.shape:
         raise ValueError("k, v: expected [rows, kv_heads, head_dim] of the cache's sizes, as many of "
@@ -720,7 +720,7 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, offset: torch.Tensor,
     s has the queries offset[s] .. offset[s+1] (int64 [seqs + 1]), at most max_count; rows of no
     sequence (a padded batch) are left as they are.
     MASK_CAUSAL: its last tokens; MASK_NONE: candidates to follow it."""
-    _whole(layer=layer, max_count=max_count, window=window, sinks=sinks, flags=flags)
+    _whole(layer | max_count | window | sinks | flags)
     ld = _heads("q", q, torch.bfloat16)
     total, heads, D = q.shape
     if D != cache.s.head_dim:
@@ -759,7 +759,7 @@ def kv_free(cache: KvCache, drop: torch.Tensor, stream=None):
 def kv_trim(cache: KvCache, window: int, sinks: int = 0, stream=None):
     """tav2_kv_trim: every sequence gives up the pages that this window and these sinks no longer
     see."""
-    _whole(window=window, sinks=sinks)
+    _whole(window | sinks)
     _run("tav2_kv_trim", cache.index, stream, (cache.ref, window, sinks), keep=cache.buffers)
 
 
