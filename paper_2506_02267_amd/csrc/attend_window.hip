@@ -7,8 +7,8 @@
 // visited, and a wave skips those that none of its own sees, so the work is that of the window.
 // Bound by the vector units: an exponential, a scaling, a maximum, a sum and a rounding for each
 // score, beside 4 D matrix operations; the two add up, as the three waves a SIMD (four with the kernel of
-// eight waves) seldom meet in different ones.  16384 tokens with a window of 1024, 4 heads of 64: 34 us (13 at a large product's rate); 32 sequences
-// of 203 - 4000 tokens, 4 heads on 2: 134 us (73).
+// eight waves) seldom meet in different ones.  16384 tokens with a window of 1024, 4 heads of 64: 34 us (13 at
+// a large product's rate); 32 sequences of 203 - 4000 tokens, 4 heads on 2: 143 us (73).
 #include <algorithm>
 
 #include "attend_core.h"

@@ -17,7 +17,7 @@
 // One query a sequence is bound by HBM: 64 sequences of 16384 tokens, 8 kv heads, are read at 5.6 TB/s
 // with 64 features and 5.7 with 128 (a large copy: 4.7, read and written).  Many queries are bound by the vector
 // units, which turn codes into fp16 and scores into weights while the matrix units wait, and the
-// reverse: 1000 candidates of one 16384-token history, 4 heads of 64, take 38 us, 13 at a large product's rate.
+// reverse: 1000 candidates of one 16384-token history, 4 heads of 64, take 39 us, 13 at a large product's rate.
 #include <algorithm>
 
 #include "attend_core.h"
