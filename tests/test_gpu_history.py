@@ -1214,3 +1214,15 @@ def test_two_graphs_that_share_a_workspace():
             torch.cuda.synchronize()
             assert torch.equal(outs[i], want[i]), (step, i)
         T.kv_trim(p.gpu, 2 ** 31 - 1)
+
+
+@pytest.mark.parametrize("seqs", [1, 200])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_attend_window_of_one_token_gives_its_value(seqs, D):
+    """A weight that is a row's largest is not rounded: a window of 1 gives v itself, to the bit."""
+    L, H, Hkv = 70, 8, 4
+    g = torch.Generator().manual_seed(D)
+    q, k, v = (rows(g, seqs * L, h, D) for h in (H, Hkv, Hkv))
+    out = T.attend_window(q, k, v, torch.arange(seqs).cuda() * L,
+                          torch.full((seqs,), L, dtype=torch.int32).cuda(), L, window=1)
+    assert torch.equal(out, v.repeat_interleave(H // Hkv, 1))
