@@ -423,7 +423,8 @@ tav2_status tav2_kv_extend(const tav2_kv* c, const int32_t* count, void* stream)
  * The keys and values of the tokens that the last tav2_kv_extend granted, for one layer
  * (once per layer and extension): sequence s's fresh[s] tokens are rows offset[s].. of k and v
  * (bf16 rows of [kv_heads, head_dim], row strides k_ld and v_ld elements as in tav2_window; 16-byte
- * aligned; finite; v's magnitudes at most 2^80).  Blocks that are full now go to their pages, the rest to the tail.
+ * aligned; finite; v's magnitudes at most 2^80).  Blocks that are full now go to their pages, the rest
+ * to the tail.
  *   offset    device int64 [num_seqs]
  *   max_count host-side bound of fresh[s]; tokens of a sequence past it are not written
  */
@@ -440,13 +441,14 @@ tav2_status tav2_kv_append(const tav2_kv* c, int32_t layer, const void* k, int64
  *     every cached token.
  * window and sinks as for tav2_attend_window, counted from the query's position; blocks that were
  * released (tav2_kv_trim) are not seen.  out and lse as there; a query that sees nothing gets
- * zeros and -inf.  Queries (finite; scores up to 2^125) and outputs are bf16; products take the codes exactly, the scales in fp32.
+ * zeros and -inf.  Queries (finite; scores up to 2^125) and outputs are bf16; products take the codes
+ * exactly, the scales in fp32, the weights in fp16 (by at most 2^-11 of one).
  *   ws  device workspace of tav2_kv_attend_workspace() bytes, 256-byte aligned.
  * Errors: those above, TAV2_ERR_WORKSPACE.
  */
 typedef struct tav2_kv_queries {
   const void*    q;            /* device bf16: query i's head h at q + i * ld + h * head_dim */
-  const int64_t* offset;       /* device [num_seqs + 1], not descending, from 0 to at most total */
+  const int64_t* offset;       /* device [num_seqs + 1]: 0 .. total, not descending */
   int64_t total;               /* host: queries there is room for (>= 0); those before offset[0] and
                                   from offset[num_seqs] on are left as they are in out and lse */
   int64_t ld;                  /* elements between queries, as in tav2_window */
