@@ -491,6 +491,101 @@ tav2_status tav2_kv_compact(const tav2_kv* c, int32_t* used, void* ws, size_t ws
                             void* stream);
 
 /*
+ * Continuations that share a history: a beam search over a resident history, drafts or slates that branch from it.
+ * The history is one sequence of the cache, and so is each continuation (a member), which holds only
+ * its own tokens; nothing of the history is copied.  Group g's members are the sequences
+ * offset[g] .. offset[g+1] - 1.  A step of a beam search: tav2_kv_reorder by the beams selected last,
+ * tav2_kv_extend and, layer by layer, tav2_kv_append and tav2_kv_attend_prefix, then tav2_beam_select
+ * on the model's logits.
+ */
+typedef struct tav2_kv_groups {
+  const int32_t* offset;       /* device [num_groups + 1]: 0 .. num_seqs, not descending */
+  const int32_t* prefix;       /* device [num_groups]: the sequence that stands before the members'
+                                  tokens, -1: none (not read by tav2_kv_reorder, which takes NULL) */
+  int32_t num_groups;          /* >= 0 */
+  int32_t max_members;         /* host-side bound of a group's members, 1 .. TAV2_BEAMS_MAX; members past it
+                                  are left out of a call */
+  int32_t max_own;             /* host-side estimate of the longest member: tav2_kv_attend_prefix
+                                  divides its work by it, as by tav2_kv's max_len */
+  int32_t reserved;            /* set to 0 */
+} tav2_kv_groups;
+
+/*
+ * Members continue others: with p = parent[s - offset[0]], sequence s becomes a continuation of
+ * member p of its group (0: the group's first) as that was before the call; all at once, so that beams
+ * may change places.  It shares that one's pages, gets a copy of its tail in every layer, and
+ * gives up its own pages.  p < 0: it gives up its pages and is empty; p its own place, or past the
+ * group's members: it stays as it is.
+ *   parent   device int32 [members]; members past it stay as they are.
+ */
+tav2_status tav2_kv_reorder(const tav2_kv* c, const tav2_kv_groups* g, const int32_t* parent,
+                            int32_t members, void* stream);
+
+/*
+ * Attention of the members' queries over their group's prefix and their own tokens, as one softmax
+ * over both; the prefix is read once for all members of the group.  q is tav2_kv_attend's: sequence
+ * s's queries are offset[s] .. offset[s+1]; those of sequences in no group, and those past
+ * max_count of a member, are left as they are in out and lse.  Query i of n of a member with len tokens
+ * of its own stands o = len - n + i (TAV2_MASK_CAUSAL) or o = len (TAV2_MASK_NONE) places behind the prefix:
+ * it sees the prefix, and its own tokens up to o (none where that is negative).  With a window,
+ * positions are counted from the prefix's first token, as if the member had followed it in one
+ * sequence.  Blocks that were released are not seen.
+ * Rounding, types, scales, out and lse as for tav2_kv_attend.
+ *   ws  device workspace of tav2_kv_attend_prefix_workspace() bytes, 256-byte aligned.
+ */
+size_t tav2_kv_attend_prefix_workspace(const tav2_kv* c, const tav2_kv_groups* g,
+                                       const tav2_kv_queries* q);
+tav2_status tav2_kv_attend_prefix(const tav2_kv* c, int32_t layer, const tav2_kv_groups* g,
+                                  const tav2_kv_queries* q, uint32_t flags, void* out, float* lse,
+                                  void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Selection of beams.  Row n = r beams + b holds the logits z[n, v] of beam b of request r, which is
+ * worth score[n] (the log-probability of what it holds) so far.  A beam continued by token v is worth
+ *   (score[n] - Z_n) + z[n, v] ,  Z_n = log sum_v exp z[n, v] ,
+ * computed in 64 bits; the `keep` best continuations of a request are selected, in the order (value
+ * desc, beam asc, token asc).  A finished beam (done[n] != 0) has one continuation, itself, with its
+ * score as it stands, token eos (in the order as token 0 where eos is negative).
+ * Logits that are no finite numbers are not there; a token whose bit in `allowed` is 0 counts in Z_n
+ * but is no continuation; a beam whose score is not finite is none.
+ *   out_parent device int32 [requests, keep]: the beam b that is continued, -1 where there are fewer
+ *              continuations than `keep`
+ *   out_token  device int32 [requests, keep]: token v, -1 there
+ *   out_score  device float32 [requests, keep]: the value (at least -FLT_MAX), -inf there
+ *   out_done   device uint8 [requests, keep] or NULL: the token is eos or the beam was finished
+ *   flags      TAV2_BEAM_RANKED: in the order above.  TAV2_BEAM_IN_PLACE (keep == beams): a beam that
+ *              is continued keeps its place for the best of its continuations, and the others take the
+ *              places of beams that are not, in the order above: with the places as members of a
+ *              group, tav2_kv_reorder then moves only those.
+ *   ws  device workspace of tav2_beam_select_workspace() bytes, 256-byte aligned.
+ * Outputs may not overlap inputs.  Errors: TAV2_ERR_NULL, TAV2_ERR_SHAPE, TAV2_ERR_DTYPE, TAV2_ERR_UNSUPPORTED (over
+ * 2^31 - 1 logits a request or rows in all; over 2^24 - 1 workgroups), TAV2_ERR_WORKSPACE, TAV2_ERR_HIP.
+ */
+#define TAV2_BEAMS_MAX 1024
+#define TAV2_VOCAB_MAX (1 << 24)
+#define TAV2_BEAM_RANKED   0u
+#define TAV2_BEAM_IN_PLACE 1u
+typedef struct tav2_beams {
+  const void*    logits;       /* device [requests * beams, vocab], dtype */
+  const float*   score;        /* device [requests, beams], or NULL: all 0 */
+  const uint8_t* done;         /* device [requests, beams], or NULL: none finished */
+  const uint8_t* allowed;      /* device bits: token v is bit v % 8 of byte v / 8 of its row; or NULL: all */
+  int64_t ld;                  /* elements from a row of logits to the next, >= vocab */
+  int64_t allowed_ld;          /* bytes from a row of `allowed` to the next, >= (vocab + 7) / 8, or 0: one row
+                                  for every beam */
+  int32_t num_requests;        /* >= 0 */
+  int32_t beams;               /* 1 .. TAV2_BEAMS_MAX */
+  int32_t vocab;               /* 1 .. TAV2_VOCAB_MAX */
+  int32_t dtype;               /* TAV2_F32 or TAV2_BF16 */
+  int32_t eos;                 /* below vocab; negative: none */
+  int32_t reserved;            /* set to 0 */
+} tav2_beams;
+size_t tav2_beam_select_workspace(const tav2_beams* b, int32_t keep);
+tav2_status tav2_beam_select(const tav2_beams* b, int32_t keep, uint32_t flags, int32_t* out_parent,
+                             int32_t* out_token, float* out_score, uint8_t* out_done, void* ws,
+                             size_t ws_bytes, void* stream);
+
+/*
  * Measurement hook for benchmarks and profilers (not needed for serving).
  * tav2_profile_enable(1, site) makes every later kernel launch of the library
  * whose site name equals `site` (NULL: every site) record a HIP event before
@@ -506,7 +601,8 @@ tav2_status tav2_kv_compact(const tav2_kv* c, int32_t* used, void* ws, size_t ws
  * materialised score rows), gather, pack_weights, cand_proj, encoder_fused (the
  * bf16 encoder of d_model 256), encoder_small (d_model 64), encode_f32, attend_window,
  * kv_extend, kv_append, kv_attend, kv_merge (kv_attend's second launch), kv_fork, kv_free,
- * kv_trim, kv_plan and kv_compact (the two of tav2_kv_compact).
+ * kv_trim, kv_plan and kv_compact (the two of tav2_kv_compact), kv_reorder (two launches), kv_prefix and
+ * kv_join (the two of tav2_kv_attend_prefix), beam_scan and beam_pick (the two of tav2_beam_select).
  */
 int32_t tav2_profile_enable(int32_t on, const char* only_site);
 int64_t tav2_profile_report(char* buf, size_t buf_bytes);

@@ -9,7 +9,8 @@ encoding with early fusion of Eq. 4, the causal transformer encoder and the
 linear + max-pool head (Sec. 3.2.2, 'Transformer Encoder').  Only the tests,
 the package's smoke check and the benchmark's CPU-baseline leg may import it;
 the GPU library never does, and this package imports nothing from it.
-`oracle.history` states attention over whole histories and the paged 8-bit cache.
+`oracle.history` states attention over whole histories and the paged 8-bit cache, `oracle.beams` a beam
+search over them.
 
 Arithmetic: scores are exact (integer arithmetic on the inputs' dyadic grid);
 the encoder runs in float64 on the same (bf16-rounded where applicable) values

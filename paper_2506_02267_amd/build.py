@@ -20,7 +20,8 @@ SOURCES = ["api.cpp", "batcher.cpp", "profile.cpp", "select.hip", "select_fused.
            "select_resident.hip", "gather.hip",
            "encoder_fused.hip", "encoder_fused_unmasked.hip", "encoder_fused_short.hip",
            "encoder_small.hip", "encoder_f32.hip", "attend_window.hip", "kv_attend.hip",
-           "kv_append.hip", "kv_pages.hip", "kv_api.cpp"]
+           "kv_append.hip", "kv_pages.hip", "kv_prefix.hip", "kv_reorder.hip", "beam_select.hip",
+           "kv_api.cpp"]
 ARCH = "gfx950"
 
 
@@ -55,6 +56,7 @@ EXTRA_FLAGS = {"encoder_fused.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                                      "-amdgpu-sched-strategy=max-ilp"],
                "attend_window.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "kv_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "kv_prefix.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "kv_append.hip": ["-fhip-fp32-correctly-rounded-divide-sqrt"],
                "select.hip": ["-fhip-fp32-correctly-rounded-divide-sqrt"],
                "select_resident.hip": ["-fhip-fp32-correctly-rounded-divide-sqrt", "-mllvm",

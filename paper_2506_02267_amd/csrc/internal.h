@@ -154,4 +154,20 @@ size_t kv_attend_bytes(const tav2_kv& c, const tav2_kv_queries& q);
 hipError_t launch_kv_attend(const tav2_kv& c, int layer, const tav2_kv_queries& q, bool causal,
                             void* out, float* lse, void* ws, hipStream_t st);
 
+// ---- kv_reorder.hip, kv_prefix.hip: continuations that share a history
+int64_t kv_reorder_parts(const tav2_kv& c);   // workgroups for a group
+hipError_t launch_kv_reorder(const tav2_kv& c, const tav2_kv_groups& g, const int32_t* parent,
+                             int members, hipStream_t st);
+double kv_prefix_workgroups(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q);
+size_t kv_prefix_bytes(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q);
+hipError_t launch_kv_prefix(const tav2_kv& c, int layer, const tav2_kv_groups& g,
+                            const tav2_kv_queries& q, bool causal, void* out, float* lse, void* ws,
+                            hipStream_t st);
+
+// ---- beam_select.hip
+int64_t beam_select_groups(const tav2_beams& b, int keep);   // workgroups of the larger launch
+size_t beam_select_bytes(const tav2_beams& b, int keep);
+hipError_t launch_beam_select(const tav2_beams& b, int keep, bool in_place, int32_t* parent,
+                              int32_t* token, float* score, uint8_t* done, void* ws, hipStream_t st);
+
 }  // namespace tav2

@@ -1,5 +1,5 @@
-// C ABI of attention over whole histories: argument checks and launches of the windowed attention and
-// of the paged 8-bit cache.  No allocation, no synchronisation.
+// C ABI of attention over whole histories: argument checks and launches of the windowed attention, of
+// the paged 8-bit cache, and of the beams that continue its sequences.  No allocation, no synchronisation.
 #include "common.h"
 #include "internal.h"
 
@@ -47,7 +47,7 @@ tav2_status check_layer(const tav2_kv* c, int32_t layer) {
   return layer >= 0 && layer < c->layers ? TAV2_OK : TAV2_ERR_SHAPE;
 }
 
-tav2_status check_queries(const tav2_kv* c, const tav2_kv_queries* q) {
+tav2_status check_query_sizes(const tav2_kv* c, const tav2_kv_queries* q) {
   if (!q) return TAV2_ERR_NULL;
   if (q->total < 0 || q->max_count < 0 || q->max_count > q->total) return TAV2_ERR_SHAPE;
   if (q->total > 0 && q->max_count == 0) return TAV2_ERR_SHAPE;
@@ -55,7 +55,45 @@ tav2_status check_queries(const tav2_kv* c, const tav2_kv_queries* q) {
     return TAV2_ERR_SHAPE;
   if (q->heads > MAX_HEADS || q->total > MAX_ROWS / q->heads) return TAV2_ERR_UNSUPPORTED;
   if (!stride_ok(q->ld, q->heads, c->head_dim, 8)) return TAV2_ERR_SHAPE;
+  return TAV2_OK;
+}
+
+tav2_status check_queries(const tav2_kv* c, const tav2_kv_queries* q) {
+  if (const tav2_status st = check_query_sizes(c, q)) return st;
   if (q->total > 0 && kv_attend_groups(*c, *q) > MAX_GROUPS) return TAV2_ERR_UNSUPPORTED;
+  return TAV2_OK;
+}
+
+tav2_status check_groups(const tav2_kv_groups* g, bool prefix) {
+  if (!g) return TAV2_ERR_NULL;
+  if (g->num_groups < 0 || g->max_members < 1 || g->max_members > TAV2_BEAMS_MAX || g->max_own < 0)
+    return TAV2_ERR_SHAPE;
+  if (g->num_groups > TAV2_KV_SEQS_MAX) return TAV2_ERR_UNSUPPORTED;
+  if (g->num_groups > 0 && (!g->offset || (prefix && !g->prefix))) return TAV2_ERR_NULL;
+  return TAV2_OK;
+}
+
+// The queries over groups of members, besides their sizes.
+tav2_status check_prefix(const tav2_kv* c, const tav2_kv_groups* g, const tav2_kv_queries* q) {
+  if (q->total > 0 && g->num_groups > 0 && kv_prefix_workgroups(*c, *g, *q) > double(MAX_GROUPS))
+    return TAV2_ERR_UNSUPPORTED;
+  return TAV2_OK;
+}
+
+tav2_status check_beams(const tav2_beams* b, int32_t keep) {
+  if (!b) return TAV2_ERR_NULL;
+  if (b->dtype != TAV2_F32 && b->dtype != TAV2_BF16) return TAV2_ERR_DTYPE;
+  if (b->num_requests < 0 || b->beams < 1 || b->beams > TAV2_BEAMS_MAX || b->vocab < 1 ||
+      b->vocab > TAV2_VOCAB_MAX || keep < 1 || keep > TAV2_K_MAX || b->ld < b->vocab ||
+      b->eos >= b->vocab)
+    return TAV2_ERR_SHAPE;
+  if (b->allowed && b->allowed_ld != 0 && b->allowed_ld < (int64_t(b->vocab) + 7) / 8) return TAV2_ERR_SHAPE;
+  if (!aligned(b->logits, b->dtype == TAV2_BF16 ? 2 : 4)) return TAV2_ERR_SHAPE;
+  const int64_t rows = int64_t(b->num_requests) * b->beams, most = int64_t(1) << 60;
+  if (int64_t(b->beams) * b->vocab > MAX_ROWS || rows > MAX_ROWS) return TAV2_ERR_UNSUPPORTED;
+  if (rows > 0 && (b->ld > most / rows || (b->allowed && b->allowed_ld > most / rows)))
+    return TAV2_ERR_UNSUPPORTED;
+  if (beam_select_groups(*b, keep) > MAX_GROUPS) return TAV2_ERR_UNSUPPORTED;
   return TAV2_OK;
 }
 
@@ -162,6 +200,59 @@ tav2_status tav2_kv_compact(const tav2_kv* c, int32_t* used, void* ws, size_t ws
   if (!used) return TAV2_ERR_NULL;
   if ((st = check_ws(ws, ws_bytes, kv_plan_bytes(*c)))) return st;
   return hip_status(launch_kv_compact(*c, used, ws, static_cast<hipStream_t>(stream)));
+}
+
+tav2_status tav2_kv_reorder(const tav2_kv* c, const tav2_kv_groups* g, const int32_t* parent,
+                            int32_t members, void* stream) {
+  tav2_status st;
+  if ((st = check_kv(c)) || (st = check_groups(g, false))) return st;
+  if (members < 0) return TAV2_ERR_SHAPE;
+  if (members == 0 || g->num_groups == 0) return TAV2_OK;
+  if (!parent) return TAV2_ERR_NULL;
+  if (kv_reorder_parts(*c) * g->num_groups > MAX_GROUPS) return TAV2_ERR_UNSUPPORTED;
+  return hip_status(launch_kv_reorder(*c, *g, parent, members, static_cast<hipStream_t>(stream)));
+}
+
+size_t tav2_kv_attend_prefix_workspace(const tav2_kv* c, const tav2_kv_groups* g,
+                                       const tav2_kv_queries* q) {
+  if (check_kv(c) || check_groups(g, true) || check_query_sizes(c, q) || check_prefix(c, g, q) ||
+      q->total == 0 || g->num_groups == 0)
+    return 0;
+  return kv_prefix_bytes(*c, *g, *q);
+}
+
+tav2_status tav2_kv_attend_prefix(const tav2_kv* c, int32_t layer, const tav2_kv_groups* g,
+                                  const tav2_kv_queries* q, uint32_t flags, void* out, float* lse,
+                                  void* ws, size_t ws_bytes, void* stream) {
+  tav2_status st;
+  if ((st = check_kv(c)) || (st = check_layer(c, layer)) || (st = check_groups(g, true)) ||
+      (st = check_query_sizes(c, q)) || (st = check_prefix(c, g, q)))
+    return st;
+  if (flags != TAV2_MASK_CAUSAL && flags != TAV2_MASK_NONE) return TAV2_ERR_SHAPE;
+  if (q->total == 0 || g->num_groups == 0) return TAV2_OK;
+  if (!q->q || !q->offset || !out) return TAV2_ERR_NULL;
+  if (!aligned(q->q, 16) || !aligned(out, 16)) return TAV2_ERR_SHAPE;
+  if ((st = check_ws(ws, ws_bytes, kv_prefix_bytes(*c, *g, *q)))) return st;
+  return hip_status(launch_kv_prefix(*c, layer, *g, *q, flags == TAV2_MASK_CAUSAL, out, lse, ws,
+                                     static_cast<hipStream_t>(stream)));
+}
+
+size_t tav2_beam_select_workspace(const tav2_beams* b, int32_t keep) {
+  return check_beams(b, keep) || b->num_requests == 0 ? 0 : beam_select_bytes(*b, keep);
+}
+
+tav2_status tav2_beam_select(const tav2_beams* b, int32_t keep, uint32_t flags, int32_t* out_parent,
+                             int32_t* out_token, float* out_score, uint8_t* out_done, void* ws,
+                             size_t ws_bytes, void* stream) {
+  tav2_status st;
+  if ((st = check_beams(b, keep))) return st;
+  if (flags != TAV2_BEAM_RANKED && flags != TAV2_BEAM_IN_PLACE) return TAV2_ERR_SHAPE;
+  if (flags == TAV2_BEAM_IN_PLACE && keep != b->beams) return TAV2_ERR_SHAPE;
+  if (b->num_requests == 0) return TAV2_OK;
+  if (!b->logits || !out_parent || !out_token || !out_score) return TAV2_ERR_NULL;
+  if ((st = check_ws(ws, ws_bytes, beam_select_bytes(*b, keep)))) return st;
+  return hip_status(launch_beam_select(*b, keep, flags == TAV2_BEAM_IN_PLACE, out_parent, out_token,
+                                       out_score, out_done, ws, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

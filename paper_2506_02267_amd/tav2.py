@@ -21,6 +21,8 @@ F32, BF16, I8 = 0, 1, 2
 MASK_CAUSAL, MASK_NONE = 0, 1
 K_MAX, T_MAX = 1024, 2048
 KV_PAGE, KV_SEQS_MAX = 64, 32768
+BEAMS_MAX, VOCAB_MAX = 1024, 1 << 24
+BEAM_RANKED, BEAM_IN_PLACE = 0, 1
 STATUS = {0: "ok", -1: "null", -2: "shape", -3: "dtype", -4: "unsupported", -5: "workspace",
           -6: "hip", -7: "too_large"}
 
@@ -96,6 +98,17 @@ class KvQueries(ctypes.Structure):
                 ("sinks", c_int32), ("scale", c_float), ("reserved", c_int32)]
 
 
+class KvGroupsStruct(ctypes.Structure):
+    _fields_ = [("offset", c_void_p), ("prefix", c_void_p), ("num_groups", c_int32),
+                ("max_members", c_int32), ("max_own", c_int32), ("reserved", c_int32)]
+
+
+class Beams(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("logits", "score", "done", "allowed")] + [
+        ("ld", c_int64), ("allowed_ld", c_int64)] + [
+        (n, c_int32) for n in ("num_requests", "beams", "vocab", "dtype", "eos", "reserved")]
+
+
 FUNCTIONS = {
     "tav2_status_string": (ctypes.c_char_p, [c_int32]),
     "tav2_abi_version": (c_int32, []),
@@ -141,6 +154,15 @@ FUNCTIONS = {
     "tav2_kv_trim": (c_int32, [POINTER(Kv), c_int32, c_int32, c_void_p]),
     "tav2_kv_compact_workspace": (c_size_t, [POINTER(Kv)]),
     "tav2_kv_compact": (c_int32, [POINTER(Kv), c_void_p, c_void_p, c_size_t, c_void_p]),
+    "tav2_kv_reorder": (c_int32, [POINTER(Kv), POINTER(KvGroupsStruct), c_void_p, c_int32, c_void_p]),
+    "tav2_kv_attend_prefix_workspace": (c_size_t, [POINTER(Kv), POINTER(KvGroupsStruct),
+                                                   POINTER(KvQueries)]),
+    "tav2_kv_attend_prefix": (c_int32, [POINTER(Kv), c_int32, POINTER(KvGroupsStruct),
+                                        POINTER(KvQueries), ctypes.c_uint32, c_void_p, c_void_p,
+                                        c_void_p, c_size_t, c_void_p]),
+    "tav2_beam_select_workspace": (c_size_t, [POINTER(Beams), c_int32]),
+    "tav2_beam_select": (c_int32, [POINTER(Beams), c_int32, ctypes.c_uint32, c_void_p, c_void_p,
+                                   c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     "tav2_profile_enable": (c_int32, [c_int32, ctypes.c_char_p]),
     "tav2_profile_report": (ctypes.c_int64, [ctypes.c_char_p, c_size_t]),
 }
@@ -775,6 +797,128 @@ def kv_compact(cache: KvCache, used: Optional[torch.Tensor] = None,
     _run("tav2_kv_compact", cache.index, stream,
          (cache.ref, used.data_ptr(), wp, wb), used, ws.buf, keep=cache.buffers)
     return used
+
+
+class KvGroups:
+    """A tav2_kv_groups: members of group g are the cache's sequences offset[g] .. offset[g+1] - 1
+    (int32 [groups + 1] on the GPU), which continue sequence prefix[g] (int32 [groups], -1: none; None
+    where the groups are only reordered).  max_members bounds a group's members; max_own is the host's
+    estimate of the longest member's own tokens, by which kv_attend_prefix divides its work; it may be
+    set anew as members grow."""
+
+    def __init__(self, offset: torch.Tensor, prefix: Optional[torch.Tensor] = None,
+                 max_members: int = BEAMS_MAX, max_own: int = KV_PAGE):
+        if offset.dim() != 1 or offset.shape[0] < 1:
+            raise ValueError("offset: expected int32 [groups + 1]")
+        groups = offset.shape[0] - 1
+        _dense("offset", offset, (groups + 1,), torch.int32)
+        _dense("prefix", prefix, (groups,), torch.int32)
+        _whole(max_members | max_own)
+        self.offset, self.prefix, self.groups = offset, prefix, groups
+        self.s = KvGroupsStruct(offset.data_ptr(), None if prefix is None else prefix.data_ptr(), groups,
+                                max_members, max_own, 0)
+        self.ref = ctypes.byref(self.s)
+
+    @property
+    def max_own(self) -> int:
+        return self.s.max_own
+
+    @max_own.setter
+    def max_own(self, n: int):
+        _whole(n)
+        self.s.max_own = n
+
+
+def kv_reorder(cache: KvCache, groups: KvGroups, parent: torch.Tensor, stream=None):
+    """tav2_kv_reorder: member number i of all (int32 parent [members], counted from the first group's
+    first) becomes a continuation of its group's member parent[i] as that was before; negative: it is
+    emptied."""
+    if parent.dtype != torch.int32 or not parent.is_contiguous():
+        raise ValueError("parent: expected contiguous int32 [members]")
+    _whole(parent.numel())
+    _run("tav2_kv_reorder", cache.index, stream,
+         (cache.ref, groups.ref, parent.data_ptr(), parent.numel()), parent, groups.offset,
+         keep=cache.buffers)
+
+
+def kv_attend_prefix(cache: KvCache, layer: int, groups: KvGroups, q: torch.Tensor,
+                     offset: torch.Tensor, max_count: int, out: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, flags: int = MASK_CAUSAL, window: int = 0,
+                     sinks: int = 0, scale: float = 0.0, ws: Optional[Workspace] = None,
+                     stream=None) -> torch.Tensor:
+    """tav2_kv_attend_prefix: the groups' members' queries (q and offset as kv_attend takes them) over
+    their group's prefix, which is read once for all of them, and each one's own tokens.
+    MASK_CAUSAL: the queries are the member's last tokens; MASK_NONE: candidates to follow it.  Rows
+    of other sequences are left as they are."""
+    _whole(layer | max_count | window | sinks | flags)
+    ld = _heads("q", q, torch.bfloat16)
+    total, heads, D = q.shape
+    if D != cache.s.head_dim:
+        raise ValueError("q: expected the cache's head_dim")
+    _dense("offset", offset, (cache.seqs + 1,), torch.int64)
+    if out is None:
+        out = torch.empty((total, heads, D), dtype=torch.bfloat16, device=q.device)
+    _dense("out", out, (total, heads, D), torch.bfloat16)
+    _dense("lse", lse, (total, heads), torch.float32)
+    a = ctypes.byref(KvQueries(q.data_ptr(), offset.data_ptr(), total, ld, max_count, heads, window,
+                               sinks, _scale(scale), 0))
+    ws = ws or Workspace(q.device)
+    wp, wb = ws.get(load_library().tav2_kv_attend_prefix_workspace(cache.ref, groups.ref, a))
+    _run("tav2_kv_attend_prefix", cache.index, stream,
+         (cache.ref, layer, groups.ref, a, flags, out.data_ptr(),
+          None if lse is None else lse.data_ptr(), wp, wb), q, offset, out, lse, ws.buf,
+         groups.offset, groups.prefix, keep=cache.buffers)
+    return out
+
+
+def beam_select(logits: torch.Tensor, beams: int, keep: int, score: Optional[torch.Tensor] = None,
+                done: Optional[torch.Tensor] = None, allowed: Optional[torch.Tensor] = None,
+                eos: int = -1, flags: int = BEAM_RANKED, out=None, ws: Optional[Workspace] = None,
+                stream=None):
+    """tav2_beam_select: the `keep` best continuations of every request's beams.
+
+    logits [requests * beams, vocab], bf16 or fp32, rows possibly slices of wider ones; score fp32
+    [requests, beams] (None: zeros), done uint8 [requests, beams], allowed uint8 bits
+    [requests * beams or 1, (vocab + 7) / 8 or more].  Returns (parent int32, token int32,
+    score fp32, done uint8), each [requests, keep]; out: four tensors to use instead."""
+    _whole(beams | keep)
+    _whole(eos)
+    _whole(flags)
+    dt = torch.float32 if logits.dtype == torch.float32 else torch.bfloat16
+    if logits.dim() != 2 or logits.dtype != dt:
+        raise ValueError("logits: expected bf16 or fp32 [requests * beams, vocab]")
+    rows, V = logits.shape
+    if beams < 1 or rows % beams:
+        raise ValueError(f"logits: {rows} rows are no whole requests of {beams} beams")
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError("logits: the tokens of a row must be contiguous")
+    R = rows // beams
+    _whole(R | V)
+    ld = logits.stride(0) if rows > 1 else V
+    _dense("score", score, (R, beams), torch.float32)
+    _dense("done", done, (R, beams), torch.uint8)
+    ald = 0
+    if allowed is not None:
+        if allowed.dim() != 2 or allowed.dtype != torch.uint8 or allowed.shape[0] not in (1, rows) or \
+                allowed.shape[1] < (V + 7) // 8 or allowed.stride(1) != 1:
+            raise ValueError("allowed: expected uint8 [requests * beams or 1, (vocab + 7) / 8 or more]")
+        ald = allowed.stride(0) if allowed.shape[0] > 1 else 0
+    dev = logits.device
+    if out is None:
+        e = lambda t: torch.empty((R, max(keep, 0)), dtype=t, device=dev)
+        out = e(torch.int32), e(torch.int32), e(torch.float32), e(torch.uint8)
+    for name, x, t in zip(("parent", "token", "score", "done"), out,
+                          (torch.int32, torch.int32, torch.float32, torch.uint8)):
+        _dense(f"out's {name}", x, (R, keep), t)
+    p = lambda t: None if t is None else t.data_ptr()
+    b = ctypes.byref(Beams(p(logits), p(score), p(done), p(allowed), ld, ald, R, beams, V,
+                           F32 if dt == torch.float32 else BF16, eos, 0))
+    ws = ws or Workspace(dev)
+    wp, wb = ws.get(load_library().tav2_beam_select_workspace(b, keep))
+    _run("tav2_beam_select", logits.get_device(), stream,
+         (b, keep, flags, p(out[0]), p(out[1]), p(out[2]), p(out[3]), wp, wb), logits, score, done,
+         allowed, *out, ws.buf)
+    return out
 
 
 class Batcher:

@@ -1,0 +1,547 @@
+"""A beam search over resident histories on the GPU against the 64-bit oracle (oracle/beams.py): the
+selection of beams, the reordering of the cache's sequences, and attention to a shared prefix.
+
+Bounds.  A selected value is computed in 64 bits from a sum of exponentials that are off by at most
+2^-36 of themselves, so Z by at most 2^-36 (and fp64's own roundings, below 2^-44 for the sizes
+here), and is rounded to fp32 once: |error| <= 2^-24 |value| + 2^-35.  Beams, tokens and flags are compared exactly: the
+inputs' values either tie exactly (equal logits of a row, equal rows) or lie further apart than 2^-30.
+Attention: as derived in test_gpu_history, where the same products and roundings are taken; one more
+factor joins the two launches' sums (its exponential and products are among the few 2^-23 there)."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import beams as ob
+from paper_2506_02267_amd import tav2 as T
+from test_gpu_history import BF, HALF, Pair, bound, rows
+
+pytestmark = pytest.mark.gpu
+
+F32 = torch.float32
+P = T.KV_PAGE
+
+
+# ------------------------------------------------------------------------- beam_select
+def bits_of(allowed):
+    """Truth values [rows, V] as the call's bits."""
+    return torch.from_numpy(np.packbits(np.asarray(allowed), axis=1, bitorder="little")).cuda()
+
+
+def run_select(z, B, keep, score=None, done=None, allowed=None, eos=-1, in_place=False, ws=None,
+               stream=None):
+    d = lambda x, t: None if x is None else torch.as_tensor(np.asarray(x)).to(t).cuda()
+    return T.beam_select(z, B, keep, score=d(score, F32), done=d(done, torch.uint8),
+                         allowed=None if allowed is None else bits_of(allowed), eos=eos,
+                         flags=T.BEAM_IN_PLACE if in_place else T.BEAM_RANKED, ws=ws, stream=stream)
+
+
+def same_selection(got, want):
+    parent, token, value, ends = want
+    p, t, s, e = (x.cpu().numpy() for x in got)
+    assert np.array_equal(p, parent), np.argwhere(p != parent)[:5].tolist()
+    assert np.array_equal(t, token), np.argwhere(t != token)[:5].tolist()
+    assert np.array_equal(e, ends)
+    none = ~np.isfinite(value)
+    assert np.array_equal(np.isneginf(s), none)
+    s, value = s[~none].astype(np.float64), value[~none]
+    low = -float(np.finfo(np.float32).max)
+    assert (np.abs(s - np.maximum(value, low)) <= 2.0 ** -24 * np.abs(value) + 2.0 ** -35).all()
+
+
+def check_select(z, B, keep, score=None, done=None, allowed=None, eos=-1, in_place=False):
+    rows_ = z.double().cpu().numpy()
+    full = None if allowed is None else np.broadcast_to(allowed, rows_.shape)
+    sc = None if score is None else np.asarray(score, dtype=np.float32)
+    want = ob.select(rows_, B, keep, sc, done, full, eos, in_place)
+    got = run_select(z, B, keep, sc, done, allowed, eos, in_place)
+    torch.cuda.synchronize()
+    same_selection(got, want)
+    return got
+
+
+def logits(seed, R, B, V, dtype, spread=2.0, pad=0, shift=0):
+    g = torch.Generator().manual_seed(seed)
+    z = (torch.randn(R * B, V, generator=g) * spread).to(dtype)
+    buf = torch.full((R * B, shift + V + pad), float("nan"), dtype=dtype, device="cuda")
+    buf[:, shift:shift + V] = z.cuda()
+    return buf[:, shift:shift + V]
+
+
+SELECT = [
+    # R, B, V, keep, dtype, pad, shift
+    (1, 1, 1, 1, BF, 0, 0),
+    (2, 1, 2, 5, F32, 0, 0),
+    (1, 8, 256, 8, BF, 0, 0),
+    (3, 4, 7, 4, BF, 1, 0),
+    (2, 3, 63, 100, F32, 0, 0),
+    (5, 2, 64, 1, BF, 0, 3),
+    (2, 7, 100, 13, F32, 5, 1),
+    (4, 32, 255, 32, BF, 0, 0),
+    (1, 5, 1000, 64, BF, 24, 0),
+    (2, 16, 2048, 16, F32, 0, 0),
+    (3, 9, 4097, 33, BF, 0, 5),
+    (1, 3, 8191, 7, BF, 2, 1),
+    (2, 6, 16384, 50, BF, 0, 0),
+    (1, 4, 16385, 20, F32, 3, 0),
+    (1, 2, 40000, 300, BF, 0, 0),
+    (2, 3, 70001, 11, F32, 1, 2),
+    (1, 1, 131072, 1000, BF, 0, 0),
+    (1, 200, 40, 200, BF, 0, 0),
+    (1, 1024, 33, 1024, F32, 0, 0),
+    (1, 2, 300007, 40, BF, 0, 0),
+    (300, 2, 50, 4, BF, 0, 0),
+]
+
+
+@pytest.mark.parametrize("R,B,V,keep,dtype,pad,shift", SELECT)
+def test_select(R, B, V, keep, dtype, pad, shift):
+    print(f"beam_select {R} x {B} beams of {V}, keep {keep}, {dtype}, pad {pad} shift {shift}", flush=True)
+    z = logits(R * 31 + V, R, B, V, dtype, pad=pad, shift=shift)
+    g = np.random.default_rng(V)
+    check_select(z, B, keep, score=-5 * g.random((R, B)), eos=V // 2)
+
+
+@pytest.mark.parametrize("R,B,V,dtype", [(2, 8, 100, BF), (3, 32, 1025, F32), (1, 5, 30000, BF), (4, 1, 77, F32)])
+def test_select_in_place_with_masks_and_finished_beams(R, B, V, dtype):
+    g = np.random.default_rng(B)
+    z = logits(V, R, B, V, dtype)
+    score = -3 * g.random((R, B))
+    score[0, 0] = -np.inf                      # no beam
+    if B > 4:
+        score[0, 1], score[-1, 2] = np.nan, np.inf
+    done = (g.random((R, B)) < 0.3).astype(np.uint8)
+    allowed = g.random((R * B, V)) < 0.3
+    allowed[B // 2] = False                    # nothing is allowed
+    one = g.random((1, V)) < 0.5
+    for a in (None, allowed, one):
+        for eos in (-1, 0, V - 1):
+            for place in (False, True):
+                check_select(z, B, B, score, done, a, eos, place)
+
+
+def test_select_fewer_than_asked():
+    """Rows without a finite logit, beams without a score, requests without anything."""
+    R, B, V = 4, 3, 50
+    z = logits(5, R, B, V, F32)
+    z[0:3] = float("nan")
+    z[3] = float("-inf")
+    z[4, 7:] = float("inf")                    # seven are left
+    score = np.zeros((R, B))
+    score[2] = -np.inf
+    score[3, 1:] = np.nan
+    allowed = np.ones((R * B, V), dtype=bool)
+    allowed[9, 5:] = False
+    for keep in (1, 3, 200):
+        check_select(z, B, keep, score, allowed=allowed)
+    check_select(z, B, B, score, allowed=allowed, in_place=True)
+    got = run_select(z, B, 4)
+    assert (got[0][0].cpu() == -1).all() and np.isneginf(got[2][0].cpu().numpy()).all()
+
+
+@pytest.mark.parametrize("V,keep", [(40, 8), (5000, 64), (33000, 300), (33000, 1024)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_select_ties(V, keep, dtype):
+    """Equal logits everywhere, few different ones, and beams that are alike."""
+    B = 4
+    g = torch.Generator().manual_seed(V)
+    flat = torch.zeros(B, V, dtype=dtype).cuda()
+    check_select(flat, B, keep)
+    coarse = (torch.randint(-3, 4, (B, V), generator=g) / 2).to(dtype).cuda()
+    check_select(coarse, B, keep, score=[[-1.0, 0.0, 0.0, -0.5]])
+    alike = (torch.randn(1, V, generator=g) * 3).to(dtype).expand(B, V).contiguous().cuda()
+    check_select(alike, B, keep, score=[[0.25] * B])
+    ends = coarse.clone()
+    ends[:, : V // 2] = -0.0                   # zeros of both signs are one logit
+    ends[:, V // 2:] = 0.0
+    check_select(ends, B, keep)
+    rows_alike = logits(9, 1, B, V, dtype, pad=3)   # alike at different alignments
+    rows_alike[:] = rows_alike[0].clone()
+    check_select(rows_alike, B, keep, score=[[0.25] * B])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_select_logits_of_every_size(dtype):
+    V, B = 3001, 3
+    g = torch.Generator().manual_seed(1)
+    for scale in (0.0, 1e-38, 1e-20, 100.0, 1e4, 1e30):
+        z = (torch.randn(B, V, generator=g) * scale).to(dtype).cuda()
+        if scale == 0.0:
+            z[1] = 1.0
+        check_select(z, B, 20, score=[[0.0, -1e3, 1e3]])
+    top = torch.finfo(dtype).max
+    z = torch.full((B, V), -top, dtype=dtype, device="cuda")
+    z[0, 5], z[1, 9], z[1, 3000] = top, 0.0, -1.0
+    check_select(z, B, 10)
+    # values that increase and decrease along a row, and one that lies apart
+    z = torch.linspace(-30, 30, V).repeat(B, 1)
+    z[1] = z[1].flip(0)
+    z[2] = 0.0
+    z[2, 77] = 90.0
+    check_select(z.to(dtype).cuda(), B, 50, score=[[0.0, -0.3, 5.0]])
+
+
+def test_select_values_close_together():
+    """Beams whose values differ by 2^-28: below what fp32 sums would tell apart."""
+    V, B = 6000, 8
+    g = torch.Generator().manual_seed(3)
+    z = (torch.randn(1, V, generator=g) * 3).to(BF).expand(B, V).contiguous()
+    score = np.array([[-k * 2.0 ** -28 for k in (3, 1, 7, 0, 2, 6, 5, 4)]])
+    check_select(z.cuda(), B, 64, score=score)
+    # rows that are alike but for the order of their tokens: Z differs by roundings alone
+    x = torch.stack([z[b][torch.randperm(V, generator=g)] for b in range(B)]).cuda()
+    check_select(x, B, 64, score=score)
+
+
+def test_select_outputs_and_neighbours():
+    """Given outputs, without flags; what lies around them stays."""
+    R, B, V, K = 3, 4, 500, 6
+    z = logits(2, R, B, V, BF)
+    bufs = [torch.full((R * K + 2,), 9, dtype=t, device="cuda")
+            for t in (torch.int32, torch.int32, F32, torch.uint8)]
+    outs = [b[1:-1].view(R, K) for b in bufs]
+    got = T.beam_select(z, B, K, eos=3, out=outs)
+    same_selection(got, ob.select(z.double().cpu().numpy(), B, K, eos=3))
+    assert all(b[0] == 9 and b[-1] == 9 for b in bufs)
+    again = T.beam_select(z, B, K, eos=3, out=(outs[0].clone(), outs[1].clone(), outs[2].clone(), None))
+    assert torch.equal(again[0], outs[0]) and torch.equal(again[2], outs[2]) and again[3] is None
+    empty = T.beam_select(torch.zeros(0, 5, device="cuda"), 3, 2)
+    assert empty[0].shape == (0, 2)
+
+
+# ------------------------------------------------------------------------- kv_reorder
+class Beams(Pair):
+    """A cache whose first sequences are histories and whose others are members of groups."""
+
+    def __init__(self, members, first=1, pages=200, blocks=12, H=2, D=64, layers=1, seed=0, prefix=None):
+        super().__init__(first + sum(members), pages, blocks, H, D, layers, seed)
+        self.offset = [first]
+        for n in members:
+            self.offset.append(self.offset[-1] + n)
+        self.prefix = prefix
+        self.groups = T.KvGroups(torch.tensor(self.offset, dtype=torch.int32).cuda(),
+                                 None if prefix is None else torch.tensor(prefix, dtype=torch.int32).cuda(),
+                                 max_members=max(members))
+
+    def reorder(self, parent):
+        T.kv_reorder(self.gpu, self.groups, torch.tensor(parent, dtype=torch.int32).cuda())
+        ob.reorder(self.ref, self.offset, parent)
+
+
+@pytest.mark.parametrize("D,H,layers", [(32, 3, 1), (64, 2, 3), (128, 1, 2)])
+def test_reorder(D, H, layers):
+    """Copies, permutations, cycles, members that are emptied, own places and places past the group."""
+    p = Beams([4, 1, 6, 3], first=2, H=H, D=D, layers=layers, seed=D)
+    p.grow([70, 5] + [1, 64, 63, 0] + [9] + [130, 127, 8, 64, 1, 200] + [7, 15, 16])
+    p.same()
+    p.reorder([1, 0, 3, 2] + [0] + [5, 0, 1, 2, 3, 4] + [2, 0, 1])      # cycles
+    p.same()
+    p.reorder([0, 0, 1, 9] + [3] + [2, 2, 2, 0, 0, 5] + [-1, 1, -7])    # copies, emptied
+    p.same()
+    p.grow([0, 0] + [1, 63, 64, 65] + [200] + [1, 60, 130, 0, 5, 64] + [3, 49, 0])   # each goes its own way
+    p.same()
+    p.reorder([3, 3, 3, 3] + [-1] + [1, 2, 3, 4, 5, 0] + [1, 2, 0])
+    p.same()
+    p.reorder([3, 3, 3])                                                # the others stay
+    p.same()
+    p.free([1] * p.seqs)
+    p.same()
+    assert int(p.gpu.refs.abs().sum()) == 0 and int((p.gpu.table != -1).sum()) == 0
+
+
+def test_reorder_after_a_trim():
+    p = Beams([3], first=1, H=1, D=32, layers=2, seed=4)
+    p.grow([10, 300, 200, 129])
+    p.trim(100, 0)
+    p.reorder([2, 0, 0])
+    p.same()
+    p.free([0, 1, 1, 0])
+    p.same()
+
+
+def test_reorder_random_steps():
+    g = np.random.default_rng(5)
+    members = [17, 32, 5]
+    p = Beams(members, first=1, pages=400, blocks=8, H=1, D=64, layers=2, seed=6)
+    for _ in range(8):
+        p.grow([int(x) for x in g.integers(0, 40, size=p.seqs)])
+        p.reorder([int(x) for n in members for x in g.integers(-1 if g.random() < 0.3 else 0, n, size=n)])
+        p.same()
+
+
+def test_reorder_many_members():
+    """A group of the most members, long tables, and a bound below the group's members."""
+    n = T.BEAMS_MAX
+    g = np.random.default_rng(7)
+    p = Beams([n], first=0, pages=3000, blocks=4, H=1, D=32, layers=1, seed=8)
+    p.grow([int(x) for x in g.integers(0, 200, size=n)])
+    p.reorder([int(x) for x in g.permutation(n)])
+    p.reorder([int(x) for x in g.integers(-1, n, size=n)])
+    p.same()
+    q = Beams([5], first=0, pages=3000, blocks=600, H=1, D=32, seed=9)
+    q.grow([64 * 590 + 3, 64 * 300, 1, 0, 64 * 599 + 63])
+    for order in ([4, 0, 1, 2, 3], [1, 1, 1, 1, 1]):
+        q.reorder(order)
+        q.same(content=False)
+    q.groups = T.KvGroups(q.groups.offset, max_members=3)
+    T.kv_reorder(q.gpu, q.groups, torch.tensor([2, 4, -1, -1, -1], dtype=torch.int32).cuda())
+    ob.reorder(q.ref, q.offset, [2, 4, -1, -1, -1], 3)
+    q.same(content=False)
+
+
+def test_reorder_leaves_what_is_out_of_range():
+    """Groups that are not among the sequences, and a table that names no page: nothing is touched out
+    of bounds, other groups are reordered."""
+    p = Beams([2, 2], first=1, H=1, D=32, seed=10)
+    p.grow([3, 70, 5, 130, 9])
+    odd = T.KvGroups(torch.tensor([1, 3, 9], dtype=torch.int32).cuda())
+    T.kv_reorder(p.gpu, odd, torch.tensor([1, 0, 1, 0], dtype=torch.int32).cuda())
+    ob.reorder(p.ref, [1, 3], [1, 0])
+    p.same()
+    for offset in ([-1, 2], [3, 1], [2, 2], [5, 6]):
+        T.kv_reorder(p.gpu, T.KvGroups(torch.tensor(offset, dtype=torch.int32).cuda()),
+                     torch.tensor([1, 0], dtype=torch.int32).cuda())
+    p.same()
+    p.gpu.table[2, 0], p.gpu.table[1, 0] = 10 ** 6, -5
+    T.kv_reorder(p.gpu, T.KvGroups(torch.tensor([1, 3], dtype=torch.int32).cuda()),
+                 torch.tensor([1, 0], dtype=torch.int32).cuda())
+    torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------------- kv_attend_prefix
+def attend(p, counts, heads, layer=0, mask=T.MASK_CAUSAL, window=0, sinks=0, scale=0.0, seed=1, ws=None,
+           max_count=None):
+    """Queries of every sequence (counts) against the oracle; rows of nobody stay as they were."""
+    g = torch.Generator().manual_seed(seed)
+    off = np.concatenate([[0], np.cumsum(counts)])
+    total = int(off[-1]) + 3                     # three rows behind the last sequence
+    q = rows(g, total, heads, p.D, scale=1.5)
+    out = torch.full((total, heads, p.D), 7.0, dtype=BF, device="cuda")
+    lse = torch.full((total, heads), 7.0, device="cuda")
+    T.kv_attend_prefix(p.gpu, layer, p.groups, q, torch.from_numpy(off).cuda(),
+                       max_count or max(counts), out=out, lse=lse, flags=mask, window=window,
+                       sinks=sinks, scale=scale, ws=ws)
+    torch.cuda.synchronize()
+    mine = torch.zeros(total, dtype=torch.bool)
+    for gi, (a, b) in enumerate(zip(p.offset, p.offset[1:])):
+        pre = p.prefix[gi] if 0 <= p.prefix[gi] < p.seqs else -1
+        for s in range(a, b):
+            n = int(off[s + 1] - off[s])
+            if n == 0:
+                continue
+            sl = slice(int(off[s]), int(off[s + 1]))
+            o, z, size, reach = ob.attend_prefix(p.ref, pre, s, layer, q[sl].double().cpu().numpy(),
+                                                 mask == T.MASK_CAUSAL, window, sinks, scale or None)
+            keys = p.ref.len[s] + (p.ref.len[pre] if pre >= 0 else 0)
+            vmax = max(p.vmax(s, layer), p.vmax(pre, layer) if pre >= 0 else 0.0)
+            tol, ltol = bound(o, size, reach, keys, p.D, HALF, vmax)
+            got = out[sl].double().cpu().numpy()
+            assert np.isfinite(got).all(), s
+            assert (np.abs(got - o) <= tol).all(), (s, float(np.max(np.abs(got - o) / tol)))
+            zz = lse[sl].double().cpu().numpy()
+            some = ~np.isinf(z)
+            assert np.isneginf(zz[~some]).all(), s
+            assert (np.abs(zz[some] - z[some]) <= ltol[some] + 2.0 ** -23 * np.abs(z[some])).all(), s
+            mine[sl] = True
+    rest = ~mine.cuda()
+    assert (out[rest] == 7.0).all() and (lse[rest] == 7.0).all()
+    return q, out, lse
+
+
+PREFIX = [
+    # prefix lengths, members, own lengths (repeated), queries each (repeated), heads, kv heads, D
+    ([1], [1], [1], [1], 1, 1, 64),
+    ([64], [2], [0, 1], [1], 2, 2, 32),
+    ([63, 0], [3, 2], [1, 64, 63], [1], 4, 2, 64),
+    ([129, 300], [8, 5], [3, 2, 1, 7], [1], 4, 4, 64),
+    ([1000], [16], [2, 20], [1], 8, 2, 64),
+    ([500, 65, 700], [3, 1, 20], [5, 70, 128, 200], [1, 3, 2], 8, 4, 128),
+    ([640], [40], [6], [2], 2, 2, 32),
+    ([2100, 90], [33, 7], [1, 65], [1], 4, 1, 64),
+    ([200], [2], [90, 30], [25, 40], 8, 2, 32),
+    ([777], [70], [4, 3], [1], 2, 1, 128),
+    ([5000], [5], [9], [1], 4, 4, 64),
+    ([1500], [100], [9], [1, 2], 8, 1, 64),
+]
+
+
+@pytest.mark.parametrize("lens,members,owns,ns,heads,kv_heads,D", PREFIX)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 5)])
+def test_attend_prefix(lens, members, owns, ns, heads, kv_heads, D, window, sinks):
+    print(f"prefix {lens} members {members} heads {heads}/{kv_heads} D {D} window {window}", flush=True)
+    M = sum(members)
+    p = Beams(members, first=len(lens), pages=400, blocks=90, H=kv_heads, D=D, seed=M,
+              prefix=list(range(len(lens))))
+    p.grow(lens + [owns[i % len(owns)] for i in range(M)])
+    counts = [0] * len(lens) + [ns[i % len(ns)] for i in range(M)]
+    for mask in (T.MASK_CAUSAL, T.MASK_NONE):
+        attend(p, counts, heads, mask=mask, window=window, sinks=sinks, seed=M + window)
+
+
+def test_attend_prefix_groups_of_every_kind():
+    """No prefix, an empty one, a sequence that is none, one that another group shares, members without
+    queries or tokens, more queries than own tokens; sequences of no group have queries too."""
+    p = Beams([2, 3, 2, 4, 1], first=3, H=2, D=64, seed=2, prefix=[-1, 1, 99, 0, 0])
+    p.grow([200, 0, 70] + [5, 130, 0, 1, 64, 3, 0, 10, 9, 0, 2, 66])
+    counts = [2, 1, 3] + [1, 4, 1, 0, 2, 1, 1, 3, 12, 2, 0, 1]
+    for mask in (T.MASK_CAUSAL, T.MASK_NONE):
+        for window, sinks in ((0, 0), (1, 0), (40, 130), (210, 3)):
+            attend(p, counts, 4, mask=mask, window=window, sinks=sinks, seed=window)
+
+
+def test_attend_prefix_released_blocks():
+    """Blocks of the prefix and of members that were given up are not seen."""
+    p = Beams([3, 2], first=2, H=1, D=64, layers=2, seed=3, prefix=[1, 0])
+    p.grow([300, 500, 200, 10, 140, 64, 300])
+    p.trim(100, 65)
+    for layer in (0, 1):
+        attend(p, [0, 0, 1, 1, 2, 1, 1], 2, layer=layer)
+        attend(p, [0, 0, 1, 1, 2, 1, 1], 2, layer=layer, window=90, sinks=65)
+    p.trim(1, 0)
+    attend(p, [0, 0, 1, 1, 2, 1, 1], 2, layer=1, mask=T.MASK_NONE)
+
+
+@pytest.mark.parametrize("max_len,max_own", [(0, 0), (100, 1), (100000, 5000)])
+def test_attend_prefix_estimates_only_divide_the_work(max_len, max_own):
+    p = Beams([9, 2], first=2, blocks=30, H=2, D=64, seed=4, prefix=[0, 1])
+    p.grow([1500, 130] + [20, 70, 5, 64, 300, 1, 2, 3, 4, 9, 8])
+    p.gpu.max_len, p.groups.max_own = max_len, max_own
+    for window in (0, 300):
+        attend(p, [0, 0] + [1] * 11, 4, window=window, sinks=2)
+
+
+def test_attend_prefix_extreme_scores():
+    """One-hot softmaxes, in the prefix and in the own tokens; values of very different sizes."""
+    for spread in (1e-30, 40.0, 1e4):
+        p = Beams([6], first=1, H=2, D=64, seed=5, prefix=[0])
+        p.grow([330, 1, 2, 70, 64, 10, 0], spread=spread)
+        attend(p, [0] + [1] * 6, 4, scale=1e-3 if spread > 1e3 else 0.0)
+
+
+def test_attend_prefix_as_one_sequence():
+    """The same tokens as prefix and own tokens, and as one sequence that kv_attend takes."""
+    H, D, heads = 2, 64, 4
+    p = Beams([1], first=1, H=H, D=D, seed=6, prefix=[0])
+    p.grow([256, 70])
+    one = Pair(1, 20, 8, H, D, seed=6)
+    kv = np.stack([p.ref.k[0] + p.ref.k[1], p.ref.v[0] + p.ref.v[1]])[:, :, 0]      # [2, 326, H, D]
+    kv = torch.from_numpy(np.concatenate([kv[0], kv[1]], axis=1)).to(BF).cuda()
+    T.kv_extend(one.gpu, torch.tensor([326], dtype=torch.int32).cuda())
+    T.kv_append(one.gpu, 0, kv[:, :H], kv[:, H:], torch.zeros(1, dtype=torch.int64).cuda(), 326)
+    q, out, lse = attend(p, [0, 3], heads, window=100, sinks=9)
+    z = torch.empty(6, heads, device="cuda")
+    o = T.kv_attend(one.gpu, 0, q, torch.tensor([0, 3]).cuda(), 3, lse=z, window=100, sinks=9)
+    assert (out[:3].float() - o[:3].float()).abs().max() <= 2.0 ** -6 * o[:3].abs().max()
+    assert (lse[:3] - z[:3]).abs().max() <= 1e-5
+
+
+def test_attend_prefix_row_bits_do_not_depend_on_neighbours():
+    """A member's rows with and without other members' queries (a tile of the same height)."""
+    p = Beams([5], first=1, H=1, D=64, seed=7, prefix=[0])
+    p.grow([700, 3, 3, 3, 70, 3])
+    g = torch.Generator().manual_seed(1)
+    q = rows(g, 5, 2, 64)
+    call = lambda q, counts: T.kv_attend_prefix(
+        p.gpu, 0, p.groups, q, torch.from_numpy(np.concatenate([[0], np.cumsum([0] + counts)])).cuda(), 1)
+    both = call(q, [1, 1, 1, 1, 1])
+    for i in range(5):
+        other = q.clone() * 30
+        other[i] = q[i]
+        assert torch.equal(call(other, [1] * 5)[i], both[i])
+
+
+# ------------------------------------------------------------------------- together
+def test_a_search():
+    """Steps of a search as they are made: reorder, extend, append, attend, select; against the oracle."""
+    R, B, V, H, D, heads = 2, 6, 90, 2, 64, 4
+    p = Beams([B] * R, first=R, pages=300, blocks=8, H=H, D=D, layers=2, seed=8, prefix=[0, 1])
+    p.grow([400, 130] + [0] * (R * B))
+    g = np.random.default_rng(9)
+    z = logits(0, R, 1, V, BF, spread=3.0)
+    got = check_select(z, 1, B, eos=7)
+    ws = T.Workspace()
+    for step in range(70):
+        score, done = got[2], got[3]
+        p.grow([0] * R + [1] * (R * B))
+        if step % 23 == 0 or 61 <= step <= 66:
+            attend(p, [0] * R + [1] * (R * B), heads, layer=step % 2, seed=step, ws=ws)
+        z = logits(step + 1, R, B, V, BF, spread=3.0)
+        place = step % 2 == 0
+        want = ob.select(z.double().cpu().numpy(), B, B, score.cpu().numpy(), done.cpu().numpy(), eos=7,
+                         in_place=place)
+        got = T.beam_select(z, B, B, score=score, done=done, eos=7, ws=ws,
+                            flags=T.BEAM_IN_PLACE if place else T.BEAM_RANKED)
+        torch.cuda.synchronize()
+        same_selection(got, want)
+        T.kv_reorder(p.gpu, p.groups, got[0])
+        ob.reorder(p.ref, p.offset, got[0].flatten().tolist())
+        if step % 10 == 0:
+            p.same()
+    p.same()
+
+
+def test_a_step_in_a_graph():
+    """reorder + extend + append + attend + select captured, replayed between eager work, each replay
+    against the eager calls on a second cache."""
+    R, B, V, H, D, heads = 2, 4, 300, 2, 64, 4
+    M = R * B
+    a, b = (Beams([B] * R, first=R, pages=100, blocks=8, H=H, D=D, seed=11, prefix=[0, 1])
+            for _ in range(2))
+    for p in (a, b):
+        p.grow([300, 130] + [60] * M)
+    g = torch.Generator().manual_seed(2)
+    count = torch.tensor([0] * R + [1] * M, dtype=torch.int32).cuda()
+    off = torch.tensor([0] * R + list(range(M + 1))).cuda()
+    kv, q = rows(g, M, 2 * H, D), rows(g, M, heads, D)
+    z = logits(3, R, B, V, BF)
+    state = [torch.arange(B, dtype=torch.int32).repeat(R, 1).cuda(), torch.zeros(R, B, dtype=torch.int32).cuda(),
+             torch.zeros(R, B).cuda(), torch.zeros(R, B, dtype=torch.uint8).cuda()]
+
+    def step(p, st, out, lse, ws):
+        T.kv_reorder(p.gpu, p.groups, st[0])
+        T.kv_extend(p.gpu, count)
+        T.kv_append(p.gpu, 0, kv[:, :H], kv[:, H:], off, 1)
+        T.kv_attend_prefix(p.gpu, 0, p.groups, q, off, 1, out=out, lse=lse, ws=ws)
+        new = T.beam_select(z, B, B, score=st[2], done=st[3], eos=5, ws=ws)
+        for x, y in zip(st, new):
+            x.copy_(y)
+
+    outs = [(torch.zeros(M, heads, D, dtype=BF, device="cuda"), torch.zeros(M, heads, device="cuda"))
+            for _ in range(2)]
+    sts = [[x.clone() for x in state] for _ in range(2)]
+    wss = [T.Workspace(), T.Workspace()]
+    for i, p in enumerate((a, b)):                # sizes the workspaces
+        step(p, sts[i], *outs[i], wss[i])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a, sts[0], *outs[0], wss[0])
+    for i in range(12):
+        z.copy_(logits(50 + i, R, B, V, BF))
+        q.copy_(rows(g, M, heads, D))
+        kv.copy_(rows(g, M, 2 * H, D))
+        graph.replay()
+        step(b, sts[1], *outs[1], wss[1])
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1]), i
+        assert all(torch.equal(x, y) for x, y in zip(*sts)), i
+        assert torch.equal(a.gpu.table, b.gpu.table) and torch.equal(a.gpu.refs, b.gpu.refs), i
+        assert torch.equal(a.gpu.length, b.gpu.length)
+
+
+def test_on_another_stream():
+    p = Beams([4], first=1, H=1, D=32, seed=12, prefix=[0])
+    p.grow([100, 3, 4, 5, 70])
+    g = torch.Generator().manual_seed(3)
+    q, z = rows(g, 4, 2, 32), logits(4, 2, 4, 5000, F32)
+    off = torch.tensor([0, 0, 1, 2, 3, 4]).cuda()
+    eager = T.kv_attend_prefix(p.gpu, 0, p.groups, q, off, 1), T.beam_select(z, 4, 9)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    other = (T.kv_attend_prefix(p.gpu, 0, p.groups, q, off, 1, stream=s), T.beam_select(z, 4, 9, stream=s))
+    T.kv_reorder(p.gpu, p.groups, torch.tensor([3, 2, 1, 0], dtype=torch.int32).cuda(), stream=s)
+    s.synchronize()
+    assert torch.equal(eager[0], other[0])
+    assert all(torch.equal(x, y) for x, y in zip(eager[1], other[1]))
+    ob.reorder(p.ref, p.offset, [3, 2, 1, 0])
+    p.same()
