@@ -13,6 +13,7 @@
 // request's continuations.
 #include <float.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -62,23 +63,70 @@ __device__ __forceinline__ float logit(const BeamArgs& a, int64_t row, int v) {
   return __builtin_isfinite(z) ? z : NONE;
 }
 
-// 2^t for t <= 0 or so: 2^n times a polynomial of f = t - n, |f| <= 1/2, that is off by at most 8e-13 of 2^f (fitted
-// to the relative error's maximum).  Far below 0: 0.
-__device__ __forceinline__ double exp2_neg(double t) {
-  const double n = __builtin_rint(t), f = t - n;
-  double p = 1.3175854784954272e-06;
-  p = __builtin_fma(p, f, 1.530973767019622e-05);
-  p = __builtin_fma(p, f, 1.5403851768737496e-04);
-  p = __builtin_fma(p, f, 1.333345206150456e-03);
-  p = __builtin_fma(p, f, 9.61812854282085e-03);
-  p = __builtin_fma(p, f, 5.550410939341938e-02);
-  p = __builtin_fma(p, f, 0.24022650698880715);
-  p = __builtin_fma(p, f, 0.6931471805465146);
-  p = __builtin_fma(p, f, 0.9999999999997632);
-  return __builtin_ldexp(p, int(n));
+// 2^f for |f| <= 1/2, off by at most 4.7e-11 of it (2^-34; fitted to the relative error's maximum, exact at 0), times 2^(the
+// low 32 bits of k): added to the exponent, as what converts or scales 64-bit numbers takes several times as long.
+__device__ __forceinline__ double exp2_part(double f, double k) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  double p = 1.5196156439583103e-05;
+  p = __builtin_fma(p, f, 1.5466756326706064e-04);
+  p = __builtin_fma(p, f, 1.3333935055974677e-03);
+  p = __builtin_fma(p, f, 9.618038132024047e-03);
+  p = __builtin_fma(p, f, 5.5504103659910264e-02);
+  p = __builtin_fma(p, f, 0.24022651066561432);
+  p = __builtin_fma(p, f, 0.6931471807045319);
+  p = __builtin_fma(p, f, 1.0);
+  u32x2 u = __builtin_bit_cast(u32x2, p);
+  u.y += __builtin_bit_cast(u32x2, k).x << 20;
+  return __builtin_bit_cast(double, u);
+}
+constexpr double LOG2E_64 = 1.4426950408889634074;
+constexpr double ROUND = 6755399441055744.0;   // 1.5 2^52: a sum with it is rounded to a whole number, which its low bits hold
+
+// exp(x - m) for x <= m, where x is not there 0 or next to it.
+__device__ __forceinline__ double weight(float x, double m) {
+  const double d = __builtin_fmax(double(x) - m, -700.0), k = __builtin_fma(d, LOG2E_64, ROUND);
+  return exp2_part(__builtin_fma(d, LOG2E_64, -(k - ROUND)), k);
 }
 
-constexpr double LOG2E_64 = 1.4426950408889634074;
+// v joined over a wave's lanes by op, alike in all of them, on the vector unit alone: neighbours in fours, eights and
+// sixteens, then the halves (a third of the time that six passes through LDS take).
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane_move(uint32_t v) {
+  return uint32_t(__builtin_amdgcn_update_dpp(int(v), int(v), CTRL, 0xF, 0xF, false));
+}
+template <class T, class Op>
+__device__ __forceinline__ T wave_all(T v, Op op) {
+  constexpr int N = sizeof(T) / 4;
+  struct Words { uint32_t w[N]; };
+  auto moved = [](T x, auto f) {
+    Words a = __builtin_bit_cast(Words, x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) a.w[i] = f(a.w[i]);
+    return __builtin_bit_cast(T, a);
+  };
+  v = op(v, moved(v, [](uint32_t w) { return lane_move<0xB1>(w); }));    // 1 0 3 2
+  v = op(v, moved(v, [](uint32_t w) { return lane_move<0x4E>(w); }));    // 2 3 0 1
+  v = op(v, moved(v, [](uint32_t w) { return lane_move<0x141>(w); }));   // 7 - i of eight
+  v = op(v, moved(v, [](uint32_t w) { return lane_move<0x140>(w); }));   // 15 - i of sixteen
+  T a = v, b = v;
+  auto swap = [&](auto f) {
+    Words x = __builtin_bit_cast(Words, v), y = x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const auto r = f(x.w[i]);
+      x.w[i] = r[0];
+      y.w[i] = r[1];
+    }
+    a = __builtin_bit_cast(T, x);
+    b = __builtin_bit_cast(T, y);
+  };
+  swap([](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false); });
+  v = op(a, b);
+  swap([](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false); });
+  return op(a, b);
+}
+__device__ __forceinline__ float wave_max(float v) { return wave_all(v, [](float a, float b) { return vmax(a, b); }); }
+__device__ __forceinline__ double wave_sum(double v) { return wave_all(v, [](double a, double b) { return a + b; }); }
 
 // A segment of a row: each lane's largest logit that may be selected, and, alike in all lanes, the segment's
 // largest logit and sum.
@@ -94,34 +142,59 @@ __device__ __forceinline__ Segment scan(const BeamArgs& a, int64_t row, int seg)
   const typename L::T* const p = static_cast<const typename L::T*>(a.b.logits) + row * a.b.ld;
   const int v0 = seg * SEG + lane * EL;   // of load i: + i 64 EL
   float z[VPT][EL];
+  typename L::piece w[VPT];
   if (seg * SEG + SEG <= V) {
-    typename L::piece w[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
       w[i] = *reinterpret_cast<const typename L::piece*>(p + v0 + i * WAVE * EL);
+  } else if (V >= EL) {
+    // the row ends in this segment: its last 16 bytes in place of those that pass it, moved to where they would stand
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
+      w[i] = *reinterpret_cast<const typename L::piece*>(p + min(v0 + i * WAVE * EL, V - EL));
 #pragma unroll
-      for (int e = 0; e < EL; ++e)
-        z[i][e] = __uint_as_float(!BF ? w[i][e] : e % 2 ? w[i][e / 2] & 0xFFFF0000u : w[i][e / 2] << 16);
+    for (int i = 0; i < VPT; ++i) {
+      const int past = v0 + i * WAVE * EL - (V - EL);   // tokens
+      const auto bits = __builtin_bit_cast(unsigned __int128, w[i]);
+      w[i] = __builtin_bit_cast(typename L::piece, past > 0 ? bits >> (past < EL ? past * (128 / EL) : 127) : bits);
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i)
-#pragma unroll
-      for (int e = 0; e < EL; ++e) {
-        const int v = v0 + i * WAVE * EL + e;
-        z[i][e] = v < V ? L::one(p + v) : NONE;
+    for (int i = 0; i < VPT; ++i) w[i] = (typename L::piece){0, 0, 0, 0};
+    if (v0 < V)
+      for (int v = 0; v < V; ++v) {   // (the first lane has them all)
+        const uint32_t u = __float_as_uint(L::one(p + v));
+        w[0][BF ? v / 2 : v] |= !BF || v % 2 ? u : u >> 16;
       }
   }
-  Segment r;
-  float top = NONE;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+#pragma unroll
+    for (int e = 0; e < EL; ++e)
+      z[i][e] = __uint_as_float(!BF ? w[i][e] : e % 2 ? w[i][e / 2] & 0xFFFF0000u : w[i][e / 2] << 16);
+  }
+  // the largest and the least, NaN where one is; what is no finite number is not there
+  float top = z[0][0], low = z[0][0];
 #pragma unroll
   for (int i = 0; i < VPT; ++i)
 #pragma unroll
     for (int e = 0; e < EL; ++e) {
-      z[i][e] = __builtin_isfinite(z[i][e]) ? z[i][e] : NONE;
       top = vmax(top, z[i][e]);
+      low = __builtin_elementwise_minimum(low, z[i][e]);
     }
+  const bool odd = !(top < INFINITY && low > -INFINITY);
+  if (seg * SEG + SEG > V || __any(odd)) {
+    top = NONE;
+    low = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int e = 0; e < EL; ++e) {
+        z[i][e] = v0 + i * WAVE * EL + e < V && __builtin_isfinite(z[i][e]) ? z[i][e] : NONE;
+        top = vmax(top, z[i][e]);
+      }
+  }
+  Segment r;
   r.best = top;
   if (a.b.allowed) {
     const uint8_t* const ok = a.b.allowed + row * a.b.allowed_ld;
@@ -134,20 +207,28 @@ __device__ __forceinline__ Segment scan(const BeamArgs& a, int64_t row, int seg)
       for (int e = 0; e < EL; ++e) r.best = bits >> e & 1 ? vmax(r.best, z[i][e]) : r.best;
     }
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) top = vmax(top, __shfl_xor(top, o, WAVE));
+  top = wave_max(top);
   r.top = top;
   double s = 0.0;
-  if (top > NONE) {
-    const double m = top;
+  const double m = top;
+  if (__all(low >= top - 700.f && __builtin_fabsf(top) < 16384.f)) {
+    // the usual sizes: exp(z) against 2^N next to exp(m), two instructions less for each
+    const double N = __builtin_rint(m * LOG2E_64), R = ROUND - N;
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
-      for (int e = 0; e < EL; ++e) s += exp2_neg(__builtin_fmax(double(z[i][e]) - m, -1e4) * LOG2E_64);
-  }
+      for (int e = 0; e < EL; ++e) {
+        const double x = z[i][e], k = __builtin_fma(x, LOG2E_64, R);
+        s += exp2_part(__builtin_fma(x, LOG2E_64, -(k - R)), k);
+      }
+    s *= exp2_part(__builtin_fma(m, -LOG2E_64, N), ROUND);
+  } else if (top > NONE) {
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, WAVE);
-  r.sum = s;
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int e = 0; e < EL; ++e) s += weight(z[i][e], m);
+  }
+  r.sum = wave_sum(s);
   return r;
 }
 
@@ -162,9 +243,7 @@ __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
   const Segment r = scan<BF, VPT>(a, row, seg);
   const int64_t at = row * a.segs + seg;
   a.best[at * WAVE + threadIdx.x % WAVE] = r.best;
-  float b = r.best;
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) b = vmax(b, __shfl_xor(b, o, WAVE));
+  const float b = wave_max(r.best);
   if (threadIdx.x % WAVE == 0) {
     a.seg_sum[at] = r.sum;
     a.seg_top[at] = r.top;
@@ -185,7 +264,7 @@ __device__ __forceinline__ uint32_t near_key(double x) { return score_key(float(
 
 constexpr int PICK = 1024;    // threads
 constexpr int NW = PICK / WAVE;
-constexpr int BINS = 2048;
+constexpr int BIN_BITS = 11, BINS = 1 << BIN_BITS;
 constexpr int CAP = 2048;     // continuations that are put in order at last
 constexpr int LIST = 4096;    // segments, and then groups, that may hold some of the best
 
@@ -214,12 +293,15 @@ struct PickShared {
 __device__ __forceinline__ void find_bin(PickShared& sh, uint32_t need) {
   const int tid = threadIdx.x, lane = tid % WAVE, wid = tid / WAVE;
   const uint32_t c0 = sh.bins[BINS - 1 - 2 * tid], c1 = sh.bins[BINS - 2 - 2 * tid];
+  // the sum over the lanes up to this one: within sixteen by shifts of 1, 2, 4 and 8 (0x110 + n), then from lane 15 of each
+  // sixteen to the next (0x142), and from lane 31 to the upper half (0x143)
   uint32_t v = c0 + c1;
-#pragma unroll
-  for (int o = 1; o < WAVE; o <<= 1) {
-    const uint32_t u = __shfl_up(v, o, WAVE);
-    if (lane >= o) v += u;
-  }
+  v += __builtin_amdgcn_update_dpp(0, int(v), 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, int(v), 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, int(v), 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, int(v), 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, int(v), 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, int(v), 0x143, 0xC, 0xF, false);
   if (lane == WAVE - 1) sh.wsum[wid] = v;
   if (tid == 0) sh.bin = BINS;
   __syncthreads();
@@ -244,16 +326,15 @@ __device__ __forceinline__ uint32_t bound_of(PickShared& sh, Visit visit, uint32
     if (k) lo = min(lo, k);
     hi = max(hi, k);
   });
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    lo = min(lo, uint32_t(__shfl_xor(int(lo), o, WAVE)));
-    hi = max(hi, uint32_t(__shfl_xor(int(hi), o, WAVE)));
-  }
+  lo = wave_all(lo, [](uint32_t a, uint32_t b) { return min(a, b); });
+  hi = wave_all(hi, [](uint32_t a, uint32_t b) { return max(a, b); });
   if (tid % WAVE == 0) {
     sh.wmin[tid / WAVE] = lo;
     sh.wmax[tid / WAVE] = hi;
   }
+  for (int i = tid; i < BINS; i += PICK) sh.bins[i] = 0;
   __syncthreads();
+#pragma unroll
   for (int w = 0; w < NW; ++w) {
     lo = min(lo, sh.wmin[w]);
     hi = max(hi, sh.wmax[w]);
@@ -261,10 +342,7 @@ __device__ __forceinline__ uint32_t bound_of(PickShared& sh, Visit visit, uint32
   if (hi == 0) return 1;
   uint32_t above = 0;
   while (true) {
-    int shift = 0;
-    while ((hi - lo) >> shift >= BINS) ++shift;
-    for (int i = tid; i < BINS; i += PICK) sh.bins[i] = 0;
-    __syncthreads();
+    const int shift = max(0, 32 - __builtin_clz(hi - lo | 1) - BIN_BITS);
     visit([&](uint32_t k) {
       if (k >= lo && k <= hi && k) atomicAdd(&sh.bins[(k - lo) >> shift], 1u);
     });
@@ -277,61 +355,36 @@ __device__ __forceinline__ uint32_t bound_of(PickShared& sh, Visit visit, uint32
     hi = min(hi, h);
     __syncthreads();
     if (above + in <= most || shift == 0) return lo;
+    for (int i = tid; i < BINS; i += PICK) sh.bins[i] = 0;
+    __syncthreads();
   }
 }
 
-// A workgroup a request.
-template <bool BF>
-__global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
+// A beam's base, from its row's largest logit and its sum of exponentials.
+__device__ __forceinline__ double base_of(const BeamArgs& a, int64_t n, float top, double sum) {
+  const float s = a.b.score ? a.b.score[n] : 0.f;
+  if (!__builtin_isfinite(s)) return __builtin_nan("");
+  if (a.b.done && a.b.done[n]) return s;
+  return top > NONE ? double(s) - (double(top) + log(sum)) : __builtin_nan("");
+}
+
+// What a segment or a group of beam b holds at best, of which z is the largest logit; a finished beam's one
+// continuation counts as its first one's.
+__device__ __forceinline__ uint32_t best_key(double base, bool done, bool first, float z) {
+  if (done) return first && base == base ? near_key(base) : 0;
+  return base == base && z > NONE ? near_key(base + double(z)) : 0;
+}
+
+// The selection of a request, whose bases are in sh.  visit(f) calls f(key, group) for the groups that hold all of the
+// best; a group is (beam * segments + segment) * 64 + lane.
+template <bool BF, class Visit>
+__device__ __forceinline__ void pick(const BeamArgs& a, PickShared& sh, int64_t row0, uint32_t bound, bool fits, Visit visit) {
   constexpr int EL = Logits<BF>::EL;
-  __shared__ PickShared sh;
   const int B = a.b.beams, V = a.b.vocab, K = a.keep, S = a.segs;
   const int tid = threadIdx.x, lane = tid % WAVE, wid = __builtin_amdgcn_readfirstlane(tid / WAVE);
-  const int64_t row0 = int64_t(blockIdx.x) * B;
   const int eos0 = a.b.eos < 0 ? 0 : a.b.eos;
   const uint8_t* const done = a.b.done ? a.b.done + row0 : nullptr;
-  // the beams' bases: a wave a beam
-  for (int b = wid; b < B; b += NW) {
-    const float s = a.b.score ? a.b.score[row0 + b] : 0.f;
-    double x = __builtin_nan("");
-    if (__builtin_isfinite(s)) {
-      if (done && done[b]) {
-        x = s;
-      } else {
-        const float* const tops = a.seg_top + (row0 + b) * S;
-        const double* const sums = a.seg_sum + (row0 + b) * S;
-        float m = NONE;
-        for (int i = lane; i < S; i += WAVE) m = vmax(m, tops[i]);
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) m = vmax(m, __shfl_xor(m, o, WAVE));
-        double z = 0.0;
-        for (int i = lane; i < S; i += WAVE)
-          z += sums[i] * exp2_neg(__builtin_fmax(double(tops[i]) - double(m), -1e4) * LOG2E_64);
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) z += __shfl_xor(z, o, WAVE);
-        if (m > NONE) x = double(s) - (double(m) + log(z));
-      }
-    }
-    if (lane == 0) sh.base[b] = x;
-  }
-  __syncthreads();
-
-  // what segment s of beam b, and lane l's group of it, hold at best; a finished beam's one continuation counts as its first
-  // segment's first group
-  auto seg_key = [&](int b, int s) -> uint32_t {
-    const double x = sh.base[b];
-    if (x != x) return 0;
-    if (done && done[b]) return s == 0 ? near_key(x) : 0;
-    const float z = a.seg_best[(row0 + b) * S + s];
-    return z > NONE ? near_key(x + double(z)) : 0;
-  };
-  auto group_key = [&](int b, int s, int l) -> uint32_t {
-    const double x = sh.base[b];
-    if (x != x) return 0;
-    if (done && done[b]) return s == 0 && l == 0 ? near_key(x) : 0;
-    const float z = a.best[((row0 + b) * S + s) * WAVE + l];
-    return z > NONE ? near_key(x + double(z)) : 0;
-  };
+  const uint32_t total = uint32_t(B) * uint32_t(V);   // below 2^31
   // the key of beam b continued by v
   auto key_of = [&](int b, int v) -> uint64_t {
     const double x = sh.base[b];
@@ -349,63 +402,56 @@ __global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
       sh.flats[at] = flat;
     }
   };
-
-  const uint32_t total = uint32_t(B) * uint32_t(V), segs = uint32_t(B) * uint32_t(S);   // below 2^31
-  bool fits = true;
-  uint32_t bound = 1;
-  if (segs >= 2 * uint32_t(K))
-    bound = bound_of(sh, [&](auto f) {
-      for (uint32_t i = tid; i < segs; i += PICK) f(seg_key(i / S, i % S));
-    }, K, K + K / 4);
-  if (tid == 0) sh.n = 0;
-  __syncthreads();
-  for (uint32_t i = tid; i < segs; i += PICK) {
-    if (seg_key(i / S, i % S) < bound) continue;
-    const uint32_t at = atomicAdd(&sh.n, 1u);
-    if (at < LIST) sh.segs[at] = i;
-  }
-  __syncthreads();
-  const uint32_t n_segs = sh.n;
-  fits = n_segs <= LIST;
-  if (fits) {
-    auto groups = [&](auto f) {
-#pragma unroll 4
-      for (uint32_t i = wid; i < n_segs; i += NW) {
-        const uint32_t s = sh.segs[i];
-        f(group_key(s / S, s % S, lane));
-      }
-    };
-    bound = max(bound, bound_of(sh, groups, K, K + K / 8));
-    __syncthreads();
+  uint32_t n_groups = 0;
+  auto list_groups = [&]() {
     if (tid == 0) sh.n = 0;
     __syncthreads();
-    for (uint32_t i = wid; i < n_segs; i += NW) {
-      const uint32_t s = sh.segs[i];
-      if (group_key(s / S, s % S, lane) < bound) continue;
+    visit([&](uint32_t k, uint32_t g) {
+      if (k < bound) return;
       const uint32_t at = atomicAdd(&sh.n, 1u);
-      if (at < LIST) sh.groups[at] = s * WAVE + lane;
-    }
+      if (at < LIST) sh.groups[at] = g;
+    });
     __syncthreads();
-    const uint32_t n_groups = sh.n;
+    n_groups = sh.n;
+    __syncthreads();
+  };
+  // (the groups' own bound where the segments' leaves too many, or there is none)
+  if (fits && bound > 1) list_groups();
+  if (fits && (bound == 1 || n_groups > 2 * uint32_t(K) + 64)) {
+    bound = max(bound, bound_of(sh, [&](auto f) { visit([&](uint32_t k, uint32_t) { f(k); }); }, K, K + K / 8));
+    list_groups();
+  }
+  if (fits) {
     fits = n_groups <= LIST;
-    __syncthreads();
     if (tid == 0) sh.n = 0;
     __syncthreads();
     if (fits) {
-      // a group's tokens: those of one load are neighbours
+      // a wave a group, four at once, so that their loads are on the way together; a group's tokens: those of one load are
+      // neighbours
       const int i = lane / EL, e = lane % EL;
-#pragma unroll 2
-      for (uint32_t k = wid; k < n_groups; k += NW) {
-        const uint32_t g = sh.groups[k], s = g / WAVE;
-        const int b = int(s / S), seg = int(s % S);
-        if (done && done[b]) {
-          if (lane == 0) list(value_key(sh.base[b]), uint32_t(b) * V + eos0);
-          continue;
+      for (uint32_t k0 = wid; k0 < n_groups; k0 += 4 * NW) {
+        int beam[4], v[4];
+        float z[4];
+        uint32_t ok[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t g = sh.groups[min(k0 + u * NW, n_groups - 1)], s = g / WAVE;
+          beam[u] = int(s / S);
+          v[u] = (int(s % S) * a.vpt + i) * (WAVE * EL) + int(g % WAVE) * EL + e;
+          if (k0 + u * NW >= n_groups || i >= a.vpt || v[u] >= V) v[u] = -1;
+          const int at = max(v[u], 0);
+          z[u] = logit<BF>(a, row0 + beam[u], at);
+          ok[u] = a.b.allowed ? a.b.allowed[(row0 + beam[u]) * a.b.allowed_ld + at / 8] >> (at % 8) & 1 : 1;
         }
-        const int v = (seg * a.vpt + i) * (WAVE * EL) + int(g % WAVE) * EL + e;
-        if (i >= a.vpt || v >= V) continue;
-        const uint64_t x = key_of(b, v);
-        if (x && near_key(key_value(x)) >= bound) list(x, uint32_t(b) * V + v);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const double base = sh.base[beam[u]];
+          if (done && done[beam[u]]) {
+            if (lane == 0 && k0 + u * NW < n_groups) list(value_key(base), uint32_t(beam[u]) * V + eos0);
+          } else if (v[u] >= 0 && ok[u] && z[u] > NONE && near_key(base + double(z[u])) >= bound) {
+            list(value_key(base + double(z[u])), uint32_t(beam[u]) * V + v[u]);
+          }
+        }
       }
     }
     __syncthreads();
@@ -466,12 +512,21 @@ __global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
   for (int k = tid; k < K; k += PICK) sh.parent[k] = -1;
   for (int b = tid; b < TAV2_BEAMS_MAX; b += PICK) sh.first_of[b] = TAV2_K_MAX;
   __syncthreads();
-  for (uint32_t i = tid; i < n; i += PICK) {
+  // sixteen threads each, which look at every sixteenth
+  for (uint32_t i0 = 0; i0 < n; i0 += PICK / 16) {
+    const uint32_t i = min(i0 + tid / 16, n - 1), f = sh.flats[i];
     const uint64_t k = sh.keys[i];
-    const uint32_t f = sh.flats[i];
     uint32_t rank = 0;
-    for (uint32_t j = 0; j < n; ++j) rank += sh.keys[j] > k || (sh.keys[j] == k && sh.flats[j] < f);
-    if (rank < uint32_t(K)) {
+#pragma unroll 4
+    for (uint32_t j = tid % 16; j < n; j += 16) {
+      const uint64_t kj = sh.keys[j];
+      rank += kj > k || (kj == k && sh.flats[j] < f);
+    }
+    rank += lane_move<0xB1>(rank);
+    rank += lane_move<0x4E>(rank);
+    rank += lane_move<0x141>(rank);
+    rank += lane_move<0x140>(rank);
+    if (tid % 16 == 0 && i0 + tid / 16 < n && rank < uint32_t(K)) {
       sh.parent[rank] = int(f / V);
       sh.token[rank] = int(f % V);
       sh.value[rank] = key_value(k);
@@ -507,6 +562,127 @@ __global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
   if (a.done) a.done[at] = p >= 0 && (was || (a.b.eos >= 0 && sh.token[tid] == a.b.eos));
 }
 
+// A workgroup a request, whose segments the first launch took.
+template <bool BF>
+__global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
+  __shared__ PickShared sh;
+  const int B = a.b.beams, K = a.keep, S = a.segs;
+  const int tid = threadIdx.x, lane = tid % WAVE, wid = __builtin_amdgcn_readfirstlane(tid / WAVE);
+  const int64_t row0 = int64_t(blockIdx.x) * B;
+  const uint8_t* const done = a.b.done ? a.b.done + row0 : nullptr;
+  const float* const seg_best = a.seg_best + row0 * S;
+  const float* const best = a.best + row0 * S * WAVE;
+  // the beams' bases: a wave a beam
+  for (int b = wid; b < B; b += NW) {
+    const float* const tops = a.seg_top + (row0 + b) * S;
+    const double* const sums = a.seg_sum + (row0 + b) * S;
+    float m = NONE;
+    double z = 0.0;
+    if (!(done && done[b]) && !(a.b.score && !__builtin_isfinite(a.b.score[row0 + b]))) {
+      const float top = lane < S ? tops[lane] : NONE;
+      const double sum = lane < S ? sums[lane] : 0.0;
+      m = top;
+      for (int i = lane + WAVE; i < S; i += WAVE) m = vmax(m, tops[i]);
+      m = wave_max(m);
+      z = sum * weight(top, m);
+      for (int i = lane + WAVE; i < S; i += WAVE) z += sums[i] * weight(tops[i], m);
+      z = wave_sum(z);
+    }
+    const double x = base_of(a, row0 + b, m, z);
+    if (lane == 0) sh.base[b] = x;
+  }
+  __syncthreads();
+
+  const uint32_t segs = uint32_t(B) * uint32_t(S);
+  auto seg_key = [&](uint32_t i) -> uint32_t {
+    const int b = int(i / S);
+    return best_key(sh.base[b], done && done[b], i % S == 0, seg_best[i]);
+  };
+  uint32_t bound = 1;
+  if (segs >= 2 * uint32_t(K)) {
+    if (segs <= 4 * PICK) {
+      uint32_t keys[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t i = tid + e * PICK;
+        keys[e] = i < segs ? seg_key(i) : 0;
+      }
+      bound = bound_of(sh, [&](auto f) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f(keys[e]);
+      }, K, K + K / 4);
+    } else {
+      bound = bound_of(sh, [&](auto f) {
+        for (uint32_t i = tid; i < segs; i += PICK) f(seg_key(i));
+      }, K, K + K / 4);
+    }
+  }
+  if (tid == 0) sh.n = 0;
+  __syncthreads();
+  for (uint32_t i = tid; i < segs; i += PICK) {
+    if (seg_key(i) < bound) continue;
+    const uint32_t at = atomicAdd(&sh.n, 1u);
+    if (at < LIST) sh.segs[at] = i;
+  }
+  __syncthreads();
+  const uint32_t n_segs = sh.n;
+  __syncthreads();
+  auto group_key = [&](uint32_t i) -> uint32_t {
+    const int b = int(i / S);
+    return best_key(sh.base[b], done && done[b], i % S == 0 && lane == 0, best[int64_t(i) * WAVE + lane]);
+  };
+  constexpr int HELD = 8;   // segments of a wave whose groups' keys it holds
+  if (n_segs <= HELD * NW) {
+    uint32_t at[HELD], keys[HELD];
+#pragma unroll
+    for (int e = 0; e < HELD; ++e) {
+      const uint32_t k = wid + e * NW;
+      at[e] = k < n_segs ? sh.segs[k] : 0;
+      keys[e] = k < n_segs ? group_key(at[e]) : 0;
+    }
+    pick<BF>(a, sh, row0, bound, true, [&](auto f) {
+#pragma unroll
+      for (int e = 0; e < HELD; ++e) f(keys[e], at[e] * WAVE + lane);
+    });
+  } else {
+    pick<BF>(a, sh, row0, bound, n_segs <= LIST, [&](auto f) {
+#pragma unroll 4
+      for (uint32_t k = wid; k < n_segs; k += NW) {
+        const uint32_t i = sh.segs[k];
+        f(group_key(i), i * WAVE + lane);
+      }
+    });
+  }
+}
+
+// Rows of one segment, few enough for one workgroup a request: both in one launch, with nothing between them in memory.
+template <bool BF, int VPT, int ROWS>
+__global__ __launch_bounds__(PICK) void beam_small_kernel(BeamArgs a) {
+  __shared__ PickShared sh;
+  const int B = a.b.beams;
+  const int lane = threadIdx.x % WAVE, wid = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int64_t row0 = int64_t(blockIdx.x) * B;
+  const uint8_t* const done = a.b.done ? a.b.done + row0 : nullptr;
+  uint32_t keys[ROWS];
+#pragma unroll
+  for (int e = 0; e < ROWS; ++e) {
+    const int b = wid + e * NW;
+    keys[e] = 0;
+    if (b >= B) continue;
+    const bool ended = done && done[b];
+    Segment r{NONE, NONE, 0.0};
+    if (!ended && !(a.b.score && !__builtin_isfinite(a.b.score[row0 + b]))) r = scan<BF, VPT>(a, row0 + b, 0);
+    const double x = base_of(a, row0 + b, r.top, r.sum);
+    if (lane == 0) sh.base[b] = x;
+    keys[e] = best_key(x, ended, lane == 0, r.best);
+  }
+  __syncthreads();
+  pick<BF>(a, sh, row0, 1, true, [&](auto f) {
+#pragma unroll
+    for (int e = 0; e < ROWS; ++e) f(keys[e], uint32_t(wid + e * NW) * WAVE + lane);
+  });
+}
+
 // Loads a lane: as many as leave workgroups enough to fill the CUs, and no row mostly empty segments.
 int vectors(const tav2_beams& b) {
   const int el = b.dtype == TAV2_BF16 ? 8 : 4;
@@ -518,23 +694,47 @@ int vectors(const tav2_beams& b) {
 int64_t segments(const tav2_beams& b) {
   return cdiv(b.vocab, WAVE * (b.dtype == TAV2_BF16 ? 8 : 4) * vectors(b));
 }
-
-}  // namespace
-
-int64_t beam_select_groups(const tav2_beams& b, int keep) {
-  return int64_t(b.num_requests) * b.beams * cdiv(segments(b), 4);
-}
-
-size_t beam_select_bytes(const tav2_beams& b, int keep) {
-  return align_up(size_t(b.num_requests) * b.beams * segments(b) * (8 + 4 + 4 + 4 * WAVE), 256);
+// Of beam_small_kernel: loads a lane, 0: not with these sizes.
+int small_vectors(const tav2_beams& b) {
+  const int el = b.dtype == TAV2_BF16 ? 8 : 4;
+  if (b.beams > 4 * NW || b.vocab > WAVE * el * 8) return 0;
+  int vpt = 8;
+  while (vpt > 1 && b.vocab <= WAVE * el * vpt / 2) vpt /= 2;
+  return vpt;
 }
 
 template <bool BF>
-static void launch_scan(const BeamArgs& a, unsigned n, hipStream_t st) {
+void launch_scan(const BeamArgs& a, unsigned n, hipStream_t st) {
   if (a.vpt == 8) beam_scan_kernel<BF, 8><<<n, 256, 0, st>>>(a);
   else if (a.vpt == 4) beam_scan_kernel<BF, 4><<<n, 256, 0, st>>>(a);
   else if (a.vpt == 2) beam_scan_kernel<BF, 2><<<n, 256, 0, st>>>(a);
   else beam_scan_kernel<BF, 1><<<n, 256, 0, st>>>(a);
+}
+template <bool BF, int VPT>
+void launch_small(const BeamArgs& a, hipStream_t st) {
+  const unsigned n = unsigned(a.b.num_requests);
+  if (a.b.beams <= NW) beam_small_kernel<BF, VPT, 1><<<n, PICK, 0, st>>>(a);
+  else if (a.b.beams <= 2 * NW) beam_small_kernel<BF, VPT, 2><<<n, PICK, 0, st>>>(a);
+  else beam_small_kernel<BF, VPT, 4><<<n, PICK, 0, st>>>(a);
+}
+template <bool BF>
+void launch_small(const BeamArgs& a, hipStream_t st) {
+  if (a.vpt == 8) launch_small<BF, 8>(a, st);
+  else if (a.vpt == 4) launch_small<BF, 4>(a, st);
+  else if (a.vpt == 2) launch_small<BF, 2>(a, st);
+  else launch_small<BF, 1>(a, st);
+}
+
+}  // namespace
+
+int64_t beam_select_groups(const tav2_beams& b, int keep) {
+  if (small_vectors(b)) return int64_t(b.num_requests) * (PICK / 256);
+  return std::max(int64_t(b.num_requests) * b.beams * cdiv(segments(b), 4), int64_t(b.num_requests) * (PICK / 256));
+}
+
+size_t beam_select_bytes(const tav2_beams& b, int keep) {
+  if (small_vectors(b)) return 0;
+  return align_up(size_t(b.num_requests) * b.beams * segments(b) * (8 + 4 + 4 + 4 * WAVE), 256);
 }
 
 hipError_t launch_beam_select(const tav2_beams& b, int keep, bool in_place, int32_t* parent,
@@ -547,6 +747,13 @@ hipError_t launch_beam_select(const tav2_beams& b, int keep, bool in_place, int3
   a.token = token;
   a.score = score;
   a.done = done;
+  if ((a.vpt = small_vectors(b))) {
+    a.segs = 1;
+    ProfScope prof("beam_pick", st);
+    if (b.dtype == TAV2_BF16) launch_small<true>(a, st);
+    else launch_small<false>(a, st);
+    return hipGetLastError();
+  }
   a.vpt = vectors(b);
   a.segs = int(segments(b));
   const size_t n = size_t(b.num_requests) * b.beams * a.segs;
@@ -556,7 +763,7 @@ hipError_t launch_beam_select(const tav2_beams& b, int keep, bool in_place, int3
   a.seg_best = a.seg_top + n;
   {
     ProfScope prof("beam_scan", st);
-    const unsigned groups = unsigned(beam_select_groups(b, keep));
+    const unsigned groups = unsigned(int64_t(b.num_requests) * b.beams * cdiv(a.segs, 4));
     if (b.dtype == TAV2_BF16) launch_scan<true>(a, groups, st);
     else launch_scan<false>(a, groups, st);
   }
