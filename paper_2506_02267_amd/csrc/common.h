@@ -42,6 +42,21 @@ __device__ __forceinline__ float xsum16(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// v moved around within sixteen lanes by N, on the vector unit.
+template <int N>
+__device__ __forceinline__ float ror16(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x120 + N, 0xF, 0xF, true));
+}
+// v joined by op with those of the lanes of the same sixteen that lie a multiple of `step` (1, 2, 4, 8 or 16) away.
+template <class Op>
+__device__ __forceinline__ float steps16(float v, int step, Op op) {
+  if (step <= 8) v = op(v, ror16<8>(v));
+  if (step <= 4) v = op(v, ror16<4>(v));
+  if (step <= 2) v = op(v, ror16<2>(v));
+  if (step <= 1) v = op(v, ror16<1>(v));
+  return v;
+}
+
 __device__ __forceinline__ float bf2f(bf16_t b) { return __uint_as_float(uint32_t(b) << 16); }
 
 // float -> bf16, round to nearest even (inputs are finite).

@@ -408,57 +408,61 @@ __device__ __forceinline__ void attend_rows(const A& a, const J& j) {
   }
 }
 
-// At most 16 query rows, on the 16x16x32 instructions, a page's 64 keys at once.  S^T comes in four tiles
+// At most 16 query rows of a wave, on the 16x16x32 instructions, a page's 64 keys at once.  S^T comes in four tiles
 // of 16 keys, in the order that makes a lane's 16 scores its quarter's 16 consecutive keys
 // (16 g + 4 i + r in register r of tile i, g = l / 16), again the operand of O^T = V^T P^T as they
-// stand.  A lane's row (l % 16) is query qi's head g_row of its kv head, and sees the positions below hi that
-// are at least lo or among the sinks.  feed has been asked for the share's first pages; stage and mm are
-// the workgroup's LDS: a wave's page on its way, then its state.  open_blocks(f) calls f(sequence) for
-// the open blocks that are this wave's; finish(M, l, tile) gets a row's reference and sum, and tile(d) its features
-// 16 d + 4 g .. + 3.
-template <int D, class A, class J, class Open, class Finish>
-__device__ __forceinline__ void attend16(const A& a, const J& j, Feed<D>& feed, int page, u32x4 (&stage)[4][8 * D],
-                                         float (&mm)[4][2][16], int64_t qi, int g_row, int& hi, int lo, Open open_blocks,
-                                         Finish finish) {
-  constexpr int F = D / 4;           // features of a lane's quarter
-  constexpr int NK = D / 32;         // products over the features
-  constexpr int ND = D / 16;         // tiles of O^T
-  const tav2_kv& c = a.c;
-  const int lane = threadIdx.x % WAVE, m = lane % 16, g = lane / 16;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  const int full = j.len / KVP, sinks_ = tile_sinks(a, j);
-  u32x4* const my = stage[wave];
-  int all_hi = hi, all_lo = lo;   // what all rows see: from the last one's first key to the first's last
-#pragma unroll
-  for (int o = 8; o >= 1; o >>= 1) {
-    all_hi = min(all_hi, __shfl_xor(all_hi, o, WAVE));
-    all_lo = max(all_lo, __shfl_xor(all_lo, o, WAVE));
-  }
-  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+// stand.  A lane's row is l % 16.
+template <int D>
+struct Tile16 {
+  static constexpr int F = D / 4;    // features of a lane's quarter
+  static constexpr int NK = D / 32;  // products over the features
+  static constexpr int ND = D / 16;  // tiles of O^T
   f16x8 qf[NK];
-  int cq;   // a power of two
-  {
-    const bf16_t* p = static_cast<const bf16_t*>(a.q.q) + qi * a.q.ld + (j.h * j.G + g_row) * D + g * F;
+  int cq;                            // a power of two
+  int lo, all_hi, all_lo, sinks;     // what the row sees (besides hi, which a caller keeps), and what all rows do
+  f32x4 o[ND];
+  float ref, wref, ratio, sum;       // (m, n, d, l of attend_core.h)
+
+  // The row's query, at its first feature.
+  __device__ __forceinline__ void query(const bf16_t* p, int scale_e) {
     u32x4 w[NK];
     float top = 0.f, f, back;
 #pragma unroll
-    for (int t = 0; t < NK; ++t) w[t] = *reinterpret_cast<const u32x4*>(p + 8 * t);
+    for (int t = 0; t < NK; ++t)
+      w[t] = *reinterpret_cast<const u32x4*>(p + int(threadIdx.x) % WAVE / 16 * F + 8 * t);
 #pragma unroll
     for (int t = 0; t < NK; ++t) top = max8(w[t], top);
     into_half<TO_TOP>(xmax32(xmax16(top)), &f, &back);
 #pragma unroll
     for (int t = 0; t < NK; ++t) qf[t] = scaled8h(w[t], f);
-    cq = a.scale_e + __builtin_amdgcn_frexp_expf(back) - 1;
+    cq = scale_e + __builtin_amdgcn_frexp_expf(back) - 1;
+  }
+  // The rows see the positions below hi that are at least lo or among the sinks.
+  __device__ __forceinline__ void sees(int hi, int lo_, int sinks_) {
+    lo = lo_;
+    sinks = sinks_;
+    all_hi = hi;   // from the last one's first key to the first's last
+    all_lo = lo;
+#pragma unroll
+    for (int x = 8; x >= 1; x >>= 1) {
+      all_hi = min(all_hi, __shfl_xor(all_hi, x, WAVE));
+      all_lo = max(all_lo, __shfl_xor(all_lo, x, WAVE));
+    }
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  }
+  __device__ __forceinline__ void clear() {
+    ref = wref = -FLT_MAX;
+    ratio = 1.f;
+    sum = 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) o[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
 
-  f32x4 o[ND];
-  float ref = -FLT_MAX, wref = -FLT_MAX, ratio = 1.f, sum = 0.f;   // (m, n, d, l of attend_core.h)
-#pragma unroll
-  for (int d = 0; d < ND; ++d) o[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
-
-  // one page: keys(i, kf) sets the operands of S^T's tile i, values(d, vf) those of O^T's tile d
-  auto step = [&](auto keys, auto values, float cs, AttScale vs, int key0) {
+  // One page: keys(i, kf) sets the operands of S^T's tile i, values(d, vf) those of O^T's tile d.
+  template <class Keys, class Values>
+  __device__ __forceinline__ void step(Keys keys, Values values, float cs, AttScale vs, int key0, const int& hi) {
+    const int g = int(threadIdx.x) % WAVE / 16;
     f32x4 s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -468,11 +472,11 @@ __device__ __forceinline__ void attend16(const A& a, const J& j, Feed<D>& feed, 
 #pragma unroll
       for (int t = 0; t < NK; ++t) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[t], qf[t], s[i], 0, 0, 0);
     }
-    if (key0 + KVP > all_hi || (key0 < all_lo && key0 + KVP > sinks_)) {
-      const int k0 = key0 + 16 * g, hi_ = hi - k0, lo_ = lo - k0, sinks = sinks_ - k0;
+    if (key0 + KVP > all_hi || (key0 < all_lo && key0 + KVP > sinks)) {
+      const int k0 = key0 + 16 * g, hi_ = hi - k0, lo_ = lo - k0, sinks_ = sinks - k0;
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        s[r / 4][r % 4] = r < hi_ && (r >= lo_ || r < sinks) ? s[r / 4][r % 4] : -INFINITY;
+        s[r / 4][r % 4] = r < hi_ && (r >= lo_ || r < sinks_) ? s[r / 4][r % 4] : -INFINITY;
     }
     float top = s[0][0];
 #pragma unroll
@@ -510,8 +514,77 @@ __device__ __forceinline__ void attend16(const A& a, const J& j, Feed<D>& feed, 
       for (int t = 0; t < 2; ++t)
         o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[t], pf[t], o[d], 0, 0, 0);
     }
-  };
-  const int krow = 16 * (m / 4) + m % 4;   // + 4 i: the key of tile i that this lane's row is
+  }
+  // The key of tile 0 that this lane's row of the operand is (+ 4 i: of tile i).
+  static __device__ __forceinline__ int key() {
+    const int m = int(threadIdx.x) % 16;
+    return 16 * (m / 4) + m % 4;
+  }
+
+  // The open block of a sequence of `full` pages, in bf16 (as in attend_rows).
+  __device__ __forceinline__ void open_block(const tav2_kv& c, int layer, int of, int h, int full, float scale,
+                                             const int& hi) {
+    const int m = int(threadIdx.x) % 16, g = int(threadIdx.x) % WAVE / 16, krow = key();
+    const int64_t tail = kv_tail(c, layer, of, h);
+    const int held = kv_len(c, of) - full * KVP;
+    float kt = 0.f, vt = 0.f, fk, backk, fv, backv;
+    auto raw_key = [&](int i, int t) {
+      return first_of8(*reinterpret_cast<const u32x4*>(c.k_tail + tail + (krow + 4 * i) * D + g * F + 8 * t),
+                       krow + 4 * i < held ? 8 : 0);
+    };
+    auto raw_value = [&](int d, int t) {
+      return first_of8(*reinterpret_cast<const u32x4*>(c.v_tail + tail + (16 * d + m) * KVP + 16 * g + 8 * t),
+                       held - 16 * g - 8 * t);
+    };
+    // (read twice, as there)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < NK; ++t) kt = max8(raw_key(i, t), kt);
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) vt = max8(raw_value(d, t), vt);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int x = 32; x >= 1; x >>= 1) {
+      kt = fmaxf(kt, __shfl_xor(kt, x, WAVE));
+      vt = fmaxf(vt, __shfl_xor(vt, x, WAVE));
+    }
+    into_half<TO_TOP>(kt, &fk, &backk);
+    into_half<TO_CODES>(vt, &fv, &backv);
+    auto keys = [&](int i, f16x8(&kf)[NK]) {
+#pragma unroll
+      for (int t = 0; t < NK; ++t) kf[t] = scaled8h(raw_key(i, t), fk);
+    };
+    auto values = [&](int d, f16x8(&vf)[2]) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) vf[t] = scaled8h(raw_value(d, t), fv);
+    };
+    step(keys, values, score_factor(scale * backk, cq), tail_scale(vt, backv, fv), full * KVP, hi);
+  }
+};
+
+// At most 16 query rows of a workgroup, whose four waves take the share's pages in turn.  A lane's row is
+// query qi's head g_row of its kv head.  feed has been asked for the share's first pages; stage and mm are the workgroup's
+// LDS: a wave's page on its way, then its state.  open_blocks(f) calls f(sequence) for the open blocks that are this
+// wave's; finish(M, l, tile) gets a row's reference and sum, and tile(d) its features 16 d + 4 g .. + 3.
+template <int D, class A, class J, class Open, class Finish>
+__device__ __forceinline__ void attend16(const A& a, const J& j, Feed<D>& feed, int page, u32x4 (&stage)[4][8 * D],
+                                         float (&mm)[4][2][16], int64_t qi, int g_row, int& hi, int lo, Open open_blocks,
+                                         Finish finish) {
+  using T = Tile16<D>;
+  constexpr int NK = T::NK, ND = T::ND;
+  const tav2_kv& c = a.c;
+  const int lane = threadIdx.x % WAVE, m = lane % 16, g = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int full = j.len / KVP;
+  u32x4* const my = stage[wave];
+  T st;
+  st.sees(hi, lo, tile_sinks(a, j));
+  st.query(static_cast<const bf16_t*>(a.q.q) + qi * a.q.ld + (j.h * j.G + g_row) * D, a.scale_e);
+  st.clear();
+  const int krow = T::key();
   for (int i = j.c0 + wave, t = 0; i < j.c1; i += 4, ++t) {
     if (t == WAVE) {
       t = 0;
@@ -547,62 +620,21 @@ __device__ __forceinline__ void attend16(const A& a, const J& j, Feed<D>& feed, 
         vf[0] = codes8h(w.x, w.y);
         vf[1] = codes8h(w.z, w.w);
       };
-      step(keys, values, score_factor(a.scale * ks, cq), vs, b * KVP);
+      st.step(keys, values, score_factor(a.scale * ks, st.cq), vs, b * KVP, hi);
     }
     page = next;
   }
-  // the open block, in bf16 (as in the kernel above): this sequence's, or, of several taken together,
-  // each one's, which its own rows alone see, by the waves in turn
-  auto open_block = [&](int of) {
-    const int64_t tail = kv_tail(c, a.layer, of, j.h);
-    const int held = kv_len(c, of) - full * KVP;
-    float kt = 0.f, vt = 0.f, fk, backk, fv, backv;
-    auto raw_key = [&](int i, int t) {
-      return first_of8(*reinterpret_cast<const u32x4*>(c.k_tail + tail + (krow + 4 * i) * D + g * F + 8 * t),
-                       krow + 4 * i < held ? 8 : 0);
-    };
-    auto raw_value = [&](int d, int t) {
-      return first_of8(*reinterpret_cast<const u32x4*>(c.v_tail + tail + (16 * d + m) * KVP + 16 * g + 8 * t),
-                       held - 16 * g - 8 * t);
-    };
-    // (read twice, as above)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int t = 0; t < NK; ++t) kt = max8(raw_key(i, t), kt);
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) vt = max8(raw_value(d, t), vt);
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) {
-      kt = fmaxf(kt, __shfl_xor(kt, x, WAVE));
-      vt = fmaxf(vt, __shfl_xor(vt, x, WAVE));
-    }
-    into_half<TO_TOP>(kt, &fk, &backk);
-    into_half<TO_CODES>(vt, &fv, &backv);
-    auto keys = [&](int i, f16x8(&kf)[NK]) {
-#pragma unroll
-      for (int t = 0; t < NK; ++t) kf[t] = scaled8h(raw_key(i, t), fk);
-    };
-    auto values = [&](int d, f16x8(&vf)[2]) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) vf[t] = scaled8h(raw_value(d, t), fv);
-    };
-    step(keys, values, score_factor(a.scale * backk, cq), tail_scale(vt, backv, fv), full * KVP);
-  };
-  open_blocks(open_block);
+  open_blocks([&](int of) { st.open_block(c, a.layer, of, j.h, full, a.scale, hi); });
 
   // the four waves' states meet in LDS; wave w joins every fourth tile of O^T, in the order of the waves
   __builtin_amdgcn_wave_barrier();
-  sum = xsum32(xsum16(sum));
+  const float sum = xsum32(xsum16(st.sum));
   if (g == 0) {
-    mm[wave][0][m] = wref;
+    mm[wave][0][m] = st.wref;
     mm[wave][1][m] = sum;
   }
 #pragma unroll
-  for (int d = 0; d < ND; ++d) my[d * WAVE + lane] = __builtin_bit_cast(u32x4, o[d] * ratio);
+  for (int d = 0; d < ND; ++d) my[d * WAVE + lane] = __builtin_bit_cast(u32x4, st.o[d] * st.ratio);
   __syncthreads();
   float M = -FLT_MAX, l = 0.f, f[4];
 #pragma unroll

@@ -22,32 +22,50 @@ struct PrefixArgs {
   float* lse;          // nullable
   float* part_o;       // [splits, total, heads, D]
   float* part_ml;      // [splits, total, heads, 2]: reference and sum
+  int32_t* plan;       // pages to a share, as the first launch chose
   int most_rows;       // rows of a group and kv head, at most
-  int tiles;           // row tiles of a group and kv head
-  int splits, chunk;   // shares of a prefix's pages, and pages to a share
-  int units;           // (share, group, kv head), padded to a multiple of 8
+  int tile, tiles;     // rows of a tile, and tiles of a group and kv head, at most
+  int splits;          // shares of a prefix's pages, at most
+  int chunk;           // pages to a share; 0: every workgroup finds it out
+  int least, target;   // then: the least, and workgroups that share all pages
+  bool fit;            // no more than those
+  int seen;            // pages that a row sees at most, by the host's estimate, with a window
   int own_tiles;       // 16-row tiles of a member and kv head
   __device__ __forceinline__ bool parts() const { return true; }
 };
 
-// The members and queries of a group; false: none, or out of the arguments' range.
+// The members and queries of a group, and its prefix's length; n 0: none, or out of the arguments' range.
 struct Group {
   int first, n, prefix, len;   // prefix -1 and len 0: none
   int64_t q0, nq;
 };
-__device__ __forceinline__ bool group_of(const PrefixArgs& a, int g, Group& r) {
-  r.first = a.g.offset[g];
-  const int end = a.g.offset[g + 1];
-  if (r.first < 0 || end > a.c.num_seqs || r.first >= end) return false;
-  r.n = min(end - r.first, a.g.max_members);
+// (The reads depend on one another in two steps only: what is out of range is read from somewhere in range, and judged
+// afterwards.)
+__device__ __forceinline__ Group group_of(const PrefixArgs& a, int g) {
+  Group r;
+  const int most = a.c.num_seqs;
+  const int first = a.g.offset[g], end = a.g.offset[g + 1], prefix = a.g.prefix[g];
+  const bool ok = first >= 0 && first < end && end <= most;
+  const bool has = prefix >= 0 && prefix < most;
+  r.first = ok ? first : 0;
+  r.n = ok ? min(end - first, a.g.max_members) : 0;
+  r.prefix = has ? prefix : -1;
   r.q0 = a.q.offset[r.first];
   const int64_t q1 = a.q.offset[r.first + r.n];
-  if (r.q0 < 0 || q1 < r.q0 || q1 > a.q.total) return false;
+  const int len = kv_len(a.c, has ? prefix : 0);
+  r.len = has ? len : 0;
   r.nq = q1 - r.q0;
-  r.prefix = a.g.prefix[g];
-  if (r.prefix >= a.c.num_seqs) r.prefix = -1;
-  r.len = r.prefix < 0 ? 0 : kv_len(a.c, r.prefix);
-  return true;
+  if (r.q0 < 0 || r.nq < 0 || q1 > a.q.total) r.n = 0, r.nq = 0;
+  return r;
+}
+__device__ __forceinline__ int group_rows(const PrefixArgs& a, const Group& r) {
+  const int64_t rows = r.nq * (a.q.heads / a.c.kv_heads);
+  return int(rows < a.most_rows ? rows : a.most_rows);
+}
+// Pages that its shares are counted by: those of the prefix; with a window about as many as a row sees.
+__device__ __forceinline__ int group_pages(const PrefixArgs& a, int len) {
+  const int n = (len + KVP - 1) / KVP;
+  return a.q.window > 0 ? min(n, a.seen) : n;
 }
 
 __device__ __forceinline__ int64_t member_count(const PrefixArgs& a, int s) {
@@ -77,40 +95,129 @@ __device__ __forceinline__ int64_t place_of(const PrefixArgs& a, const Group& r,
 struct PrefixJob {
   int s, h, split, row0, G, rows;
   int64_t q0;
-  int len, chunk, n, c0, c1;
+  int len, n, c0, c1;
   PageList list;
   const int32_t* table;
   int lo;            // the first position that row row0 + lane sees
   int all_lo;        // and that all rows of the tile see
 };
 
+// Sums of v over the lanes up to this one: within sixteen by shifts of 1, 2, 4 and 8 (0x110 + n), then from lane 15 of each
+// sixteen to the next (0x142), and from lane 31 to the upper half (0x143).
+__device__ __forceinline__ int lanes_upto(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+
+// Every workgroup divides the work by itself, from the groups' lengths, a lane a group: the tiles' pages over the
+// target of workgroups in shares of one size, so that long and short prefixes end together.  (In shares by the
+// host's estimate of the longest prefix, 64 prefixes of 1024 - 16384 tokens took TODO us for TODO.)
+constexpr int PLAN = 4;   // groups of a lane: at most 64 PLAN groups in all
+
+// Shares of a prefix that `pages` are counted for.
+__device__ __forceinline__ int shares_of(const PrefixArgs& a, int pages, int chunk) {
+  return min(a.splits, (pages + chunk - 1) / chunk);
+}
+// Workgroups for a group with T tiles and S shares; where there are tiles, of a multiple of eight pairs (share, head).
+__device__ __forceinline__ int group_jobs(const PrefixArgs& a, int T, int S) {
+  const int pairs = S * a.c.kv_heads;
+  return (a.tiles > 1 ? (pairs + 7) / 8 * 8 : pairs) * T;
+}
+
 __device__ __forceinline__ bool prefix_job(const PrefixArgs& a, int cap, PrefixJob& j) {
-  // Eight neighbouring workgroups take a tile of eight units, one on each XCD; the units' further tiles follow, so
-  // that they find the pages in that XCD's L2.  First shares come first, the later ones, which short
-  // prefixes lack, at the end.
-  const int unit = int(blockIdx.x / unsigned(8 * a.tiles)) * 8 + int(blockIdx.x % 8);
-  const int tile = int(blockIdx.x / 8 % unsigned(a.tiles));
-  const int per = a.g.num_groups * a.c.kv_heads;
-  j.split = unit / per;
-  if (j.split >= a.splits) return false;
-  const int g = unit % per / a.c.kv_heads;
-  j.h = unit % a.c.kv_heads;
-  Group r;
-  if (!group_of(a, g, r)) return false;
-  j.s = r.prefix;
-  j.G = a.q.heads / a.c.kv_heads;
-  j.q0 = r.q0;
-  const int64_t rows = r.nq * j.G;
-  j.rows = int(rows < a.most_rows ? rows : a.most_rows);
+  const int lane = threadIdx.x % WAVE, H = a.c.kv_heads, G = a.g.num_groups;
+  Group my;
+  int at = -1, x = 0, T = 0, S = 0, chunk = a.chunk;
+  if (chunk == 0) {
+    Group r[PLAN];
+    int tiles[PLAN], pages[PLAN], sum = 0, most = 0;
+#pragma unroll
+    for (int e = 0; e < PLAN; ++e) {
+      tiles[e] = pages[e] = 0;
+      if (64 * e >= G) continue;
+      r[e] = group_of(a, min(64 * e + lane, G - 1));
+      if (64 * e + lane < G) {
+        tiles[e] = (group_rows(a, r[e]) + cap - 1) / cap;
+        pages[e] = group_pages(a, r[e].len);
+        sum += tiles[e] * pages[e];
+        if (tiles[e] > 0) most = max(most, pages[e]);
+      }
+    }
+    sum = __builtin_amdgcn_readlane(lanes_upto(sum), 63);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) most = max(most, __shfl_xor(most, o, WAVE));
+    most = __builtin_amdgcn_readfirstlane(most);
+    // (a multiple of four: the waves of a workgroup take pages in turn)
+    const int64_t each = (int64_t(sum) * H + a.target - 1) / a.target;
+    chunk = (max(max(a.least, int(each)), (most + a.splits - 1) / a.splits) + 3) / 4 * 4;
+    if (a.fit) {   // larger until all run at once
+      while (true) {
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < PLAN; ++e) n += tiles[e] * shares_of(a, pages[e], chunk);
+        n = __builtin_amdgcn_readlane(lanes_upto(n), 63);
+        if (n * H <= a.target || chunk >= most) break;
+        chunk += 4;
+      }
+    }
+    int before = 0;
+#pragma unroll
+    for (int e = 0; e < PLAN; ++e) {
+      if (64 * e >= G) continue;
+      const int shares = shares_of(a, pages[e], chunk), n = group_jobs(a, tiles[e], shares);
+      const int upto = before + lanes_upto(n);
+      const uint64_t mine = __ballot(int(blockIdx.x) >= upto - n && int(blockIdx.x) < upto);
+      if (mine) {
+        const int l = __builtin_ctzll(mine);
+        at = 64 * e + l;
+        x = int(blockIdx.x) - __builtin_amdgcn_readlane(upto - n, l);
+        T = __builtin_amdgcn_readlane(tiles[e], l);
+        S = __builtin_amdgcn_readlane(shares, l);
+        my.first = __builtin_amdgcn_readlane(r[e].first, l);
+        my.n = __builtin_amdgcn_readlane(r[e].n, l);
+        my.prefix = __builtin_amdgcn_readlane(r[e].prefix, l);
+        my.len = __builtin_amdgcn_readlane(r[e].len, l);
+        my.q0 = __builtin_amdgcn_readlane(int(r[e].q0), l);   // (below 2^31)
+        my.nq = __builtin_amdgcn_readlane(int(r[e].nq), l);
+      }
+      before = __builtin_amdgcn_readlane(upto, 63);
+    }
+  } else {
+    const int per = group_jobs(a, a.tiles, a.splits);
+    at = int(blockIdx.x) / per;
+    x = int(blockIdx.x) % per;
+    my = group_of(a, at);
+    T = a.tiles;
+    S = shares_of(a, group_pages(a, my.len), chunk);
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.plan = chunk;
+  if (at < 0) return false;
+  int tile = 0, pair = x;
+  if (a.tiles > 1) {
+    pair = x / (8 * T) * 8 + x % 8;
+    tile = x / 8 % T;
+  }
+  j.split = pair / H;
+  j.h = pair % H;
+  if (j.split >= S) return false;
+  j.s = my.prefix;
+  j.G = a.q.heads / H;
+  j.q0 = my.q0;
+  j.rows = group_rows(a, my);
   j.row0 = tile * cap;
   if (j.row0 >= j.rows) return false;
-  j.len = r.len;
+  j.len = my.len;
   j.lo = j.all_lo = 0;
   int64_t first = 0;
   if (a.q.window > 0) {
-    const int row = min(j.row0 + int(threadIdx.x % WAVE), min(j.row0 + cap, j.rows) - 1);
-    const int64_t low = r.len + place_of(a, r, row / j.G) - a.q.window + 1;   // below 2^32 either way
-    j.lo = low > 0 ? int(low < r.len ? low : r.len) : 0;
+    const int row = min(j.row0 + lane, min(j.row0 + cap, j.rows) - 1);
+    const int64_t low = my.len + place_of(a, my, row / j.G) - a.q.window + 1;   // below 2^32 either way
+    j.lo = low > 0 ? int(low < my.len ? low : my.len) : 0;
     int least = j.lo, most = j.lo;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
@@ -125,12 +232,9 @@ __device__ __forceinline__ bool prefix_job(const PrefixArgs& a, int cap, PrefixJ
   const int64_t sink_pages = (int64_t(a.q.sinks) + KVP - 1) / KVP;
   j.list.sink = a.q.window > 0 ? min(int(sink_pages < j.list.first ? sink_pages : j.list.first), j.list.last) : 0;
   j.n = j.list.count();
-  // shares of one size, so that a long prefix has more of them (larger ones where it is longer
-  // than the host's estimate)
-  j.chunk = max(a.chunk, (j.n + a.splits - 1) / a.splits);
-  j.c0 = j.split * j.chunk;
-  j.c1 = min(j.n, j.c0 + j.chunk);
-  if (j.c0 >= j.n) {   // an empty share: a sum of zero and no features
+  j.c0 = min(j.n, j.split * chunk);
+  j.c1 = j.split == S - 1 ? j.n : min(j.n, j.c0 + chunk);   // (more than its share where members are longer than estimated)
+  if (j.c0 >= j.c1) {   // an empty share: a sum of zero and no features
     const int row = j.row0 + int(threadIdx.x);
     if (int(threadIdx.x) < cap && row < j.rows) {
       const int64_t part = int64_t(j.split) * a.q.total * a.q.heads +
@@ -199,147 +303,343 @@ struct OwnJob {
   int s, h, G, len, c0, c1, sinks;
   PageList list;
   const int32_t* table;
+  bool open;                       // the open block is among what is seen
+  int64_t q0, first;               // its first query, and how far behind the prefix that stands
+  int rows, row0, R;               // (query, head) pairs of the member; this tile's first, and how many are its
+  int shares;                      // of the prefix
 };
 __device__ __forceinline__ int tile_sinks(const PrefixArgs& a, const OwnJob& j) { return j.sinks; }
 
-template <int D>
-__global__ __launch_bounds__(256, D <= 64 ? 3 : 2) void kv_join_kernel(PrefixArgs a) {
-  constexpr int ND = D / 16, Q = D / 4;
-  __shared__ u32x4 stage[4][8 * D];
-  __shared__ float mm[4][2][16];
-  __shared__ f32x4 joined[16][Q];   // the prefix's features, against jm
-  __shared__ float jm[16], jl[16];
+// Job number b: (member, group, tile, head), the last one fastest: members that only some groups have come last.
+__device__ __forceinline__ bool own_job(const PrefixArgs& a, unsigned b, OwnJob& j) {
   const tav2_kv& c = a.c;
-  OwnJob j;
-  unsigned b = blockIdx.x;
   j.h = int(b % c.kv_heads);
   b /= c.kv_heads;
   const int tile = int(b % a.own_tiles);
   b /= a.own_tiles;
-  const int member = int(b % a.g.max_members);
-  Group r;
-  if (!group_of(a, int(b / a.g.max_members), r) || member >= r.n) return;
-  j.s = r.first + member;
+  const int member = int(b / a.g.num_groups);
+  b %= a.g.num_groups;
+  if (member >= a.g.max_members) return false;
+  const int chunk = *a.plan;
+  const Group r = group_of(a, int(b));
+  j.s = r.first + min(member, r.n - 1 > 0 ? r.n - 1 : 0);
   j.G = a.q.heads / c.kv_heads;
-  const int64_t q0 = a.q.offset[j.s], most = a.most_rows / j.G;   // queries that the first launch took
-  const int64_t nq = member_count(a, j.s);
-  if (q0 < r.q0 || q0 + nq > r.q0 + (r.nq < most ? r.nq : most)) return;
-  const int rows = int(nq) * j.G, row0 = 16 * tile;
-  if (row0 >= rows) return;
-  const int tid = threadIdx.x, lane = tid % WAVE, m = lane % 16, g = lane / 16;
-  const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
-  const int64_t n = a.q.total * a.q.heads;
-  auto at_of = [&](int row) { return (q0 + row / j.G) * a.q.heads + j.h * j.G + row % j.G; };
-
-  // the shares' references and sums: 16 threads a row
-  const int R = min(16, rows - row0);
-  {
-    const int k = tid / 16;
-    const int64_t at = at_of(row0 + min(k, R - 1));
-    float M = -FLT_MAX, l = 0.f;
-    for (int s = tid % 16; s < a.splits; s += 16) M = vmax(M, a.part_ml[2 * (s * n + at)]);
-#pragma unroll
-    for (int o = 8; o >= 1; o >>= 1) M = vmax(M, __shfl_xor(M, o, WAVE));
-    for (int s = tid % 16; s < a.splits; s += 16) {
-      const float w = half_factor(a.part_ml[2 * (s * n + at)] - M);
-      l += a.part_ml[2 * (s * n + at) + 1] * w * w;
-    }
-#pragma unroll
-    for (int o = 8; o >= 1; o >>= 1) l += __shfl_xor(l, o, WAVE);
-    if (tid % 16 == 0) {
-      jm[k] = M;
-      jl[k] = l;
-    }
-  }
-  __syncthreads();
-  // their features: a thread takes four of a row, in every ng-th share
-  {
-    const int RQ = R * Q, ng = RQ < 256 ? 256 / RQ : 1;
-    f32x4* const red = reinterpret_cast<f32x4*>(&stage[0][0]);
-    for (int p = tid % (RQ < 256 ? RQ : 256), sg = RQ < 256 ? tid / RQ : 0; p < RQ; p += 256) {
-      const int k = p / Q, d = p % Q;
-      const int64_t at = at_of(row0 + k);
-      f32x4 x = (f32x4){0.f, 0.f, 0.f, 0.f};
-      // (an empty share's features are not written: read all the same, so that no load waits for the sum that
-      // says so, and dropped)
-#pragma unroll 8
-      for (int s = sg; s < a.splits; s += ng) {
-        const int64_t q = s * n + at;
-        const float w = half_factor(a.part_ml[2 * q] - jm[k]);
-        const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + q * D + 4 * d);
-        const bool some = a.part_ml[2 * q + 1] != 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] += some ? o[e] * w * w : 0.f;
-      }
-      if (sg >= ng) continue;   // (threads that are left over)
-      if (ng == 1) joined[k][d] = x;
-      else red[sg * RQ + p] = x;
-    }
-    if (ng > 1) {
-      __syncthreads();
-      for (int p = tid; p < RQ; p += 256) {
-        f32x4 x = red[p];
-        for (int sg = 1; sg < ng; ++sg) x += red[sg * RQ + p];
-        joined[p / Q][p % Q] = x;
-      }
-    }
-  }
-  __syncthreads();
-
-  // the own tokens
+  j.q0 = a.q.offset[j.s];
   j.len = kv_len(c, j.s);
-  const int full = j.len / KVP;
-  const int64_t o0 = a.causal ? j.len - nq : j.len;   // the first query's place
-  const int row = min(row0 + m, rows - 1), i = row / j.G;
-  const int64_t lo_pos = a.causal ? o0 + row0 / j.G : o0;
-  const int64_t hi_pos = a.causal ? o0 + (row0 + R - 1) / j.G : o0;
+  const int64_t most = a.most_rows / j.G;   // queries that the first launch took
+  const int64_t nq = member_count(a, j.s);
+  if (member >= r.n || j.q0 < r.q0 || j.q0 + nq > r.q0 + (r.nq < most ? r.nq : most)) return false;
+  j.shares = shares_of(a, group_pages(a, r.len), chunk);
+  j.rows = int(nq) * j.G;
+  j.row0 = 16 * tile;
+  if (j.row0 >= j.rows) return false;
+  j.R = min(16, j.rows - j.row0);
+  j.first = a.causal ? j.len - nq : j.len;
+  const int64_t lo = a.causal ? j.first + j.row0 / j.G : j.first;
+  const int64_t hi = a.causal ? j.first + (j.row0 + j.R - 1) / j.G : j.first;
   j.sinks = max(0, a.q.sinks - r.len);
-  j.list = pages_seen(j.len, lo_pos, hi_pos, a.q.window, j.sinks);
+  j.list = pages_seen(j.len, lo, hi, a.q.window, j.sinks);
   const int count = j.list.count();
-  const bool open = count > 0 && j.list.at(count - 1) >= full;
+  j.open = count > 0 && j.list.at(count - 1) >= j.len / KVP;
   j.c0 = 0;
-  j.c1 = count - (open ? 1 : 0);
+  j.c1 = count - (j.open ? 1 : 0);
   j.table = c.table + int64_t(j.s) * c.max_blocks;
-  const int64_t pos = a.causal ? o0 + i : o0, low = pos - a.q.window + 1;
-  const int64_t end = pos + 1 < j.len ? pos + 1 : j.len;
-  int hi = int(end > 0 ? end : 0);
-  const int lo = a.q.window > 0 && low > 0 ? int(low) : 0;
-  Feed<D> feed = {};
-  int page = -1;
-  if (j.c1 > 0) {
-    feed.look_up(a, j, wave);
-    page = feed.page(0);
-    feed.load(a, j, page);
-  }
-  auto open_blocks = [&](auto open_block) {
-    if (open && j.c1 % 4 == wave) open_block(j.s);
-  };
-  auto finish = [&](float M, float l, auto tile) {
-    if (row0 + m >= rows) return;
-    const int64_t at = at_of(row);
-    const float all = vmax(M, jm[m]), f = half_factor(M - all), fp = half_factor(jm[m] - all);
-    const float sum = l * f * f + jl[m] * fp * fp;
-    const bool some = sum > 0.f || sum != sum;
-    const float inv = some ? 1.f / sum : 0.f;
-    for (int d = wave; d < ND; d += 4) {
-      const f32x4 own = tile(d), pre = joined[m][4 * d + g];
-      f32x4 x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = (own[e] * f * f + pre[e] * fp * fp) * inv;
-      *reinterpret_cast<uint2*>(a.out + at * D + 16 * d + 4 * g) =
-          make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
-    }
-    if (wave == 0 && g == 0 && a.lse)
-      a.lse[at] = some ? (all + __builtin_amdgcn_logf(sum)) * LN2 : -INFINITY;
-  };
-  attend16<D>(a, j, feed, page, stage, mm, q0 + i, row % j.G, hi, lo, open_blocks, finish);
+  return true;
 }
+__device__ __forceinline__ int64_t row_at(const PrefixArgs& a, const OwnJob& j, int row) {
+  return (j.q0 + row / j.G) * a.q.heads + j.h * j.G + row % j.G;
+}
+__device__ __forceinline__ void row_seen(const PrefixArgs& a, const OwnJob& j, int row, int* hi, int* lo) {
+  const int64_t pos = a.causal ? j.first + row / j.G : j.first, low = pos - a.q.window + 1;
+  const int64_t end = pos + 1 < j.len ? pos + 1 : j.len;
+  *hi = int(end > 0 ? end : 0);
+  *lo = a.q.window > 0 && low > 0 ? int(low) : 0;
+}
+
+// A part of a row's softmax: reference, sum, and features 16 d + 4 g .. against it.
+template <int D>
+struct Part {
+  float M, l;
+  f32x4 x[D / 16];
+  __device__ __forceinline__ void add(float M2, float l2, const f32x4 (&x2)[D / 16]) {
+    const float all = vmax(M, M2), f = half_factor(M - all), f2 = half_factor(M2 - all);
+    M = all;
+    l = l * f * f + l2 * f2 * f2;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[d][e] = x[d][e] * f * f + x2[d][e] * f2 * f2;
+  }
+};
+
+// An open block for the 16 rows of a wave (tiles as in Tile16), in bf16 as it lies: the scores' products are exact, the
+// weights against the block's own largest score enter theirs as the sum of two bf16, 2^-16 of each.  A query's features
+// are scaled by the power of two that takes the largest products to 2^20 or so, whatever the keys' size.
+template <int D>
+struct OpenBlock {
+  static constexpr int F = D / 4, NK = D / 32, ND = D / 16;
+  u32x4 k[4][NK], v[ND][2];
+
+  // What lies behind the last token is not fetched: the first row and the first tokens stand in its place.
+  __device__ __forceinline__ void load(const tav2_kv& c, int layer, int of, int h, int held) {
+    const int m = int(threadIdx.x) % 16, g = int(threadIdx.x) % WAVE / 16, krow = Tile16<D>::key();
+    const int64_t tail = kv_tail(c, layer, of, h);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bf16_t* const p = c.k_tail + tail + (krow + 4 * i < held ? krow + 4 * i : 0) * D + g * F;
+#pragma unroll
+      for (int t = 0; t < NK; ++t) k[i][t] = *reinterpret_cast<const u32x4*>(p + 8 * t);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const bf16_t* const p = c.v_tail + tail + m * KVP + (16 * g + 8 * t < held ? 16 * g + 8 * t : 0);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) v[d][t] = *reinterpret_cast<const u32x4*>(p + 16 * d * KVP);
+    }
+  }
+
+  // w: the row's query as it lies.  hi, lo, sinks: what it sees, counted from the block's first token.
+  __device__ __forceinline__ void attend(const u32x4 (&w)[NK], const PrefixArgs& a, int held, int hi, int lo, int sinks,
+                                         Part<D>& r) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const int g = int(threadIdx.x) % WAVE / 16;
+    auto most = [](float a, float b) { return vmax(a, b); };
+    // the largest magnitudes, as the upper bits of a float
+    auto top_of = [&](const u32x4& x, u16x2 t) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, x[e] & 0x7FFF7FFFu));
+      return t;
+    };
+    auto both = [](u16x2 t) { return __uint_as_float(uint32_t(t.x > t.y ? t.x : t.y) << 16); };
+    u16x2 kt = {0, 0}, qt = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < NK; ++t) kt = top_of(k[i][t], kt);
+#pragma unroll
+    for (int t = 0; t < NK; ++t) qt = top_of(w[t], qt);
+    const int ek = __builtin_amdgcn_frexp_expf(xmax32(xmax16(steps16(both(kt), 1, most))));
+    const int eq = __builtin_amdgcn_frexp_expf(xmax32(xmax16(both(qt))));
+    const int to = min(20 - ek, 120);          // the queries' exponent
+    bf16x8 q[NK];
+#pragma unroll
+    for (int t = 0; t < NK; ++t) {
+      uint32_t y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        y[e] = pack2(__builtin_amdgcn_ldexpf(__uint_as_float(w[t][e] << 16), to - eq),
+                     __builtin_amdgcn_ldexpf(__uint_as_float(w[t][e] & 0xFFFF0000u), to - eq));
+      q[t] = as_bf16x8(make_uint4(y[0], y[1], y[2], y[3]));
+    }
+    f32x4 s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < NK; ++t)
+        s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[i][t]), q[t], s[i], 0, 0, 0);
+    }
+    const float cs = score_factor(a.scale, a.scale_e + eq - to);
+    const int k0 = 16 * g, hi_ = min(hi, held) - k0, lo_ = lo - k0, sinks_ = sinks - k0;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i / 4][i % 4] = i < hi_ && (i >= lo_ || i < sinks_) ? s[i / 4][i % 4] : -INFINITY;
+      top = vmax(top, s[i / 4][i % 4]);
+    }
+    top = xmax32(xmax16(top)) * cs;
+    const bool some = top > -INFINITY;
+    // a whole number as the reference, as everywhere
+    r.M = some ? __builtin_floorf(top) : -FLT_MAX;
+    const float b = some ? -r.M : 0.f;
+    float sum = 0.f;
+    uint32_t ph[8], pl[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][2 * i % 4], cs, b));
+      const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][2 * i % 4 + 1], cs, b));
+      sum += x;
+      sum += y;
+      ph[i] = pack2(x, y);
+      pl[i] = pack2(x - __uint_as_float(ph[i] << 16), y - __uint_as_float(ph[i] & 0xFFFF0000u));
+    }
+    r.l = xsum32(xsum16(sum));
+    // the tokens behind the last one, of the piece that it lies in (and of those that the first one stands in for)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (held % 8 == 0 || (held > 8 && held / 8 % 2 != t)) continue;
+      const int start = 16 * g + 8 * t, n = start < held ? held - start : held < 8 ? 0 : 8;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) v[d][t] = first_of8(v[d][t], n);
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      r.x[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bf16x8 vv = __builtin_bit_cast(bf16x8, v[d][t]);
+        r.x[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            vv, as_bf16x8(make_uint4(ph[4 * t], ph[4 * t + 1], ph[4 * t + 2], ph[4 * t + 3])), r.x[d], 0, 0, 0);
+        r.x[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            vv, as_bf16x8(make_uint4(pl[4 * t], pl[4 * t + 1], pl[4 * t + 2], pl[4 * t + 3])), r.x[d], 0, 0, 0);
+      }
+    }
+  }
+};
+
+// The prefix's shares and the own tokens of a job, by one wave, through no LDS, so that as many as registers allow are on
+// the way (the launch is a chain of dependent reads), or, where jobs are few or long, by the four of a workgroup: the
+// first takes the open block, the others the shares, all of them the pages.  Rows fewer than 16 are repeated over
+// the tile, and the repetitions take the shares in turn.
+template <int D, int WAVES>
+__global__ __launch_bounds__(256, 2) void kv_join_kernel(PrefixArgs a) {
+  using T = Tile16<D>;
+  constexpr int ND = T::ND, NK = T::NK, KL = D == 128 ? 2 : 1;   // loads of a key's quarter
+  const tav2_kv& c = a.c;
+  OwnJob j;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  if (!own_job(a, WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x, j)) return;
+  const int lane = threadIdx.x % WAVE, m = lane % 16, g = lane / 16;
+  const int Rp = j.R <= 1 ? 1 : j.R <= 2 ? 2 : j.R <= 4 ? 4 : j.R <= 8 ? 8 : 16;
+  const int row = j.row0 + min(m % Rp, j.R - 1);
+  const int64_t at = row_at(a, j, row), n = a.q.total * a.q.heads;
+  const bf16_t* const q = static_cast<const bf16_t*>(a.q.q) + (j.q0 + row / j.G) * a.q.ld + (j.h * j.G + row % j.G) * D;
+
+  // the open block and the queries are on the way while the prefix's shares are joined
+  const int full = j.len / KVP, held = j.open && (WAVES == 1 || wave == 0) ? j.len - full * KVP : 0;
+  OpenBlock<D> open;
+  u32x4 w[NK];
+  if (held > 0) {
+    open.load(c, a.layer, j.s, j.h, held);
+#pragma unroll
+    for (int t = 0; t < NK; ++t) w[t] = *reinterpret_cast<const u32x4*>(q + g * (D / 4) + 8 * t);
+  }
+  int hi, lo;
+  row_seen(a, j, row, &hi, &lo);
+
+  // the prefix: references, sums, features
+  auto most = [](float a, float b) { return vmax(a, b); };
+  auto plus = [](float a, float b) { return a + b; };
+  const float2* const ml = reinterpret_cast<const float2*>(a.part_ml) + at;
+  Part<D> r;
+  r.M = -FLT_MAX;
+  r.l = 0.f;
+  const bool takes = WAVES == 1 || wave > 0;   // shares, in turn with the other waves that do
+  const int turns = WAVES == 1 ? 1 : WAVES - 1, turn = WAVES > 1 && takes ? wave - 1 : 0;
+  const int shares = takes ? j.shares : 0, reps = 16 / Rp;
+  for (int s = (m / Rp + reps * g) * turns + turn; s < shares; s += 4 * reps * turns) {   // (one, but for very long prefixes)
+    const float2 x = ml[s * n];
+    const float top = vmax(r.M, x.x), f = half_factor(x.x - top), of = half_factor(r.M - top);
+    r.l = r.l * of * of + x.y * f * f;
+    r.M = top;
+  }
+  {
+    const float top = xmax32(xmax16(steps16(r.M, Rp, most))), f = half_factor(r.M - top);
+    r.l = xsum32(xsum16(steps16(r.l * f * f, Rp, plus)));
+    r.M = top;
+  }
+#pragma unroll
+  for (int d = 0; d < ND; ++d) r.x[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll D <= 64 ? 4 : 2
+  for (int s = m / Rp * turns + turn; s < shares; s += reps * turns) {
+    const float2 x = ml[s * n];
+    const float f = half_factor(x.x - r.M);
+    const f32x4* const o = reinterpret_cast<const f32x4*>(a.part_o + (s * n + at) * D) + g;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      const f32x4 v = o[4 * d];   // (an empty share's are not written: read all the same, and dropped)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.x[d][e] += x.y != 0.f ? v[e] * f * f : 0.f;
+    }
+  }
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r.x[d][e] = steps16(r.x[d][e], Rp, plus);
+
+  // the own tokens: the open block, then pages as they lie
+  if (held > 0) {
+    Part<D> own;
+    open.attend(w, a, held, hi - full * KVP, lo - full * KVP, j.sinks - full * KVP, own);
+    r.add(own.M, own.l, own.x);
+  }
+  if (j.c1 > 0) {
+    T st;
+    st.sees(hi, lo, j.sinks);
+    st.query(q, a.scale_e);
+    st.clear();
+    const int krow = T::key();
+    for (int i = WAVES == 1 ? 0 : wave; i < j.c1; i += WAVES) {
+      const int b = j.list.at(i), page = __builtin_amdgcn_readfirstlane(j.table[b]);
+      if (page < 0 || page >= c.pages) continue;
+      const int64_t unit = kv_unit(c, a.layer, page, j.h);
+      const float ks = c.k_scale[unit], vs = c.v_scale[unit];
+      const int8_t* const kp = c.k + unit * KVP * D;
+      const int8_t* const vp = c.v + unit * KVP * D;
+      u32x4 kc[4][KL], vc[ND];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if constexpr (D == 32) {
+          const uint2 x = *reinterpret_cast<const uint2*>(kp + (krow + 4 * t) * D + g * 8);
+          kc[t][0] = (u32x4){x.x, x.y, 0, 0};
+        } else {
+#pragma unroll
+          for (int u = 0; u < KL; ++u)
+            kc[t][u] = *reinterpret_cast<const u32x4*>(kp + (krow + 4 * t) * D + g * (D / 4) + 16 * u);
+        }
+      }
+      uint32_t any = 0;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        vc[d] = *reinterpret_cast<const u32x4*>(vp + (16 * d + m) * KVP + 16 * g);
+        any |= vc[d].x | vc[d].y | vc[d].z | vc[d].w;
+      }
+      AttScale v{__builtin_amdgcn_logf(vs), __builtin_amdgcn_rcpf(vs)};
+      if (v.lv == 0.f && !__any(any != 0)) v.lv = -INFINITY;   // a block of zeros, whose scale counts as none
+      auto keys = [&](int t, f16x8(&kf)[NK]) {
+#pragma unroll
+        for (int u = 0; u < NK; ++u)
+          kf[u] = u % 2 ? codes8h(kc[t][u / 2].z, kc[t][u / 2].w) : codes8h(kc[t][u / 2].x, kc[t][u / 2].y);
+      };
+      auto values = [&](int d, f16x8(&vf)[2]) {
+        vf[0] = codes8h(vc[d].x, vc[d].y);
+        vf[1] = codes8h(vc[d].z, vc[d].w);
+      };
+      st.step(keys, values, score_factor(a.scale * ks, st.cq), v, b * KVP, hi);
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d) st.o[d] *= st.ratio;
+    r.add(st.wref, xsum32(xsum16(st.sum)), st.o);
+  }
+
+  if constexpr (WAVES > 1) {   // the first wave joins the others', in their order
+    __shared__ Part<D> parts[WAVES - 1][WAVE];
+    if (wave > 0) parts[wave - 1][lane] = r;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < WAVES - 1; ++w) r.add(parts[w][lane].M, parts[w][lane].l, parts[w][lane].x);
+  }
+  if (m >= j.R) return;
+  const bool some = r.l > 0.f || r.l != r.l;
+  const float inv = some ? 1.f / r.l : 0.f;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+    *reinterpret_cast<uint2*>(a.out + at * D + 16 * d + 4 * g) =
+        make_uint2(pack2(r.x[d][0] * inv, r.x[d][1] * inv), pack2(r.x[d][2] * inv, r.x[d][3] * inv));
+  if (g == 0 && a.lse) a.lse[at] = some ? (r.M + __builtin_amdgcn_logf(r.l)) * LN2 : -INFINITY;
+}
+
+constexpr size_t PLAN_BYTES = 256;   // before the parts
 
 // How the work on the prefixes is divided.
 struct Plan {
   int64_t rows;        // of a group and kv head
   int64_t pages;       // that a tile of the longest prefix sees, by the host's estimate
-  int tile, chunk, splits;
+  int64_t grid;
+  int tile, tiles, chunk, least, target, splits;
+  bool fit;
 };
 Plan plan_of(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q) {
   Plan p;
@@ -351,18 +651,28 @@ Plan plan_of(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q
   p.pages = std::max<int64_t>(1, cdiv(tokens, KVP));
   const int64_t work = int64_t(g.num_groups) * c.kv_heads * cdiv(p.rows, 64) * p.pages;
   p.tile = p.rows <= 16 ? 16
-           : p.rows > 32 && c.head_dim <= 64 && work > (c.head_dim == 64 ? 9000 : 100000) ? 64 : 32;
-  const int64_t tiles = int64_t(g.num_groups) * c.kv_heads * cdiv(p.rows, p.tile);
-  const int64_t least = std::max<int64_t>(4, std::min<int64_t>(p.rows, p.tile) / 2);
-  p.chunk = int(std::max(least, std::min<int64_t>(SHARE_MOST, cdiv(tiles * p.pages, SHARES))));
-  p.splits = int(cdiv(p.pages, p.chunk));
+           : p.rows > 48 && c.head_dim <= 64 && work > (c.head_dim == 64 ? 20000 : 100000) ? 64 : 32;
+  p.tiles = int(cdiv(p.rows, p.tile));
+  const int64_t units = int64_t(g.num_groups) * c.kv_heads * p.tiles;
+  p.least = 4;
+  p.fit = units <= 384;
+  p.target = !p.fit ? 1024 : p.tile == 64 ? 512 : 448;
+  // prefixes are a quarter of the longest at least, on average, or shares are larger than they might be
+  const bool planned = g.num_groups <= WAVE * PLAN;
+  const int64_t chunk = std::max<int64_t>(p.least, cdiv(units * p.pages, (planned ? 4 : 2) * p.target));
+  p.chunk = planned ? 0 : int(chunk);
+  p.splits = int(cdiv(p.pages, chunk));
+  const int64_t pads = p.tiles > 1 ? 8 * int64_t(p.tiles) : 0;
+  p.grid = planned ? p.target + units + g.num_groups * pads
+                   : g.num_groups * (int64_t(p.splits) * c.kv_heads * p.tiles + pads);
   return p;
-}
-int64_t prefix_units(const tav2_kv& c, const tav2_kv_groups& g, const Plan& p) {
-  return cdiv(int64_t(p.splits) * g.num_groups * c.kv_heads, 8) * 8;
 }
 int64_t own_tiles(const tav2_kv& c, const tav2_kv_queries& q) {
   return cdiv(int64_t(q.max_count) * (q.heads / c.kv_heads), 16);
+}
+// Whether a job is a workgroup's work instead of a wave's: few of them, or of many pages.
+bool join_by_four(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q) {
+  return g.max_own > 512 || int64_t(g.num_groups) * g.max_members * c.kv_heads * own_tiles(c, q) <= 1024;
 }
 
 }  // namespace
@@ -370,13 +680,12 @@ int64_t own_tiles(const tav2_kv& c, const tav2_kv_queries& q) {
 // (their product may pass 64 bits)
 double kv_prefix_workgroups(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q) {
   const Plan p = plan_of(c, g, q);
-  return std::max(double(prefix_units(c, g, p)) * double(cdiv(p.rows, p.tile)),
-                  double(g.num_groups) * g.max_members * c.kv_heads * double(own_tiles(c, q)));
+  return std::max(double(p.grid), double(g.num_groups) * g.max_members * c.kv_heads * double(own_tiles(c, q)));
 }
 
 size_t kv_prefix_bytes(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q) {
   const Plan p = plan_of(c, g, q);
-  return align_up(size_t(p.splits) * size_t(q.total) * q.heads * (c.head_dim + 2) * 4, 256);
+  return PLAN_BYTES + align_up(size_t(p.splits) * size_t(q.total) * q.heads * (c.head_dim + 2) * 4, 256);
 }
 
 hipError_t launch_kv_prefix(const tav2_kv& c, int layer, const tav2_kv_groups& g,
@@ -392,17 +701,22 @@ hipError_t launch_kv_prefix(const tav2_kv& c, int layer, const tav2_kv_groups& g
   a.scale = frexpf((q.scale > 0.f ? q.scale : 1.f / sqrtf(float(c.head_dim))) * LOG2E, &a.scale_e);
   a.out = static_cast<bf16_t*>(out);
   a.lse = lse;
-  a.part_o = static_cast<float*>(ws);
+  a.plan = static_cast<int32_t*>(ws);
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + PLAN_BYTES);
   a.part_ml = a.part_o + size_t(p.splits) * q.total * q.heads * c.head_dim;
   a.most_rows = int(p.rows);
-  a.tiles = int(cdiv(p.rows, p.tile));
+  a.tile = p.tile;
+  a.tiles = p.tiles;
   a.splits = p.splits;
   a.chunk = p.chunk;
-  a.units = int(prefix_units(c, g, p));
+  a.least = p.least;
+  a.target = p.target;
+  a.fit = p.fit;
+  a.seen = int(p.pages);
   a.own_tiles = int(own_tiles(c, q));
   {
     ProfScope prof("kv_prefix", st);
-    const unsigned grid = unsigned(a.units) * unsigned(a.tiles);
+    const unsigned grid = unsigned(p.grid);
     if (c.head_dim == 32) {
       if (p.tile == 16) kv_prefix16_kernel<32><<<grid, 256, 0, st>>>(a);
       else if (p.tile == 32) kv_prefix_kernel<32, 1><<<grid, 256, 0, st>>>(a);
@@ -419,9 +733,16 @@ hipError_t launch_kv_prefix(const tav2_kv& c, int layer, const tav2_kv_groups& g
   ProfScope prof("kv_join", st);
   const unsigned grid = unsigned(g.num_groups) * unsigned(g.max_members) * unsigned(c.kv_heads) *
                         unsigned(a.own_tiles);
-  if (c.head_dim == 32) kv_join_kernel<32><<<grid, 256, 0, st>>>(a);
-  else if (c.head_dim == 64) kv_join_kernel<64><<<grid, 256, 0, st>>>(a);
-  else kv_join_kernel<128><<<grid, 256, 0, st>>>(a);
+  if (join_by_four(c, g, q)) {
+    if (c.head_dim == 32) kv_join_kernel<32, 4><<<grid, 256, 0, st>>>(a);
+    else if (c.head_dim == 64) kv_join_kernel<64, 4><<<grid, 256, 0, st>>>(a);
+    else kv_join_kernel<128, 4><<<grid, 256, 0, st>>>(a);
+  } else {
+    const unsigned n = (grid + 3) / 4;
+    if (c.head_dim == 32) kv_join_kernel<32, 1><<<n, 256, 0, st>>>(a);
+    else if (c.head_dim == 64) kv_join_kernel<64, 1><<<n, 256, 0, st>>>(a);
+    else kv_join_kernel<128, 1><<<n, 256, 0, st>>>(a);
+  }
   return hipGetLastError();
 }
 

@@ -375,8 +375,9 @@ def test_attend_prefix(lens, members, owns, ns, heads, kv_heads, D, window, sink
               prefix=list(range(len(lens))))
     p.grow(lens + [owns[i % len(owns)] for i in range(M)])
     counts = [0] * len(lens) + [ns[i % len(ns)] for i in range(M)]
-    for mask in (T.MASK_CAUSAL, T.MASK_NONE):
-        attend(p, counts, heads, mask=mask, window=window, sinks=sinks, seed=M + window)
+    for p.groups.max_own in (64, 5000):      # a wave and a workgroup a member
+        for mask in (T.MASK_CAUSAL, T.MASK_NONE):
+            attend(p, counts, heads, mask=mask, window=window, sinks=sinks, seed=M + window)
 
 
 def test_attend_prefix_groups_of_every_kind():
@@ -385,9 +386,10 @@ def test_attend_prefix_groups_of_every_kind():
     p = Beams([2, 3, 2, 4, 1], first=3, H=2, D=64, seed=2, prefix=[-1, 1, 99, 0, 0])
     p.grow([200, 0, 70] + [5, 130, 0, 1, 64, 3, 0, 10, 9, 0, 2, 66])
     counts = [2, 1, 3] + [1, 4, 1, 0, 2, 1, 1, 3, 12, 2, 0, 1]
-    for mask in (T.MASK_CAUSAL, T.MASK_NONE):
-        for window, sinks in ((0, 0), (1, 0), (40, 130), (210, 3)):
-            attend(p, counts, 4, mask=mask, window=window, sinks=sinks, seed=window)
+    for p.groups.max_own in (64, 5000):
+        for mask in (T.MASK_CAUSAL, T.MASK_NONE):
+            for window, sinks in ((0, 0), (1, 0), (40, 130), (210, 3)):
+                attend(p, counts, 4, mask=mask, window=window, sinks=sinks, seed=window)
 
 
 def test_attend_prefix_released_blocks():
@@ -396,8 +398,9 @@ def test_attend_prefix_released_blocks():
     p.grow([300, 500, 200, 10, 140, 64, 300])
     p.trim(100, 65)
     for layer in (0, 1):
-        attend(p, [0, 0, 1, 1, 2, 1, 1], 2, layer=layer)
-        attend(p, [0, 0, 1, 1, 2, 1, 1], 2, layer=layer, window=90, sinks=65)
+        for p.groups.max_own in (64, 5000):
+            attend(p, [0, 0, 1, 1, 2, 1, 1], 2, layer=layer)
+            attend(p, [0, 0, 1, 1, 2, 1, 1], 2, layer=layer, window=90, sinks=65)
     p.trim(1, 0)
     attend(p, [0, 0, 1, 1, 2, 1, 1], 2, layer=1, mask=T.MASK_NONE)
 
