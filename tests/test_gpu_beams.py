@@ -229,10 +229,17 @@ class Beams(Pair):
         ob.reorder(self.ref, self.offset, parent)
 
 
-@pytest.mark.parametrize("D,H,layers", [(32, 3, 1), (64, 2, 3), (128, 1, 2)])
-def test_reorder(D, H, layers):
+# The host's estimate of the members' tokens decides between two forms of the reordering: one workgroup a
+# group, or many.
+FORMS = [0, 10 ** 6]
+
+
+@pytest.mark.parametrize("D,H,layers,form", [(32, 3, 1, 0), (64, 2, 3, 0), (128, 1, 2, 0), (128, 1, 9, 10 ** 6),
+                                             (64, 2, 8, 10 ** 6), (32, 3, 12, 10 ** 6)])
+def test_reorder(D, H, layers, form):
     """Copies, permutations, cycles, members that are emptied, own places and places past the group."""
     p = Beams([4, 1, 6, 3], first=2, H=H, D=D, layers=layers, seed=D)
+    p.groups.max_own = form
     p.grow([70, 5] + [1, 64, 63, 0] + [9] + [130, 127, 8, 64, 1, 200] + [7, 15, 16])
     p.same()
     p.reorder([1, 0, 3, 2] + [0] + [5, 0, 1, 2, 3, 4] + [2, 0, 1])      # cycles
@@ -260,31 +267,36 @@ def test_reorder_after_a_trim():
     p.same()
 
 
-def test_reorder_random_steps():
+@pytest.mark.parametrize("form", FORMS)
+def test_reorder_random_steps(form):
     g = np.random.default_rng(5)
     members = [17, 32, 5]
     p = Beams(members, first=1, pages=400, blocks=8, H=1, D=64, layers=2, seed=6)
+    p.groups.max_own = form
     for _ in range(8):
         p.grow([int(x) for x in g.integers(0, 40, size=p.seqs)])
         p.reorder([int(x) for n in members for x in g.integers(-1 if g.random() < 0.3 else 0, n, size=n)])
         p.same()
 
 
-def test_reorder_many_members():
+@pytest.mark.parametrize("form", FORMS)
+def test_reorder_many_members(form):
     """A group of the most members, long tables, and a bound below the group's members."""
     n = T.BEAMS_MAX
     g = np.random.default_rng(7)
     p = Beams([n], first=0, pages=3000, blocks=4, H=1, D=32, layers=1, seed=8)
+    p.groups.max_own = form
     p.grow([int(x) for x in g.integers(0, 200, size=n)])
     p.reorder([int(x) for x in g.permutation(n)])
     p.reorder([int(x) for x in g.integers(-1, n, size=n)])
     p.same()
     q = Beams([5], first=0, pages=3000, blocks=600, H=1, D=32, seed=9)
+    q.groups.max_own = form
     q.grow([64 * 590 + 3, 64 * 300, 1, 0, 64 * 599 + 63])
     for order in ([4, 0, 1, 2, 3], [1, 1, 1, 1, 1]):
         q.reorder(order)
         q.same(content=False)
-    q.groups = T.KvGroups(q.groups.offset, max_members=3)
+    q.groups = T.KvGroups(q.groups.offset, max_members=3, max_own=form)
     T.kv_reorder(q.gpu, q.groups, torch.tensor([2, 4, -1, -1, -1], dtype=torch.int32).cuda())
     ob.reorder(q.ref, q.offset, [2, 4, -1, -1, -1], 3)
     q.same(content=False)
