@@ -63,29 +63,54 @@ __device__ __forceinline__ float logit(const BeamArgs& a, int64_t row, int v) {
   return __builtin_isfinite(z) ? z : NONE;
 }
 
-// 2^f for |f| <= 1/2, off by at most 4.7e-11 of it (2^-34; fitted to the relative error's maximum, exact at 0), times 2^(the
-// low 32 bits of k): added to the exponent, as what converts or scales 64-bit numbers takes several times as long.
-__device__ __forceinline__ double exp2_part(double f, double k) {
-  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  double p = 1.5196156439583103e-05;
-  p = __builtin_fma(p, f, 1.5466756326706064e-04);
-  p = __builtin_fma(p, f, 1.3333935055974677e-03);
-  p = __builtin_fma(p, f, 9.618038132024047e-03);
-  p = __builtin_fma(p, f, 5.5504103659910264e-02);
-  p = __builtin_fma(p, f, 0.24022651066561432);
-  p = __builtin_fma(p, f, 0.6931471807045319);
-  p = __builtin_fma(p, f, 1.0);
-  u32x2 u = __builtin_bit_cast(u32x2, p);
-  u.y += __builtin_bit_cast(u32x2, k).x << 20;
-  return __builtin_bit_cast(double, u);
+// Exponentials in 64 bits: 2^(n / 64) from a table in LDS, times 1 + g (C1 + g (C2 + g C3)) for the rest g / 64, |g| <= 1/2:
+// off by at most 6.2e-12 of it (2^-37; fitted to the relative error's maximum, exact at 0).  n comes from the low bits of a
+// sum with 1.5 2^52; its multiples of 64 go into the exponent by an addition, as what converts or scales 64-bit numbers
+// takes several times as long.  14.7 instructions a logit; with a polynomial alone, 16.7, the largest case took 77.7 us for 74.
+constexpr double ROUND = 6755399441055744.0;
+constexpr double LOG2E_64 = 64 * 1.4426950408889634074;
+constexpr double C1 = 0.01083042469637773, C2 = 5.86491682817601e-05, C3 = 2.1173090131387150e-07;
+__device__ const double EXP2_64[64] = {
+    1.0, 1.0108892860517005, 1.0218971486541166, 1.0330248790212284,
+    1.0442737824274138, 1.0556451783605572, 1.0671404006768237, 1.0787607977571199,
+    1.0905077326652577, 1.102382583307841, 1.1143867425958924, 1.1265216186082418,
+    1.1387886347566916, 1.1511892299529827, 1.1637248587775775, 1.1763969916502812,
+    1.189207115002721, 1.202156731452703, 1.215247359980469, 1.22848053610687,
+    1.241857812073484, 1.255380757024691, 1.2690509571917332, 1.2828700160787783,
+    1.2968395546510096, 1.3109612115247644, 1.3252366431597413, 1.339667524053303,
+    1.3542555469368927, 1.3690024229745905, 1.383909881963832, 1.3989796725383112,
+    1.4142135623730951, 1.42961333839197, 1.4451808069770467, 1.460917794180647,
+    1.4768261459394993, 1.4929077282912648, 1.5091644275934228, 1.5255981507445384,
+    1.5422108254079407, 1.559004400237837, 1.5759808451078865, 1.593142151342267,
+    1.6104903319492543, 1.6280274218573478, 1.645755478153965, 1.6636765803267364,
+    1.681792830507429, 1.7001063537185235, 1.718619298122478, 1.7373338352737062,
+    1.7562521603732995, 1.7753764925265212, 1.7947090750031072, 1.8142521755003989,
+    1.8340080864093424, 1.8539791250833855, 1.8741676341103, 1.8945759815869656,
+    1.9152065613971474, 1.9360617934922943, 1.9571441241754002, 1.978456026387951,
+};
+
+// The table in LDS, an entry's exponent less what its own n adds (n << 14).
+__device__ __forceinline__ void load_table(uint2* table) {
+  if (threadIdx.x < 64) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, EXP2_64[threadIdx.x]);
+    table[threadIdx.x] = make_uint2(uint32_t(u), uint32_t(u >> 32) - (threadIdx.x << 14));
+  }
+  __syncthreads();
 }
-constexpr double LOG2E_64 = 1.4426950408889634074;
-constexpr double ROUND = 6755399441055744.0;   // 1.5 2^52: a sum with it is rounded to a whole number, which its low bits hold
+// s + 2^((n + g) / 64), n the low 32 bits of k.
+__device__ __forceinline__ double add_exp2(double s, double g, double k, const uint2* table) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const uint32_t n = __builtin_bit_cast(u32x2, k).x;
+  const uint2 t = table[n & 63];
+  const u32x2 u = {t.x, t.y + (n << 14)};
+  const double q = __builtin_fma(__builtin_fma(C3, g, C2), g, C1);
+  return __builtin_fma(__builtin_bit_cast(double, u), __builtin_fma(q, g, 1.0), s);
+}
 
 // exp(x - m) for x <= m, where x is not there 0 or next to it.
-__device__ __forceinline__ double weight(float x, double m) {
+__device__ __forceinline__ double weight(float x, double m, const uint2* table) {
   const double d = __builtin_fmax(double(x) - m, -700.0), k = __builtin_fma(d, LOG2E_64, ROUND);
-  return exp2_part(__builtin_fma(d, LOG2E_64, -(k - ROUND)), k);
+  return add_exp2(0.0, __builtin_fma(d, LOG2E_64, -(k - ROUND)), k, table);
 }
 
 // v joined over a wave's lanes by op, alike in all of them, on the vector unit alone: neighbours in fours, eights and
@@ -135,7 +160,7 @@ struct Segment {
   double sum;
 };
 template <bool BF, int VPT>
-__device__ __forceinline__ Segment scan(const BeamArgs& a, int64_t row, int seg) {
+__device__ __forceinline__ Segment scan(const BeamArgs& a, int64_t row, int seg, const uint2* table) {
   using L = Logits<BF>;
   constexpr int EL = L::EL, SEG = WAVE * VPT * EL;
   const int lane = threadIdx.x % WAVE, V = a.b.vocab;
@@ -212,42 +237,44 @@ __device__ __forceinline__ Segment scan(const BeamArgs& a, int64_t row, int seg)
   double s = 0.0;
   const double m = top;
   if (__all(low >= top - 700.f && __builtin_fabsf(top) < 16384.f)) {
-    // the usual sizes: exp(z) against 2^N next to exp(m), two instructions less for each
+    // the usual sizes: exp(z) against 2^(N / 64) next to exp(m), two instructions less for each
     const double N = __builtin_rint(m * LOG2E_64), R = ROUND - N;
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
       for (int e = 0; e < EL; ++e) {
         const double x = z[i][e], k = __builtin_fma(x, LOG2E_64, R);
-        s += exp2_part(__builtin_fma(x, LOG2E_64, -(k - R)), k);
+        s = add_exp2(s, __builtin_fma(x, LOG2E_64, -(k - R)), k, table);
       }
-    s *= exp2_part(__builtin_fma(m, -LOG2E_64, N), ROUND);
+    s *= add_exp2(0.0, __builtin_fma(m, -LOG2E_64, N), ROUND, table);
   } else if (top > NONE) {
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
-      for (int e = 0; e < EL; ++e) s += weight(z[i][e], m);
+      for (int e = 0; e < EL; ++e) s += weight(z[i][e], m, table);
   }
   r.sum = wave_sum(s);
   return r;
 }
 
-// Four segments a workgroup.
+// Waves take segments in turn.
 template <bool BF, int VPT>
 __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
-  const int per = (a.segs + 3) / 4;
-  const int64_t row = blockIdx.x / per;
-  if ((a.b.done && a.b.done[row]) || (a.b.score && !__builtin_isfinite(a.b.score[row]))) return;
-  const int seg = int(blockIdx.x % per) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  if (seg >= a.segs) return;
-  const Segment r = scan<BF, VPT>(a, row, seg);
-  const int64_t at = row * a.segs + seg;
-  a.best[at * WAVE + threadIdx.x % WAVE] = r.best;
-  const float b = wave_max(r.best);
-  if (threadIdx.x % WAVE == 0) {
-    a.seg_sum[at] = r.sum;
-    a.seg_top[at] = r.top;
-    a.seg_best[at] = b;
+  __shared__ uint2 table[64];
+  load_table(table);
+  const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int64_t all = int64_t(a.b.num_requests) * a.b.beams * a.segs;
+  for (int64_t at = int64_t(blockIdx.x) * 4 + wave; at < all; at += int64_t(gridDim.x) * 4) {
+    const int64_t row = at / a.segs;
+    if ((a.b.done && a.b.done[row]) || (a.b.score && !__builtin_isfinite(a.b.score[row]))) continue;
+    const Segment r = scan<BF, VPT>(a, row, int(at % a.segs), table);
+    a.best[at * WAVE + lane] = r.best;
+    const float b = wave_max(r.best);
+    if (lane == 0) {
+      a.seg_sum[at] = r.sum;
+      a.seg_top[at] = r.top;
+      a.seg_best[at] = b;
+    }
   }
 }
 
@@ -270,7 +297,10 @@ constexpr int LIST = 4096;    // segments, and then groups, that may hold some o
 
 struct PickShared {
   double base[TAV2_BEAMS_MAX];   // score - Z; a finished beam's score; NaN: no beam
-  uint32_t bins[BINS];
+  union {
+    uint32_t bins[BINS];
+    float top[TAV2_BEAMS_MAX];   // the largest logit; read before the bins are needed
+  };
   union {
     struct {
       uint64_t keys[CAP];
@@ -287,6 +317,7 @@ struct PickShared {
   };
   uint32_t wsum[NW], wmin[NW], wmax[NW];
   uint32_t n, bin, above;
+  uint2 table[64];
 };
 
 // The bin that the `need`-th from the top is in (BINS: there are fewer), and how many lie in the bins above it.
@@ -426,19 +457,20 @@ __device__ __forceinline__ void pick(const BeamArgs& a, PickShared& sh, int64_t 
     if (tid == 0) sh.n = 0;
     __syncthreads();
     if (fits) {
-      // a wave a group, four at once, so that their loads are on the way together; a group's tokens: those of one load are
-      // neighbours
-      const int i = lane / EL, e = lane % EL;
-      for (uint32_t k0 = wid; k0 < n_groups; k0 += 4 * NW) {
+      // a lane a token, four at once, so that their loads are on the way together
+      const int size = a.vpt * EL;   // of a group: 4 .. 64, a power of two; tokens of one load are neighbours
+      const int each = WAVE / size, mine = lane / size, i = lane % size / EL, e = lane % EL;
+      for (uint32_t k0 = wid * each + mine; k0 - mine < n_groups; k0 += 4 * NW * each) {
         int beam[4], v[4];
         float z[4];
         uint32_t ok[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const uint32_t g = sh.groups[min(k0 + u * NW, n_groups - 1)], s = g / WAVE;
+          const uint32_t k = k0 + u * NW * each;
+          const uint32_t g = sh.groups[min(k, n_groups - 1)], s = g / WAVE;
           beam[u] = int(s / S);
           v[u] = (int(s % S) * a.vpt + i) * (WAVE * EL) + int(g % WAVE) * EL + e;
-          if (k0 + u * NW >= n_groups || i >= a.vpt || v[u] >= V) v[u] = -1;
+          if (k >= n_groups || v[u] >= V) v[u] = -1;
           const int at = max(v[u], 0);
           z[u] = logit<BF>(a, row0 + beam[u], at);
           ok[u] = a.b.allowed ? a.b.allowed[(row0 + beam[u]) * a.b.allowed_ld + at / 8] >> (at % 8) & 1 : 1;
@@ -447,7 +479,7 @@ __device__ __forceinline__ void pick(const BeamArgs& a, PickShared& sh, int64_t 
         for (int u = 0; u < 4; ++u) {
           const double base = sh.base[beam[u]];
           if (done && done[beam[u]]) {
-            if (lane == 0 && k0 + u * NW < n_groups) list(value_key(base), uint32_t(beam[u]) * V + eos0);
+            if (lane % size == 0 && k0 + u * NW * each < n_groups) list(value_key(base), uint32_t(beam[u]) * V + eos0);
           } else if (v[u] >= 0 && ok[u] && z[u] > NONE && near_key(base + double(z[u])) >= bound) {
             list(value_key(base + double(z[u])), uint32_t(beam[u]) * V + v[u]);
           }
@@ -572,57 +604,78 @@ __global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
   const uint8_t* const done = a.b.done ? a.b.done + row0 : nullptr;
   const float* const seg_best = a.seg_best + row0 * S;
   const float* const best = a.best + row0 * S * WAVE;
-  // the beams' bases: a wave a beam
-  for (int b = wid; b < B; b += NW) {
-    const float* const tops = a.seg_top + (row0 + b) * S;
-    const double* const sums = a.seg_sum + (row0 + b) * S;
-    float m = NONE;
-    double z = 0.0;
-    if (!(done && done[b]) && !(a.b.score && !__builtin_isfinite(a.b.score[row0 + b]))) {
-      const float top = lane < S ? tops[lane] : NONE;
-      const double sum = lane < S ? sums[lane] : 0.0;
-      m = top;
-      for (int i = lane + WAVE; i < S; i += WAVE) m = vmax(m, tops[i]);
-      m = wave_max(m);
-      z = sum * weight(top, m);
-      for (int i = lane + WAVE; i < S; i += WAVE) z += sums[i] * weight(tops[i], m);
-      z = wave_sum(z);
+  load_table(sh.table);
+  // (the segments' best logits are on the way while the bases are found)
+  const uint32_t segs = uint32_t(B) * uint32_t(S);
+  const bool held = segs <= 4 * PICK;
+  float seg_z[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) seg_z[e] = held && tid + e * PICK < segs ? seg_best[tid + e * PICK] : NONE;
+  // the beams' largest logits and sums, a wave two beams at once; then their bases, a thread a beam
+  for (int b0 = wid; b0 < B; b0 += 2 * NW) {
+    float top[2], m[2];
+    double sum[2], z[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int b = min(b0 + u * NW, B - 1);
+      const bool there = lane < S && !(done && done[b]) && !(a.b.score && !__builtin_isfinite(a.b.score[row0 + b]));
+      top[u] = there ? a.seg_top[(row0 + b) * S + lane] : NONE;
+      sum[u] = there ? a.seg_sum[(row0 + b) * S + lane] : 0.0;
     }
-    const double x = base_of(a, row0 + b, m, z);
-    if (lane == 0) sh.base[b] = x;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int b = min(b0 + u * NW, B - 1);
+      const float* const tops = a.seg_top + (row0 + b) * S;
+      const double* const sums = a.seg_sum + (row0 + b) * S;
+      const bool there = !(done && done[b]) && !(a.b.score && !__builtin_isfinite(a.b.score[row0 + b]));
+      m[u] = top[u];
+      if (there)
+        for (int i = lane + WAVE; i < S; i += WAVE) m[u] = vmax(m[u], tops[i]);
+      m[u] = wave_max(m[u]);
+      z[u] = sum[u] * weight(top[u], m[u], sh.table);
+      if (there)
+        for (int i = lane + WAVE; i < S; i += WAVE) z[u] += sums[i] * weight(tops[i], m[u], sh.table);
+      z[u] = wave_sum(z[u]);
+      if (lane == 0 && b0 + u * NW < B) {
+        sh.base[b] = z[u];
+        sh.top[b] = m[u];
+      }
+    }
   }
   __syncthreads();
+  if (tid < B) sh.base[tid] = base_of(a, row0 + tid, sh.top[tid], sh.base[tid]);
+  __syncthreads();
 
-  const uint32_t segs = uint32_t(B) * uint32_t(S);
-  auto seg_key = [&](uint32_t i) -> uint32_t {
+  auto seg_key = [&](uint32_t i, float z) -> uint32_t {
     const int b = int(i / S);
-    return best_key(sh.base[b], done && done[b], i % S == 0, seg_best[i]);
+    return best_key(sh.base[b], done && done[b], i % S == 0, z);
   };
-  uint32_t bound = 1;
+  uint32_t bound = 1, seg_keys[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    seg_keys[e] = held && tid + e * PICK < segs ? seg_key(tid + e * PICK, seg_z[e]) : 0;
   if (segs >= 2 * uint32_t(K)) {
-    if (segs <= 4 * PICK) {
-      uint32_t keys[4];
+    bound = bound_of(sh, [&](auto f) {
+      if (held) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t i = tid + e * PICK;
-        keys[e] = i < segs ? seg_key(i) : 0;
+        for (int e = 0; e < 4; ++e) f(seg_keys[e]);
+      } else {
+        for (uint32_t i = tid; i < segs; i += PICK) f(seg_key(i, seg_best[i]));
       }
-      bound = bound_of(sh, [&](auto f) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f(keys[e]);
-      }, K, K + K / 4);
-    } else {
-      bound = bound_of(sh, [&](auto f) {
-        for (uint32_t i = tid; i < segs; i += PICK) f(seg_key(i));
-      }, K, K + K / 4);
-    }
+    }, K, K + K / 4);
   }
   if (tid == 0) sh.n = 0;
   __syncthreads();
-  for (uint32_t i = tid; i < segs; i += PICK) {
-    if (seg_key(i) < bound) continue;
+  auto list_segment = [&](uint32_t i, uint32_t key) {
+    if (key < bound) return;
     const uint32_t at = atomicAdd(&sh.n, 1u);
     if (at < LIST) sh.segs[at] = i;
+  };
+  if (held) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) list_segment(tid + e * PICK, seg_keys[e]);
+  } else {
+    for (uint32_t i = tid; i < segs; i += PICK) list_segment(i, seg_key(i, seg_best[i]));
   }
   __syncthreads();
   const uint32_t n_segs = sh.n;
@@ -663,6 +716,7 @@ __global__ __launch_bounds__(PICK) void beam_small_kernel(BeamArgs a) {
   const int lane = threadIdx.x % WAVE, wid = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int64_t row0 = int64_t(blockIdx.x) * B;
   const uint8_t* const done = a.b.done ? a.b.done + row0 : nullptr;
+  load_table(sh.table);
   uint32_t keys[ROWS];
 #pragma unroll
   for (int e = 0; e < ROWS; ++e) {
@@ -671,7 +725,7 @@ __global__ __launch_bounds__(PICK) void beam_small_kernel(BeamArgs a) {
     if (b >= B) continue;
     const bool ended = done && done[b];
     Segment r{NONE, NONE, 0.0};
-    if (!ended && !(a.b.score && !__builtin_isfinite(a.b.score[row0 + b]))) r = scan<BF, VPT>(a, row0 + b, 0);
+    if (!ended && !(a.b.score && !__builtin_isfinite(a.b.score[row0 + b]))) r = scan<BF, VPT>(a, row0 + b, 0, sh.table);
     const double x = base_of(a, row0 + b, r.top, r.sum);
     if (lane == 0) sh.base[b] = x;
     keys[e] = best_key(x, ended, lane == 0, r.best);
@@ -682,6 +736,9 @@ __global__ __launch_bounds__(PICK) void beam_small_kernel(BeamArgs a) {
     for (int e = 0; e < ROWS; ++e) f(keys[e], uint32_t(wid + e * NW) * WAVE + lane);
   });
 }
+
+// Workgroups of the first launch, at most: as many as run at once.
+constexpr int64_t SCANS = 2048;
 
 // Loads a lane: as many as leave workgroups enough to fill the CUs, and no row mostly empty segments.
 int vectors(const tav2_beams& b) {
@@ -729,7 +786,7 @@ void launch_small(const BeamArgs& a, hipStream_t st) {
 
 int64_t beam_select_groups(const tav2_beams& b, int keep) {
   if (small_vectors(b)) return int64_t(b.num_requests) * (PICK / 256);
-  return std::max(int64_t(b.num_requests) * b.beams * cdiv(segments(b), 4), int64_t(b.num_requests) * (PICK / 256));
+  return std::max<int64_t>(SCANS, int64_t(b.num_requests) * (PICK / 256));
 }
 
 size_t beam_select_bytes(const tav2_beams& b, int keep) {
@@ -763,7 +820,7 @@ hipError_t launch_beam_select(const tav2_beams& b, int keep, bool in_place, int3
   a.seg_best = a.seg_top + n;
   {
     ProfScope prof("beam_scan", st);
-    const unsigned groups = unsigned(int64_t(b.num_requests) * b.beams * cdiv(a.segs, 4));
+    const unsigned groups = unsigned(std::min<int64_t>(SCANS, cdiv(int64_t(n), 4)));
     if (b.dtype == TAV2_BF16) launch_scan<true>(a, groups, st);
     else launch_scan<false>(a, groups, st);
   }
