@@ -881,43 +881,45 @@ def beam_select(logits: torch.Tensor, beams: int, keep: int, score: Optional[tor
     [requests, beams] (None: zeros), done uint8 [requests, beams], allowed uint8 bits
     [requests * beams or 1, (vocab + 7) / 8 or more].  Returns (parent int32, token int32,
     score fp32, done uint8), each [requests, keep]; out: four tensors to use instead."""
-    _whole(beams | keep)
+    _whole(beams | keep | flags)
     _whole(eos)
-    _whole(flags)
-    dt = torch.float32 if logits.dtype == torch.float32 else torch.bfloat16
-    if logits.dim() != 2 or logits.dtype != dt:
+    dt = logits.dtype
+    if logits.dim() != 2 or (dt != torch.bfloat16 and dt != torch.float32):
         raise ValueError("logits: expected bf16 or fp32 [requests * beams, vocab]")
     rows, V = logits.shape
+    ld, one = logits.stride()
     if beams < 1 or rows % beams:
         raise ValueError(f"logits: {rows} rows are no whole requests of {beams} beams")
-    if V > 1 and logits.stride(1) != 1:
+    if V > 1 and one != 1:
         raise ValueError("logits: the tokens of a row must be contiguous")
     R = rows // beams
     _whole(R | V)
-    ld = logits.stride(0) if rows > 1 else V
-    _dense("score", score, (R, beams), torch.float32)
-    _dense("done", done, (R, beams), torch.uint8)
-    ald = 0
+    before, after = (R, beams), (R, keep)
+    _dense("score", score, before, torch.float32)
+    _dense("done", done, before, torch.uint8)
+    bits, ald = None, 0
     if allowed is not None:
         if allowed.dim() != 2 or allowed.dtype != torch.uint8 or allowed.shape[0] not in (1, rows) or \
                 allowed.shape[1] < (V + 7) // 8 or allowed.stride(1) != 1:
             raise ValueError("allowed: expected uint8 [requests * beams or 1, (vocab + 7) / 8 or more]")
-        ald = allowed.stride(0) if allowed.shape[0] > 1 else 0
-    dev = logits.device
+        bits, ald = allowed.data_ptr(), allowed.stride(0) if allowed.shape[0] > 1 else 0
     if out is None:
-        e = lambda t: torch.empty((R, max(keep, 0)), dtype=t, device=dev)
+        e = lambda t: torch.empty((R, max(keep, 0)), dtype=t, device=logits.device)
         out = e(torch.int32), e(torch.int32), e(torch.float32), e(torch.uint8)
-    for name, x, t in zip(("parent", "token", "score", "done"), out,
-                          (torch.int32, torch.int32, torch.float32, torch.uint8)):
-        _dense(f"out's {name}", x, (R, keep), t)
-    p = lambda t: None if t is None else t.data_ptr()
-    b = ctypes.byref(Beams(p(logits), p(score), p(done), p(allowed), ld, ald, R, beams, V,
-                           F32 if dt == torch.float32 else BF16, eos, 0))
-    ws = ws or Workspace(dev)
+    parent, token, best, ends = out
+    _dense("out's parent", parent, after, torch.int32)
+    _dense("out's token", token, after, torch.int32)
+    _dense("out's score", best, after, torch.float32)
+    _dense("out's done", ends, after, torch.uint8)
+    b = ctypes.byref(Beams(logits.data_ptr(), None if score is None else score.data_ptr(),
+                           None if done is None else done.data_ptr(), bits, ld if rows > 1 else V, ald, R, beams,
+                           V, BF16 if dt == torch.bfloat16 else F32, eos, 0))
+    ws = ws or Workspace(logits.device)
     wp, wb = ws.get(load_library().tav2_beam_select_workspace(b, keep))
     _run("tav2_beam_select", logits.get_device(), stream,
-         (b, keep, flags, p(out[0]), p(out[1]), p(out[2]), p(out[3]), wp, wb), logits, score, done,
-         allowed, *out, ws.buf)
+         (b, keep, flags, parent.data_ptr(), token.data_ptr(), best.data_ptr(),
+          None if ends is None else ends.data_ptr(), wp, wb), logits, score, done, allowed, parent, token,
+         best, ends, ws.buf if wb else None)
     return out
 
 
