@@ -505,8 +505,8 @@ typedef struct tav2_kv_groups {
   int32_t num_groups;          /* >= 0 */
   int32_t max_members;         /* host-side bound of a group's members, 1 .. TAV2_BEAMS_MAX; members past it
                                   are left out of a call */
-  int32_t max_own;             /* host-side estimate of the longest member: tav2_kv_attend_prefix
-                                  divides its work by it, as by tav2_kv's max_len */
+  int32_t max_own;             /* host-side estimate of the longest member's own tokens: the calls divide
+                                  their work by it, as by tav2_kv's max_len */
   int32_t reserved;            /* set to 0 */
 } tav2_kv_groups;
 
@@ -525,12 +525,14 @@ tav2_status tav2_kv_reorder(const tav2_kv* c, const tav2_kv_groups* g, const int
  * Attention of the members' queries over their group's prefix and their own tokens, as one softmax
  * over both; the prefix is read once for all members of the group.  q is tav2_kv_attend's: sequence
  * s's queries are offset[s] .. offset[s+1]; those of sequences in no group, and those past
- * max_count of a member, are left as they are in out and lse.  Query i of n of a member with len tokens
+ * max_count of a member, are left as they are in out and lse (and where a member has more, so may be those of
+ * members that follow it in its group).  Query i of n of a member with len tokens
  * of its own stands o = len - n + i (TAV2_MASK_CAUSAL) or o = len (TAV2_MASK_NONE) places behind the prefix:
  * it sees the prefix, and its own tokens up to o (none where that is negative).  With a window,
  * positions are counted from the prefix's first token, as if the member had followed it in one
  * sequence.  Blocks that were released are not seen.
- * Rounding, types, scales, out and lse as for tav2_kv_attend.
+ * Rounding, types, scales, out and lse as for tav2_kv_attend, but for a member's open block, where the products of
+ * queries and keys are exact and weights enter theirs with 2^-16.
  *   ws  device workspace of tav2_kv_attend_prefix_workspace() bytes, 256-byte aligned.
  */
 size_t tav2_kv_attend_prefix_workspace(const tav2_kv* c, const tav2_kv_groups* g,

@@ -135,7 +135,8 @@ __device__ __forceinline__ bool prefix_job(const PrefixArgs& a, int cap, PrefixJ
   int at = -1, x = 0, T = 0, S = 0, chunk = a.chunk;
   if (chunk == 0) {
     Group r[PLAN];
-    int tiles[PLAN], pages[PLAN], sum = 0, most = 0;
+    int tiles[PLAN], pages[PLAN], most = 0;
+    int64_t mine = 0;
 #pragma unroll
     for (int e = 0; e < PLAN; ++e) {
       tiles[e] = pages[e] = 0;
@@ -144,17 +145,19 @@ __device__ __forceinline__ bool prefix_job(const PrefixArgs& a, int cap, PrefixJ
       if (64 * e + lane < G) {
         tiles[e] = (group_rows(a, r[e]) + cap - 1) / cap;
         pages[e] = group_pages(a, r[e].len);
-        sum += tiles[e] * pages[e];
+        mine += int64_t(tiles[e]) * pages[e];
         if (tiles[e] > 0) most = max(most, pages[e]);
       }
     }
-    sum = __builtin_amdgcn_readlane(lanes_upto(sum), 63);
+    // (all groups have fewer than 2^24 tiles of at most 2^20 + 1 pages)
+    const int64_t sum = (int64_t(__builtin_amdgcn_readlane(lanes_upto(int(mine >> 24)), 63)) << 24) +
+                        __builtin_amdgcn_readlane(lanes_upto(int(mine & 0xFFFFFF)), 63);
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) most = max(most, __shfl_xor(most, o, WAVE));
     most = __builtin_amdgcn_readfirstlane(most);
     // (a multiple of four: the waves of a workgroup take pages in turn)
-    const int64_t each = (int64_t(sum) * H + a.target - 1) / a.target;
-    chunk = (max(max(a.least, int(each)), (most + a.splits - 1) / a.splits) + 3) / 4 * 4;
+    const int64_t each = (sum * H + a.target - 1) / a.target;
+    chunk = (max(max(a.least, each < most ? int(each) : most), (most + a.splits - 1) / a.splits) + 3) / 4 * 4;
     if (a.fit) {   // larger until all run at once
       while (true) {
         int n = 0;
@@ -162,7 +165,7 @@ __device__ __forceinline__ bool prefix_job(const PrefixArgs& a, int cap, PrefixJ
         for (int e = 0; e < PLAN; ++e) n += tiles[e] * shares_of(a, pages[e], chunk);
         n = __builtin_amdgcn_readlane(lanes_upto(n), 63);
         if (n * H <= a.target || chunk >= most) break;
-        chunk += 4;
+        chunk += 4 + chunk / 128 * 4;
       }
     }
     int before = 0;
@@ -191,9 +194,9 @@ __device__ __forceinline__ bool prefix_job(const PrefixArgs& a, int cap, PrefixJ
     const int per = group_jobs(a, a.tiles, a.splits);
     at = int(blockIdx.x) / per;
     x = int(blockIdx.x) % per;
-    my = group_of(a, at);
+    my = group_of(a, min(at, G - 1));
     T = a.tiles;
-    S = shares_of(a, group_pages(a, my.len), chunk);
+    S = at < G ? shares_of(a, group_pages(a, my.len), chunk) : 0;   // (the grid may be larger)
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.plan = chunk;
   if (at < 0) return false;
@@ -649,18 +652,19 @@ Plan plan_of(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q
   if (q.window > 0)
     tokens = std::min(tokens, int64_t(q.window) + g.max_own + q.sinks + 2 * KVP);
   p.pages = std::max<int64_t>(1, cdiv(tokens, KVP));
-  const int64_t work = int64_t(g.num_groups) * c.kv_heads * cdiv(p.rows, 64) * p.pages;
+  const double work = double(g.num_groups) * c.kv_heads * cdiv(p.rows, 64) * p.pages;
   p.tile = p.rows <= 16 ? 16
            : p.rows > 48 && c.head_dim <= 64 && work > (c.head_dim == 64 ? 20000 : 100000) ? 64 : 32;
   p.tiles = int(cdiv(p.rows, p.tile));
-  const int64_t units = int64_t(g.num_groups) * c.kv_heads * p.tiles;
+  // (a product with the pages is below 2^51; more units than 2^30 are refused as too many workgroups)
+  const int64_t units = std::min(int64_t(g.num_groups) * c.kv_heads * p.tiles, int64_t(1) << 30);
   p.least = 4;
   p.fit = units <= 384;
   p.target = !p.fit ? 1024 : p.tile == 64 ? 512 : 448;
   // prefixes are a quarter of the longest at least, on average, or shares are larger than they might be
   const bool planned = g.num_groups <= WAVE * PLAN;
   const int64_t chunk = std::max<int64_t>(p.least, cdiv(units * p.pages, (planned ? 4 : 2) * p.target));
-  p.chunk = planned ? 0 : int(chunk);
+  p.chunk = planned ? 0 : int(std::min(chunk, p.pages));
   p.splits = int(cdiv(p.pages, chunk));
   const int64_t pads = p.tiles > 1 ? 8 * int64_t(p.tiles) : 0;
   p.grid = planned ? p.target + units + g.num_groups * pads

@@ -2,12 +2,13 @@
 selection of beams, the reordering of the cache's sequences, and attention to a shared prefix.
 
 Bounds.  A selected value is computed in 64 bits from a sum of exponentials.  Each is off by at most
-4.7e-11 of itself (its polynomial), and so may be the factor that takes a part of the sum to the row's
-largest logit: Z is off by at most 9.4e-11, with fp64's own roundings below 2^-33; the value is rounded to fp32 once:
+6.2e-12 of itself (its polynomial), and so may be the factor that takes a part of the sum to the row's
+largest logit: Z is off by at most 1.3e-11, with fp64's own roundings below 2^-33; the value is rounded to fp32 once:
 |error| <= 2^-24 |value| + 2^-33.  Beams, tokens and flags are compared exactly: the
 inputs' values either tie exactly (equal logits of a row, equal rows) or lie further apart than 2^-30.
 Attention: as derived in test_gpu_history, where the same products and roundings are taken; one more
-factor joins the two launches' sums (its exponential and products are among the few 2^-23 there)."""
+factor joins the two launches' sums (its exponential and products are among the few 2^-23 there).
+A member's open block is nearer: its products are exact in fp32's sum, its weights off by 2^-16."""
 
 import numpy as np
 import pytest
@@ -210,6 +211,24 @@ def test_select_outputs_and_neighbours():
     assert empty[0].shape == (0, 2)
 
 
+@pytest.mark.parametrize("R,B,V,keep,dtype", [(1, 1, 1 << 20, 1024, F32), (2, 1024, 5, 1024, BF),
+                                              (1, 1, 1 << 24, 3, BF), (1, 64, 4096, 64, BF), (1, 64, 4097, 64, BF), (2, 65, 300, 65, F32),
+                                              (1, 3, 2049, 9, F32), (1500, 1, 9, 2, F32)])
+def test_select_largest_sizes(R, B, V, keep, dtype):
+    """The most tokens, beams and requests, and the sizes around which the work is divided in another way."""
+    check_select(logits(V, R, B, V, dtype), B, keep, score=[[-0.001 * b for b in range(B)]] * R)
+
+
+def test_select_rows_far_apart():
+    """Elements past 2^32 of the logits."""
+    V, ld = 5000, 640_000_000
+    near = logits(17, 2, 4, V, BF)
+    far = torch.empty(8, ld, dtype=BF, device="cuda")[:, 7:7 + V]
+    far.copy_(near)
+    a, b = T.beam_select(near, 4, 9), T.beam_select(far, 4, 9)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
 # ------------------------------------------------------------------------- kv_reorder
 class Beams(Pair):
     """A cache whose first sequences are histories and whose others are members of groups."""
@@ -321,6 +340,37 @@ def test_reorder_leaves_what_is_out_of_range():
     torch.cuda.synchronize()
 
 
+def test_tails_far_apart():
+    """Elements past 2^31 of the tails: the last layer reordered, and its open blocks read."""
+    L, S, H, D = 34, 1025, 8, 128
+    c = T.KvCache.create(L, 4, S, 2, H, D)
+    assert c.k_tail.numel() > 1 << 31
+    g = torch.Generator().manual_seed(5)
+    lens = torch.randint(0, P, (S,), generator=g, dtype=torch.int32)
+    c.length.copy_(lens)
+    for t in (c.k_tail, c.v_tail):
+        t[-1] = torch.randn(t[-1].shape, generator=g).to(BF).cuda()
+    k, v = c.k_tail[-1].clone(), c.v_tail[-1].clone()
+    groups = T.KvGroups(torch.tensor([1, 1025], dtype=torch.int32).cuda(), torch.tensor([0], dtype=torch.int32).cuda(),
+                        max_members=1024, max_own=63)
+    parent = torch.randint(0, 1024, (1024,), generator=g, dtype=torch.int32)
+    T.kv_reorder(c, groups, parent.cuda())
+    off = torch.tensor([0] + list(range(S)), dtype=torch.int64).cuda()
+    q = rows(g, S - 1, H, D)
+    out = T.kv_attend_prefix(c, L - 1, groups, q, off, 1)
+    one = T.KvCache.create(1, 4, S, 2, H, D)
+    src = torch.cat([torch.zeros(1, dtype=torch.long), parent.long() + 1]).cuda()
+    one.length.copy_(lens.cuda()[src])
+    one.k_tail[0], one.v_tail[0] = k[src], v[src]
+    assert torch.equal(c.length, one.length)
+    places = torch.arange(P).cuda()
+    held = (places[None] < one.length[:, None])[:, None]
+    same = lambda x, y, mask: torch.equal(torch.where(mask, x, 0), torch.where(mask, y, 0))
+    assert same(c.k_tail[-1], one.k_tail[0], held[..., None])
+    assert same(c.v_tail[-1], one.v_tail[0], held[:, :, None])
+    assert torch.equal(out, T.kv_attend_prefix(one, 0, groups, q, off, 1))
+
+
 # ------------------------------------------------------------------------- kv_attend_prefix
 def attend(p, counts, heads, layer=0, mask=T.MASK_CAUSAL, window=0, sinks=0, scale=0.0, seed=1, ws=None,
            max_count=None):
@@ -402,6 +452,58 @@ def test_attend_prefix_groups_of_every_kind():
         for mask in (T.MASK_CAUSAL, T.MASK_NONE):
             for window, sinks in ((0, 0), (1, 0), (40, 130), (210, 3)):
                 attend(p, counts, 4, mask=mask, window=window, sinks=sinks, seed=window)
+
+
+@pytest.mark.parametrize("groups", [256, 257, 600])
+@pytest.mark.parametrize("most", [2, 40])
+def test_attend_prefix_many_groups(groups, most):
+    """More groups than a workgroup divides the work of by itself, in one tile a group and in several."""
+    members = [1 + i % 2 for i in range(groups)]
+    members[groups - 2], members[3] = most, most
+    M = sum(members)
+    p = Beams(members, first=5, pages=200, blocks=20, H=1, D=32, seed=groups, prefix=[i % 7 - 1 for i in range(groups)])
+    p.grow([1100, 64, 0, 700, 130] + [(3 * i) % 71 if i % 50 == 0 else i % 3 for i in range(M)])
+    for window in (0, 90):
+        attend(p, [0] * 5 + [1 if i % 9 else 0 for i in range(M)], 2, window=window, sinks=2)
+
+
+def test_attend_prefix_a_very_long_prefix():
+    """One row, and more shares than it joins at once."""
+    p = Beams([1], first=1, pages=700, blocks=640, H=1, D=32, seed=13, prefix=[0])
+    p.grow([40001, 70])
+    attend(p, [0, 1], 1)
+    attend(p, [0, 2], 2, window=30000, sinks=100)
+
+
+def test_attend_prefix_bounds_below_what_is_given():
+    """Queries past max_count and members past max_members stay as they are."""
+    p = Beams([3, 2], first=2, H=2, D=64, seed=14, prefix=[0, 1])
+    p.grow([200, 90] + [5, 70, 9, 3, 64])
+    g = torch.Generator().manual_seed(1)
+    off = torch.tensor([0, 0, 0, 2, 4, 9, 10, 14]).cuda()      # five of the third member, four of the fifth
+    q = rows(g, 14, 4, 64)
+    out = torch.full_like(q, 7.0)
+    T.kv_attend_prefix(p.gpu, 0, p.groups, q, off, 2, out=out)
+    short = torch.tensor([0, 0, 0, 2, 4, 6, 7, 9]).cuda()
+    keep = torch.tensor([0, 1, 2, 3, 4, 5, 9, 10, 11]).cuda()
+    want = T.kv_attend_prefix(p.gpu, 0, p.groups, q[keep], short, 2)
+    assert torch.equal(out[keep], want)
+    assert (out[6:9] == 7.0).all() and (out[12:] == 7.0).all()
+    few = T.KvGroups(p.groups.offset, p.groups.prefix, max_members=2, max_own=70)
+    out = torch.full_like(want, 7.0)
+    T.kv_attend_prefix(p.gpu, 0, few, q[keep], short, 2, out=out)
+    assert torch.equal(out[:4], want[:4]) and torch.equal(out[6:], want[6:]) and (out[4:6] == 7.0).all()
+
+
+def test_attend_prefix_strided_queries():
+    p = Beams([3], first=1, H=2, D=32, seed=15, prefix=[0])
+    p.grow([200, 5, 70, 9])
+    g = torch.Generator().manual_seed(1)
+    qkv = rows(g, 3, 4 + 2 * 2, 32)
+    off = torch.tensor([0, 0, 1, 2, 3]).cuda()
+    a = T.kv_attend_prefix(p.gpu, 0, p.groups, qkv[:, :4], off, 1)
+    b = T.kv_attend_prefix(p.gpu, 0, p.groups, qkv[:, :4].contiguous(), off, 1)
+    assert torch.equal(a, b)
 
 
 def test_attend_prefix_released_blocks():
@@ -543,6 +645,53 @@ def test_a_step_in_a_graph():
         assert all(torch.equal(x, y) for x, y in zip(*sts)), i
         assert torch.equal(a.gpu.table, b.gpu.table) and torch.equal(a.gpu.refs, b.gpu.refs), i
         assert torch.equal(a.gpu.length, b.gpu.length)
+
+
+def test_two_graphs_share_a_workspace():
+    """Captured calls of both operators over one workspace, replayed in turn with eager calls between."""
+    p = Beams([9, 3], first=2, pages=100, blocks=30, H=2, D=64, seed=16, prefix=[0, 1])
+    p.grow([1500, 300] + [10, 70, 3] * 4)
+    g = torch.Generator().manual_seed(3)
+    off = torch.tensor([0, 0] + list(range(13))).cuda()
+    q, z = rows(g, 12, 4, 64), logits(4, 3, 4, 9000, BF)
+    ws = T.Workspace()
+    call_a = lambda: (T.kv_attend_prefix(p.gpu, 0, p.groups, q, off, 1, ws=ws),) + T.beam_select(z, 4, 20, ws=ws)
+    call_b = lambda: T.beam_select(z, 2, 30, ws=ws) + (
+        T.kv_attend_prefix(p.gpu, 0, p.groups, q, off, 1, window=99, ws=ws),)
+    call_a(), call_b()
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for call in (call_a, call_b):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(call())
+    for i in range(4):
+        z.copy_(logits(60 + i, 3, 4, 9000, BF))
+        q.copy_(rows(g, 12, 4, 64))
+        for k in (i % 2, 1 - i % 2):
+            graphs[k].replay()
+        want = call_a(), call_b()
+        torch.cuda.synchronize()
+        for got, ref in zip(outs, want):
+            assert all(torch.equal(x, y) for x, y in zip(got, ref)), i
+
+
+def test_two_calls_at_once():
+    """On two streams, a workspace each."""
+    p = Beams([20] * 4, first=4, pages=300, blocks=70, H=2, D=64, seed=17, prefix=[0, 1, 2, 3])
+    p.grow([4000, 300, 2000, 64] + [10, 70, 3, 0] * 20)
+    g = torch.Generator().manual_seed(3)
+    off = torch.tensor([0] * 4 + list(range(81))).cuda()
+    q, z = rows(g, 80, 8, 64), logits(4, 4, 20, 30000, BF)
+    call = lambda ws=None, st=None: (T.kv_attend_prefix(p.gpu, 0, p.groups, q, off, 1, ws=ws, stream=st),) + \
+        T.beam_select(z, 20, 20, ws=ws, stream=st)
+    want = call()
+    torch.cuda.synchronize()
+    streams, wss = [torch.cuda.Stream() for _ in range(2)], [T.Workspace() for _ in range(2)]
+    got = [call(wss[i % 2], streams[i % 2]) for i in range(8)]
+    torch.cuda.synchronize()
+    for x in got:
+        assert all(torch.equal(a, b) for a, b in zip(x, want))
 
 
 def test_on_another_stream():
