@@ -4,6 +4,9 @@
 // is taken first: the queries of all members of a group are rows of one tile set over the history's pages (as one
 // sequence's queries are in kv_attend), each page read and turned into operands once for 16, 32 or 64 rows of any
 // members.  A second launch takes each member's own tokens, joins the shares of its rows, and writes them.
+#include <algorithm>
+#include <type_traits>
+
 #include "kv_attend_core.h"
 
 namespace tav2 {
@@ -545,15 +548,17 @@ __global__ __launch_bounds__(256, 2) void kv_join_kernel(PrefixArgs a) {
   const int64_t at = row_at(a, j, row), n = a.q.total * a.q.heads;
   const bf16_t* const q = static_cast<const bf16_t*>(a.q.q) + (j.q0 + row / j.G) * a.q.ld + (j.h * j.G + row % j.G) * D;
 
-  // the open block and the queries are on the way while the prefix's shares are joined
+  // the open block and the queries are on the way while the prefix's shares are joined (by this wave; where others do
+  // that, no registers are held for both)
   const int full = j.len / KVP, held = j.open && (WAVES == 1 || wave == 0) ? j.len - full * KVP : 0;
   OpenBlock<D> open;
   u32x4 w[NK];
-  if (held > 0) {
+  auto fetch = [&]() {
     open.load(c, a.layer, j.s, j.h, held);
 #pragma unroll
     for (int t = 0; t < NK; ++t) w[t] = *reinterpret_cast<const u32x4*>(q + g * (D / 4) + 8 * t);
-  }
+  };
+  if (WAVES == 1 && held > 0) fetch();
   int hi, lo;
   row_seen(a, j, row, &hi, &lo);
 
@@ -580,17 +585,36 @@ __global__ __launch_bounds__(256, 2) void kv_join_kernel(PrefixArgs a) {
   }
 #pragma unroll
   for (int d = 0; d < ND; ++d) r.x[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll D <= 64 ? 4 : 2
-  for (int s = m / Rp * turns + turn; s < shares; s += reps * turns) {
-    const float2 x = ml[s * n];
-    const float f = half_factor(x.x - r.M);
-    const f32x4* const o = reinterpret_cast<const f32x4*>(a.part_o + (s * n + at) * D) + g;
+  // (N shares at once, as their loads are what takes the time; past the last one it is read again and dropped)
+  auto join = [&](int s0, auto count) {
+    constexpr int N = decltype(count)::value;
+    float2 x[N];
+    f32x4 v[N][ND];
 #pragma unroll
-    for (int d = 0; d < ND; ++d) {
-      const f32x4 v = o[4 * d];   // (an empty share's are not written: read all the same, and dropped)
+    for (int u = 0; u < N; ++u) {
+      const int s = s0 + u * reps * turns;
+      const int64_t i = min(s, shares - 1) * n;
+      x[u] = ml[i];
+      if (s >= shares) x[u].y = 0.f;
+      const f32x4* const o = reinterpret_cast<const f32x4*>(a.part_o + (i + at) * D) + g;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) r.x[d][e] += x.y != 0.f ? v[e] * f * f : 0.f;
+      for (int d = 0; d < ND; ++d) v[u][d] = o[4 * d];   // (an empty share's are not written: read all the same, and dropped)
     }
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const float f = half_factor(x[u].x - r.M);
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.x[d][e] += x[u].y != 0.f ? v[u][d][e] * f * f : 0.f;
+    }
+  };
+  constexpr int MOST = WAVES == 1 ? 1 : D <= 64 ? 4 : 2;
+  const int step = reps * turns;
+  int s0 = m / Rp * turns + turn;
+  for (int left = (shares + step - 1) / step; left > 0; left -= MOST, s0 += MOST * step) {
+    if (left > 1) join(s0, std::integral_constant<int, MOST>{});
+    else join(s0, std::integral_constant<int, 1>{});
   }
 #pragma unroll
   for (int d = 0; d < ND; ++d)
@@ -599,6 +623,7 @@ __global__ __launch_bounds__(256, 2) void kv_join_kernel(PrefixArgs a) {
 
   // the own tokens: the open block, then pages as they lie
   if (held > 0) {
+    if (WAVES > 1) fetch();
     Part<D> own;
     open.attend(w, a, held, hi - full * KVP, lo - full * KVP, j.sinks - full * KVP, own);
     r.add(own.M, own.l, own.x);
@@ -672,6 +697,27 @@ __global__ __launch_bounds__(256, 2) void kv_join_kernel(PrefixArgs a) {
 
 constexpr size_t PLAN_BYTES = 256;   // before the parts
 
+int64_t own_tiles(const tav2_kv& c, const tav2_kv_queries& q) {
+  return cdiv(int64_t(q.max_count) * (q.heads / c.kv_heads), 16);
+}
+bool count_members(const tav2_kv& c, const tav2_kv_groups& g) {
+  return g.num_groups <= WAVE * PLAN && c.num_seqs < int64_t(g.num_groups) * g.max_members;
+}
+double own_jobs(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q) {
+  const double members = count_members(c, g) ? c.num_seqs : double(g.num_groups) * g.max_members;
+  return members * c.kv_heads * double(own_tiles(c, q));
+}
+// Whether a job is a workgroup's work instead of a wave's: few of them (32 jobs 14.7 us for 18.4, 2048 jobs 67.8 for 64.7), or
+// of many pages (8 groups of 16 members with 500 - 2000 tokens 33.2 us for 63.3).
+bool join_by_four(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q) {
+  return g.max_own > 512 || own_jobs(c, g, q) <= 1024;
+}
+int pow2_from(int64_t n) {   // the least power of two from n on, up to 16
+  int p = 1;
+  while (p < 16 && p < n) p *= 2;
+  return p;
+}
+
 // How the work on the prefixes is divided.
 struct Plan {
   int64_t rows;        // of a group and kv head
@@ -688,14 +734,26 @@ Plan plan_of(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q
   if (q.window > 0)
     tokens = std::min(tokens, int64_t(q.window) + g.max_own + q.sinks + 2 * KVP);
   p.pages = std::max<int64_t>(1, cdiv(tokens, KVP));
+  // Rows of a tile.  64, which read and turn a page once for twice as many, where there are enough pairs of such a tile and a
+  // page: groups of 64 rows over 1024 - 16384 tokens, 16 of them (8224 pairs) 30.7 us for 27.6 with 32, 32 of them 42.1
+  // for 54.4, 64 of them with 32 features 45.9 for 82.8.
   const double work = double(g.num_groups) * c.kv_heads * cdiv(p.rows, 64) * p.pages;
   p.tile = p.rows <= 16 ? 16
-           : p.rows > 48 && c.head_dim <= 64 && work > (c.head_dim == 64 ? 20000 : 100000) ? 64 : 32;
+           : p.rows > 48 && c.head_dim <= 64 && work > 12000 ? 64 : 32;
   p.tiles = int(cdiv(p.rows, p.tile));
   // (a product with the pages is below 2^51; more units than 2^30 are refused as too many workgroups)
   const int64_t units = std::min(int64_t(g.num_groups) * c.kv_heads * p.tiles, int64_t(1) << 30);
-  p.least = 4;
-  p.fit = units <= 384;
+  // Workgroups: all at once where few tiles' shares can be made larger until they are (48 groups of 64 rows, 96 units: 54.7 us
+  // for 70.7), and in turn where a unit would be left whole (32 groups of 256 rows, 256 units: 122 for 177).  What runs at once
+  // is two a CU, a little fewer with 32 rows: 64 groups 64.9 us with 512, 70.5 with 448, 75.9 with 768; 16 groups
+  // in tiles of 32 27.6 with 448, 32.9 with 512, 33.9 with 256.
+  p.fit = units <= 192;
+  // A page more for each wave takes about as long as the join of as many shares as it takes at once (0.9 and 0.5 us): shares
+  // are of at least the pages for which both come to the least.  (16 rows of one group, 16384 tokens: 4 pages 16.5 us, 8
+  // 15.4, 16 16.6; 65536 tokens: 4 - 12 pages 22.7, 16 20.3.)
+  const int together = 16 / pow2_from(int64_t(q.max_count) * G) * (join_by_four(c, g, q) ? 3 : 1);
+  p.least = int(cdiv(int64_t(sqrt(2.2 / (p.tile == 64 ? 2 : 1) * double(p.pages) / together)), 4)) * 4;
+  p.least = std::max(p.least, 4);
   p.target = !p.fit ? 1024 : p.tile == 64 ? 512 : 448;
   // prefixes are a quarter of the longest at least, on average, or shares are larger than they might be
   const bool planned = g.num_groups <= WAVE * PLAN;
@@ -707,21 +765,6 @@ Plan plan_of(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q
                    : g.num_groups * (int64_t(p.splits) * c.kv_heads * p.tiles + pads);
   return p;
 }
-int64_t own_tiles(const tav2_kv& c, const tav2_kv_queries& q) {
-  return cdiv(int64_t(q.max_count) * (q.heads / c.kv_heads), 16);
-}
-bool count_members(const tav2_kv& c, const tav2_kv_groups& g) {
-  return g.num_groups <= WAVE * PLAN && c.num_seqs < int64_t(g.num_groups) * g.max_members;
-}
-double own_jobs(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q) {
-  const double members = count_members(c, g) ? c.num_seqs : double(g.num_groups) * g.max_members;
-  return members * c.kv_heads * double(own_tiles(c, q));
-}
-// Whether a job is a workgroup's work instead of a wave's: few of them, or of many pages.
-bool join_by_four(const tav2_kv& c, const tav2_kv_groups& g, const tav2_kv_queries& q) {
-  return g.max_own > 512 || own_jobs(c, g, q) <= 1024;
-}
-
 }  // namespace
 
 // (their product may pass 64 bits)
