@@ -803,8 +803,8 @@ class KvGroups:
     """A tav2_kv_groups: members of group g are the cache's sequences offset[g] .. offset[g+1] - 1
     (int32 [groups + 1] on the GPU), which continue sequence prefix[g] (int32 [groups], -1: none; None
     where the groups are only reordered).  max_members bounds a group's members; max_own is the host's
-    estimate of the longest member's own tokens, by which kv_attend_prefix divides its work; it may be
-    set anew as members grow."""
+    estimate of the longest member's own tokens, by which the calls divide their work; it may be set
+    anew as members grow."""
 
     def __init__(self, offset: torch.Tensor, prefix: Optional[torch.Tensor] = None,
                  max_members: int = BEAMS_MAX, max_own: int = KV_PAGE):
