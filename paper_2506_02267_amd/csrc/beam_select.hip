@@ -295,6 +295,9 @@ constexpr int BIN_BITS = 11, BINS = 1 << BIN_BITS;
 constexpr int CAP = 2048;     // continuations that are put in order at last
 constexpr int LIST = 4096;    // segments, and then groups, that may hold some of the best
 
+static_assert(BINS == 2 * PICK && TAV2_K_MAX <= PICK && TAV2_BEAMS_MAX <= PICK && TAV2_K_MAX <= CAP,
+              "two bins, a place, a beam for each thread; room for all that is asked for");
+
 struct PickShared {
   double base[TAV2_BEAMS_MAX];   // score - Z; a finished beam's score; NaN: no beam
   union {

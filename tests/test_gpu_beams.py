@@ -536,6 +536,34 @@ def test_attend_prefix_extreme_scores():
         attend(p, [0] + [1] * 6, 4, scale=1e-3 if spread > 1e3 else 0.0)
 
 
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_attend_prefix_values_of_every_size(D):
+    """Values up to 2^79 and down to 2^-70 beside each other, in pages and in open blocks; scores up to 2^20."""
+    p = Beams([5], first=1, H=2, D=D, seed=18, prefix=[0])
+    for n, spread in ((70, 2.0 ** -70), (90, 2.0 ** 76), (100, 1.0)):
+        p.grow([n, n, 3, 0, 70, 1], spread=spread)
+    for p.groups.max_own in (64, 5000):
+        for scale in (2.0 ** -80, 2.0 ** -66):
+            attend(p, [0, 1, 1, 1, 3, 1], 4, scale=scale)
+
+
+def test_workspace_contents_do_not_matter():
+    p = Beams([3, 9], first=2, blocks=30, H=2, D=64, seed=19, prefix=[0, 1])
+    p.grow([1100, 90] + [5, 70, 9] + [1, 0, 3, 4, 64, 2, 2, 2, 2])
+    g = torch.Generator().manual_seed(3)
+    off = torch.tensor([0, 0] + list(range(13))).cuda()
+    q, z = rows(g, 12, 4, 64), logits(4, 3, 4, 9000, BF)
+    ws = T.Workspace()
+    call = lambda: (T.kv_attend_prefix(p.gpu, 0, p.groups, q, off, 1, window=700, sinks=3, ws=ws),) + \
+        T.beam_select(z, 4, 20, ws=ws, done=done, eos=1)
+    done = torch.zeros(3, 4, dtype=torch.uint8, device="cuda")
+    done[1, 2] = 1
+    want = call()
+    for byte in (0, 255):
+        ws.buf.fill_(byte)
+        assert all(torch.equal(x, y) for x, y in zip(call(), want)), byte
+
+
 def test_attend_prefix_as_one_sequence():
     """The same tokens as prefix and own tokens, and as one sequence that kv_attend takes."""
     H, D, heads = 2, 64, 4
