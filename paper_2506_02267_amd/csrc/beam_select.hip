@@ -300,6 +300,7 @@ static_assert(BINS == 2 * PICK && TAV2_K_MAX <= PICK && TAV2_BEAMS_MAX <= PICK &
 
 struct PickShared {
   double base[TAV2_BEAMS_MAX];   // score - Z; a finished beam's score; NaN: no beam
+  bool ended[TAV2_BEAMS_MAX];    // finished
   union {
     uint32_t bins[BINS];
     float top[TAV2_BEAMS_MAX];   // the largest logit; read before the bins are needed
@@ -394,11 +395,10 @@ __device__ __forceinline__ uint32_t bound_of(PickShared& sh, Visit visit, uint32
   }
 }
 
-// A beam's base, from its row's largest logit and its sum of exponentials.
-__device__ __forceinline__ double base_of(const BeamArgs& a, int64_t n, float top, double sum) {
-  const float s = a.b.score ? a.b.score[n] : 0.f;
+// A beam's base, from its score, its row's largest logit and its sum of exponentials.
+__device__ __forceinline__ double base_of(float s, bool ended, float top, double sum) {
   if (!__builtin_isfinite(s)) return __builtin_nan("");
-  if (a.b.done && a.b.done[n]) return s;
+  if (ended) return s;
   return top > NONE ? double(s) - (double(top) + log(sum)) : __builtin_nan("");
 }
 
@@ -417,13 +417,12 @@ __device__ __forceinline__ void pick(const BeamArgs& a, PickShared& sh, int64_t 
   const int B = a.b.beams, V = a.b.vocab, K = a.keep, S = a.segs;
   const int tid = threadIdx.x, lane = tid % WAVE, wid = __builtin_amdgcn_readfirstlane(tid / WAVE);
   const int eos0 = a.b.eos < 0 ? 0 : a.b.eos;
-  const uint8_t* const done = a.b.done ? a.b.done + row0 : nullptr;
   const uint32_t total = uint32_t(B) * uint32_t(V);   // below 2^31
   // the key of beam b continued by v
   auto key_of = [&](int b, int v) -> uint64_t {
     const double x = sh.base[b];
     if (x != x) return 0;
-    if (done && done[b]) return v == eos0 ? value_key(x) : 0;
+    if (sh.ended[b]) return v == eos0 ? value_key(x) : 0;
     const float z = logit<BF>(a, row0 + b, v);
     if (!(z > NONE)) return 0;
     if (a.b.allowed && !(a.b.allowed[(row0 + b) * a.b.allowed_ld + v / 8] >> (v % 8) & 1)) return 0;
@@ -481,7 +480,7 @@ __device__ __forceinline__ void pick(const BeamArgs& a, PickShared& sh, int64_t 
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const double base = sh.base[beam[u]];
-          if (done && done[beam[u]]) {
+          if (sh.ended[beam[u]]) {
             if (lane % size == 0 && k0 + u * NW * each < n_groups) list(value_key(base), uint32_t(beam[u]) * V + eos0);
           } else if (v[u] >= 0 && ok[u] && z[u] > NONE && near_key(base + double(z[u])) >= bound) {
             list(value_key(base + double(z[u])), uint32_t(beam[u]) * V + v[u]);
@@ -591,7 +590,7 @@ __device__ __forceinline__ void pick(const BeamArgs& a, PickShared& sh, int64_t 
   if (tid >= K) return;
   const int64_t at = int64_t(blockIdx.x) * K + slot;
   a.parent[at] = p;
-  const bool was = p >= 0 && done && done[p];
+  const bool was = p >= 0 && sh.ended[p];
   a.token[at] = p < 0 ? -1 : was ? a.b.eos : sh.token[tid];
   a.score[at] = p < 0 ? -INFINITY : fmaxf(float(sh.value[tid]), -FLT_MAX);
   if (a.done) a.done[at] = p >= 0 && (was || (a.b.eos >= 0 && sh.token[tid] == a.b.eos));
@@ -604,7 +603,9 @@ __global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
   const int B = a.b.beams, K = a.keep, S = a.segs;
   const int tid = threadIdx.x, lane = tid % WAVE, wid = __builtin_amdgcn_readfirstlane(tid / WAVE);
   const int64_t row0 = int64_t(blockIdx.x) * B;
-  const uint8_t* const done = a.b.done ? a.b.done + row0 : nullptr;
+  // (all that does not depend on anything is on the way first; what a finished beam's rows hold is not used)
+  const bool ended = tid < B && a.b.done && a.b.done[row0 + tid];
+  const float score = tid < B && a.b.score ? a.b.score[row0 + tid] : 0.f;
   const float* const seg_best = a.seg_best + row0 * S;
   const float* const best = a.best + row0 * S * WAVE;
   load_table(sh.table);
@@ -621,23 +622,19 @@ __global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int b = min(b0 + u * NW, B - 1);
-      const bool there = lane < S && !(done && done[b]) && !(a.b.score && !__builtin_isfinite(a.b.score[row0 + b]));
-      top[u] = there ? a.seg_top[(row0 + b) * S + lane] : NONE;
-      sum[u] = there ? a.seg_sum[(row0 + b) * S + lane] : 0.0;
+      top[u] = lane < S ? a.seg_top[(row0 + b) * S + lane] : NONE;
+      sum[u] = lane < S ? a.seg_sum[(row0 + b) * S + lane] : 0.0;
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int b = min(b0 + u * NW, B - 1);
       const float* const tops = a.seg_top + (row0 + b) * S;
       const double* const sums = a.seg_sum + (row0 + b) * S;
-      const bool there = !(done && done[b]) && !(a.b.score && !__builtin_isfinite(a.b.score[row0 + b]));
       m[u] = top[u];
-      if (there)
-        for (int i = lane + WAVE; i < S; i += WAVE) m[u] = vmax(m[u], tops[i]);
+      for (int i = lane + WAVE; i < S; i += WAVE) m[u] = vmax(m[u], tops[i]);
       m[u] = wave_max(m[u]);
       z[u] = sum[u] * weight(top[u], m[u], sh.table);
-      if (there)
-        for (int i = lane + WAVE; i < S; i += WAVE) z[u] += sums[i] * weight(tops[i], m[u], sh.table);
+      for (int i = lane + WAVE; i < S; i += WAVE) z[u] += sums[i] * weight(tops[i], m[u], sh.table);
       z[u] = wave_sum(z[u]);
       if (lane == 0 && b0 + u * NW < B) {
         sh.base[b] = z[u];
@@ -646,12 +643,15 @@ __global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
     }
   }
   __syncthreads();
-  if (tid < B) sh.base[tid] = base_of(a, row0 + tid, sh.top[tid], sh.base[tid]);
+  if (tid < B) {
+    sh.base[tid] = base_of(score, ended, sh.top[tid], sh.base[tid]);
+    sh.ended[tid] = ended;
+  }
   __syncthreads();
 
   auto seg_key = [&](uint32_t i, float z) -> uint32_t {
     const int b = int(i / S);
-    return best_key(sh.base[b], done && done[b], i % S == 0, z);
+    return best_key(sh.base[b], sh.ended[b], i % S == 0, z);
   };
   uint32_t bound = 1, seg_keys[4];
 #pragma unroll
@@ -685,7 +685,7 @@ __global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
   __syncthreads();
   auto group_key = [&](uint32_t i) -> uint32_t {
     const int b = int(i / S);
-    return best_key(sh.base[b], done && done[b], i % S == 0 && lane == 0, best[int64_t(i) * WAVE + lane]);
+    return best_key(sh.base[b], sh.ended[b], i % S == 0 && lane == 0, best[int64_t(i) * WAVE + lane]);
   };
   constexpr int HELD = 8;   // segments of a wave whose groups' keys it holds
   if (n_segs <= HELD * NW) {
@@ -727,10 +727,14 @@ __global__ __launch_bounds__(PICK) void beam_small_kernel(BeamArgs a) {
     keys[e] = 0;
     if (b >= B) continue;
     const bool ended = done && done[b];
+    const float score = a.b.score ? a.b.score[row0 + b] : 0.f;
     Segment r{NONE, NONE, 0.0};
-    if (!ended && !(a.b.score && !__builtin_isfinite(a.b.score[row0 + b]))) r = scan<BF, VPT>(a, row0 + b, 0, sh.table);
-    const double x = base_of(a, row0 + b, r.top, r.sum);
-    if (lane == 0) sh.base[b] = x;
+    if (!ended && __builtin_isfinite(score)) r = scan<BF, VPT>(a, row0 + b, 0, sh.table);
+    const double x = base_of(score, ended, r.top, r.sum);
+    if (lane == 0) {
+      sh.base[b] = x;
+      sh.ended[b] = ended;
+    }
     keys[e] = best_key(x, ended, lane == 0, r.best);
   }
   __syncthreads();
