@@ -561,7 +561,8 @@ tav2_status tav2_kv_attend_prefix(const tav2_kv* c, int32_t layer, const tav2_kv
  *              places of beams that are not, in the order above: with the places as members of a
  *              group, tav2_kv_reorder then moves only those.
  *   ws  device workspace of tav2_beam_select_workspace() bytes, 256-byte aligned.
- * Outputs may not overlap inputs.  Errors: TAV2_ERR_NULL, TAV2_ERR_SHAPE, TAV2_ERR_DTYPE, TAV2_ERR_UNSUPPORTED (over
+ * Outputs may not overlap inputs, but out_score and out_done may be score and done where keep == beams.
+ * Errors: TAV2_ERR_NULL, TAV2_ERR_SHAPE, TAV2_ERR_DTYPE, TAV2_ERR_UNSUPPORTED (over
  * 2^31 - 1 logits a request or rows in all; over 2^24 - 1 workgroups), TAV2_ERR_WORKSPACE, TAV2_ERR_HIP.
  */
 #define TAV2_BEAMS_MAX 1024

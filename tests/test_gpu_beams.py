@@ -211,6 +211,25 @@ def test_select_outputs_and_neighbours():
     assert empty[0].shape == (0, 2)
 
 
+@pytest.mark.parametrize("R,B,V", [(40, 8, 300), (9, 32, 9000), (3, 100, 70)])
+def test_select_over_its_own_scores_and_flags(R, B, V):
+    """Scores and flags that are replaced by the call, ties that take the exact path among them."""
+    g = np.random.default_rng(V)
+    ws = T.Workspace()
+    score = torch.from_numpy(-g.random((R, B))).to(F32).cuda()
+    done = torch.zeros(R, B, dtype=torch.uint8, device="cuda")
+    parent, token = (torch.empty(R, B, dtype=torch.int32, device="cuda") for _ in range(2))
+    for step in range(4):
+        z = logits(step, R, B, V, BF)
+        z[:B] = 0.5
+        want = ob.select(z.double().cpu().numpy(), B, B, score.cpu().numpy(), done.cpu().numpy(), eos=1,
+                         in_place=step % 2 == 0)
+        got = T.beam_select(z, B, B, score=score, done=done, eos=1, out=(parent, token, score, done), ws=ws,
+                            flags=T.BEAM_RANKED if step % 2 else T.BEAM_IN_PLACE)
+        torch.cuda.synchronize()
+        same_selection(got, want)
+
+
 @pytest.mark.parametrize("R,B,V,keep,dtype", [(1, 1, 1 << 20, 1024, F32), (2, 1024, 5, 1024, BF),
                                               (1, 1, 1 << 24, 3, BF), (1, 64, 4096, 64, BF), (1, 64, 4097, 64, BF), (2, 65, 300, 65, F32),
                                               (1, 3, 2049, 9, F32), (1500, 1, 9, 2, F32)])
