@@ -545,11 +545,13 @@ tav2_status tav2_kv_attend_prefix(const tav2_kv* c, int32_t layer, const tav2_kv
 /*
  * Selection of beams.  Row n = r beams + b holds the logits z[n, v] of beam b of request r, which is
  * worth score[n] (the log-probability of what it holds) so far.  A beam continued by token v is worth
- *   (score[n] - Z_n) + z[n, v] ,  Z_n = log sum_v exp z[n, v] ,
- * computed in 64 bits (off by at most 2^-32); the `keep` best continuations of a request are selected, in the order
- * (value desc, beam asc, token asc).  Equal rows are computed alike; of values of beams whose rows differ and that lie
- * within the error of each other, as where the same logits stand in another order, either may come first.  A finished beam (done[n] != 0) has one continuation, itself, with its
- * score as it stands, token eos (in the order as token 0 where eos is negative).
+ *   score[n] + (z[n, v] - Z_n) ,  Z_n = log sum_v exp z[n, v] ,
+ * computed in 64 bits, whatever the logits' size (off by at most 2^-32, and by 2^-50 of the larger of score and value); the
+ * `keep` best continuations of a request are selected, in the order (value desc, beam asc, token asc).  Equal rows are
+ * computed alike; of values of beams whose rows differ and that lie within the error of each other, as where the same logits
+ * stand in another order, either may come first, and logits of a row whose values are the same number in 64 bits are equal.
+ * A finished beam (done[n] != 0) has one continuation, itself, with its score as it stands, token eos (in the order as
+ * token 0 where eos is negative).
  * Logits that are no finite numbers are not there; a token whose bit in `allowed` is 0 counts in Z_n
  * but is no continuation; a beam whose score is not finite is none.
  *   out_parent device int32 [requests, keep]: the beam b that is continued, -1 where there are fewer

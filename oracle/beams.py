@@ -9,13 +9,13 @@ import numpy as np
 from .history import attend
 
 
-def log_sum_exp(z):
-    """log of the sum of exp over the finite numbers of z (-inf: there are none)."""
-    z = [float(x) for x in z if math.isfinite(x)]
-    if not z:
-        return -math.inf
-    m = max(z)
-    return m + math.log(math.fsum(np.exp(np.array(z) - m)))
+def log_sum(z):
+    """(m, log of the sum of exp(z - m)) over the finite numbers of z, m the largest of them (None: there are none).  Apart,
+    since next to a large m their sum would lose the logarithm."""
+    z = np.array([float(x) for x in z if math.isfinite(x)])
+    if not len(z):
+        return None, 0.0
+    return z.max(), math.log(math.fsum(np.exp(z - z.max())))
 
 
 def select(logits, beams, keep, score=None, done=None, allowed=None, eos=-1, in_place=False):
@@ -37,13 +37,15 @@ def select(logits, beams, keep, score=None, done=None, allowed=None, eos=-1, in_
             if done is not None and done[r][b]:
                 found.append((-s, b, max(eos, 0)))
                 continue
-            base = s - log_sum_exp(logits[n])
+            m, total = log_sum(logits[n])
+            if m is None:
+                continue
+            base = s - total
             ok = np.isfinite(logits[n])
             if allowed is not None:
                 ok = ok & allowed[n]
             v = np.flatnonzero(ok)
-            with np.errstate(invalid="ignore"):
-                c = base + logits[n][v]
+            c = base + (logits[n][v] - m)
             best = np.lexsort((v, -c))[:keep]
             found += [(-float(c[i]), b, int(v[i])) for i in best]
         found = sorted(found)[:keep]

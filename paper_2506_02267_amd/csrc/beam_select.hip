@@ -1,8 +1,9 @@
 // Selection of the best continuations of a request's beams over the vocabulary.
 //
-// A continuation is worth c = (score - Z) + z, Z the row's log-sum-exp; it is computed in 64 bits, since the values
-// of different beams have to be put in order: with an error of 1e-7 two of a request's best would change places
-// now and then.
+// A continuation is worth c = (score - log S) + (z - top), S the row's sum of exp(z - top), top its largest logit; it is
+// computed in 64 bits, since the values of different beams have to be put in order: with an error of 1e-7 two of a
+// request's best would change places now and then.  top and log S stay apart: their sum would drop log S where logits are
+// large (a row filled with the type's lowest value: every token would be worth the score itself).
 //
 // The first launch reads the logits once.  A wave takes a segment of a row, VPT 16-byte loads a lane, holds it in
 // registers, and leaves its largest logit, its sum of exponentials, and each lane's largest logit (a group's: the
@@ -299,12 +300,10 @@ static_assert(BINS == 2 * PICK && TAV2_K_MAX <= PICK && TAV2_BEAMS_MAX <= PICK &
               "two bins, a place, a beam for each thread; room for all that is asked for");
 
 struct PickShared {
-  double base[TAV2_BEAMS_MAX];   // score - Z; a finished beam's score; NaN: no beam
+  double base[TAV2_BEAMS_MAX];   // score - log S; a finished beam's score; NaN: no beam
+  float top[TAV2_BEAMS_MAX];     // the largest logit (of a finished beam: anything)
   bool ended[TAV2_BEAMS_MAX];    // finished
-  union {
-    uint32_t bins[BINS];
-    float top[TAV2_BEAMS_MAX];   // the largest logit; read before the bins are needed
-  };
+  uint32_t bins[BINS];
   union {
     struct {
       uint64_t keys[CAP];
@@ -399,17 +398,19 @@ __device__ __forceinline__ uint32_t bound_of(PickShared& sh, Visit visit, uint32
 __device__ __forceinline__ double base_of(float s, bool ended, float top, double sum) {
   if (!__builtin_isfinite(s)) return __builtin_nan("");
   if (ended) return s;
-  return top > NONE ? double(s) - (double(top) + log(sum)) : __builtin_nan("");
+  return top > NONE ? double(s) - log(sum) : __builtin_nan("");
 }
+// What the token of logit z is worth.
+__device__ __forceinline__ double worth(double base, float top, float z) { return base + (double(z) - double(top)); }
 
 // What a segment or a group of beam b holds at best, of which z is the largest logit; a finished beam's one
 // continuation counts as its first one's.
-__device__ __forceinline__ uint32_t best_key(double base, bool done, bool first, float z) {
+__device__ __forceinline__ uint32_t best_key(double base, float top, bool done, bool first, float z) {
   if (done) return first && base == base ? near_key(base) : 0;
-  return base == base && z > NONE ? near_key(base + double(z)) : 0;
+  return base == base && z > NONE ? near_key(worth(base, top, z)) : 0;
 }
 
-// The selection of a request, whose bases are in sh.  visit(f) calls f(key, group) for the groups that hold all of the
+// The selection of a request, whose bases and largest logits are in sh.  visit(f) calls f(key, group) for the groups that hold all of the
 // best; a group is (beam * segments + segment) * 64 + lane.
 template <bool BF, class Visit>
 __device__ __forceinline__ void pick(const BeamArgs& a, PickShared& sh, int64_t row0, uint32_t bound, bool fits, Visit visit) {
@@ -426,7 +427,7 @@ __device__ __forceinline__ void pick(const BeamArgs& a, PickShared& sh, int64_t 
     const float z = logit<BF>(a, row0 + b, v);
     if (!(z > NONE)) return 0;
     if (a.b.allowed && !(a.b.allowed[(row0 + b) * a.b.allowed_ld + v / 8] >> (v % 8) & 1)) return 0;
-    return value_key(x + double(z));
+    return value_key(worth(x, sh.top[b], z));
   };
   auto list = [&](uint64_t k, uint32_t flat) {
     const uint32_t at = atomicAdd(&sh.n, 1u);
@@ -479,11 +480,12 @@ __device__ __forceinline__ void pick(const BeamArgs& a, PickShared& sh, int64_t 
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const double base = sh.base[beam[u]];
+          const double c = worth(sh.base[beam[u]], sh.top[beam[u]], z[u]);
           if (sh.ended[beam[u]]) {
-            if (lane % size == 0 && k0 + u * NW * each < n_groups) list(value_key(base), uint32_t(beam[u]) * V + eos0);
-          } else if (v[u] >= 0 && ok[u] && z[u] > NONE && near_key(base + double(z[u])) >= bound) {
-            list(value_key(base + double(z[u])), uint32_t(beam[u]) * V + v[u]);
+            if (lane % size == 0 && k0 + u * NW * each < n_groups)
+              list(value_key(sh.base[beam[u]]), uint32_t(beam[u]) * V + eos0);
+          } else if (v[u] >= 0 && ok[u] && z[u] > NONE && near_key(c) >= bound) {
+            list(value_key(c), uint32_t(beam[u]) * V + v[u]);
           }
         }
       }
@@ -651,7 +653,7 @@ __global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
 
   auto seg_key = [&](uint32_t i, float z) -> uint32_t {
     const int b = int(i / S);
-    return best_key(sh.base[b], sh.ended[b], i % S == 0, z);
+    return best_key(sh.base[b], sh.top[b], sh.ended[b], i % S == 0, z);
   };
   uint32_t bound = 1, seg_keys[4];
 #pragma unroll
@@ -685,7 +687,7 @@ __global__ __launch_bounds__(PICK) void beam_pick_kernel(BeamArgs a) {
   __syncthreads();
   auto group_key = [&](uint32_t i) -> uint32_t {
     const int b = int(i / S);
-    return best_key(sh.base[b], sh.ended[b], i % S == 0 && lane == 0, best[int64_t(i) * WAVE + lane]);
+    return best_key(sh.base[b], sh.top[b], sh.ended[b], i % S == 0 && lane == 0, best[int64_t(i) * WAVE + lane]);
   };
   constexpr int HELD = 8;   // segments of a wave whose groups' keys it holds
   if (n_segs <= HELD * NW) {
@@ -733,9 +735,10 @@ __global__ __launch_bounds__(PICK) void beam_small_kernel(BeamArgs a) {
     const double x = base_of(score, ended, r.top, r.sum);
     if (lane == 0) {
       sh.base[b] = x;
+      sh.top[b] = r.top;
       sh.ended[b] = ended;
     }
-    keys[e] = best_key(x, ended, lane == 0, r.best);
+    keys[e] = best_key(x, r.top, ended, lane == 0, r.best);
   }
   __syncthreads();
   pick<BF>(a, sh, row0, 1, true, [&](auto f) {

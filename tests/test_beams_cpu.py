@@ -2,6 +2,7 @@
 argument error is reported before anything is launched), the binding's, and pins of the oracle
 (oracle/beams.py) against brute force."""
 import ctypes
+import decimal
 import math
 import os
 import subprocess
@@ -252,6 +253,55 @@ def test_select_against_all_continuations():
             for k in range(n - 1):                # equal ones of a beam: the lower token first
                 if p[r, k] == p[r, k + 1] and v[r, k] == v[r, k + 1]:
                     assert t[r, k] < t[r, k + 1]
+
+
+def by_definition(z, keep, score):
+    """(beam, token, score + log(e^z / sum of e^z)) of the `keep` best of one request, in decimals of 120 digits."""
+    d = decimal.Decimal
+    with decimal.localcontext() as ctx:
+        ctx.prec = 120
+        every = []
+        for b, row in enumerate(np.asarray(z, dtype=np.float64)):
+            row = [d(float(x)) for x in row]
+            m = max(row)
+            total, exps = d(0), {}
+            for x in row:
+                if x not in exps:
+                    exps[x] = (x - m).exp() if x - m > -2000 else d(0)
+                total += exps[x]
+            base = d(float(score[b])) - total.ln() - m
+            every += [(-(base + x), b, v) for v, x in enumerate(row)]
+        return [(b, v, float(-c)) for c, b, v in sorted(every)[:keep]]
+
+
+def large_logits(V, dtype):
+    """(logits, scores, keep): rows of logits so large that their own size drowns the logarithm of their sum."""
+    g = torch.Generator().manual_seed(V)
+    top = torch.finfo(dtype).max
+    normal = torch.randn(V, generator=g)
+    flat = lambda x: torch.full((V,), x)
+    masked = flat(-top)
+    masked[V // 3], masked[V - 1] = 0.0, -1.5
+    spike = flat(-top)
+    spike[V // 2] = top
+    steps = flat(2.0 ** 30)
+    steps[1::2] = -(2.0 ** 30)
+    # a beam whose tokens are all masked by the type's lowest value; all of one size; a few of each
+    for rows, score, keep in (([normal, flat(-top)], (0.0, 0.0), 4), ([normal, flat(-top), normal * 3], (-9.0, -0.5, -30.0), 9),
+                              ([flat(2.0 ** 30)], (0.0,), 2), ([flat(2.0 ** 24), flat(-top), flat(top), flat(0.0)], (-1.0, -0.25, -0.5, 0.0), 7),
+                              ([masked, spike, normal], (-2.0, -1.0, 0.0), 5), ([steps, flat(1.0)], (-0.5, 0.25), 6)):
+        z = torch.stack(rows).to(dtype)
+        yield z, score, min(keep, z.numel())
+
+
+@pytest.mark.parametrize("V", [2, 3, 100, 3000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_select_of_large_logits(V, dtype):
+    for z, score, keep in large_logits(V, dtype):
+        p, t, v, _ = beams.select(z.double().numpy(), len(z), keep, [score])
+        want = by_definition(z.double().numpy(), keep, score)
+        assert list(zip(p[0], t[0])) == [x[:2] for x in want]
+        assert np.allclose(v[0], [x[2] for x in want], rtol=2.0 ** -50, atol=2.0 ** -45)
 
 
 def test_select_in_place():

@@ -16,6 +16,7 @@ import torch
 
 from oracle import beams as ob
 from paper_2506_02267_amd import tav2 as T
+from test_beams_cpu import by_definition, large_logits
 from test_gpu_history import BF, HALF, Pair, bound, rows
 
 pytestmark = pytest.mark.gpu
@@ -181,6 +182,24 @@ def test_select_logits_of_every_size(dtype):
     z[2] = 0.0
     z[2, 77] = 90.0
     check_select(z.to(dtype).cuda(), B, 50, score=[[0.0, -0.3, 5.0]])
+
+
+@pytest.mark.parametrize("V", [2, 100, 3000, 5000])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_select_of_large_logits(V, dtype):
+    """A continuation is worth its score plus its logit less its row's sum, however large the logits are."""
+    for z, score, keep in large_logits(V, dtype):
+        want = by_definition(z.double().numpy(), keep, score)
+        got = run_select(z.cuda(), len(z), keep, [score])
+        assert list(zip(got[0][0].tolist(), got[1][0].tolist())) == [x[:2] for x in want]
+        value = np.maximum([x[2] for x in want], -float(np.finfo(np.float32).max))
+        off = np.abs(got[2][0].double().cpu().numpy() - value)
+        assert (off <= 2.0 ** -24 * np.abs(value) + 2.0 ** -33).all()
+        check_select(z.cuda(), len(z), keep, [score])
+    # more equal values than are put in order at once
+    z = torch.zeros(3, 5000)
+    z[1], z[2] = -torch.finfo(dtype).max, 2.0 ** 30
+    check_select(z.to(dtype).cuda(), 3, 40, [[-1.0, 0.0, -0.5]])
 
 
 def test_select_values_close_together():
