@@ -441,8 +441,7 @@ tav2_status tav2_kv_append(const tav2_kv* c, int32_t layer, const void* k, int64
  *     every cached token.
  * window and sinks as for tav2_attend_window, counted from the query's position; blocks that were
  * released (tav2_kv_trim) are not seen.  out and lse as there; a query that sees nothing gets
- * zeros and -inf.  Queries (finite; scores up to 2^20, as fp32 rounds larger ones by more than a weight
- * bears) and outputs are bf16; products take the codes
+ * zeros and -inf.  Queries (finite; scores up to 2^125, as fp32 rounds them) and outputs are bf16; products take the codes
  * exactly, the scales in fp32, the weights in fp16 (off by at most 2^-11 of one, or 2^-31 of the largest).
  *   ws  device workspace of tav2_kv_attend_workspace() bytes, 256-byte aligned.
  * Errors: those above, TAV2_ERR_WORKSPACE.

@@ -19,10 +19,14 @@
 //
 // Values may come with a scale 2^lv of their own for each block of keys.  What is multiplied is then a weight
 // times 2^lv, against m; the weights' sum l has a reference of its own, n, since scales lie further apart
-// than fp32's powers of two reach.  A block's part of it comes from the same exponentials,
-// 2^(c s + lv - m): times 2^-lv 2^(m - n) = inv d.  A block whose products are all below 2^(m - FLOOR), or
+// than fp32's powers of two reach (m is kept as what it lies above n).  A block's part of it comes from the same
+// exponentials, 2^(c s + lv - m): times 2^-lv 2^(m - n) = inv d.  A block whose products are all below 2^(m - FLOOR), or
 // whose values are zeros (lv = -inf), adds nothing to the features, its weights being zeros in fp16; its
 // exponentials are taken against its own largest score, for the sum alone.
+//
+// References past 2^20 are numbers that fp32 rounds to the size of an exponent and more, c s in the fused multiply-add
+// is not rounded: their difference may then be anything, infinite weights included.  Such rows' scores are taken
+// against the block's own largest one first, which leaves differences that are exact, of scores as fp32 rounds them.
 #pragma once
 
 #include <float.h>
@@ -37,7 +41,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 
-constexpr float RAISE = 14.f, ROOM = 6.f, FLOOR = 32.f;
+constexpr float RAISE = 14.f, ROOM = 6.f, FLOOR = 32.f, FAR = 0x1p20f;
 
 __device__ __forceinline__ f32x16 mfma32(const f16x8& a, const f16x8& b, const f32x16& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
@@ -76,7 +80,7 @@ struct AttSeen {
   int sinks;
 };
 
-// With scaled values: m refers to the products, n to the weights, d = 2^(m - n).
+// With scaled values: n refers to the weights, n + m to the products, d = 2^m.
 template <int D, int QT>
 struct AttScaledState : AttState<D, QT> {
   float n[QT], d[QT];
@@ -84,6 +88,7 @@ struct AttScaledState : AttState<D, QT> {
     AttState<D, QT>::clear();
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
+      this->m[q] = 0.f;
       n[q] = -FLT_MAX;
       d[q] = 1.f;
     }
@@ -129,14 +134,27 @@ __device__ __forceinline__ float att_exp(f32x16 (&s)[NB], float c, float b) {
   return sum;
 }
 
+// A largest score as a power of two, a number by itself: with the product fused into the subtractions that follow, a
+// reference would not be what it is compared with.
+__device__ __forceinline__ float att_top(float raw, float c) {
+#pragma clang fp contract(off)
+  return raw * c;
+}
+// Whether a reference is that large (the first one, of no key yet, is not), and whether one of the wave's may be: seldom,
+// so the branch is laid out apart.
+__device__ __forceinline__ bool att_far(float m) { return m > FAR || (m < -FAR && m > -FLT_MAX); }
+__device__ __forceinline__ bool att_any_far(float m) { return __builtin_expect(__any(__builtin_fabsf(m) > FAR), false); }
+// What a far row's scores are taken against, `raw` the block's largest one.
+__device__ __forceinline__ float att_own(bool far, float raw) { return far && raw > -FLT_MAX ? raw : 0.f; }
+
 // s: this lane's scores of query tile q against NB blocks of 32 keys; c s (c > 0) are powers of two; key0:
 // position of the first key.  Leaves in s the weights (times the values' scale), against m.
 template <int D, int QT, int NB>
 __device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16 (&s)[NB], float c, AttNoScale,
                                             bool masked, const AttSeen<QT>& seen, int key0) {
-  const float top = att_mask(s, q, masked, seen, key0) * c;
-  if (__any(top > st.m[q] + RAISE)) {
-    const float m = top > st.m[q] + RAISE ? top - ROOM : st.m[q];
+  const float raw = att_mask(s, q, masked, seen, key0), top = att_top(raw, c);
+  if (__any(top - st.m[q] > RAISE)) {
+    const float m = top - st.m[q] > RAISE ? top - ROOM : st.m[q];
     const float f = __builtin_amdgcn_exp2f(st.m[q] - m);
     st.m[q] = m;
     st.l[q] *= f;
@@ -145,30 +163,46 @@ __device__ __forceinline__ void att_softmax(AttState<D, QT>& st, int q, f32x16 (
 #pragma unroll
       for (int r = 0; r < 16; ++r) st.o[d][q][r] *= f;
   }
-  st.l[q] += att_exp(s, c, -st.m[q]);
+  float b = -st.m[q];
+  if (att_any_far(st.m[q])) {
+    const bool far = att_far(st.m[q]);
+    const float own = att_own(far, raw);
+    b = far ? top - st.m[q] : b;
+#pragma unroll
+    for (int r = 0; r < 16 * NB; ++r) s[r / 16][r % 16] -= own;
+  }
+  st.l[q] += att_exp(s, c, b);
 }
 
 // Where a block's largest score `top` passes the references, those that it does not: m, n and d, and the factors
 // of the features and of the sum so far.
 __device__ __forceinline__ void att_raise(float top, float lv, float& m, float& n, float& d, float* of, float* lf) {
-  const float m1 = top + (lv - m) > RAISE ? __builtin_floorf(top + lv) - ROOM : m;
   const float n1 = top - n > RAISE ? __builtin_floorf(top) - ROOM : n;
-  *of = __builtin_amdgcn_exp2f(m - m1);
-  *lf = __builtin_amdgcn_exp2f(n - n1);
-  d = __builtin_amdgcn_exp2f(m1 - n1);
+  const float down = vmax(n - n1, -0x1p100f);   // (finite, from the first one on)
+  const float t = top - n1, m0 = m + down;
+  const float m1 = t + (lv - m0) > RAISE ? __builtin_floorf(t + lv) - ROOM : m0;
+  *of = __builtin_amdgcn_exp2f(m0 - m1);
+  *lf = __builtin_amdgcn_exp2f(down);
+  d = __builtin_amdgcn_exp2f(m1);
   m = m1;
   n = n1;
 }
 __device__ __forceinline__ bool att_passes(float top, float lv, float m, float n) {
-  return vmax(top + (lv - m), top - n) > RAISE;
+  const float t = top - n;
+  return t > RAISE || t + (lv - m) > RAISE;   // (the first may be infinite, the second then a NaN)
 }
 
-// The exponentials' offset b and the factor e of their sum.
-__device__ __forceinline__ void att_offset(float top, AttScale v, float m, float n, float d, float* b, float* e) {
-  *b = v.lv - m;
+// The exponentials' offset b, the factor e of their sum, and what the scores are taken against first (`raw` is the block's
+// largest one, `top` the same as a power of two).  Returns whether that is anything but zero for some row.  Far rows are
+// looked for with the other exception: with a test of their own 1000 candidates of one history took 40.6 us for 38.6.
+__device__ __forceinline__ bool att_offset(float raw, float top, AttScale v, float m, float n, float d, float* b, float* e,
+                                           float* own) {
+  *b = v.lv - (n + m);
   *e = v.inv * d;
+  *own = 0.f;
   const bool low = top + *b < -FLOOR;
-  if (__any(low)) {
+  bool some_far = false;
+  if (__any(low || __builtin_fabsf(n) > FAR)) {
     // (a score of 2^20 and more is itself rounded by 2^-24 of it: further below then.  Nothing seen: the
     // exponentials are zeros whatever they are taken against)
     const bool some = top > -FLT_MAX;
@@ -176,13 +210,22 @@ __device__ __forceinline__ void att_offset(float top, AttScale v, float m, float
     const float el = some ? __builtin_amdgcn_exp2f(-bl - n) : 0.f;
     *b = low ? bl : *b;
     *e = low ? el : *e;
+    const bool far = att_far(n);
+    some_far = __any(far);
+    if (some_far) {
+      const float t = top - n, bt = t + (v.lv - m);
+      *own = att_own(far, raw);
+      *b = !far ? *b : bt < -FLOOR ? -FLOOR : bt;
+      *e = !far ? *e : bt < -FLOOR ? __builtin_amdgcn_exp2f(t + FLOOR) : v.inv * d;
+    }
   }
+  return some_far;
 }
 
 template <int D, int QT, int NB>
 __device__ __forceinline__ void att_softmax(AttScaledState<D, QT>& st, int q, f32x16 (&s)[NB], float c, AttScale v,
                                             bool masked, const AttSeen<QT>& seen, int key0) {
-  const float top = att_mask(s, q, masked, seen, key0) * c;
+  const float raw = att_mask(s, q, masked, seen, key0), top = att_top(raw, c);
   if (__any(att_passes(top, v.lv, st.m[q], st.n[q]))) {
     float of, lf;
     att_raise(top, v.lv, st.m[q], st.n[q], st.d[q], &of, &lf);
@@ -192,8 +235,11 @@ __device__ __forceinline__ void att_softmax(AttScaledState<D, QT>& st, int q, f3
 #pragma unroll
       for (int r = 0; r < 16; ++r) st.o[d][q][r] *= of;
   }
-  float b, e;
-  att_offset(top, v, st.m[q], st.n[q], st.d[q], &b, &e);
+  float b, e, own;
+  if (att_offset(raw, top, v, st.m[q], st.n[q], st.d[q], &b, &e, &own)) {
+#pragma unroll
+    for (int r = 0; r < 16 * NB; ++r) s[r / 16][r % 16] -= own;
+  }
   st.l[q] = __builtin_fmaf(att_exp(s, c, b), e, st.l[q]);
 }
 

@@ -421,7 +421,7 @@ struct Tile16 {
   int cq;                            // a power of two
   int lo, all_hi, all_lo, sinks;     // what the row sees (besides hi, which a caller keeps), and what all rows do
   f32x4 o[ND];
-  float ref, wref, ratio, sum;       // (m, n, d, l of attend_core.h)
+  float ref, wref, ratio, sum;       // (m, n, d, l of attend_core.h: ref is above wref)
 
   // The row's query, at its first feature.
   __device__ __forceinline__ void query(const bf16_t* p, int scale_e) {
@@ -452,7 +452,8 @@ struct Tile16 {
     all_lo = __builtin_amdgcn_readfirstlane(all_lo);
   }
   __device__ __forceinline__ void clear() {
-    ref = wref = -FLT_MAX;
+    ref = 0.f;
+    wref = -FLT_MAX;
     ratio = 1.f;
     sum = 0.f;
 #pragma unroll
@@ -481,7 +482,8 @@ struct Tile16 {
     float top = s[0][0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = vmax(top, s[r / 4][r % 4]);
-    top = xmax32(xmax16(top)) * cs;
+    const float raw = xmax32(xmax16(top));
+    top = att_top(raw, cs);
     if (__any(att_passes(top, vs.lv, ref, wref))) {
       float of, lf;
       att_raise(top, vs.lv, ref, wref, ratio, &of, &lf);
@@ -489,8 +491,11 @@ struct Tile16 {
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] *= of;
     }
-    float b, e;
-    att_offset(top, vs, ref, wref, ratio, &b, &e);
+    float b, e, own;
+    if (att_offset(raw, top, vs, ref, wref, ratio, &b, &e, &own)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r / 4][r % 4] -= own;
+    }
     float part = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {

@@ -490,11 +490,19 @@ struct OpenBlock {
       s[i / 4][i % 4] = i < hi_ && (i >= lo_ || i < sinks_) ? s[i / 4][i % 4] : -INFINITY;
       top = vmax(top, s[i / 4][i % 4]);
     }
-    top = xmax32(xmax16(top)) * cs;
+    const float raw = xmax32(xmax16(top));
+    top = att_top(raw, cs);
     const bool some = top > -INFINITY;
     // a whole number as the reference, as everywhere
     r.M = some ? __builtin_floorf(top) : -FLT_MAX;
-    const float b = some ? -r.M : 0.f;
+    float b = some ? -r.M : 0.f;
+    if (att_any_far(r.M)) {   // (large scores: as in attend_core.h)
+      const bool far = att_far(r.M);
+      const float own = att_own(far, raw);
+      b = far ? top - r.M : b;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i / 4][i % 4] -= own;
+    }
     float sum = 0.f;
     uint32_t ph[8], pl[8];
 #pragma unroll

@@ -17,7 +17,7 @@ import torch
 from oracle import beams as ob
 from paper_2506_02267_amd import tav2 as T
 from test_beams_cpu import by_definition, large_logits
-from test_gpu_history import BF, HALF, Pair, bound, rows
+from test_gpu_history import BF, FAR_SIZES, HALF, Pair, bound, check_far, far_keys, far_queries, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -583,6 +583,39 @@ def test_attend_prefix_values_of_every_size(D):
     for p.groups.max_own in (64, 5000):
         for scale in (2.0 ** -80, 2.0 ** -66):
             attend(p, [0, 1, 1, 1, 3, 1], 4, scale=scale)
+
+
+@pytest.mark.parametrize("size", FAR_SIZES)
+@pytest.mark.parametrize("members,n,D", [(2, 1, 32), (2, 1, 64), (2, 1, 128), (9, 2, 64), (40, 2, 32), (40, 2, 64), (40, 2, 128)])
+def test_attend_prefix_large_scores(members, n, D, size):
+    """Scores of up to 2^125 in the prefix, in members' pages and in their open blocks, beside ordinary ones."""
+    lens = [5 * P + 40] + [(3, 70, 0, 2 * P, 40)[m % 5] for m in range(members)]
+    H, heads, total = 2, 4, sum(lens)
+    p = Beams([members], first=1, pages=100, blocks=400000, H=H, D=D, seed=20, prefix=[0])
+    off = np.concatenate([[0], np.cumsum(lens)])
+    k = torch.cat([far_keys(p.g, x, H, D) for x in lens])
+    kv = torch.cat([k, rows(p.g, total, H, D).cpu()], 1)
+    x = kv.cuda()
+    T.kv_extend(p.gpu, torch.tensor(lens, dtype=torch.int32).cuda())
+    T.kv_append(p.gpu, 0, x[:, :H], x[:, H:], torch.from_numpy(off).cuda(), max(lens))
+    p.ref.extend(lens)
+    h = kv.double().numpy()[None]
+    p.ref.append(h[:, :, :H], h[:, :, H:], off)
+    q, far = far_queries(p.g, members * n, heads, D, size)
+    q_off = torch.tensor([0] + [n * m for m in range(members + 1)]).cuda()
+    for p.groups.max_own, p.gpu.max_len, mask, window in ((64, 400, T.MASK_CAUSAL, 0), (5000, 400, T.MASK_NONE, 150),
+                                                          (64, 400000 * P, T.MASK_NONE, 0)):
+        lse = torch.empty(members * n, heads, device="cuda")
+        call = lambda q, lse=None: T.kv_attend_prefix(p.gpu, 0, p.groups, q.cuda(), q_off, n, flags=mask, window=window,
+                                                      sinks=2, scale=size / 128 / D, lse=lse)
+        out = call(q, lse)
+        for m in range(members):
+            sl = slice(m * n, m * n + n)
+            want = ob.attend_prefix(p.ref, 0, 1 + m, 0, q[sl].double().numpy(), mask == T.MASK_CAUSAL, window, 2,
+                                    size / 128 / D)
+            check_far(out[sl], lse[sl], want, D, HALF, lens[0] + lens[1 + m], max(p.vmax(0, 0), p.vmax(1 + m, 0)))
+        near = call(torch.where(far.view(-1, 1, 1), q / 64 * 4 / size, q).to(BF))
+        assert torch.equal(out[~far], near[~far])
 
 
 def test_workspace_contents_do_not_matter():

@@ -1226,3 +1226,92 @@ def test_attend_window_of_one_token_gives_its_value(seqs, D):
     out = T.attend_window(q, k, v, torch.arange(seqs).cuda() * L,
                           torch.full((seqs,), L, dtype=torch.int32).cuda(), L, window=1)
     assert torch.equal(out, v.repeat_interleave(H // Hkv, 1))
+
+
+# ------------------------------------------------------------------------- scores past 2^20
+# Scores that fp32 holds exactly, of up to 2^125: a key's features are all one whole number, which a code holds exactly
+# where its block's largest is 127, a query's all one power of two.  Scores are then whole numbers times one power of
+# two, and those that are not equal lie so far apart that the softmax is the mean over the largest ones: nothing is left of
+# bound()'s terms for the rounding of scores.
+FAR_SIZES = [2.0 ** k for k in (22, 27, 33, 66, 125)]
+
+
+def far_keys(g, L, H, D, unit=1.0, dtype=BF):
+    x = torch.randint(-100, 91, (L, H, 1), generator=g).float()
+    x[torch.rand(L, H, 1, generator=g) < 0.1] = 99.0
+    x[7::P] = -127.0
+    return (x.expand(L, H, D) * unit).to(dtype)
+
+
+def far_queries(g, n, H, D, size, dtype=BF):
+    """Scores of up to `size` with far_keys and a scale of size / (128 D unit), of either sign; every third row's of up to 4.
+    Returns the rows, and which are large."""
+    q = torch.where(torch.rand(n, H, 1, generator=g) < 0.5, -1.0, 1.0)
+    far = (torch.arange(n) % 3 != 1).view(n, 1, 1)
+    return torch.where(far, q, q * 4.0 / size).expand(n, H, D).to(dtype).contiguous(), far.view(n)
+
+
+def check_far(got, lse, want, D, dtype, n, vmax=0.0):
+    out, ref_lse, size, reach = want
+    g = got.double().cpu().numpy()
+    assert np.isfinite(g).all()
+    tol, _ = bound(out, size, np.where(reach > 1e3, 0.0, reach), n, D, dtype, vmax)
+    assert (np.abs(g - out) <= tol).all(), float(np.max(np.abs(g - out) / tol))
+    _, ltol = bound(out, size, reach, n, D, dtype, vmax)
+    z = lse.double().cpu().numpy()
+    some = ~np.isinf(ref_lse)
+    assert (z[~some] == -np.inf).all()
+    assert (np.abs(z - ref_lse)[some] <= ltol[some] + 2.0 ** -23 * np.abs(ref_lse[some])).all()
+
+
+@pytest.mark.parametrize("size", FAR_SIZES)
+@pytest.mark.parametrize("seqs,dtype,D", [(1, BF, 32), (1, BF, 64), (1, BF, 128), (200, BF, 32), (200, BF, 64), (200, BF, 128),
+                                          (1, F32, 32), (1, F32, 64), (1, F32, 128)])
+def test_attend_window_large_scores(seqs, dtype, D, size):
+    L, H, Hkv = 333, 4, 2
+    g = torch.Generator().manual_seed(D)
+    k, v = far_keys(g, L, Hkv, D, dtype=dtype), rows(g, L, Hkv, D, dtype)
+    q, far = far_queries(g, L, H, D, size, dtype)
+    all_ = lambda x: x.cuda().repeat(seqs, 1, 1)
+    off, length = torch.arange(seqs).cuda() * L, torch.full((seqs,), L, dtype=torch.int32).cuda()
+    for window, sinks in ((0, 0), (100, 3)):
+        lse = torch.empty(seqs * L, H, device="cuda")
+        call = lambda q, lse=None: T.attend_window(all_(q), all_(k), all_(v), off, length, L, window, sinks, size / 128 / D,
+                                                   lse=lse)
+        out = call(q, lse)
+        want = history.window_attention(*(x.double().cpu().numpy() for x in (q, k, v)), window, sinks, size / 128 / D)
+        for s in {0, seqs - 1}:
+            check_far(out[s * L:s * L + L], lse[s * L:s * L + L], want, D, dtype, L)
+        near = call(torch.where(far.view(L, 1, 1), q / 64 * 4 / size, q).to(dtype))
+        assert torch.equal(out.view(seqs, L, H, D)[:, ~far], near.view(seqs, L, H, D)[:, ~far])
+
+
+@pytest.mark.parametrize("size", FAR_SIZES)
+@pytest.mark.parametrize("unit", [1.0, 2.0 ** 60])
+@pytest.mark.parametrize("n,D,blocks", [(1, 32, 20), (1, 64, 20), (1, 128, 20), (20, 32, 20), (20, 64, 20), (20, 128, 20),
+                                        (70, 32, 100001), (70, 64, 10001), (70, 128, 20)])
+def test_kv_attend_large_scores(n, D, blocks, unit, size):
+    """In pages and the open block, with 16, 32 and 64 rows a workgroup, shares of all pages and of some, blocks of values
+    of very different sizes."""
+    L, H = 11 * P + 29, 4
+    p = Pair(seqs=1, pages=11, blocks=blocks, H=2, D=D, seed=3)
+    kv = torch.cat([far_keys(p.g, L, 2, D, unit), rows(p.g, L, 2, D).cpu()], 1)
+    kv[:, 2:] *= 2.0 ** torch.randint(-30, 31, (L // P + 1,), generator=p.g).repeat_interleave(P)[:L].view(L, 1, 1)
+    kv[3 * P:4 * P, 2:] = 0.0
+    x = kv.cuda()
+    T.kv_extend(p.gpu, torch.tensor([L], dtype=torch.int32).cuda())
+    T.kv_append(p.gpu, 0, x[:, :2], x[:, 2:], torch.zeros(1, dtype=torch.int64).cuda(), L)
+    p.ref.extend([L])
+    h = kv.double().numpy()[None]
+    p.ref.append(h[:, :, :2], h[:, :, 2:], [0])
+    q, far = far_queries(p.g, n, H, D, size)
+    off, scale = torch.tensor([0, n]).cuda(), size / 128 / D / unit
+    for max_len, causal, window, sinks in ((0, False, 0, 0), (blocks * P, True, 0, 0), (blocks * P, False, 200, 3)):
+        p.gpu.max_len = max_len
+        lse = torch.empty(n, H, device="cuda")
+        call = lambda q, lse=None: T.kv_attend(p.gpu, 0, q.cuda(), off, n, flags=T.MASK_CAUSAL if causal else T.MASK_NONE,
+                                               window=window, sinks=sinks, scale=scale, lse=lse)
+        out = call(q, lse)
+        check_far(out, lse, p.ref.attend(0, 0, q.double().numpy(), causal, window, sinks, scale), D, HALF, L, p.vmax(0, 0))
+        near = call(torch.where(far.view(n, 1, 1), q / 64 * 4 / size, q).to(BF))
+        assert torch.equal(out[~far], near[~far])
