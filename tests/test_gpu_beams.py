@@ -378,6 +378,36 @@ def test_reorder_leaves_what_is_out_of_range():
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("form", FORMS)
+def test_reorder_moves_numbers_of_no_page_uncounted(form):
+    """Table entries that name no page move as numbers; pages alone are counted, and nothing beside the counts is."""
+    p = Beams([3, 1], first=1, pages=40, H=1, D=32, layers=5, seed=11)
+    p.groups.max_own = form
+    p.grow([100, 70, 200, 64, 130])
+    c, pages = p.gpu, p.gpu.refs.numel()
+    around = torch.full((pages + 16,), 1000, dtype=torch.int32, device="cuda")   # what lies on either side of the counts
+    around[8:-8] = c.refs
+    p.gpu = c = T.KvCache(c.k, c.v, c.k_scale, c.v_scale, c.k_tail, c.v_tail, c.table, c.length, c.fresh, around[8:-8],
+                          c.max_len)
+    # (the pages that they named stay counted once more than they are held)
+    c.table[1, 0], c.table[2, 1], c.table[2, 2], c.table[3, 0] = -5, pages + 3, pages, -1
+    table, lens, extra = c.table.cpu(), c.length.tolist(), None
+    for parent in ([1, 0, 2, 0], [2, 1, 0, 0], [0, 2, 2, 0], [1, -1, 1, 0]):
+        was_table, was_len = table.clone(), list(lens)
+        for i, from_ in enumerate(parent[:3]):
+            table[1 + i] = was_table[1 + from_] if from_ >= 0 else -1
+            lens[1 + i] = was_len[1 + from_] if from_ >= 0 else 0
+        held = torch.tensor([int((table == x).sum()) for x in range(pages)], dtype=torch.int32)
+        if extra is None:   # (what the swap before counted: nothing)
+            extra = c.refs.cpu() - held
+            assert sorted(extra[extra != 0].tolist()) == [1, 1, 1, 1]
+        T.kv_reorder(c, p.groups, torch.tensor(parent, dtype=torch.int32).cuda())
+        torch.cuda.synchronize()
+        assert torch.equal(c.table.cpu(), table) and c.length.tolist() == lens, parent
+        assert torch.equal(c.refs.cpu(), held + extra), parent
+        assert (around[:8] == 1000).all() and (around[-8:] == 1000).all(), parent
+
+
 def test_tails_far_apart():
     """Elements past 2^31 of the tails: the last layer reordered, and its open blocks read."""
     L, S, H, D = 34, 1025, 8, 128
