@@ -10,6 +10,9 @@ Attention: as derived in test_gpu_history, where the same products and roundings
 factor joins the two launches' sums (its exponential and products are among the few 2^-23 there).
 A member's open block is nearer: its products are exact in fp32's sum, its weights off by 2^-16."""
 
+import os
+import re
+
 import numpy as np
 import pytest
 import torch
@@ -725,6 +728,31 @@ def test_a_search():
         if step % 10 == 0:
             p.same()
     p.same()
+
+
+def test_the_example_of_the_readme():
+    """As it stands there, from empty beams on: they part at the first step, and go on as the oracle's do."""
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    code = next(x for x in re.findall(r"```python\n(.*?)```", text, re.S) if "KvGroups" in x)
+    R, B, V, H, D, heads, steps = 2, 5, 60, 2, 64, 4, 3
+    p = Beams([B] * R, first=R, H=H, D=D, layers=2, seed=21, prefix=[0, 1])
+    p.grow([100, 70] + [0] * (R * B))
+    g = torch.Generator().manual_seed(4)
+    kv, z = rows(g, R * B, 2 * H, D), logits(5, R, B, V, F32)
+    z[:] = z[::B].repeat_interleave(B, 0)        # the beams of a request hold the same
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()
+    names = dict(torch=torch, tav2=T, cache=p.gpu, R=R, B=B, steps=steps, layers=2, eos=7, k=kv[:, :H], v=kv[:, H:],
+                 q=rows(g, R * B, heads, D), logits=z, count=i32([0] * R + [1] * (R * B)), offset=i32(p.offset),
+                 prefix=i32([0, 1]), row_of=torch.tensor([0] * R + list(range(R * B + 1))).cuda())
+    exec(code, names)
+    torch.cuda.synchronize()
+    want, held = (None, None, np.array([[0.0] + [-np.inf] * (B - 1)] * R), np.zeros((R, B))), [[()] * B for _ in range(R)]
+    for _ in range(steps):
+        want = ob.select(z.double().cpu().numpy(), B, B, want[2].astype(np.float32), want[3], eos=7, in_place=True)
+        held = [[held[r][want[0][r][b]] + (int(want[1][r][b]),) for b in range(B)] for r in range(R)]
+        assert all(len(set(h)) == B for h in held)
+    same_selection([names[x] for x in ("parent", "token", "score", "done")], want)
+    assert p.gpu.length.tolist() == [100, 70] + [steps] * (R * B)
 
 
 def test_a_step_in_a_graph():
