@@ -553,6 +553,9 @@ tav2_status tav2_kv_attend_prefix(const tav2_kv* c, int32_t layer, const tav2_kv
  * token 0 where eos is negative).
  * Logits that are no finite numbers are not there; a token whose bit in `allowed` is 0 counts in Z_n
  * but is no continuation; a beam whose score is not finite is none.
+ * Time: where more than some two thousand continuations of a request share the value of its `keep`-th one (rows of equal
+ * logits, or logits masked by a large finite number with fewer than `keep` others), one workgroup goes over all of the
+ * request's logits several times, about 10 ns a logit (32 beams of 131072: 40 ms instead of 20 us): mask by -inf or `allowed`.
  *   out_parent device int32 [requests, keep]: the beam b that is continued, -1 where there are fewer
  *              continuations than `keep`
  *   out_token  device int32 [requests, keep]: token v, -1 there
